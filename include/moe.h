@@ -459,6 +459,52 @@ int moe_route_topk_e4m3(const uint8_t* xq, const float* x_scale, const uint8_t* 
                         int flags, float* logits, int32_t* topk_idx, float* topk_gate,
                         void* stream);
 
+/*
+ * MXFP4 matrices (microscaled 4-bit floating point): rows of E2M1 elements in
+ * blocks of 32, each block with one E8M0 scale.
+ *
+ *   E2M1: 1 sign, 2 exponent and 1 mantissa bits: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+ *         their negatives (codes 0..7, plus 8 for the sign); no infinities, no NaN
+ *   E8M0: the byte b is the scale 2^(b - 127); 255 is NaN
+ *
+ * A matrix of `cols` columns is stored with its rows padded to
+ * P = MOE_MXFP4_COLS(cols) columns, the next multiple of 128:
+ *   codes   uint8 [rows][P / 2]: column 2 i in the lower, 2 i + 1 in the upper half
+ *           of byte i
+ *   scales  uint8 [rows][P / 32]: byte j scales columns 32 j .. 32 j + 31
+ * Padding columns hold code 0; a block of padding alone has scale byte 0.
+ */
+#define MOE_MXFP4_COLS(cols) (((int64_t)(cols) + 127) / 128 * 128)
+
+/*
+ * moe_quantize_mxfp4 -- a matrix to MXFP4.  For every block of 32 columns (the last
+ * one of a row padded with zeros):
+ *
+ *   b = max(E - 2, 0), E the biased exponent of the block's largest |x| (as a float;
+ *       0 if that is zero or subnormal)
+ *   code = E2M1(x * 2^(127 - b)), round to nearest, ties to the even code, magnitudes
+ *       above 6 saturate; the sign of x is kept, also on a zero
+ *
+ * A block that holds an infinity or a NaN gets scale byte 255 and zero codes: all of
+ * it reads as NaN, its neighbours are not touched.
+ * x       device [rows][cols] of `dtype` (MOE_F32 or MOE_BF16)
+ * codes, scales  device outputs as above
+ * Requires rows >= 0, 1 <= cols < 2^28 (else MOE_ERR_SHAPE), codes 16-byte and scales
+ * 4-byte aligned.  Results are exact (bitwise reproducible).
+ */
+int moe_quantize_mxfp4(const void* x, int dtype, int64_t rows, int cols, uint8_t* codes,
+                       uint8_t* scales, void* stream);
+
+/*
+ * moe_dequantize_mxfp4 -- the values an MXFP4 matrix holds: y[r][c] = E2M1(code) *
+ * 2^(b - 127), NaN where b = 255.  Exact in MOE_F32, and in MOE_BF16 for every value
+ * above its subnormal range (rounded to nearest even there).
+ * codes, scales  device, as above;  y  device [rows][cols] of `dtype` output
+ * Requirements as for moe_quantize_mxfp4.
+ */
+int moe_dequantize_mxfp4(const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols,
+                         int dtype, void* y, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -4,12 +4,14 @@
 #include <string.h>
 
 #include "common.h"
+#include "mxfp4.h"
 
 namespace {
 
 using namespace moe;
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 
 // Validation shared by moe_route_topk and moe_route_package.
 int route_check(const void* x, int dtype, const void* w_router, int64_t T, int d, int E, int k,
@@ -231,6 +233,19 @@ int ffn_check(const void* x_perm, int dtype, const int32_t* group_offsets, int n
     return MOE_OK;
 }
 
+// Validation of the two conversions between a matrix m and MXFP4.
+int mx_check(const void* m, int dtype, int64_t rows, int cols, const uint8_t* codes,
+             const uint8_t* scales) {
+    if (dtype != MOE_F32 && dtype != MOE_BF16) return MOE_ERR_ARG;
+    if (rows < 0 || cols < 1) return MOE_ERR_ARG;
+    // a piece's place in its row is a 32-bit number, and the grid's size another
+    if (cols >= 1 << 28 || rows > (int64_t)0x7fffffff * 8192 / mx_cols(cols)) return MOE_ERR_SHAPE;
+    if (rows > 0 && (!m || !codes || !scales)) return MOE_ERR_ARG;
+    if (((uintptr_t)m & (dtype == MOE_BF16 ? 1u : 3u)) || !aligned16(codes) || !aligned4(scales))
+        return MOE_ERR_ARG;
+    return MOE_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -381,6 +396,20 @@ int moe_route_topk_e4m3(const uint8_t* xq, const float* x_scale, const uint8_t* 
     if (!aligned16(wq) || (xq && !aligned16(xq))) return MOE_ERR_ARG;
     return launch_route_topk_e4m3(xq, x_scale, wq, w_scale, bias, T, d, E, k, flags, logits,
                                   topk_idx, topk_gate, (hipStream_t)stream);
+}
+
+int moe_quantize_mxfp4(const void* x, int dtype, int64_t rows, int cols, uint8_t* codes,
+                       uint8_t* scales, void* stream) {
+    const int st = mx_check(x, dtype, rows, cols, codes, scales);
+    if (st != MOE_OK) return st;
+    return launch_quantize_mxfp4(x, dtype, rows, cols, codes, scales, (hipStream_t)stream);
+}
+
+int moe_dequantize_mxfp4(const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols,
+                         int dtype, void* y, void* stream) {
+    const int st = mx_check(y, dtype, rows, cols, codes, scales);
+    if (st != MOE_OK) return st;
+    return launch_dequantize_mxfp4(codes, scales, rows, cols, dtype, y, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -32,7 +32,8 @@ EXPORTS = ("moe_status_string", "moe_route_topk", "moe_route_topk_ws_bytes",
            "moe_grouped_ffn_products", "moe_grouped_ffn_combine",
            "moe_grouped_ffn_rows", "moe_grouped_ffn_rows_products", "moe_grouped_ffn_rows_shared",
            "moe_combine", "moe_combine_shared",
-           "moe_quantize_e4m3", "moe_route_topk_e4m3")
+           "moe_quantize_e4m3", "moe_route_topk_e4m3",
+           "moe_quantize_mxfp4", "moe_dequantize_mxfp4")
 
 _lib = None
 
@@ -92,6 +93,10 @@ def load_library(path: str = LIB_PATH):
     lib.moe_quantize_e4m3.restype = I
     lib.moe_route_topk_e4m3.argtypes = [P, P, P, P, P, L, I, I, I, I, P, P, P, P]
     lib.moe_route_topk_e4m3.restype = I
+    lib.moe_quantize_mxfp4.argtypes = [P, I, L, I, P, P, P]
+    lib.moe_quantize_mxfp4.restype = I
+    lib.moe_dequantize_mxfp4.argtypes = [P, P, L, I, I, P, P]
+    lib.moe_dequantize_mxfp4.restype = I
     _lib = lib
     return lib
 
@@ -558,3 +563,46 @@ def moe_combine_shared(y_perm: torch.Tensor, token_row: torch.Tensor, topk_gate:
                                 _dev(y, "y", y.dtype), _stream(stream))
     _check("moe_combine_shared", st)
     return y
+
+
+def mxfp4_cols(cols: int) -> int:
+    """Columns of an MXFP4 row: `cols` padded to a multiple of 128 (MOE_MXFP4_COLS)."""
+    return (int(cols) + 127) // 128 * 128
+
+
+def moe_quantize_mxfp4(x: torch.Tensor, *, q: Optional[torch.Tensor] = None,
+                       scales: Optional[torch.Tensor] = None, stream=None):
+    """x [rows, cols] as an MXFP4 matrix.  Returns (codes uint8 [rows, P / 2], scales uint8
+    [rows, P / 32]), P = mxfp4_cols(cols)."""
+    lib = load_library()
+    rows, cols = x.shape
+    P = mxfp4_cols(cols)
+    if q is None:
+        q = _empty((rows, P // 2), torch.uint8, x.device)
+    if scales is None:
+        scales = _empty((rows, P // 32), torch.uint8, x.device)
+    _holds(q, "q", rows, P // 2)
+    _holds(scales, "scales", rows, P // 32)
+    st = lib.moe_quantize_mxfp4(_dev(x, "x"), _dtype_code(x), rows, cols, _dev(q, "q", torch.uint8),
+                                _dev(scales, "scales", torch.uint8), _stream(stream))
+    _check("moe_quantize_mxfp4", st)
+    return q, scales
+
+
+def moe_dequantize_mxfp4(q: torch.Tensor, scales: torch.Tensor, cols: int, *,
+                         dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
+                         stream=None) -> torch.Tensor:
+    """The values [rows, cols] that an MXFP4 matrix holds, in `dtype` (float32 or bfloat16)."""
+    lib = load_library()
+    rows, P = q.shape[0], mxfp4_cols(cols)
+    if cols < 1 or tuple(q.shape) != (rows, P // 2) or tuple(scales.shape) != (rows, P // 32):
+        raise ValueError("an MXFP4 matrix of %d columns has codes [rows, %d] and scales [rows, %d]"
+                         % (cols, P // 2, P // 32))
+    if out is None:
+        out = _empty((rows, cols), dtype, q.device)
+    _holds(out, "out", rows, cols)
+    st = lib.moe_dequantize_mxfp4(_dev(q, "q", torch.uint8), _dev(scales, "scales", torch.uint8),
+                                  rows, cols, _dtype_code(out), _dev(out, "out", dtype),
+                                  _stream(stream))
+    _check("moe_dequantize_mxfp4", st)
+    return out
