@@ -505,6 +505,55 @@ int moe_quantize_mxfp4(const void* x, int dtype, int64_t rows, int cols, uint8_t
 int moe_dequantize_mxfp4(const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols,
                          int dtype, void* y, void* stream);
 
+/*
+ * moe_mxfp4_scale_words -- the scales of an MXFP4 matrix as moe_grouped_ffn_mxfp4 reads a
+ * weight's: words[g][r], uint32, holds scale bytes 4 g .. 4 g + 3 of row r (byte i in bits
+ * 8 i), so that a product's step of 128 columns finds its rows' scales side by side.
+ * Made once for a weight matrix that is kept.
+ * scales  device uint8 [rows][P / 32], 4-byte aligned;  words  device uint32 [P / 128][rows]
+ *         output, P = MOE_MXFP4_COLS(cols).  Requirements as for moe_quantize_mxfp4.
+ */
+int moe_mxfp4_scale_words(const uint8_t* scales, int64_t rows, int cols, uint32_t* words,
+                          void* stream);
+
+/* Workspace bytes moe_grouped_ffn_mxfp4 needs (T rows of x; all groups together n_groups,
+ * rows of every group, shared ones included, at most cap_rows). */
+size_t moe_grouped_ffn_mxfp4_ws_bytes(int64_t T, int64_t cap_rows, int d, int f, int n_groups);
+
+/*
+ * moe_grouped_ffn_mxfp4 -- moe_grouped_ffn of experts whose weights are MXFP4
+ * matrices.  The rows of x are quantized to MXFP4 once, and the hidden rows between
+ * the products, so both products multiply 4-bit operands (the matrix cores do so
+ * natively, block scales included):
+ *
+ *   for each group s and row p of it, with Q(.) = the values moe_quantize_mxfp4 keeps:
+ *     a = W1_s Q(x_p),  b = W3_s Q(x_p),  h = SiLU(a) * b          (fp32)
+ *     y_perm[p] = W2_s Q(h)                                        (fp32, stored in bf16)
+ *
+ * x          device [T][d] bf16: row p reads x[row_token[p]]; row_token NULL: x is the
+ *            packaged rows, row p reads x[p]
+ * row_token  device [n_shared T + cap_rows] int32, nullable, as for
+ *            moe_grouped_ffn_rows_shared (entries of rows that exist lie in [0, T))
+ * group_offsets, n_groups, n_shared, cap_rows, y_perm  as for moe_grouped_ffn_rows_shared:
+ *            n_shared leading groups of T rows each (0 without row_token)
+ * w13, s13   HOST arrays of n_shared + n_groups device pointers: codes and scale words
+ *            (moe_mxfp4_scale_words) of the MXFP4 matrix [2f][d], rows 0..f-1 W1 (gate),
+ *            f..2f-1 W3 (up)
+ * w2, s2     the same of the MXFP4 matrix [d][f]
+ * ws         moe_grouped_ffn_mxfp4_ws_bytes(T, n_shared T + cap_rows, d, f, n_shared +
+ *            n_groups) bytes, 256-byte aligned
+ * An infinity or NaN in x makes its own rows of y_perm NaN and no other.  Deterministic.
+ * Requires d % 8 == 0, d and f below 2^21, 1 <= n_shared + n_groups <= MOE_MAX_GROUPS,
+ * x, y_perm and codes 16-byte, scales 4-byte aligned; T * MOE_MXFP4_COLS(d) / 2 and a
+ * weight matrix's codes below 2^31 bytes (else MOE_ERR_SHAPE).
+ */
+int moe_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
+                          const int32_t* group_offsets, int n_groups, int n_shared,
+                          const uint8_t* const* w13, const uint32_t* const* s13,
+                          const uint8_t* const* w2, const uint32_t* const* s2, int d, int f,
+                          int64_t cap_rows, void* y_perm, void* ws, size_t ws_bytes,
+                          void* stream);
+
 #ifdef __cplusplus
 }
 #endif

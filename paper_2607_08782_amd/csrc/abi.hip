@@ -412,4 +412,56 @@ int moe_dequantize_mxfp4(const uint8_t* codes, const uint8_t* scales, int64_t ro
     return launch_dequantize_mxfp4(codes, scales, rows, cols, dtype, y, (hipStream_t)stream);
 }
 
+int moe_mxfp4_scale_words(const uint8_t* scales, int64_t rows, int cols, uint32_t* words,
+                          void* stream) {
+    if (rows < 0 || cols < 1) return MOE_ERR_ARG;
+    if (cols >= 1 << 28 || rows > (int64_t)0x7fffffff * 32) return MOE_ERR_SHAPE;
+    if (rows > 0 && (!scales || !words)) return MOE_ERR_ARG;
+    if (!aligned4(scales) || !aligned4(words)) return MOE_ERR_ARG;
+    return launch_mxfp4_scale_words(scales, rows, cols, words, (hipStream_t)stream);
+}
+
+size_t moe_grouped_ffn_mxfp4_ws_bytes(int64_t T, int64_t cap_rows, int d, int f, int n_groups) {
+    if (T < 0 || cap_rows < 0 || d < 1 || f < 1 || n_groups < 0) return 0;
+    return grouped_ffn_mxfp4_ws_bytes(T, cap_rows, d, f);
+}
+
+int moe_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
+                          const int32_t* group_offsets, int n_groups, int n_shared,
+                          const uint8_t* const* w13, const uint32_t* const* s13,
+                          const uint8_t* const* w2, const uint32_t* const* s2, int d, int f,
+                          int64_t cap_rows, void* y_perm, void* ws, size_t ws_bytes,
+                          void* stream) {
+    if (n_shared < 0 || n_groups < 0 || n_shared > MOE_MAX_GROUPS || n_groups > MOE_MAX_GROUPS)
+        return MOE_ERR_ARG;
+    const int groups = n_shared + n_groups;
+    if (T < 0 || groups < 1 || groups > MOE_MAX_GROUPS || d < 1 || f < 1 || cap_rows < 0)
+        return MOE_ERR_ARG;
+    if (n_shared > 0 && (T < 1 || !row_token)) return MOE_ERR_ARG;
+    // every row, shared and routed, has a 32-bit row index
+    if (T > 0x7fffffff || cap_rows > 0x7fffffff || (int64_t)n_shared * T > 0x7fffffffLL - cap_rows)
+        return MOE_ERR_ARG;
+    const int64_t rows = (int64_t)n_shared * T + cap_rows;
+    if (!group_offsets || !w13 || !s13 || !w2 || !s2) return MOE_ERR_ARG;
+    for (int g = 0; g < groups; ++g) {
+        if (!w13[g] || !s13[g] || !w2[g] || !s2[g]) return MOE_ERR_ARG;
+        if (!aligned16(w13[g]) || !aligned16(w2[g]) || !aligned4(s13[g]) || !aligned4(s2[g]))
+            return MOE_ERR_ARG;
+    }
+    if (rows > 0 && (!y_perm || (T > 0 && !x))) return MOE_ERR_ARG;
+    if (!aligned16(x) || !aligned16(y_perm)) return MOE_ERR_ARG;
+    if (d % 8 || d >= 1 << 21 || f >= 1 << 21) return MOE_ERR_SHAPE;
+    // token rows and weight rows are reached through 32-bit byte offsets
+    if (T * (mx_cols(d) / 2) > 0x7fffffffLL || 2 * (int64_t)f * (mx_cols(d) / 2) > 0x7fffffffLL ||
+        (int64_t)d * (mx_cols(f) / 2) > 0x7fffffffLL)
+        return MOE_ERR_SHAPE;
+    // without a row map the rows are x's own
+    if (!row_token && T < cap_rows) return MOE_ERR_SHAPE;
+    if (rows > 0 && (!ws || ws_bytes < grouped_ffn_mxfp4_ws_bytes(T, rows, d, f) ||
+                     ((uintptr_t)ws & 255u)))
+        return MOE_ERR_SHAPE;
+    return launch_grouped_ffn_mxfp4(x, T, row_token, group_offsets, groups, n_shared, (int)T, w13,
+                                    s13, w2, s2, d, f, rows, y_perm, ws, (hipStream_t)stream);
+}
+
 }  // extern "C"

@@ -69,5 +69,23 @@ int launch_quantize_mxfp4(const void* x, int dtype, int64_t rows, int cols, uint
 [[nodiscard]]
 int launch_dequantize_mxfp4(const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols,
                             int dtype, void* y, hipStream_t s);
+// the scales as words [P / 128][rows] (moe_mxfp4_scale_words), from the row-major bytes or
+// straight from the quantization of bf16 rows (cols % 8 == 0, 16-byte aligned)
+[[nodiscard]]
+int launch_mxfp4_scale_words(const uint8_t* scales, int64_t rows, int cols, uint32_t* words,
+                             hipStream_t s);
+[[nodiscard]]
+int launch_quantize_mxfp4_words(const bf16_t* x, int64_t rows, int cols, uint8_t* codes,
+                                uint32_t* words, hipStream_t s);
+
+// Grouped FFN of MXFP4 experts (ffn_mxfp4.hip): n_groups groups in all, the first `lead` of
+// lead_rows rows each; `rows`: rows of all groups at most.
+size_t grouped_ffn_mxfp4_ws_bytes(int64_t T, int64_t rows, int d, int f);
+[[nodiscard]]
+int launch_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
+                             const int32_t* offsets, int n_groups, int lead, int lead_rows,
+                             const uint8_t* const* w13, const uint32_t* const* s13,
+                             const uint8_t* const* w2, const uint32_t* const* s2, int d, int f,
+                             int64_t rows, void* y, void* ws, hipStream_t s);
 
 }  // namespace moe

@@ -10,6 +10,8 @@
 // needs a piece's row and column (not even that where rows need no padding).
 #include "mxfp4.h"
 
+#include <algorithm>
+
 namespace moe {
 namespace {
 
@@ -73,11 +75,14 @@ struct Place {
     }
 };
 
-template <typename T, Form F>
+// WORDS: the scales as words [P / 128][rows] (a word is the bytes of 16 lanes' pieces)
+// rather than row-major.
+template <typename T, Form F, bool WORDS>
 __global__ __launch_bounds__(MX_THREADS) void quantize_mxfp4_kernel(const T* __restrict__ x,
                                                                     int64_t pieces, int cols,
                                                                     uint32_t* __restrict__ codes,
-                                                                    uint8_t* __restrict__ scales) {
+                                                                    uint8_t* __restrict__ scales,
+                                                                    int64_t rows) {
     const int64_t base = (int64_t)blockIdx.x * MX_PIECES;
     const Place place(base, cols);
     float v[MX_UNROLL][8];
@@ -111,7 +116,15 @@ __global__ __launch_bounds__(MX_THREADS) void quantize_mxfp4_kernel(const T* __r
         const uint32_t w = mx_encode8(v[u], most, byte);
         if (i < pieces) {
             codes[i] = w;
-            if ((threadIdx.x & 3) == 0) scales[i >> 2] = (uint8_t)byte;
+            if ((threadIdx.x & 3) != 0) continue;
+            if (!WORDS) {
+                scales[i >> 2] = (uint8_t)byte;
+            } else {
+                const uint32_t o = place.first + u * MX_THREADS + threadIdx.x, r = o / place.per_row;
+                const int col = (int)(o - r * place.per_row) * 8;
+                scales[((int64_t)(col >> 7) * rows + place.row0 + r) * 4 + ((col >> 5) & 3)] =
+                    (uint8_t)byte;
+            }
         }
     }
 }
@@ -157,18 +170,36 @@ __global__ __launch_bounds__(MX_THREADS) void dequantize_mxfp4_kernel(
     }
 }
 
+// The transpose [rows][groups] -> [groups][rows] of the scale words, through LDS.
+__global__ __launch_bounds__(256) void scale_words_kernel(const uint32_t* __restrict__ in,
+                                                          int64_t rows, int groups,
+                                                          uint32_t* __restrict__ out) {
+    __shared__ uint32_t tile[32][33];
+    const int64_t r0 = (int64_t)blockIdx.x * 32;
+    for (int g0 = blockIdx.y * 32; g0 < groups; g0 += gridDim.y * 32) {
+        for (int i = threadIdx.y; i < 32; i += 8)
+            if (r0 + i < rows && g0 + (int)threadIdx.x < groups)
+                tile[i][threadIdx.x] = in[(r0 + i) * groups + g0 + threadIdx.x];
+        __syncthreads();
+        for (int i = threadIdx.y; i < 32; i += 8)
+            if (r0 + (int)threadIdx.x < rows && g0 + i < groups)
+                out[(int64_t)(g0 + i) * rows + r0 + threadIdx.x] = tile[threadIdx.x][i];
+        __syncthreads();
+    }
+}
+
 Form form_of(const void* p, int cols) {
     if (cols % 8 || ((uintptr_t)p & 15u)) return ELEMENTS;
     return cols % 128 ? PADDED : DENSE;
 }
 
-template <typename T>
+template <bool WORDS, typename T>
 int quantize(const T* x, int64_t rows, int cols, uint8_t* codes, uint8_t* scales, hipStream_t s) {
     const int64_t pieces = rows * (mx_cols(cols) / 8);
     const dim3 grid((unsigned)ceil_div(pieces, MX_PIECES)), block(MX_THREADS);
 #define MOE_MXQ(F)                                                                             \
-    hipLaunchKernelGGL((quantize_mxfp4_kernel<T, F>), grid, block, 0, s, x, pieces, cols,      \
-                       (uint32_t*)codes, scales)
+    hipLaunchKernelGGL((quantize_mxfp4_kernel<T, F, WORDS>), grid, block, 0, s, x, pieces,     \
+                       cols, (uint32_t*)codes, scales, rows)
     switch (form_of(x, cols)) {
         case DENSE: MOE_MXQ(DENSE); break;
         case PADDED: MOE_MXQ(PADDED); break;
@@ -200,8 +231,24 @@ int dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int co
 int launch_quantize_mxfp4(const void* x, int dtype, int64_t rows, int cols, uint8_t* codes,
                           uint8_t* scales, hipStream_t s) {
     if (rows == 0) return MOE_OK;
-    return dtype == MOE_BF16 ? quantize((const bf16_t*)x, rows, cols, codes, scales, s)
-                             : quantize((const float*)x, rows, cols, codes, scales, s);
+    return dtype == MOE_BF16 ? quantize<false>((const bf16_t*)x, rows, cols, codes, scales, s)
+                             : quantize<false>((const float*)x, rows, cols, codes, scales, s);
+}
+
+int launch_quantize_mxfp4_words(const bf16_t* x, int64_t rows, int cols, uint8_t* codes,
+                                uint32_t* words, hipStream_t s) {
+    if (rows == 0) return MOE_OK;
+    return quantize<true>(x, rows, cols, codes, (uint8_t*)words, s);
+}
+
+int launch_mxfp4_scale_words(const uint8_t* scales, int64_t rows, int cols, uint32_t* words,
+                             hipStream_t s) {
+    if (rows == 0) return MOE_OK;
+    const int groups = (int)(mx_cols(cols) / 128);
+    const dim3 grid((unsigned)ceil_div(rows, 32), (unsigned)std::min(ceil_div(groups, 32), (int64_t)65535));
+    hipLaunchKernelGGL(scale_words_kernel, grid, dim3(32, 8), 0, s, (const uint32_t*)scales, rows,
+                       groups, words);
+    return launch_status();
 }
 
 int launch_dequantize_mxfp4(const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols,

@@ -33,7 +33,8 @@ EXPORTS = ("moe_status_string", "moe_route_topk", "moe_route_topk_ws_bytes",
            "moe_grouped_ffn_rows", "moe_grouped_ffn_rows_products", "moe_grouped_ffn_rows_shared",
            "moe_combine", "moe_combine_shared",
            "moe_quantize_e4m3", "moe_route_topk_e4m3",
-           "moe_quantize_mxfp4", "moe_dequantize_mxfp4")
+           "moe_quantize_mxfp4", "moe_dequantize_mxfp4", "moe_mxfp4_scale_words",
+           "moe_grouped_ffn_mxfp4_ws_bytes", "moe_grouped_ffn_mxfp4")
 
 _lib = None
 
@@ -97,6 +98,12 @@ def load_library(path: str = LIB_PATH):
     lib.moe_quantize_mxfp4.restype = I
     lib.moe_dequantize_mxfp4.argtypes = [P, P, L, I, I, P, P]
     lib.moe_dequantize_mxfp4.restype = I
+    lib.moe_mxfp4_scale_words.argtypes = [P, L, I, P, P]
+    lib.moe_mxfp4_scale_words.restype = I
+    lib.moe_grouped_ffn_mxfp4_ws_bytes.argtypes = [L, L, I, I, I]
+    lib.moe_grouped_ffn_mxfp4_ws_bytes.restype = S
+    lib.moe_grouped_ffn_mxfp4.argtypes = [P, L, P, P, I, I, P, P, P, P, I, I, L, P, P, S, P]
+    lib.moe_grouped_ffn_mxfp4.restype = I
     _lib = lib
     return lib
 
@@ -606,3 +613,99 @@ def moe_dequantize_mxfp4(q: torch.Tensor, scales: torch.Tensor, cols: int, *,
                                   _stream(stream))
     _check("moe_dequantize_mxfp4", st)
     return out
+
+
+def moe_mxfp4_scale_words(scales: torch.Tensor, cols: int, *, words: Optional[torch.Tensor] = None,
+                          stream=None) -> torch.Tensor:
+    """The scales [rows, P / 32] of an MXFP4 matrix as the FFN reads a weight's: int32 words
+    [P / 128, rows] of four scale bytes each."""
+    lib = load_library()
+    rows, P = scales.shape[0], mxfp4_cols(cols)
+    if cols < 1 or scales.shape[1] != P // 32:
+        raise ValueError("scales must be [rows, %d] for %d columns" % (P // 32, cols))
+    if words is None:
+        words = _empty((P // 128, rows), torch.int32, scales.device)
+    _holds(words, "words", P // 128, rows)
+    st = lib.moe_mxfp4_scale_words(_dev(scales, "scales", torch.uint8), rows, cols,
+                                   _dev(words, "words", torch.int32), _stream(stream))
+    _check("moe_mxfp4_scale_words", st)
+    return words
+
+
+class MxWeightTable:
+    """Experts whose weights are MXFP4 matrices, as moe_grouped_ffn_mxfp4 takes them: w13 and
+    w2 hold one (codes, scales) pair per group, as moe_quantize_mxfp4 gives them for [2f, d]
+    and [d, f].  Keeps the codes as they are and the scales as words."""
+
+    def __init__(self, w13: Sequence, w2: Sequence, d: int, f: int):
+        if len(w13) != len(w2) or not len(w13):
+            raise ValueError("need one (w13, w2) pair per group")
+        self.d, self.f = int(d), int(f)
+        self.w13, self.s13 = self._lay_out(w13, 2 * self.f, self.d, "w13")
+        self.w2, self.s2 = self._lay_out(w2, self.d, self.f, "w2")
+        n = len(self.w13)
+        self._arrays = [(ctypes.c_void_p * n)(*[t.data_ptr() for t in ts])
+                        for ts in (self.w13, self.s13, self.w2, self.s2)]
+        self.pointers = [ctypes.cast(a, ctypes.c_void_p) for a in self._arrays]
+
+    @classmethod
+    def quantized(cls, w13: Sequence[torch.Tensor], w2: Sequence[torch.Tensor]) -> "MxWeightTable":
+        """The experts of a WeightTable (w13 [2f, d], w2 [d, f], bf16 or fp32), quantized."""
+        if not len(w13):
+            raise ValueError("need one (w13, w2) pair per group")
+        return cls([moe_quantize_mxfp4(w) for w in w13], [moe_quantize_mxfp4(w) for w in w2],
+                   w13[0].shape[1], w13[0].shape[0] // 2)
+
+    @staticmethod
+    def _lay_out(pairs, rows: int, cols: int, name: str):
+        P = mxfp4_cols(cols)
+        codes, words = [], []
+        for q, s in pairs:
+            if tuple(q.shape) != (rows, P // 2) or tuple(s.shape) != (rows, P // 32):
+                raise ValueError("%s must be MXFP4 matrices of %d rows and %d columns" % (name, rows, cols))
+            _dev(q, name, torch.uint8)
+            codes.append(q)
+            words.append(moe_mxfp4_scale_words(s, cols))
+        return codes, words
+
+    def __len__(self):
+        return len(self.w13)
+
+
+def moe_grouped_ffn_mxfp4_ws_bytes(T: int, cap_rows: int, d: int, f: int, n_groups: int) -> int:
+    return int(load_library().moe_grouped_ffn_mxfp4_ws_bytes(T, cap_rows, d, f, n_groups))
+
+
+def moe_grouped_ffn_mxfp4(x: torch.Tensor, group_offsets: torch.Tensor, weights: MxWeightTable, *,
+                          row_token: Optional[torch.Tensor] = None, n_shared: int = 0,
+                          cap_rows: Optional[int] = None, y_perm: Optional[torch.Tensor] = None,
+                          ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """SwiGLU FFN of every group with 4-bit weights and activations; x [T, d] bf16, read
+    through row_token (as moe_grouped_ffn_rows_shared's, n_shared leading groups included)
+    or, without it, the packaged rows.  Returns y_perm [n_shared * T + cap_rows, d]."""
+    lib = load_library()
+    T = x.shape[0]
+    d, f = weights.d, weights.f
+    if x.dtype != torch.bfloat16 or x.dim() != 2 or x.shape[1] != d:
+        raise ValueError("x must be bfloat16 [rows, %d]" % d)
+    if cap_rows is None:
+        if row_token is not None:
+            raise ValueError("row_token needs cap_rows")
+        cap_rows = T
+    n_groups = len(weights) - n_shared
+    if n_shared < 0 or n_groups < 0 or group_offsets.numel() != n_groups + 1:
+        raise ValueError("group_offsets must hold n_groups + 1 entries for the routed groups")
+    rows = n_shared * T + cap_rows
+    _holds(row_token, "row_token", rows)
+    if y_perm is None:
+        y_perm = _empty((max(rows, 1), d), x.dtype, x.device)
+    _holds(y_perm, "y_perm", rows, d)
+    if ws is None:
+        ws = workspace(moe_grouped_ffn_mxfp4_ws_bytes(T, rows, d, f, len(weights)), x.device)
+    st = lib.moe_grouped_ffn_mxfp4(
+        _dev(x, "x"), T, _dev(row_token, "row_token", torch.int32),
+        _dev(group_offsets, "group_offsets", torch.int32), n_groups, n_shared, *weights.pointers,
+        d, f, cap_rows, _dev(y_perm, "y_perm", torch.bfloat16), _dev(ws, "ws"), ws.numel(),
+        _stream(stream))
+    _check("moe_grouped_ffn_mxfp4", st)
+    return y_perm

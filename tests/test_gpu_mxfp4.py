@@ -128,3 +128,11 @@ def test_on_another_stream():
         y = moe.moe_dequantize_mxfp4(q, s, 1024, dtype=torch.float32)
     side.synchronize()
     np.testing.assert_array_equal(y.double().cpu().numpy(), om.rounded(x.cpu().numpy()))
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 5), (33, 128), (70, 4500), (1000, 264), (31, 1024)])
+def test_scale_words_are_the_bytes_transposed(rows, cols):
+    s = torch.randint(0, 256, (rows, moe.mxfp4_cols(cols) // 32), dtype=torch.uint8, device="cuda")
+    w = moe.moe_mxfp4_scale_words(s, cols)
+    want = s.cpu().numpy().view(np.uint32).T
+    np.testing.assert_array_equal(w.cpu().numpy().view(np.uint32), want)

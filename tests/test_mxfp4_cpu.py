@@ -77,3 +77,70 @@ def test_wrappers_refuse():
             moe.moe_dequantize_mxfp4(*bad)
     with pytest.raises(ValueError, match="out must hold"):
         moe.moe_dequantize_mxfp4(q, s, 100, out=torch.zeros(4, 99, dtype=torch.bfloat16))
+
+
+def _table(n, bad=None, value=None):
+    """Four host arrays of device pointers (stand-ins), one entry of one of them replaced."""
+    arrays = [[0x10000 * (i + 1) + 0x100 * j for j in range(n)] for i in range(4)]
+    if bad is not None:
+        arrays[bad[0]][bad[1]] = value
+    keep = [(ctypes.c_void_p * n)(*a) for a in arrays]
+    return keep, [ctypes.cast(a, ctypes.c_void_p) for a in keep]
+
+
+def test_grouped_ffn_refuses(lib):
+    need = lib.moe_grouped_ffn_mxfp4_ws_bytes(16, 40, 256, 96, 2)
+    assert need >= 16 * 128 + 40 * 64
+
+    def call(table=None, **kw):
+        a = dict(x=F, T=16, tok=F, off=F, n=2, sh=0, d=256, f=96, cap=40, y=F, ws=0x100000, nb=need)
+        a.update(kw)
+        keep, p = table or _table(max(1, min(a["n"] + a["sh"], 200)))
+        p = [a.get("p%d" % i, q) for i, q in enumerate(p)]
+        return lib.moe_grouped_ffn_mxfp4(a["x"], a["T"], a["tok"], a["off"], a["n"], a["sh"], *p, a["d"],
+                                         a["f"], a["cap"], a["y"], ctypes.c_void_p(a["ws"]), a["nb"], None)
+    for bad in (dict(x=None), dict(off=None), dict(y=None), dict(T=-1), dict(n=-1), dict(n=0), dict(sh=-1),
+                dict(n=129), dict(n=100, sh=29), dict(d=0), dict(f=0), dict(cap=-1), dict(cap=1 << 31),
+                dict(T=1 << 31), dict(sh=1, tok=None), dict(sh=1, T=0), dict(T=1 << 30, sh=2, n=1),
+                dict(x=ctypes.c_void_p(0x1008)), dict(y=ctypes.c_void_p(0x1008)),
+                dict(p0=None), dict(p1=None), dict(p2=None), dict(p3=None)):
+        assert call(**bad) == moe.MOE_ERR_ARG, bad
+    for i in range(4):
+        for value in (None, 0x10000 + (8 if i % 2 == 0 else 2)):
+            assert call(_table(2, (i, 1), value)) == moe.MOE_ERR_ARG, (i, value)
+    for bad in (dict(d=252), dict(d=1 << 21), dict(f=1 << 21), dict(d=1 << 20, f=4096, nb=1 << 40),
+                dict(d=8, f=(1 << 21) - 1, T=1 << 26, cap=1, nb=1 << 62), dict(nb=need - 1), dict(ws=0x100010),
+                dict(ws=0), dict(tok=None, T=39)):
+        assert call(**bad) == moe.MOE_ERR_SHAPE, bad
+    assert call(cap=0, n=1, y=None, ws=0, nb=0) == moe.MOE_OK        # nothing to do
+
+
+def test_scale_words_refuse(lib):
+    def call(s=F, r=4, c=64, w=F):
+        return lib.moe_mxfp4_scale_words(s, r, c, w, None)
+    for bad in (dict(s=None), dict(w=None), dict(r=-1), dict(c=0), dict(s=ctypes.c_void_p(0x1001)),
+                dict(w=ctypes.c_void_p(0x1002))):
+        assert call(**bad) == moe.MOE_ERR_ARG, bad
+    assert call(c=1 << 28) == moe.MOE_ERR_SHAPE and call(r=1 << 37) == moe.MOE_ERR_SHAPE
+    assert call(r=0, s=None, w=None) == moe.MOE_OK
+
+
+def test_ffn_wrapper_refuses():
+    u8 = dict(dtype=torch.uint8)
+    pair = (torch.zeros(64, 64, **u8), torch.zeros(64, 4, **u8))
+    for bad in (([], []), ([pair], []), ([pair], [pair])):
+        with pytest.raises(ValueError):
+            moe.MxWeightTable(*bad, 100, 31)
+    with pytest.raises(ValueError, match="must be a GPU tensor"):
+        moe.MxWeightTable([pair], [pair], 100, 32)
+    with pytest.raises(ValueError):
+        moe.MxWeightTable.quantized([], [])
+    table = moe.MxWeightTable.__new__(moe.MxWeightTable)
+    table.d, table.f, table.w13 = 64, 32, [None, None]
+    x, off = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    tok = torch.zeros(8, dtype=torch.int32)
+    for bad in (dict(x=x.float()), dict(x=x[:, :32]), dict(off=off[:2]), dict(tok=tok), dict(n_shared=3),
+                dict(tok=tok, cap_rows=9), dict(cap_rows=4, y_perm=torch.zeros(3, 64, dtype=torch.bfloat16))):
+        a = dict(dict(x=x, off=off), **bad)
+        with pytest.raises(ValueError):
+            moe.moe_grouped_ffn_mxfp4(a.pop("x"), a.pop("off"), table, row_token=a.pop("tok", None), **a)
