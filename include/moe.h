@@ -554,6 +554,76 @@ int moe_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
                           int64_t cap_rows, void* y_perm, void* ws, size_t ws_bytes,
                           void* stream);
 
+/*
+ * moe_combine_backward -- gradient of moe_combine: of dy, the loss gradient of y,
+ *
+ *   dy_perm[p]  = topk_gate[t][r] * dy[t]           for p = token_row[t][r] >= 0
+ *   dgate[t][r] = sum_i dy[t][i] * y_perm[p][i]     (fp32; 0 where token_row is -1)
+ *
+ * The gradient of y_shared is dy itself.
+ * dy         device [T][d] of `dtype`;  y_perm  device [rows][d] of `dtype`, the rows
+ *            that moe_combine read (not read, may be NULL, when dgate is NULL)
+ * token_row  device [T][k] int32, every row at most once
+ * topk_gate  device [T][k] float (not read, may be NULL, when dy_perm is NULL)
+ * dy_perm    device [rows][d] of `dtype` output, nullable; rows that no token_row names
+ *            are left untouched.  It must not overlap the inputs.
+ * dgate      device [T][k] float output, nullable
+ * Sums are fp32 in a fixed order (deterministic).  Requires T >= 0, d >= 1,
+ * 1 <= k <= MOE_MAX_K; 16-byte aligned matrices where a row is a multiple of 16 bytes.
+ */
+int moe_combine_backward(const void* dy, const void* y_perm, int dtype, const int32_t* token_row,
+                         const float* topk_gate, int64_t T, int d, int k, void* dy_perm,
+                         float* dgate, void* stream);
+
+/*
+ * moe_permute_backward -- gradient of moe_permute's row copy: a token's gradient is the
+ * sum of its rows' (every row's copy went to one expert), on top of what reached it by
+ * another way:
+ *
+ *   dx[t] = sum_{r ascending, token_row[t][r] >= 0} dx_perm[token_row[t][r]] + dx_add[t]
+ *
+ * dx_perm    device [rows][d] of `dtype`, required when T > 0 (it may hold no rows)
+ * token_row  device [T][k] int32;  dx_add  device [T][d] of `dtype`, nullable
+ * dx         device [T][d] of `dtype` output (fp32 sum, then stored; may be dx_add)
+ * Requirements as for moe_combine_backward.
+ */
+int moe_permute_backward(const void* dx_perm, int dtype, const int32_t* token_row,
+                         const void* dx_add, int64_t T, int d, int k, void* dx, void* stream);
+
+/* Workspace bytes moe_route_topk_backward needs. */
+size_t moe_route_topk_backward_ws_bytes(int dtype, int64_t T, int d, int E, int k, int flags);
+
+/*
+ * moe_route_topk_backward -- gradient of moe_route_topk from dgate, the loss gradient of
+ * topk_gate (the choice of experts itself has none):
+ *
+ *   m = sum_r topk_gate[t][r] * dgate[t][r]
+ *   with MOE_RENORM: dlogits[t][topk_idx[t][r]] = topk_gate[t][r] * (dgate[t][r] - m),
+ *                    0 for experts that were not chosen
+ *   else:            dlogits[t][e] = p_e * ((dgate[t][r] if topk_idx[t][r] == e) - m),
+ *                    p = softmax(logits[t])
+ *   dx[t] = sum_e dlogits[t][e] * w_router[e];   dw[e] = sum_t dlogits[t][e] * x[t]
+ *   dbias[e] = sum_t dlogits[t][e]
+ *
+ * dgate, topk_gate  device [T][k] float;  topk_idx  device [T][k] int32, distinct in a row
+ * logits     device [T][E] float, as moe_route_topk left them (not read, may be NULL, with
+ *            MOE_RENORM)
+ * x          device [T][d] of `dtype` (not read, may be NULL, when dw is NULL)
+ * w_router   device [E][d] of `dtype` (not read, may be NULL, when dx is NULL)
+ * dlogits    device [T][E] float, dx  device [T][d] of `dtype`, dw  device [E][d] float,
+ * dbias      device [E] float: outputs, each nullable (then not computed)
+ * ws         moe_route_topk_backward_ws_bytes(...) bytes, 256-byte aligned
+ * flags      MOE_RENORM or 0
+ * Products and sums are fp32 in a fixed order (deterministic).  Requires T >= 0,
+ * 1 <= E <= MOE_MAX_E, 1 <= k <= min(E, MOE_MAX_K), 1 <= d < 2^22 and, for MOE_BF16,
+ * d % 8 == 0 (else MOE_ERR_SHAPE); 16-byte aligned matrices where a row is a multiple of
+ * 16 bytes.
+ */
+int moe_route_topk_backward(const float* dgate, const float* topk_gate, const int32_t* topk_idx,
+                            const float* logits, const void* x, const void* w_router, int dtype,
+                            int64_t T, int d, int E, int k, int flags, float* dlogits, void* dx,
+                            float* dw, float* dbias, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

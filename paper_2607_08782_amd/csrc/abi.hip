@@ -233,6 +233,13 @@ int ffn_check(const void* x_perm, int dtype, const int32_t* group_offsets, int n
     return MOE_OK;
 }
 
+// Sizes of a gradient over token rows.
+int rows_check(int dtype, int64_t T, int d, int k) {
+    if (dtype != MOE_F32 && dtype != MOE_BF16) return MOE_ERR_ARG;
+    if (T < 0 || d < 1 || k < 1 || k > MOE_MAX_K || T > 0x7fffffff) return MOE_ERR_ARG;
+    return MOE_OK;
+}
+
 // Validation of the two conversions between a matrix m and MXFP4.
 int mx_check(const void* m, int dtype, int64_t rows, int cols, const uint8_t* codes,
              const uint8_t* scales) {
@@ -462,6 +469,59 @@ int moe_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
         return MOE_ERR_SHAPE;
     return launch_grouped_ffn_mxfp4(x, T, row_token, group_offsets, groups, n_shared, (int)T, w13,
                                     s13, w2, s2, d, f, rows, y_perm, ws, (hipStream_t)stream);
+}
+
+int moe_combine_backward(const void* dy, const void* y_perm, int dtype, const int32_t* token_row,
+                         const float* topk_gate, int64_t T, int d, int k, void* dy_perm,
+                         float* dgate, void* stream) {
+    const int st = rows_check(dtype, T, d, k);
+    if (st != MOE_OK) return st;
+    if (T > 0 && (!dy || !token_row)) return MOE_ERR_ARG;
+    if (T > 0 && ((dgate && !y_perm) || (dy_perm && !topk_gate))) return MOE_ERR_ARG;
+    if (d % (dtype == MOE_BF16 ? 8 : 4) == 0 &&
+        (!aligned16(dy) || !aligned16(y_perm) || !aligned16(dy_perm)))
+        return MOE_ERR_ARG;
+    return launch_combine_backward(dy, y_perm, dtype, token_row, topk_gate, T, d, k, dy_perm, dgate,
+                                   (hipStream_t)stream);
+}
+
+int moe_permute_backward(const void* dx_perm, int dtype, const int32_t* token_row,
+                         const void* dx_add, int64_t T, int d, int k, void* dx, void* stream) {
+    const int st = rows_check(dtype, T, d, k);
+    if (st != MOE_OK) return st;
+    if (T > 0 && (!dx_perm || !token_row || !dx)) return MOE_ERR_ARG;
+    if (d % (dtype == MOE_BF16 ? 8 : 4) == 0 &&
+        (!aligned16(dx_perm) || !aligned16(dx_add) || !aligned16(dx)))
+        return MOE_ERR_ARG;
+    return launch_combine(dx_perm, dtype, token_row, nullptr, dx_add, 1, T, d, k, dx,
+                          (hipStream_t)stream);
+}
+
+size_t moe_route_topk_backward_ws_bytes(int dtype, int64_t T, int d, int E, int k, int flags) {
+    if (T < 0 || d < 1 || E < 1 || k < 1) return 0;
+    return route_backward_ws_bytes(dtype, T, d, E, k, flags);
+}
+
+int moe_route_topk_backward(const float* dgate, const float* topk_gate, const int32_t* topk_idx,
+                            const float* logits, const void* x, const void* w_router, int dtype,
+                            int64_t T, int d, int E, int k, int flags, float* dlogits, void* dx,
+                            float* dw, float* dbias, void* ws, size_t ws_bytes, void* stream) {
+    if (dtype != MOE_F32 && dtype != MOE_BF16) return MOE_ERR_ARG;
+    if (T < 0 || d < 1 || E < 1 || E > MOE_MAX_E || k < 1 || k > MOE_MAX_K || k > E)
+        return MOE_ERR_ARG;
+    if (flags & ~MOE_RENORM) return MOE_ERR_ARG;
+    if (T > 0x7fffffff) return MOE_ERR_ARG;
+    if (T > 0 && (!dgate || !topk_gate || !topk_idx || (!(flags & MOE_RENORM) && !logits)))
+        return MOE_ERR_ARG;
+    if (T > 0 && ((dx && !w_router) || (dw && !x))) return MOE_ERR_ARG;
+    if ((dtype == MOE_BF16 && d % 8) || d >= 1 << 22) return MOE_ERR_SHAPE;
+    if (d % (dtype == MOE_BF16 ? 8 : 4) == 0 &&
+        (!aligned16(x) || !aligned16(w_router) || !aligned16(dx)))
+        return MOE_ERR_ARG;
+    if (!ws || ws_bytes < route_backward_ws_bytes(dtype, T, d, E, k, flags) || ((uintptr_t)ws & 255u))
+        return MOE_ERR_SHAPE;
+    return launch_route_backward(dgate, topk_gate, topk_idx, logits, x, w_router, dtype, T, d, E, k,
+                                 flags, dlogits, dx, dw, dbias, ws, (hipStream_t)stream);
 }
 
 }  // extern "C"

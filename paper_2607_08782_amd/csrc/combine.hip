@@ -7,7 +7,8 @@
 // is no multiple of them) of one token's output row, reads the expert rows it needs
 // (loads issued together; assignments placed on other GPUs are skipped), accumulates in
 // fp32 in ascending r, and stores once.  A wave serves one token where rows are whole
-// wave widths (combine_wave_kernel).
+// wave widths (combine_wave_kernel).  Without gates every row has weight 1: the gradient
+// of the packaging (moe_permute_backward), whose dx_add stands where y_shared does.
 #include "common.h"
 
 namespace moe {
@@ -111,7 +112,7 @@ __global__ __launch_bounds__(COMBINE_THREADS) void combine_kernel(
     for (int r = 0; r < KM; ++r) {
         const int rr = r < k ? r : k - 1;
         p[r] = r < k ? token_row[t * k + rr] : -1;
-        g[r] = gate[t * k + rr];
+        g[r] = gate ? gate[t * k + rr] : 1.f;
     }
     int32_t first = -1;
 #pragma unroll
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(COMBINE_THREADS) void combine_wave_kernel(
     const int col = ((w - t * parts) * 64 + lane) * V;
     const int rr = lane < k ? lane : k - 1;
     const int p = token_row[(int64_t)t * k + rr];
-    const float g = gate[(int64_t)t * k + rr];
+    const float g = gate ? gate[(int64_t)t * k + rr] : 1.f;
     uint64_t here = __ballot(lane < k && p >= 0);
     float acc[V];
 #pragma unroll

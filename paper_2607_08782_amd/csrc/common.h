@@ -235,10 +235,22 @@ int launch_ffn_f32(const float* x, const int32_t* offsets, int n_groups, const v
                    hipStream_t s);
 size_t grouped_ffn_ws_bytes(int dtype, int64_t cap_rows, int d, int f, int n_groups);
 
-// y_shared: n_shared slices of [T][d] (nullable: none)
+// y_shared: n_shared slices of [T][d] (nullable: none); gate null: every row's weight is 1
 [[nodiscard]]
 int launch_combine(const void* y_perm, int dtype, const int32_t* token_row, const float* gate,
                    const void* y_shared, int n_shared, int64_t T, int d, int k, void* y,
                    hipStream_t s);
+
+// gradients (grad.hip)
+[[nodiscard]]
+int launch_combine_backward(const void* dy, const void* y_perm, int dtype, const int32_t* token_row,
+                            const float* gate, int64_t T, int d, int k, void* dy_perm,
+                            float* dgate, hipStream_t s);
+size_t route_backward_ws_bytes(int dtype, int64_t T, int d, int E, int k, int flags);
+[[nodiscard]]
+int launch_route_backward(const float* dgate, const float* gate, const int32_t* idx,
+                          const float* logits, const void* x, const void* w, int dtype, int64_t T,
+                          int d, int E, int k, int flags, float* dlogits, void* dx, float* dw,
+                          float* dbias, void* ws, hipStream_t s);
 
 }  // namespace moe

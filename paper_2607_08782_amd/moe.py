@@ -34,7 +34,9 @@ EXPORTS = ("moe_status_string", "moe_route_topk", "moe_route_topk_ws_bytes",
            "moe_combine", "moe_combine_shared",
            "moe_quantize_e4m3", "moe_route_topk_e4m3",
            "moe_quantize_mxfp4", "moe_dequantize_mxfp4", "moe_mxfp4_scale_words",
-           "moe_grouped_ffn_mxfp4_ws_bytes", "moe_grouped_ffn_mxfp4")
+           "moe_grouped_ffn_mxfp4_ws_bytes", "moe_grouped_ffn_mxfp4",
+           "moe_combine_backward", "moe_permute_backward", "moe_route_topk_backward_ws_bytes",
+           "moe_route_topk_backward")
 
 _lib = None
 
@@ -104,6 +106,14 @@ def load_library(path: str = LIB_PATH):
     lib.moe_grouped_ffn_mxfp4_ws_bytes.restype = S
     lib.moe_grouped_ffn_mxfp4.argtypes = [P, L, P, P, I, I, P, P, P, P, I, I, L, P, P, S, P]
     lib.moe_grouped_ffn_mxfp4.restype = I
+    lib.moe_combine_backward.argtypes = [P, P, I, P, P, L, I, I, P, P, P]
+    lib.moe_combine_backward.restype = I
+    lib.moe_permute_backward.argtypes = [P, I, P, P, L, I, I, P, P]
+    lib.moe_permute_backward.restype = I
+    lib.moe_route_topk_backward_ws_bytes.argtypes = [I, L, I, I, I, I]
+    lib.moe_route_topk_backward_ws_bytes.restype = S
+    lib.moe_route_topk_backward.argtypes = [P, P, P, P, P, P, I, L, I, I, I, I, P, P, P, P, P, S, P]
+    lib.moe_route_topk_backward.restype = I
     _lib = lib
     return lib
 
@@ -709,3 +719,109 @@ def moe_grouped_ffn_mxfp4(x: torch.Tensor, group_offsets: torch.Tensor, weights:
         _stream(stream))
     _check("moe_grouped_ffn_mxfp4", st)
     return y_perm
+
+
+def _same(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, *shape: int):
+    """t (None passes) is of this type and shape."""
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != shape):
+        raise ValueError("%s must be %s %s, got %s %s" % (name, dtype, shape, t.dtype, tuple(t.shape)))
+
+
+def moe_combine_backward(dy: torch.Tensor, y_perm: Optional[torch.Tensor], token_row: torch.Tensor,
+                         topk_gate: Optional[torch.Tensor], *, dy_perm: Optional[torch.Tensor] = None,
+                         dgate: Optional[torch.Tensor] = None, want_dy_perm: bool = True,
+                         want_dgate: bool = True, stream=None):
+    """Gradient of moe_combine.  Returns (dy_perm of y_perm's shape or None, dgate [T, k] or
+    None); rows of dy_perm that token_row does not name are left as they were."""
+    lib = load_library()
+    T, d = dy.shape
+    k = token_row.shape[1]
+    if token_row.shape[0] != T:
+        raise ValueError("token_row must be [T, k]")
+    _same(topk_gate, "topk_gate", torch.float32, T, k)
+    if y_perm is not None and (y_perm.dtype != dy.dtype or y_perm.dim() != 2 or y_perm.shape[1] != d):
+        raise ValueError("y_perm must be [rows, d] of dy's dtype")
+    if want_dy_perm and dy_perm is None:
+        if y_perm is None:
+            raise ValueError("dy_perm's rows are y_perm's: give one of them")
+        dy_perm = _empty(y_perm.shape, dy.dtype, dy.device)
+    if want_dgate and dgate is None:
+        dgate = _empty((T, k), torch.float32, dy.device)
+    if dy_perm is not None and (dy_perm.dtype != dy.dtype or dy_perm.dim() != 2 or dy_perm.shape[1] != d):
+        raise ValueError("dy_perm must be [rows, d] of dy's dtype")
+    if dy_perm is not None and y_perm is not None and dy_perm.shape[0] < y_perm.shape[0]:
+        raise ValueError("dy_perm must hold y_perm's rows")
+    _same(dgate, "dgate", torch.float32, T, k)
+    st = lib.moe_combine_backward(_dev(dy, "dy"), _dev(y_perm, "y_perm"), _dtype_code(dy),
+                                  _dev(token_row, "token_row", torch.int32), _dev(topk_gate, "topk_gate"),
+                                  T, d, k, _dev(dy_perm, "dy_perm"), _dev(dgate, "dgate"), _stream(stream))
+    _check("moe_combine_backward", st)
+    return dy_perm, dgate
+
+
+def moe_permute_backward(dx_perm: torch.Tensor, token_row: torch.Tensor, *,
+                         dx_add: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                         stream=None) -> torch.Tensor:
+    """Gradient of moe_permute's row copy, on top of dx_add.  Returns dx [T, d]."""
+    lib = load_library()
+    d = dx_perm.shape[1]
+    T, k = token_row.shape
+    if dx is None:
+        dx = _empty((T, d), dx_perm.dtype, dx_perm.device)
+    _same(dx_add, "dx_add", dx_perm.dtype, T, d)
+    _same(dx, "dx", dx_perm.dtype, T, d)
+    st = lib.moe_permute_backward(_dev(dx_perm, "dx_perm"), _dtype_code(dx_perm),
+                                  _dev(token_row, "token_row", torch.int32), _dev(dx_add, "dx_add"),
+                                  T, d, k, _dev(dx, "dx"), _stream(stream))
+    _check("moe_permute_backward", st)
+    return dx
+
+
+def moe_route_topk_backward_ws_bytes(dtype: int, T: int, d: int, E: int, k: int, flags: int) -> int:
+    return int(load_library().moe_route_topk_backward_ws_bytes(dtype, T, d, E, k, flags))
+
+
+def moe_route_topk_backward(dgate: torch.Tensor, topk_gate: torch.Tensor, topk_idx: torch.Tensor,
+                            x: torch.Tensor, w_router: torch.Tensor, *,
+                            logits: Optional[torch.Tensor] = None, renorm: bool = True,
+                            want_dlogits: bool = True, want_dx: bool = True, want_dw: bool = True,
+                            want_dbias: bool = True, dlogits: Optional[torch.Tensor] = None,
+                            dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None,
+                            dbias: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                            stream=None):
+    """Gradient of moe_route_topk.  Returns (dlogits [T, E], dx [T, d] of x's dtype, dw [E, d],
+    dbias [E]), float32 but dx, None for what is not wanted.  renorm=False needs logits."""
+    lib = load_library()
+    T, d = x.shape
+    E, k = w_router.shape[0], topk_idx.shape[1]
+    if w_router.dtype != x.dtype or w_router.shape[1] != d:
+        raise ValueError("w_router must be [E, d] of x's dtype")
+    if not renorm and logits is None:
+        raise ValueError("gates without renormalisation need logits")
+    f32 = torch.float32
+    _same(dgate, "dgate", f32, T, k)
+    _same(topk_gate, "topk_gate", f32, T, k)
+    _same(topk_idx, "topk_idx", torch.int32, T, k)
+    _same(logits, "logits", f32, T, E)
+    if want_dlogits and dlogits is None:
+        dlogits = _empty((T, E), f32, x.device)
+    if want_dx and dx is None:
+        dx = _empty((T, d), x.dtype, x.device)
+    if want_dw and dw is None:
+        dw = _empty((E, d), f32, x.device)
+    if want_dbias and dbias is None:
+        dbias = _empty((E,), f32, x.device)
+    _same(dlogits, "dlogits", f32, T, E)
+    _same(dx, "dx", x.dtype, T, d)
+    _same(dw, "dw", f32, E, d)
+    _same(dbias, "dbias", f32, E)
+    dtype, flags = _dtype_code(x), MOE_RENORM if renorm else 0
+    if ws is None:
+        ws = workspace(moe_route_topk_backward_ws_bytes(dtype, T, d, E, k, flags), x.device)
+    st = lib.moe_route_topk_backward(
+        _dev(dgate, "dgate"), _dev(topk_gate, "topk_gate"), _dev(topk_idx, "topk_idx"),
+        None if renorm else _dev(logits, "logits"), _dev(x, "x"), _dev(w_router, "w_router"), dtype, T,
+        d, E, k, flags, _dev(dlogits, "dlogits"), _dev(dx, "dx"), _dev(dw, "dw"), _dev(dbias, "dbias"),
+        _dev(ws, "ws"), ws.numel(), _stream(stream))
+    _check("moe_route_topk_backward", st)
+    return dlogits, dx, dw, dbias

@@ -1,10 +1,10 @@
 """Grouped FFN of MXFP4 experts (marked `gpu`) against its definition in float64.
 
-Tolerance, per output: half a bf16 ulp (2^-9 of it) doubled for the fp32 sums' own error
-around a rounding boundary, 2^-20 of the sum of magnitudes for fp32 accumulation over up
-to 2^14 terms, and for every hidden value that lies within 1e-5 of a rounding boundary of
-its 4-bit grid (or whose block's largest magnitude lies so near a power of two) what the
-output would change by if it fell to the other side.
+Tolerance, per output: bf16's unit roundoff (8 significant bits: 2^-8 of it), 2^-20 of
+the sum of magnitudes for fp32 accumulation over up to 2^14 terms, and for every hidden
+value that lies within 1e-5 of a rounding boundary of its 4-bit grid (or whose block's
+largest magnitude lies so near a power of two) what the output would change by if it fell
+to the other side.
 """
 import numpy as np
 import pytest
