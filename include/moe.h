@@ -506,15 +506,20 @@ int moe_dequantize_mxfp4(const uint8_t* codes, const uint8_t* scales, int64_t ro
                          int dtype, void* y, void* stream);
 
 /*
- * moe_mxfp4_scale_words -- the scales of an MXFP4 matrix as moe_grouped_ffn_mxfp4 reads a
- * weight's: words[g][r], uint32, holds scale bytes 4 g .. 4 g + 3 of row r (byte i in bits
- * 8 i), so that a product's step of 128 columns finds its rows' scales side by side.
- * Made once for a weight matrix that is kept.
- * scales  device uint8 [rows][P / 32], 4-byte aligned;  words  device uint32 [P / 128][rows]
- *         output, P = MOE_MXFP4_COLS(cols).  Requirements as for moe_quantize_mxfp4.
+ * moe_mxfp4_lay_out -- an MXFP4 matrix as moe_grouped_ffn_mxfp4 reads a weight's:
+ * step-major, so that a product's step of 128 columns finds its rows side by side.
+ *
+ *   step_codes[g][r][0..63] = codes[r][64 g .. 64 g + 63]
+ *   step_scales[g][r] = scale bytes 4 g .. 4 g + 3 of row r (byte i in bits 8 i)
+ *
+ * Made once for a weight matrix that is kept; the row-major one is then not needed.
+ * codes, scales  device, as above;  step_codes  device uint8 [P / 128][rows][64] and
+ * step_scales  device uint32 [P / 128][rows] outputs, P = MOE_MXFP4_COLS(cols).
+ * Requires rows >= 0, 1 <= cols < 2^28 (else MOE_ERR_SHAPE), codes and step_codes 16-byte,
+ * scales and step_scales 4-byte aligned.
  */
-int moe_mxfp4_scale_words(const uint8_t* scales, int64_t rows, int cols, uint32_t* words,
-                          void* stream);
+int moe_mxfp4_lay_out(const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols,
+                      uint8_t* step_codes, uint32_t* step_scales, void* stream);
 
 /* Workspace bytes moe_grouped_ffn_mxfp4 needs (T rows of x; all groups together n_groups,
  * rows of every group, shared ones included, at most cap_rows). */
@@ -536,16 +541,16 @@ size_t moe_grouped_ffn_mxfp4_ws_bytes(int64_t T, int64_t cap_rows, int d, int f,
  *            moe_grouped_ffn_rows_shared (entries of rows that exist lie in [0, T))
  * group_offsets, n_groups, n_shared, cap_rows, y_perm  as for moe_grouped_ffn_rows_shared:
  *            n_shared leading groups of T rows each (0 without row_token)
- * w13, s13   HOST arrays of n_shared + n_groups device pointers: codes and scale words
- *            (moe_mxfp4_scale_words) of the MXFP4 matrix [2f][d], rows 0..f-1 W1 (gate),
- *            f..2f-1 W3 (up)
+ * w13, s13   HOST arrays of n_shared + n_groups device pointers: step-major codes and
+ *            scales (moe_mxfp4_lay_out) of the MXFP4 matrix [2f][d], rows 0..f-1 W1
+ *            (gate), f..2f-1 W3 (up)
  * w2, s2     the same of the MXFP4 matrix [d][f]
  * ws         moe_grouped_ffn_mxfp4_ws_bytes(T, n_shared T + cap_rows, d, f, n_shared +
  *            n_groups) bytes, 256-byte aligned
  * An infinity or NaN in x makes its own rows of y_perm NaN and no other.  Deterministic.
- * Requires d % 8 == 0, d and f below 2^21, 1 <= n_shared + n_groups <= MOE_MAX_GROUPS,
- * x, y_perm and codes 16-byte, scales 4-byte aligned; T * MOE_MXFP4_COLS(d) / 2 and a
- * weight matrix's codes below 2^31 bytes (else MOE_ERR_SHAPE).
+ * Requires d % 8 == 0, d and f below 2^21, T below 2^25 (else MOE_ERR_SHAPE),
+ * 1 <= n_shared + n_groups <= MOE_MAX_GROUPS, x, y_perm and codes 16-byte, scales 4-byte
+ * aligned.
  */
 int moe_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
                           const int32_t* group_offsets, int n_groups, int n_shared,

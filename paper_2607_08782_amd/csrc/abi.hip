@@ -419,13 +419,15 @@ int moe_dequantize_mxfp4(const uint8_t* codes, const uint8_t* scales, int64_t ro
     return launch_dequantize_mxfp4(codes, scales, rows, cols, dtype, y, (hipStream_t)stream);
 }
 
-int moe_mxfp4_scale_words(const uint8_t* scales, int64_t rows, int cols, uint32_t* words,
-                          void* stream) {
+int moe_mxfp4_lay_out(const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols,
+                      uint8_t* step_codes, uint32_t* step_scales, void* stream) {
     if (rows < 0 || cols < 1) return MOE_ERR_ARG;
     if (cols >= 1 << 28 || rows > (int64_t)0x7fffffff * 32) return MOE_ERR_SHAPE;
-    if (rows > 0 && (!scales || !words)) return MOE_ERR_ARG;
-    if (!aligned4(scales) || !aligned4(words)) return MOE_ERR_ARG;
-    return launch_mxfp4_scale_words(scales, rows, cols, words, (hipStream_t)stream);
+    if (rows > 0 && (!codes || !scales || !step_codes || !step_scales)) return MOE_ERR_ARG;
+    if (!aligned16(codes) || !aligned4(scales) || !aligned16(step_codes) || !aligned4(step_scales))
+        return MOE_ERR_ARG;
+    return launch_mxfp4_lay_out(codes, scales, rows, cols, step_codes, step_scales,
+                                (hipStream_t)stream);
 }
 
 size_t moe_grouped_ffn_mxfp4_ws_bytes(int64_t T, int64_t cap_rows, int d, int f, int n_groups) {
@@ -458,10 +460,8 @@ int moe_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
     if (rows > 0 && (!y_perm || (T > 0 && !x))) return MOE_ERR_ARG;
     if (!aligned16(x) || !aligned16(y_perm)) return MOE_ERR_ARG;
     if (d % 8 || d >= 1 << 21 || f >= 1 << 21) return MOE_ERR_SHAPE;
-    // token rows and weight rows are reached through 32-bit byte offsets
-    if (T * (mx_cols(d) / 2) > 0x7fffffffLL || 2 * (int64_t)f * (mx_cols(d) / 2) > 0x7fffffffLL ||
-        (int64_t)d * (mx_cols(f) / 2) > 0x7fffffffLL)
-        return MOE_ERR_SHAPE;
+    // a step's 64 bytes of every token row are reached through 32-bit offsets
+    if (T >= 1 << 25) return MOE_ERR_SHAPE;
     // without a row map the rows are x's own
     if (!row_token && T < cap_rows) return MOE_ERR_SHAPE;
     if (rows > 0 && (!ws || ws_bytes < grouped_ffn_mxfp4_ws_bytes(T, rows, d, f) ||

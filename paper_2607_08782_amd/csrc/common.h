@@ -241,6 +241,9 @@ int launch_combine(const void* y_perm, int dtype, const int32_t* token_row, cons
                    const void* y_shared, int n_shared, int64_t T, int d, int k, void* y,
                    hipStream_t s);
 
+// Compute units of the current device (ffn.hip).
+int num_cus();
+
 // gradients (grad.hip)
 [[nodiscard]]
 int launch_combine_backward(const void* dy, const void* y_perm, int dtype, const int32_t* token_row,

@@ -25,6 +25,7 @@
 #include <type_traits>
 
 #include "common.h"
+#include "tiles.h"
 
 namespace moe {
 namespace {
@@ -50,27 +51,6 @@ constexpr int A_LOADS = A_BYTES / 1024 / 4;        // 1 KB direct loads per wave
 constexpr int B_LOADS = BNW * ROWB / 1024 / 4;
 constexpr int LOADS = A_LOADS + B_LOADS;
 constexpr int TILE_LIST = 256;                     // tiles of a workgroup listed at a time
-constexpr int NUM_XCD = 8;
-constexpr uint32_t RSRC_WORD3 = 0x00020000;        // raw buffer: 32-bit data format
-constexpr int A_OOB = 0x7fffff00;                  // offset past any descriptor: reads zero
-
-typedef __attribute__((address_space(3))) void lds_void;
-
-// wait until at most N of this wave's vector-memory operations are outstanding
-// (they complete in issue order); no memory access moves across it
-template <int N>
-__device__ __forceinline__ void wait_vm() {
-    static_assert(N >= 0 && N < 64, "vmcnt range");
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-
-// First row of group g.  The first `lead` groups hold lead_rows rows each (the
-// shared experts' groups of moe_grouped_ffn_rows_shared, every token once); the
-// offsets array gives the row ranges of the groups after them, counted from
-// row lead * lead_rows, as moe_permute writes them.
-__device__ __forceinline__ int group_start(const int32_t* offsets, int lead, int lead_rows, int g) {
-    return g < lead ? g * lead_rows : lead * lead_rows + offsets[g - lead];
-}
 
 struct GemmArgs {
     const bf16_t* w[MOE_MAX_GROUPS];   // per-group weight matrix, rows contiguous along K
@@ -152,50 +132,6 @@ __host__ __device__ __forceinline__ SplitPlan split_plan(int total, int KT, int 
 
 __device__ __forceinline__ uint4 buffer_load16(__amdgpu_buffer_rsrc_t r, int voff, int soff) {
     return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, 0));
-}
-
-// s_tstart[g] = tiles of the groups before g, for g = 0..n_groups (a group of
-// more than small_rows rows has ceil(rows / BM) * n_tiles tiles, others none);
-// run by one whole wave.
-__device__ __forceinline__ void tile_starts(const int* s_off, int n_groups, int small_rows,
-                                            int n_tiles, int* s_tstart, int lane) {
-    int carry = 0;
-    for (int g0 = 0; g0 < n_groups; g0 += 64) {
-        const int g = g0 + lane;
-        const int rows = g < n_groups ? s_off[g + 1] - s_off[g] : 0;
-        const int v = rows > small_rows ? (int)ceil_div(rows, BM) * n_tiles : 0;
-        const int incl = wave_incl_scan(v);
-        if (g < n_groups) s_tstart[g + 1] = carry + incl;
-        carry += __shfl(incl, 63, 64);
-    }
-    if (lane == 0) s_tstart[0] = 0;
-}
-
-// Tile `local` of a group of mt x n_tiles tiles: the row tiles in blocks of at most
-// 8 (of equal size, give or take one), each block running through all column tiles,
-// rows first.  The 32 tiles an XCD works on at once then span about 8 row and 4
-// column slabs of operands, whatever the group's height (rows first over a whole
-// group of 32 row tiles, they span 32 + 1: an 8192-row expert's gate/up product at
-// d = f = 2048 x 2816 fetched twice the bytes).
-struct TilePos {
-    int m, n;
-};
-
-__device__ __forceinline__ TilePos tile_pos(int local, int mt, int n_tiles) {
-    const int nb = (mt + 7) >> 3;
-    const int base = mt / nb, extra = mt - base * nb;      // the first `extra` blocks have one more
-    const int big = extra * (base + 1) * n_tiles;
-    TilePos p;
-    if (local < big) {
-        const int b = local / ((base + 1) * n_tiles), l = local - b * (base + 1) * n_tiles;
-        p.n = l / (base + 1);
-        p.m = b * (base + 1) + l - p.n * (base + 1);
-    } else {
-        const int l0 = local - big, b = l0 / (base * n_tiles), l = l0 - b * base * n_tiles;
-        p.n = l / base;
-        p.m = extra * (base + 1) + b * base + l - p.n * base;
-    }
-    return p;
 }
 
 // Row limits of the streamed groups of the two products, run by one whole wave.
@@ -325,7 +261,7 @@ __global__ __launch_bounds__(GEMM_THREADS, 1) void grouped_gemm_kernel(GemmArgs 
                 args.limits[1] = lim_down;
             }
         }
-        tile_starts(s_off, n_groups, lim, args.n_tiles, s_tstart, lane);
+        tile_starts<BM>(s_off, n_groups, lim, args.n_tiles, s_tstart, lane);
     }
     __syncthreads();
     const int KT = args.K / BK;
@@ -1200,7 +1136,7 @@ __device__ void tile_split_reduce(const GemmArgs& t, int* s_off, int* s_tstart) 
         s_off[g] = group_start(t.offsets, t.lead, t.lead_rows, g);
     __syncthreads();
     const int lim = t.limits != nullptr ? t.limits[t.product] : t.lim0;
-    if (threadIdx.x < 64) tile_starts(s_off, n_groups, lim, t.n_tiles, s_tstart, threadIdx.x);
+    if (threadIdx.x < 64) tile_starts<BM>(s_off, n_groups, lim, t.n_tiles, s_tstart, threadIdx.x);
     __syncthreads();
     const SplitPlan plan = split_plan(s_tstart[n_groups], t.K / BK, t.split_units);
     const int S = plan.S;
@@ -1377,6 +1313,8 @@ __global__ __launch_bounds__(ST_THREADS) void stream_reduce_combine_kernel(Strea
     }
 }
 
+}  // namespace
+
 int num_cus() {
     static int cached[64] = {0};
     int dev = 0;
@@ -1390,8 +1328,6 @@ int num_cus() {
     }
     return cached[dev];
 }
-
-}  // namespace
 
 static int64_t align256(int64_t x) { return (x + 255) & ~(int64_t)255; }
 

@@ -8,32 +8,38 @@
 //      whole blocks of 32 columns, so h is written once, in 4 bits)
 //   2. y = W2 h
 //
-// Scales are kept as words [128-column step][row] (moe_mxfp4_scale_words): the lanes of a
-// fragment read them side by side, one word a row and step.
+// All operands lie step-major (moe_mxfp4_lay_out): per step of 128 columns, 64 bytes of
+// codes a row and then one word of scales a row, rows side by side.  What a product's step
+// needs of a row is then no part of a longer line, half of which the cache would fetch for
+// nothing (256 x 256 tiles over rows as a matrix has them, 128-byte lines: CHANGEME).
+#include <type_traits>
+
 #include "mxfp4.h"
+#include "tiles.h"
 
 namespace moe {
 namespace {
 
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-constexpr uint32_t RSRC_WORD3 = 0x00020000;              // raw buffer: 32-bit data format
 constexpr int STEP_BYTES = 64;                           // codes of a row's 128-column step
 
 struct MxArgs {
-    const uint8_t* w[MOE_MAX_GROUPS];    // per-group weight codes [rows][P / 2]
+    const uint8_t* w[MOE_MAX_GROUPS];    // per-group weight codes [P / 128][rows][64]
     const uint32_t* ws[MOE_MAX_GROUPS];  // and scale words [P / 128][rows]
     const int32_t* offsets;              // routed groups' row offsets (device)
     int n_groups, lead, lead_rows;       // lead groups of lead_rows rows come first
-    const uint8_t* a;                    // row codes [a_total][P / 2]
+    const uint8_t* a;                    // row codes [P / 128][a_total][64]
     const uint32_t* as;                  // and scale words [P / 128][a_total]
     const int32_t* a_rows;               // row p of the product is row a_rows[p] of a, or p
     int64_t a_total;
     int KT;                              // 128-column steps of K
     int N;                               // output columns: f (gate/up) or d
     int w_rows;                          // rows of a weight matrix: 2 f or d
-    uint8_t* h;                          // gate/up: hidden codes [h_rows][hp / 2]
+    uint8_t* h;                          // gate/up: hidden codes [hp / 128][h_rows][64]
     uint8_t* hs;                         // and scale words [hp / 128][h_rows], as bytes
     int64_t h_rows;
     int hp;                              // f padded to 128
@@ -41,10 +47,8 @@ struct MxArgs {
     int strips;                          // strips a group
 };
 
-// First row of group g: the first `lead` groups hold lead_rows rows each, the offsets
-// array counts the others' rows from there.
-__device__ __forceinline__ int group_start(const MxArgs& p, int g) {
-    return g < p.lead ? g * p.lead_rows : p.lead * p.lead_rows + p.offsets[g - p.lead];
+__device__ __forceinline__ int first_row(const MxArgs& p, int g) {
+    return group_start(p.offsets, p.lead, p.lead_rows, g);
 }
 
 __device__ __forceinline__ i32x8 operand(const i32x4& v) {
@@ -56,8 +60,7 @@ __device__ __forceinline__ i32x8 operand(const i32x4& v) {
 // of one group (32 gate rows and the same up rows: 32 hidden columns, one MXFP4 block) over
 // all of K, eight waves taking every eighth 128-column step: a weight byte goes from
 // memory to the registers of the one wave that multiplies it, no wave waits for another
-// before the end, and a row's eight steps in flight are 512 bytes of it.  The waves'
-// sums meet in LDS, in wave order.
+// before the end.  The waves' sums meet in LDS, in wave order.
 constexpr int STRIP_WAVES = 8;
 constexpr int STRIP_THREADS = STRIP_WAVES * 64;
 constexpr int STRIP_ROWS = 64;                           // weight rows
@@ -77,28 +80,26 @@ __global__ __launch_bounds__(STRIP_THREADS, 2) void strip_mxfp4_kernel(MxArgs p)
     constexpr int PARTS = MS == 4 ? 4 : STRIP_WAVES;     // sums in LDS at once (64 KB)
     __shared__ float red[PARTS][BM][RED_LD];
     const int g = blockIdx.x / p.strips, strip = blockIdx.x - g * p.strips;
-    const int row0 = group_start(p, g), rows = group_start(p, g + 1) - row0;
+    const int row0 = first_row(p, g), rows = first_row(p, g + 1) - row0;
     if (rows <= 0) return;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int i16 = lane & 15, quarter = lane >> 4;
     const int n0 = strip * (SWIGLU ? STRIP_ROWS / 2 : STRIP_ROWS);
-    const int pitch = p.KT * STEP_BYTES;                 // bytes of a row's codes
-
     // weight rows of the strip: past the matrix's (or, of the gate half, past its N)
     // columns they read as zero; the scale words start at the strip's first row
     const int valid = min(SWIGLU ? STRIP_ROWS / 2 : STRIP_ROWS, p.N - n0);
-    auto rsrc = [&](int first) {
-        return __builtin_amdgcn_make_buffer_rsrc((void*)(p.w[g] + (int64_t)first * pitch), (short)0,
-                                                 max(valid, 0) * pitch, RSRC_WORD3);
+    auto rsrc = [&](int t, int first) {
+        return __builtin_amdgcn_make_buffer_rsrc(
+            (void*)(p.w[g] + ((int64_t)t * p.w_rows + first) * STEP_BYTES), (short)0,
+            max(valid, 0) * STEP_BYTES, RSRC_WORD3);
     };
-    const auto lo = rsrc(n0), hi = rsrc(SWIGLU ? p.N + n0 : n0);
     const uint32_t* wsc = p.ws[g];
     int boff[STRIP_TILES], bsrow[STRIP_TILES];
 #pragma unroll
     for (int j = 0; j < STRIP_TILES; ++j) {
         const int r = (SWIGLU && j >= STRIP_TILES / 2 ? j - STRIP_TILES / 2 : j) * 16 + i16;
-        boff[j] = r * pitch + quarter * 16;
+        boff[j] = r * STEP_BYTES + quarter * 16;
         // a row past the end has zero codes: any scale of the matrix does
         bsrow[j] = (SWIGLU && j >= STRIP_TILES / 2 ? p.N : 0) + min(n0 + r, p.N - 1);
     }
@@ -111,7 +112,7 @@ __global__ __launch_bounds__(STRIP_THREADS, 2) void strip_mxfp4_kernel(MxArgs p)
         for (int m = 0; m < MS; ++m) {
             const int r = row0 + min(m0 + 16 * m + i16, rows - 1);
             arow[m] = p.a_rows ? p.a_rows[r] : r;
-            ap[m] = p.a + arow[m] * pitch + quarter * 16;
+            ap[m] = p.a + arow[m] * STEP_BYTES + quarter * 16;
         }
         f32x4 acc[MS][STRIP_TILES];
 #pragma unroll
@@ -119,16 +120,17 @@ __global__ __launch_bounds__(STRIP_THREADS, 2) void strip_mxfp4_kernel(MxArgs p)
 #pragma unroll
             for (int j = 0; j < STRIP_TILES; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         auto load = [&](StripStep<MS>& s, int t) {
+            const auto lo = rsrc(t, n0), hi = rsrc(t, SWIGLU ? p.N + n0 : n0);
 #pragma unroll
             for (int j = 0; j < STRIP_TILES; ++j) {
                 s.b[j] = __builtin_bit_cast(
                     i32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                               SWIGLU && j >= STRIP_TILES / 2 ? hi : lo, boff[j], t * STEP_BYTES, 0));
+                               SWIGLU && j >= STRIP_TILES / 2 ? hi : lo, boff[j], 0, 0));
                 s.bs[j] = wsc[(int64_t)t * p.w_rows + bsrow[j]];
             }
 #pragma unroll
             for (int m = 0; m < MS; ++m) {
-                s.a[m] = *(const i32x4*)(ap[m] + (int64_t)t * STEP_BYTES);
+                s.a[m] = *(const i32x4*)(ap[m] + t * p.a_total * STEP_BYTES);
                 s.as[m] = p.as[t * p.a_total + arow[m]];
             }
         };
@@ -219,7 +221,8 @@ __global__ __launch_bounds__(STRIP_THREADS, 2) void strip_mxfp4_kernel(MxArgs p)
                 w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2] * s, v[3] * s, 1.0f, 1);
                 if (byte == 255u) w = 0;
                 if (live) {
-                    *(uint16_t*)(p.h + (int64_t)row * (p.hp / 2) + (n0 + c) / 2) = (uint16_t)w;
+                    *(uint16_t*)(p.h + ((int64_t)(n0 >> 7) * p.h_rows + row) * STEP_BYTES +
+                                 ((n0 & 127) + c) / 2) = (uint16_t)w;
                     if (c == 0)
                         p.hs[((int64_t)(n0 >> 7) * p.h_rows + row) * 4 + ((n0 >> 5) & 3)] =
                             (uint8_t)byte;
@@ -231,6 +234,385 @@ __global__ __launch_bounds__(STRIP_THREADS, 2) void strip_mxfp4_kernel(MxArgs p)
             }
         }
     }
+}
+
+// ---------------------------------------------------------------------------
+// Tiles: groups of many rows, bound by the matrix rate.  A persistent grid of four-wave
+// workgroups, one 32 x 32 accumulator tile per v_mfma_scale_f32_32x32x64_f8f6f4; TM x TN of
+// them a side per wave, so 256 x 256 (TW = 4) or 128 x 128 (TW = 2) a workgroup.  A wave
+// alone on its SIMD keeps 32x32x64 at 6.5 PFLOP/s (random operands, the board's power
+// limit) but 16x16x128 only at 4.4: the larger one halves the instructions to issue.
+//
+// Both operands go straight from memory into a ring of RING steps of 128 columns in LDS,
+// the row's codes (64 bytes) and its scale word, RING - 1 steps in flight: a step's loads
+// have that many steps of products to arrive.  The steps of all of a workgroup's tiles are
+// one stream: loads run four steps ahead of the products whatever tile these belong to, so
+// a tile starts without waiting for its first operands.  One barrier per step, in its
+// middle: there every wave holds its second half's fragments in registers, so the step's
+// ring slot is free, and the next step has landed, so the fragments of its first half are
+// read during the second half's products.
+//
+// LDS rows are 64 bytes; 16-byte chunk c of row r sits at c ^ ((r >> 1) & 3), free of bank
+// conflicts for the reads of 32 rows.  The weights are the instruction's first operand; the
+// weight rows of a 32-row block are laid out in LDS so that a lane's sixteen accumulators
+// are sixteen consecutive output columns of one token row (w_order): half an MXFP4 block
+// of h, or two 16-byte stores of y.
+constexpr int TILE_THREADS = 256;
+constexpr int TILE_LIST = 32;                            // tile records kept, in two halves
+
+// TM x TN accumulator tiles per wave, four waves as 2 x 2, R steps in the ring
+template <int TM, int TN, int R>
+struct TileShape {
+    static constexpr int BM = 64 * TM, BN = 64 * TN;     // token rows, weight rows
+    static constexpr int B_CODES = BM * STEP_BYTES, A_WORDS = (BM + BN) * STEP_BYTES;
+    static constexpr int B_WORDS = A_WORDS + BM * 4, STAGE = B_WORDS + BN * 4;
+    static constexpr int LDS = R * STAGE;
+    static constexpr int LOADS = TM + TN + 2;            // direct loads per wave and step
+};
+
+struct MxTile {
+    int row0, valid, n0, none;
+    uint64_t w, ws;                                      // its group's weight codes and scale words
+};
+
+__device__ __forceinline__ uint64_t uniform(uint64_t v) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 |
+           (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+}
+
+// weight row, within its 32-row block, of LDS row r: the instruction's row 8 a + 4 h + b is
+// accumulator 4 a + b of half h of the wave, which holds columns 16 h + 0 .. 15
+__device__ __forceinline__ int w_order(int r) {
+    return (r & ~31) + 16 * ((r >> 2) & 1) + 4 * ((r >> 3) & 3) + (r & 3);
+}
+
+template <bool SWIGLU, int TM, int TN, int RING>
+__global__ __launch_bounds__(TILE_THREADS, TM * TN > 8 ? 1 : 2) void tile_mxfp4_kernel(MxArgs p) {
+#ifdef __HIP_DEVICE_COMPILE__
+    typedef TileShape<TM, TN, RING> S;
+    constexpr int BM = S::BM, BN = S::BN, BN_OUT = SWIGLU ? BN / 2 : BN;
+    extern __shared__ __attribute__((aligned(1024))) char ring[];
+    __shared__ int s_off[MOE_MAX_GROUPS + 1], s_tstart[MOE_MAX_GROUPS + 1];
+    __shared__ MxTile s_tile[TILE_LIST];
+    __shared__ int s_tok[2][BM];
+    const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave & 1, wn = wave >> 1;
+    // of h, the padding columns too (as zeros)
+    const int n_tiles = ((SWIGLU ? p.hp : p.N) + BN_OUT - 1) / BN_OUT;
+    for (int g = tid; g <= p.n_groups; g += TILE_THREADS) s_off[g] = first_row(p, g);
+    __syncthreads();
+    if (wave == 0) tile_starts<BM>(s_off, p.n_groups, 0, n_tiles, s_tstart, lane);
+    __syncthreads();
+    // each XCD takes a contiguous chunk of the tiles, its workgroups every nper-th of it
+    const int total = __builtin_amdgcn_readfirstlane(s_tstart[p.n_groups]);
+    const int nper = gridDim.x / NUM_XCD, widx = blockIdx.x / NUM_XCD;
+    const int chunk = (total + NUM_XCD - 1) / NUM_XCD;
+    const int begin = min((int)(blockIdx.x % NUM_XCD) * chunk, total), end = min(begin + chunk, total);
+    const int n_list = (end - begin - widx + nper - 1) / nper;     // this workgroup's tiles
+    if (n_list <= 0) return;
+    // records of the half of the list that starts with tile q0
+    auto list_tiles = [&](int q0) {
+        const int q = q0 + tid;
+        if (tid >= TILE_LIST / 2 || q >= n_list) return;
+        const int L = begin + widx + q * nper;
+        const int g = last_le(s_tstart, p.n_groups, L);
+        const int rows = s_off[g + 1] - s_off[g];
+        const TilePos pos = tile_pos(L - s_tstart[g], (int)ceil_div(rows, BM), n_tiles);
+        MxTile t;
+        t.w = (uint64_t)p.w[g];
+        t.ws = (uint64_t)p.ws[g];
+        t.row0 = s_off[g] + pos.m * BM;
+        t.valid = min(BM, rows - pos.m * BM);
+        t.n0 = pos.n * BN_OUT;
+        s_tile[q % TILE_LIST] = t;
+    };
+    auto tile_at = [&](int q) {
+        MxTile t = s_tile[q % TILE_LIST];
+        t.w = uniform(t.w);
+        t.ws = uniform(t.ws);
+        t.row0 = __builtin_amdgcn_readfirstlane(t.row0);
+        t.valid = __builtin_amdgcn_readfirstlane(t.valid);
+        t.n0 = __builtin_amdgcn_readfirstlane(t.n0);
+        return t;
+    };
+    list_tiles(0);
+    __syncthreads();
+
+    // the loads' side of the stream: tile, step of it, operand descriptors, row offsets
+    // load i of a wave fills LDS rows 64 i + 16 wave + lane / 4 of A or B, chunk slot lane % 4
+    const int lrow = 16 * wave + (lane >> 2);
+    const int lchunk = ((lane & 3) ^ ((lane >> 4) & 3)) * 16;
+    const int boff = w_order(lrow) * STEP_BYTES + lchunk;
+    // scale words: a load of 64 rows per wave and operand (twice the same where there are
+    // only 128 rows: every wave issues as many loads)
+    const int a_words = 64 * (wave % (BM / 64)), b_words = 64 * (wave % (BN / 64));
+    // descriptors start at the step's first row: base and bytes of each, moved on by a step
+    struct Range {
+        uint64_t base;
+        int bytes;
+    };
+    Range ra = {}, rlo = {}, rhi = {}, ras = {}, rbs = {};
+    auto rsrc = [](const Range& r) {
+        return __builtin_amdgcn_make_buffer_rsrc((void*)r.base, (short)0, r.bytes, RSRC_WORD3);
+    };
+    int aoff[TM], asoff = 0, bsoff = 0;
+    // gather: the token rows of a tile's rows come into LDS a tile ahead, by a direct load
+    // like the ring's (zero past the group): three steps later every wave's has landed
+    auto fetch_tokens = [&](int q) {
+        const MxTile t = tile_at(q);
+        if (64 * wave >= BM) return;
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)(p.a_rows + t.row0), (short)0, t.valid * 4, RSRC_WORD3);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)&s_tok[q & 1][64 * wave], 4, tid * 4, 0, 0, 0);
+    };
+    if (p.a_rows != nullptr) fetch_tokens(0);
+    int lq = -1, lkt = p.KT;                             // before the first tile
+    auto next_tile = [&]() {
+        ++lq;
+        lkt = 0;
+        const bool live = lq < n_list;
+        if ((lq + 1) % (TILE_LIST / 2) == 0 && lq + 1 < n_list) {
+            __syncthreads();                             // the half's old records are used up
+            list_tiles(lq + 1);
+            __syncthreads();
+        }
+        const MxTile t = tile_at(live ? lq : n_list - 1);
+        if (p.a_rows != nullptr) {
+            if (lq == 0 || p.KT < RING - 1) {            // no three steps since it was issued
+                wait_vm<0>();
+                asm volatile("s_barrier" ::: "memory");
+            }
+            if (lq + 1 < n_list) fetch_tokens(lq + 1);
+        }
+        // past the last tile: empty ranges, loads without traffic
+        const int some = live ? 1 : 0;
+        if (p.a_rows != nullptr) ra = {(uint64_t)p.a, some * (int)p.a_total * STEP_BYTES};
+        else ra = {(uint64_t)(p.a + (int64_t)t.row0 * STEP_BYTES), some * t.valid * STEP_BYTES};
+        ras = {(uint64_t)p.as, some * (int)p.a_total * 4};
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int r = lrow + 64 * i;
+            if (p.a_rows == nullptr) aoff[i] = r * STEP_BYTES + lchunk;
+            else aoff[i] = r < t.valid ? s_tok[lq & 1][r] * STEP_BYTES + lchunk : A_OOB;
+        }
+        asoff = (p.a_rows != nullptr ? s_tok[lq & 1][a_words + lane]
+                                     : t.row0 + min(a_words + lane, t.valid - 1)) * 4;
+        // weight rows past the matrix's, or of the gate half past its own, read as zero
+        const int cols = __builtin_amdgcn_readfirstlane(some * max(min(BN_OUT, p.N - t.n0), 0));
+        const int up = SWIGLU ? p.N + t.n0 : t.n0;
+        rlo = {t.w + (uint64_t)t.n0 * STEP_BYTES, cols * STEP_BYTES};
+        rhi = {t.w + (uint64_t)up * STEP_BYTES, cols * STEP_BYTES};
+        const int b = w_order(b_words + lane);
+        bsoff = (SWIGLU && b >= BN / 2 ? up + b - BN / 2 : t.n0 + b) * 4;
+        rbs = {t.ws, some * p.w_rows * 4};
+    };
+    // direct load i of the stream's next step
+    auto load1 = [&](char* st, int i) {
+        if (i < TM) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(ra), (lds_void*)(st + wave * 1024 + i * 4096), 16,
+                                                     aoff[i], 0, 0, 0);
+        } else if (i < TM + TN) {
+            const int b = i - TM;
+            const bool up = SWIGLU && b >= TN / 2;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                rsrc(up ? rhi : rlo), (lds_void*)(st + S::B_CODES + wave * 1024 + b * 4096), 16,
+                boff + (up ? b - TN / 2 : b) * 64 * STEP_BYTES, 0, 0, 0);
+        } else if (i == TM + TN) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(ras), (lds_void*)(st + S::A_WORDS + a_words * 4),
+                                                     4, asoff, 0, 0, 0);
+        } else {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(rbs), (lds_void*)(st + S::B_WORDS + b_words * 4),
+                                                     4, bsoff, 0, 0, 0);
+        }
+    };
+    auto next_step = [&]() {
+        ++lkt;
+        ra.base += (uint64_t)p.a_total * STEP_BYTES;
+        ras.base += (uint64_t)p.a_total * 4;
+        rlo.base += (uint64_t)p.w_rows * STEP_BYTES;
+        rhi.base += (uint64_t)p.w_rows * STEP_BYTES;
+        rbs.base += (uint64_t)p.w_rows * 4;
+    };
+    auto slot = [&](unsigned step) { return ring + (step % RING) * S::STAGE; };
+
+    // the products' side: fragment addresses within a step (16-column halves of it by kk)
+    const int swz = (r32 >> 2) & 3;
+    const int a_row = wm * (BM / 2) + r32;
+    const int b_row = wn * (SWIGLU ? BN / 4 : BN / 2) + r32;
+    auto b_tile = [](int j) { return SWIGLU && j >= TN / 2 ? BN / 2 + (j - TN / 2) * 32 : j * 32; };
+    f32x16 acc[TM][TN];                                  // [token tile][weight tile]
+    i32x4 fa[2][TM], fb[2][TN];                          // by half of a step
+    int sa[TM], sb[TN], na[TM], nb[TN];                  // scale words, this step's and the next's
+    const int chunk0 = ((0 + half) ^ swz) * 16, chunk1 = ((2 + half) ^ swz) * 16;
+    // fragment i of a half of a step: the weights', then the rows'
+    auto read1 = [&](const char* st, int kk, int i) {
+        st += kk ? chunk1 : chunk0;
+        if (i < TN) fb[kk][i] = *(const i32x4*)(st + S::B_CODES + (b_row + b_tile(i)) * STEP_BYTES);
+        else fa[kk][i - TN] = *(const i32x4*)(st + (a_row + 32 * (i - TN)) * STEP_BYTES);
+    };
+    auto read_word = [&](const char* st, int i) {
+        if (i < TN) nb[i] = *(const int*)(st + S::B_WORDS + (b_row + b_tile(i)) * 4);
+        else na[i - TN] = *(const int*)(st + S::A_WORDS + (a_row + 32 * (i - TN)) * 4);
+    };
+    // blocks `half` and 2 + half of the word are the lane's in the two halves of a step
+    auto take_words = [&]() {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) sb[j] = (int)((uint32_t)nb[j] >> (8 * half));
+#pragma unroll
+        for (int m = 0; m < TM; ++m) sa[m] = (int)((uint32_t)na[m] >> (8 * half));
+    };
+    // the products of a half that follow its read i, behind what was issued before them: the
+    // order of reads, loads and products is the source's
+    auto multiply = [&](auto half_of, int i) {
+        constexpr int KK = decltype(half_of)::value;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = i * TM * TN / (TM + TN); u < (i + 1) * TM * TN / (TM + TN); ++u) {
+            const int m = u / TN, j = u % TN;
+            acc[m][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                operand(fb[KK][j]), operand(fa[KK][m]), acc[m][j], 4, 4, 2 * KK, sb[j], 2 * KK, sa[m]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // keeps a half's products from being moved past a wait
+    auto pin = [&]() {
+#pragma unroll
+        for (int m = 0; m < TM; ++m)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                if constexpr (TM * TN > 8) asm volatile("" : "+a"(acc[m][j]));
+                else asm volatile("" : "+v"(acc[m][j]));
+            }
+    };
+    constexpr std::integral_constant<int, 0> first{};
+    constexpr std::integral_constant<int, 1> second{};
+
+    unsigned step = 0;
+    for (unsigned s = 0; s < RING; ++s) {
+        if (lkt >= p.KT) next_tile();
+#pragma unroll
+        for (int i = 0; i < S::LOADS; ++i) load1(slot(s), i);
+        next_step();
+    }
+    wait_vm<(RING - 1) * S::LOADS>();
+    asm volatile("s_barrier" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < TM + TN; ++i) {
+        read1(slot(0), 0, i);
+        read_word(slot(0), i);
+    }
+    // stores of an epilogue, which the waits of the next three steps allow for
+    constexpr int STORES = SWIGLU ? TM * TN / 2 + TM : 2 * TM * TN;
+    int fresh = 0;
+    for (int q = 0; q < n_list; ++q) {
+        const MxTile cur = tile_at(q);
+#pragma unroll
+        for (int m = 0; m < TM; ++m)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[m][j][e] = 0.f;
+        for (int t = 0; t < p.KT; ++t, ++step) {
+            take_words();
+#pragma unroll
+            for (int i = 0; i < TM + TN; ++i) {
+                read1(slot(step), 1, i);
+                multiply(first, i);
+            }
+            pin();
+            // the next step has landed: outstanding may be the two after it, and stores
+            if (fresh > 0) {
+                wait_vm<(RING - 2) * S::LOADS + STORES>();
+                --fresh;
+            } else {
+                wait_vm<(RING - 2) * S::LOADS>();
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if (lkt >= p.KT) next_tile();
+#pragma unroll
+            for (int i = 0; i < TM + TN; ++i) {
+                read1(slot(step + 1), 0, i);
+                read_word(slot(step + 1), i);
+                load1(slot(step), i);
+                if (i < 2) load1(slot(step), TM + TN + i);
+                multiply(second, i);
+            }
+            pin();
+            next_step();
+        }
+        fresh = RING - 1;
+
+        // Every store is issued, those past the group's rows or the output's columns dropped
+        // by the descriptor: the waits above count them.
+        const int lr = wm * (BM / 2) + r32;
+        if (SWIGLU) {
+            const int col = cur.n0 + wn * (BN / 4);
+            const __amdgpu_buffer_rsrc_t rh = __builtin_amdgcn_make_buffer_rsrc(
+                (void*)(p.h + ((int64_t)(col >> 7) * p.h_rows + cur.row0) * STEP_BYTES), (short)0,
+                cur.valid * STEP_BYTES, RSRC_WORD3);
+            const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+                (void*)(p.hs + ((int64_t)(col >> 7) * p.h_rows + cur.row0) * 4), (short)0,
+                cur.valid * 4, RSRC_WORD3);
+#pragma unroll
+            for (int m = 0; m < TM; ++m) {
+                uint32_t bytes = 0;
+#pragma unroll
+                for (int j = 0; j < TN / 2; ++j) {
+                    float v[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) v[e] = acc[m][j][e];
+                    silu(v);
+                    uint32_t most = 0;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        v[e] *= acc[m][TN / 2 + j][e];
+                        most = max(most, __float_as_uint(v[e]) & 0x7fffffffu);
+                    }
+                    most = max(most, (uint32_t)__shfl_xor((int)most, 32, 64));
+                    uint32_t byte;
+                    u32x2 w;
+                    w[0] = mx_encode8(v, most, byte);
+                    w[1] = mx_encode8(v + 8, most, byte);
+                    bytes |= byte << (8 * j);
+                    __builtin_amdgcn_raw_buffer_store_b64(
+                        w, rh, (lr + 32 * m) * STEP_BYTES + ((col & 127) + 32 * j + 16 * half) / 2, 0, 0);
+                }
+                const int at = half ? A_OOB : (lr + 32 * m) * 4 + ((col >> 5) & 3);
+                if (TN == 4) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)bytes, rs, at, 0, 0);
+                else __builtin_amdgcn_raw_buffer_store_b8((uint8_t)bytes, rs, at, 0, 0);
+            }
+        } else {
+            const __amdgpu_buffer_rsrc_t ry = __builtin_amdgcn_make_buffer_rsrc(
+                (void*)(p.y + (int64_t)cur.row0 * p.N), (short)0, cur.valid * p.N * 2, RSRC_WORD3);
+#pragma unroll
+            for (int m = 0; m < TM; ++m)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 8) {
+                        const int col = cur.n0 + wn * (BN / 2) + 32 * j + 16 * half + e;
+                        u32x4 w;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            w[i] = pack_bf16x2(acc[m][j][e + 2 * i], acc[m][j][e + 2 * i + 1]);
+                        __builtin_amdgcn_raw_buffer_store_b128(
+                            w, ry, col < p.N ? ((lr + 32 * m) * p.N + col) * 2 : A_OOB, 0, 0);
+                    }
+        }
+    }
+#endif
+}
+
+template <bool SWIGLU, int TM, int TN, int RING>
+int launch_tiles(const MxArgs& p, int cus, hipStream_t s) {
+    constexpr int lds = TileShape<TM, TN, RING>::LDS;
+    static LdsGrant grant;
+    const int st = allow_dynamic_lds((const void*)tile_mxfp4_kernel<SWIGLU, TM, TN, RING>, lds, grant);
+    if (st != MOE_OK) return st;
+    const int grid = cus / NUM_XCD * NUM_XCD * (TM * TN > 8 ? 1 : 2);
+    hipLaunchKernelGGL((tile_mxfp4_kernel<SWIGLU, TM, TN, RING>), dim3(grid), dim3(TILE_THREADS), lds, s, p);
+    return launch_status();
 }
 
 template <bool SWIGLU>
@@ -245,9 +627,12 @@ int launch_strips(const MxArgs& p, int64_t max_rows, hipStream_t s) {
     return launch_status();
 }
 
+constexpr int64_t STRIP_MAX_ROWS = 64;
+constexpr int64_t LARGE_WORK = (int64_t)256 * 256 * 256;
+
 int64_t align256(int64_t x) { return (x + 255) & ~(int64_t)255; }
 
-// workspace: [x codes][x scale words][h codes][h scale words]
+// workspace: [x codes][x scale words][h codes][h scale words], step-major
 struct Layout {
     int64_t xs, h, hs, total;
     Layout(int64_t T, int64_t rows, int d, int f) {
@@ -272,7 +657,7 @@ int launch_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
     if (rows == 0 || T == 0) return MOE_OK;
     const Layout at(T, rows, d, f);
     char* base = (char*)ws;
-    int st = launch_quantize_mxfp4_words((const bf16_t*)x, T, d, (uint8_t*)base,
+    int st = launch_quantize_mxfp4_steps((const bf16_t*)x, T, d, (uint8_t*)base,
                                          (uint32_t*)(base + at.xs), s);
     if (st != MOE_OK) return st;
     MxArgs p;
@@ -299,7 +684,10 @@ int launch_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
     p.strips = p.hp / (STRIP_ROWS / 2);
     // a token reaches an expert at most once
     const int64_t max_rows = row_token ? T : rows;
-    if ((st = launch_strips<true>(p, max_rows, s)) != MOE_OK) return st;
+    const int cus = num_cus();
+    st = max_rows <= STRIP_MAX_ROWS ? launch_strips<true>(p, max_rows, s)
+         : rows * p.N >= LARGE_WORK ? launch_tiles<true, 4, 4, 4>(p, cus, s) : launch_tiles<true, 2, 2, 4>(p, cus, s);
+    if (st != MOE_OK) return st;
     for (int i = 0; i < n_groups; ++i) {
         p.w[i] = w2[i];
         p.ws[i] = s2[i];
@@ -313,7 +701,9 @@ int launch_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
     p.w_rows = d;
     p.y = (bf16_t*)y;
     p.strips = (int)ceil_div(d, STRIP_ROWS);
-    return launch_strips<false>(p, max_rows, s);
+    return max_rows <= STRIP_MAX_ROWS ? launch_strips<false>(p, max_rows, s)
+           : rows * p.N >= LARGE_WORK ? launch_tiles<false, 4, 4, 4>(p, cus, s)
+                                      : launch_tiles<false, 2, 2, 4>(p, cus, s);
 }
 
 }  // namespace moe

@@ -69,13 +69,14 @@ int launch_quantize_mxfp4(const void* x, int dtype, int64_t rows, int cols, uint
 [[nodiscard]]
 int launch_dequantize_mxfp4(const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols,
                             int dtype, void* y, hipStream_t s);
-// the scales as words [P / 128][rows] (moe_mxfp4_scale_words), from the row-major bytes or
-// straight from the quantization of bf16 rows (cols % 8 == 0, 16-byte aligned)
+// step-major codes [P / 128][rows][64] and scale words [P / 128][rows] (moe_mxfp4_lay_out), of
+// a row-major MXFP4 matrix or straight from the quantization of bf16 rows (cols % 8 == 0,
+// 16-byte aligned)
 [[nodiscard]]
-int launch_mxfp4_scale_words(const uint8_t* scales, int64_t rows, int cols, uint32_t* words,
-                             hipStream_t s);
+int launch_mxfp4_lay_out(const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols,
+                         uint8_t* steps, uint32_t* words, hipStream_t s);
 [[nodiscard]]
-int launch_quantize_mxfp4_words(const bf16_t* x, int64_t rows, int cols, uint8_t* codes,
+int launch_quantize_mxfp4_steps(const bf16_t* x, int64_t rows, int cols, uint8_t* codes,
                                 uint32_t* words, hipStream_t s);
 
 // Grouped FFN of MXFP4 experts (ffn_mxfp4.hip): n_groups groups in all, the first `lead` of

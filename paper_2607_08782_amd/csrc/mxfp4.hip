@@ -75,9 +75,9 @@ struct Place {
     }
 };
 
-// WORDS: the scales as words [P / 128][rows] (a word is the bytes of 16 lanes' pieces)
-// rather than row-major.
-template <typename T, Form F, bool WORDS>
+// STEPS: step-major codes and scale words (a word is the bytes of 16 lanes' pieces) rather
+// than row-major.
+template <typename T, Form F, bool STEPS>
 __global__ __launch_bounds__(MX_THREADS) void quantize_mxfp4_kernel(const T* __restrict__ x,
                                                                     int64_t pieces, int cols,
                                                                     uint32_t* __restrict__ codes,
@@ -115,15 +115,15 @@ __global__ __launch_bounds__(MX_THREADS) void quantize_mxfp4_kernel(const T* __r
         const uint32_t most = quad_max(magnitude8(v[u]));
         const uint32_t w = mx_encode8(v[u], most, byte);
         if (i < pieces) {
-            codes[i] = w;
-            if ((threadIdx.x & 3) != 0) continue;
-            if (!WORDS) {
-                scales[i >> 2] = (uint8_t)byte;
+            if (!STEPS) {
+                codes[i] = w;
+                if ((threadIdx.x & 3) == 0) scales[i >> 2] = (uint8_t)byte;
             } else {
                 const uint32_t o = place.first + u * MX_THREADS + threadIdx.x, r = o / place.per_row;
-                const int col = (int)(o - r * place.per_row) * 8;
-                scales[((int64_t)(col >> 7) * rows + place.row0 + r) * 4 + ((col >> 5) & 3)] =
-                    (uint8_t)byte;
+                const uint32_t piece = o - r * place.per_row;
+                const int64_t at = (int64_t)(piece >> 4) * rows + place.row0 + r;
+                codes[at * 16 + (piece & 15)] = w;
+                if ((threadIdx.x & 3) == 0) scales[at * 4 + ((piece >> 2) & 3)] = (uint8_t)byte;
             }
         }
     }
@@ -170,20 +170,37 @@ __global__ __launch_bounds__(MX_THREADS) void dequantize_mxfp4_kernel(
     }
 }
 
-// The transpose [rows][groups] -> [groups][rows] of the scale words, through LDS.
-__global__ __launch_bounds__(256) void scale_words_kernel(const uint32_t* __restrict__ in,
-                                                          int64_t rows, int groups,
-                                                          uint32_t* __restrict__ out) {
-    __shared__ uint32_t tile[32][33];
-    const int64_t r0 = (int64_t)blockIdx.x * 32;
-    for (int g0 = blockIdx.y * 32; g0 < groups; g0 += gridDim.y * 32) {
-        for (int i = threadIdx.y; i < 32; i += 8)
-            if (r0 + i < rows && g0 + (int)threadIdx.x < groups)
-                tile[i][threadIdx.x] = in[(r0 + i) * groups + g0 + threadIdx.x];
+// [rows][steps] -> [steps][rows], of 64-byte code pieces and of scale words: blocks of 32
+// rows x 8 steps, so that reads are 512 contiguous bytes and writes 2 KB.
+constexpr int LAY_ROWS = 32, LAY_STEPS = 8;
+
+__global__ __launch_bounds__(256) void lay_out_kernel(const uint4* __restrict__ codes,
+                                                      const uint32_t* __restrict__ scales,
+                                                      int64_t rows, int n, uint4* __restrict__ steps,
+                                                      uint32_t* __restrict__ words) {
+    __shared__ uint4 piece[LAY_ROWS][LAY_STEPS * 4 + 1];
+    __shared__ uint32_t word[LAY_ROWS][LAY_STEPS + 1];
+    const int64_t r0 = (int64_t)blockIdx.x * LAY_ROWS;
+    const int tid = threadIdx.x;
+    for (int s0 = blockIdx.y * LAY_STEPS; s0 < n; s0 += gridDim.y * LAY_STEPS) {
+        for (int i = tid; i < LAY_ROWS * LAY_STEPS * 4; i += 256) {
+            const int r = i / (LAY_STEPS * 4), c = i % (LAY_STEPS * 4);
+            if (r0 + r < rows && s0 + c / 4 < n) piece[r][c] = codes[(r0 + r) * n * 4 + s0 * 4 + c];
+        }
+        {
+            const int r = tid / LAY_STEPS, c = tid % LAY_STEPS;
+            if (r0 + r < rows && s0 + c < n) word[r][c] = scales[(r0 + r) * n + s0 + c];
+        }
         __syncthreads();
-        for (int i = threadIdx.y; i < 32; i += 8)
-            if (r0 + (int)threadIdx.x < rows && g0 + i < groups)
-                out[(int64_t)(g0 + i) * rows + r0 + threadIdx.x] = tile[threadIdx.x][i];
+        for (int i = tid; i < LAY_ROWS * LAY_STEPS * 4; i += 256) {
+            const int c = i / (LAY_ROWS * 4), r = i % (LAY_ROWS * 4) / 4, q = i % 4;
+            if (r0 + r < rows && s0 + c < n)
+                steps[((int64_t)(s0 + c) * rows + r0 + r) * 4 + q] = piece[r][c * 4 + q];
+        }
+        {
+            const int c = tid / LAY_ROWS, r = tid % LAY_ROWS;
+            if (r0 + r < rows && s0 + c < n) words[(int64_t)(s0 + c) * rows + r0 + r] = word[r][c];
+        }
         __syncthreads();
     }
 }
@@ -193,12 +210,12 @@ Form form_of(const void* p, int cols) {
     return cols % 128 ? PADDED : DENSE;
 }
 
-template <bool WORDS, typename T>
+template <bool STEPS, typename T>
 int quantize(const T* x, int64_t rows, int cols, uint8_t* codes, uint8_t* scales, hipStream_t s) {
     const int64_t pieces = rows * (mx_cols(cols) / 8);
     const dim3 grid((unsigned)ceil_div(pieces, MX_PIECES)), block(MX_THREADS);
 #define MOE_MXQ(F)                                                                             \
-    hipLaunchKernelGGL((quantize_mxfp4_kernel<T, F, WORDS>), grid, block, 0, s, x, pieces,     \
+    hipLaunchKernelGGL((quantize_mxfp4_kernel<T, F, STEPS>), grid, block, 0, s, x, pieces,     \
                        cols, (uint32_t*)codes, scales, rows)
     switch (form_of(x, cols)) {
         case DENSE: MOE_MXQ(DENSE); break;
@@ -235,19 +252,19 @@ int launch_quantize_mxfp4(const void* x, int dtype, int64_t rows, int cols, uint
                              : quantize<false>((const float*)x, rows, cols, codes, scales, s);
 }
 
-int launch_quantize_mxfp4_words(const bf16_t* x, int64_t rows, int cols, uint8_t* codes,
+int launch_quantize_mxfp4_steps(const bf16_t* x, int64_t rows, int cols, uint8_t* codes,
                                 uint32_t* words, hipStream_t s) {
     if (rows == 0) return MOE_OK;
     return quantize<true>(x, rows, cols, codes, (uint8_t*)words, s);
 }
 
-int launch_mxfp4_scale_words(const uint8_t* scales, int64_t rows, int cols, uint32_t* words,
-                             hipStream_t s) {
+int launch_mxfp4_lay_out(const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols,
+                         uint8_t* steps, uint32_t* words, hipStream_t s) {
     if (rows == 0) return MOE_OK;
-    const int groups = (int)(mx_cols(cols) / 128);
-    const dim3 grid((unsigned)ceil_div(rows, 32), (unsigned)std::min(ceil_div(groups, 32), (int64_t)65535));
-    hipLaunchKernelGGL(scale_words_kernel, grid, dim3(32, 8), 0, s, (const uint32_t*)scales, rows,
-                       groups, words);
+    const int n = (int)(mx_cols(cols) / 128);
+    const dim3 grid((unsigned)ceil_div(rows, LAY_ROWS), (unsigned)std::min(ceil_div(n, LAY_STEPS), (int64_t)65535));
+    hipLaunchKernelGGL(lay_out_kernel, grid, dim3(256), 0, s, (const uint4*)codes,
+                       (const uint32_t*)scales, rows, n, (uint4*)steps, words);
     return launch_status();
 }
 

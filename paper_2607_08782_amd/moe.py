@@ -33,7 +33,7 @@ EXPORTS = ("moe_status_string", "moe_route_topk", "moe_route_topk_ws_bytes",
            "moe_grouped_ffn_rows", "moe_grouped_ffn_rows_products", "moe_grouped_ffn_rows_shared",
            "moe_combine", "moe_combine_shared",
            "moe_quantize_e4m3", "moe_route_topk_e4m3",
-           "moe_quantize_mxfp4", "moe_dequantize_mxfp4", "moe_mxfp4_scale_words",
+           "moe_quantize_mxfp4", "moe_dequantize_mxfp4", "moe_mxfp4_lay_out",
            "moe_grouped_ffn_mxfp4_ws_bytes", "moe_grouped_ffn_mxfp4",
            "moe_combine_backward", "moe_permute_backward", "moe_route_topk_backward_ws_bytes",
            "moe_route_topk_backward")
@@ -100,8 +100,8 @@ def load_library(path: str = LIB_PATH):
     lib.moe_quantize_mxfp4.restype = I
     lib.moe_dequantize_mxfp4.argtypes = [P, P, L, I, I, P, P]
     lib.moe_dequantize_mxfp4.restype = I
-    lib.moe_mxfp4_scale_words.argtypes = [P, L, I, P, P]
-    lib.moe_mxfp4_scale_words.restype = I
+    lib.moe_mxfp4_lay_out.argtypes = [P, P, L, I, P, P, P]
+    lib.moe_mxfp4_lay_out.restype = I
     lib.moe_grouped_ffn_mxfp4_ws_bytes.argtypes = [L, L, I, I, I]
     lib.moe_grouped_ffn_mxfp4_ws_bytes.restype = S
     lib.moe_grouped_ffn_mxfp4.argtypes = [P, L, P, P, I, I, P, P, P, P, I, I, L, P, P, S, P]
@@ -625,27 +625,27 @@ def moe_dequantize_mxfp4(q: torch.Tensor, scales: torch.Tensor, cols: int, *,
     return out
 
 
-def moe_mxfp4_scale_words(scales: torch.Tensor, cols: int, *, words: Optional[torch.Tensor] = None,
-                          stream=None) -> torch.Tensor:
-    """The scales [rows, P / 32] of an MXFP4 matrix as the FFN reads a weight's: int32 words
-    [P / 128, rows] of four scale bytes each."""
+def moe_mxfp4_lay_out(q: torch.Tensor, scales: torch.Tensor, cols: int, *, stream=None):
+    """An MXFP4 matrix (codes [rows, P / 2], scales [rows, P / 32]) as the FFN reads a
+    weight's, step-major.  Returns (codes uint8 [P / 128, rows, 64], scales int32 [P / 128,
+    rows] of four scale bytes each)."""
     lib = load_library()
-    rows, P = scales.shape[0], mxfp4_cols(cols)
-    if cols < 1 or scales.shape[1] != P // 32:
-        raise ValueError("scales must be [rows, %d] for %d columns" % (P // 32, cols))
-    if words is None:
-        words = _empty((P // 128, rows), torch.int32, scales.device)
-    _holds(words, "words", P // 128, rows)
-    st = lib.moe_mxfp4_scale_words(_dev(scales, "scales", torch.uint8), rows, cols,
-                                   _dev(words, "words", torch.int32), _stream(stream))
-    _check("moe_mxfp4_scale_words", st)
-    return words
+    rows, P = q.shape[0], mxfp4_cols(cols)
+    if cols < 1 or tuple(q.shape) != (rows, P // 2) or tuple(scales.shape) != (rows, P // 32):
+        raise ValueError("an MXFP4 matrix of %d columns has codes [rows, %d] and scales [rows, %d]"
+                         % (cols, P // 2, P // 32))
+    steps = _empty((P // 128, rows, 64), torch.uint8, q.device)
+    words = _empty((P // 128, rows), torch.int32, q.device)
+    st = lib.moe_mxfp4_lay_out(_dev(q, "q", torch.uint8), _dev(scales, "scales", torch.uint8), rows, cols,
+                               _dev(steps, "step_codes"), _dev(words, "step_scales"), _stream(stream))
+    _check("moe_mxfp4_lay_out", st)
+    return steps, words
 
 
 class MxWeightTable:
     """Experts whose weights are MXFP4 matrices, as moe_grouped_ffn_mxfp4 takes them: w13 and
     w2 hold one (codes, scales) pair per group, as moe_quantize_mxfp4 gives them for [2f, d]
-    and [d, f].  Keeps the codes as they are and the scales as words."""
+    and [d, f].  Keeps step-major copies (moe_mxfp4_lay_out), not what it was given."""
 
     def __init__(self, w13: Sequence, w2: Sequence, d: int, f: int):
         if len(w13) != len(w2) or not len(w13):
@@ -673,9 +673,9 @@ class MxWeightTable:
         for q, s in pairs:
             if tuple(q.shape) != (rows, P // 2) or tuple(s.shape) != (rows, P // 32):
                 raise ValueError("%s must be MXFP4 matrices of %d rows and %d columns" % (name, rows, cols))
-            _dev(q, name, torch.uint8)
-            codes.append(q)
-            words.append(moe_mxfp4_scale_words(s, cols))
+            step_codes, step_scales = moe_mxfp4_lay_out(q, s, cols)
+            codes.append(step_codes)
+            words.append(step_scales)
         return codes, words
 
     def __len__(self):

@@ -130,9 +130,12 @@ def test_on_another_stream():
     np.testing.assert_array_equal(y.double().cpu().numpy(), om.rounded(x.cpu().numpy()))
 
 
-@pytest.mark.parametrize("rows,cols", [(1, 5), (33, 128), (70, 4500), (1000, 264), (31, 1024)])
-def test_scale_words_are_the_bytes_transposed(rows, cols):
-    s = torch.randint(0, 256, (rows, moe.mxfp4_cols(cols) // 32), dtype=torch.uint8, device="cuda")
-    w = moe.moe_mxfp4_scale_words(s, cols)
-    want = s.cpu().numpy().view(np.uint32).T
-    np.testing.assert_array_equal(w.cpu().numpy().view(np.uint32), want)
+@pytest.mark.parametrize("rows,cols", [(1, 5), (33, 128), (70, 4500), (1000, 264), (31, 1024), (64, 14336)])
+def test_step_major_layout(rows, cols):
+    P = moe.mxfp4_cols(cols)
+    q = torch.randint(0, 256, (rows, P // 2), dtype=torch.uint8, device="cuda")
+    s = torch.randint(0, 256, (rows, P // 32), dtype=torch.uint8, device="cuda")
+    codes, words = moe.moe_mxfp4_lay_out(q, s, cols)
+    np.testing.assert_array_equal(codes.cpu().numpy(),
+                                  q.cpu().numpy().reshape(rows, P // 128, 64).transpose(1, 0, 2))
+    np.testing.assert_array_equal(words.cpu().numpy().view(np.uint32), s.cpu().numpy().view(np.uint32).T)

@@ -108,21 +108,28 @@ def test_grouped_ffn_refuses(lib):
     for i in range(4):
         for value in (None, 0x10000 + (8 if i % 2 == 0 else 2)):
             assert call(_table(2, (i, 1), value)) == moe.MOE_ERR_ARG, (i, value)
-    for bad in (dict(d=252), dict(d=1 << 21), dict(f=1 << 21), dict(d=1 << 20, f=4096, nb=1 << 40),
-                dict(d=8, f=(1 << 21) - 1, T=1 << 26, cap=1, nb=1 << 62), dict(nb=need - 1), dict(ws=0x100010),
-                dict(ws=0), dict(tok=None, T=39)):
+    for bad in (dict(d=252), dict(d=1 << 21), dict(f=1 << 21), dict(T=1 << 25, nb=1 << 62), dict(nb=need - 1),
+                dict(ws=0x100010), dict(ws=0), dict(tok=None, T=39)):
         assert call(**bad) == moe.MOE_ERR_SHAPE, bad
     assert call(cap=0, n=1, y=None, ws=0, nb=0) == moe.MOE_OK        # nothing to do
 
 
-def test_scale_words_refuse(lib):
-    def call(s=F, r=4, c=64, w=F):
-        return lib.moe_mxfp4_scale_words(s, r, c, w, None)
-    for bad in (dict(s=None), dict(w=None), dict(r=-1), dict(c=0), dict(s=ctypes.c_void_p(0x1001)),
-                dict(w=ctypes.c_void_p(0x1002))):
+def test_lay_out_refuses(lib):
+    def call(q=F, s=F, r=4, c=64, o=F, w=F):
+        return lib.moe_mxfp4_lay_out(q, s, r, c, o, w, None)
+    for bad in (dict(q=None), dict(s=None), dict(o=None), dict(w=None), dict(r=-1), dict(c=0),
+                dict(q=ctypes.c_void_p(0x1008)), dict(s=ctypes.c_void_p(0x1001)),
+                dict(o=ctypes.c_void_p(0x1008)), dict(w=ctypes.c_void_p(0x1002))):
         assert call(**bad) == moe.MOE_ERR_ARG, bad
     assert call(c=1 << 28) == moe.MOE_ERR_SHAPE and call(r=1 << 37) == moe.MOE_ERR_SHAPE
-    assert call(r=0, s=None, w=None) == moe.MOE_OK
+    assert call(r=0, q=None, s=None, o=None, w=None) == moe.MOE_OK
+    u8 = dict(dtype=torch.uint8)
+    q, s = torch.zeros(4, 64, **u8), torch.zeros(4, 4, **u8)
+    with pytest.raises(ValueError, match="must be a GPU tensor"):
+        moe.moe_mxfp4_lay_out(q, s, 100)
+    for bad in ((q, s, 0), (q, s, 129), (q[:, :32], s, 100), (q, s[:3], 100)):
+        with pytest.raises(ValueError):
+            moe.moe_mxfp4_lay_out(*bad)
 
 
 def test_ffn_wrapper_refuses():
