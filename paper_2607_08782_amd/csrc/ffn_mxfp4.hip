@@ -55,6 +55,12 @@ __device__ __forceinline__ i32x8 operand(const i32x4& v) {
     return i32x8{v[0], v[1], v[2], v[3], 0, 0, 0, 0};    // 4-bit operands use the lower half
 }
 
+// SiLU(a) b by the hardware's exponential and reciprocal, an ulp each: h keeps three bits
+// of it.  Below a = -88 the reciprocal is zero, and so is h (SiLU is under 2e-36 there).
+__device__ __forceinline__ float swiglu(float a, float b) {
+    return a * __builtin_amdgcn_rcpf(1.0f + __expf(-a)) * b;
+}
+
 // ---------------------------------------------------------------------------
 // Strips: groups of few rows, bound by the weight bytes.  A workgroup holds 64 weight rows
 // of one group (32 gate rows and the same up rows: 32 hidden columns, one MXFP4 block) over
@@ -203,12 +209,11 @@ __global__ __launch_bounds__(STRIP_THREADS, 2) void strip_mxfp4_kernel(MxArgs p)
             const bool live = m0 + r < rows;
             if (SWIGLU) {
                 const f32x4 a = sum(c), b = sum(STRIP_ROWS / 2 + c);
-                float v[4] = {a[0], a[1], a[2], a[3]};
-                silu(v);
+                float v[4];
                 uint32_t most = 0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    v[e] *= b[e];
+                    v[e] = swiglu(a[e], b[e]);
                     most = max(most, __float_as_uint(v[e]) & 0x7fffffffu);
                 }
                 // the block is the eight threads of the row
@@ -257,17 +262,21 @@ __global__ __launch_bounds__(STRIP_THREADS, 2) void strip_mxfp4_kernel(MxArgs p)
 // weight rows of a 32-row block are laid out in LDS so that a lane's sixteen accumulators
 // are sixteen consecutive output columns of one token row (w_order): half an MXFP4 block
 // of h, or two 16-byte stores of y.
-constexpr int TILE_THREADS = 256;
 constexpr int TILE_LIST = 32;                            // tile records kept, in two halves
 
-// TM x TN accumulator tiles per wave, four waves as 2 x 2, R steps in the ring
-template <int TM, int TN, int R>
+// TM x TN accumulator tiles per wave, WM x 2 waves, R steps in the ring
+template <int WM, int TM, int TN, int R>
 struct TileShape {
-    static constexpr int BM = 64 * TM, BN = 64 * TN;     // token rows, weight rows
+    static constexpr int WAVES = 2 * WM, THREADS = 64 * WAVES;
+    static constexpr int BM = 32 * WM * TM, BN = 64 * TN;          // token rows, weight rows
     static constexpr int B_CODES = BM * STEP_BYTES, A_WORDS = (BM + BN) * STEP_BYTES;
     static constexpr int B_WORDS = A_WORDS + BM * 4, STAGE = B_WORDS + BN * 4;
-    static constexpr int LDS = R * STAGE;
-    static constexpr int LOADS = TM + TN + 2;            // direct loads per wave and step
+    static constexpr int LDS = R * STAGE + 2 * BM * 4;   // the ring, and two tiles' token rows
+    // direct loads per wave and step: 16 rows of codes each, and 64 rows of scale words (of
+    // one operand a wave where there are eight, else of both)
+    static constexpr int AL = BM / 16 / WAVES, BL = BN / 16 / WAVES, WL = WAVES == 8 ? 1 : 2;
+    static constexpr int LOADS = AL + BL + WL;
+    static constexpr int PER_EU = TM * TN > 8 ? 1 : 2;   // waves a SIMD holds
 };
 
 struct MxTile {
@@ -286,21 +295,22 @@ __device__ __forceinline__ int w_order(int r) {
     return (r & ~31) + 16 * ((r >> 2) & 1) + 4 * ((r >> 3) & 3) + (r & 3);
 }
 
-template <bool SWIGLU, int TM, int TN, int RING>
-__global__ __launch_bounds__(TILE_THREADS, TM * TN > 8 ? 1 : 2) void tile_mxfp4_kernel(MxArgs p) {
+template <bool SWIGLU, int WM, int TM, int TN, int RING>
+__global__ __launch_bounds__(64 * 2 * WM, TM * TN > 8 ? 1 : 2) void tile_mxfp4_kernel(MxArgs p) {
 #ifdef __HIP_DEVICE_COMPILE__
-    typedef TileShape<TM, TN, RING> S;
+    typedef TileShape<WM, TM, TN, RING> S;
     constexpr int BM = S::BM, BN = S::BN, BN_OUT = SWIGLU ? BN / 2 : BN;
+    constexpr int AL = S::AL, BL = S::BL, ROUND = 16 * S::WAVES;
     extern __shared__ __attribute__((aligned(1024))) char ring[];
     __shared__ int s_off[MOE_MAX_GROUPS + 1], s_tstart[MOE_MAX_GROUPS + 1];
     __shared__ MxTile s_tile[TILE_LIST];
-    __shared__ int s_tok[2][BM];
+    int* const s_tok = (int*)(ring + RING * S::STAGE);   // [2][BM]
     const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave & 1, wn = wave >> 1;
+    const int wm = wave % WM, wn = wave / WM;
     // of h, the padding columns too (as zeros)
     const int n_tiles = ((SWIGLU ? p.hp : p.N) + BN_OUT - 1) / BN_OUT;
-    for (int g = tid; g <= p.n_groups; g += TILE_THREADS) s_off[g] = first_row(p, g);
+    for (int g = tid; g <= p.n_groups; g += S::THREADS) s_off[g] = first_row(p, g);
     __syncthreads();
     if (wave == 0) tile_starts<BM>(s_off, p.n_groups, 0, n_tiles, s_tstart, lane);
     __syncthreads();
@@ -340,13 +350,12 @@ __global__ __launch_bounds__(TILE_THREADS, TM * TN > 8 ? 1 : 2) void tile_mxfp4_
     __syncthreads();
 
     // the loads' side of the stream: tile, step of it, operand descriptors, row offsets
-    // load i of a wave fills LDS rows 64 i + 16 wave + lane / 4 of A or B, chunk slot lane % 4
+    // load i of a wave fills LDS rows ROUND i + 16 wave + lane / 4 of A or B, slot lane % 4
     const int lrow = 16 * wave + (lane >> 2);
     const int lchunk = ((lane & 3) ^ ((lane >> 4) & 3)) * 16;
     const int boff = w_order(lrow) * STEP_BYTES + lchunk;
-    // scale words: a load of 64 rows per wave and operand (twice the same where there are
-    // only 128 rows: every wave issues as many loads)
     const int a_words = 64 * (wave % (BM / 64)), b_words = 64 * (wave % (BN / 64));
+    const bool words_of_a = S::WL == 2 || wave < S::WAVES / 2;
     // descriptors start at the step's first row: base and bytes of each, moved on by a step
     struct Range {
         uint64_t base;
@@ -356,7 +365,7 @@ __global__ __launch_bounds__(TILE_THREADS, TM * TN > 8 ? 1 : 2) void tile_mxfp4_
     auto rsrc = [](const Range& r) {
         return __builtin_amdgcn_make_buffer_rsrc((void*)r.base, (short)0, r.bytes, RSRC_WORD3);
     };
-    int aoff[TM], asoff = 0, bsoff = 0;
+    int aoff[AL], asoff = 0, bsoff = 0;
     // gather: the token rows of a tile's rows come into LDS a tile ahead, by a direct load
     // like the ring's (zero past the group): three steps later every wave's has landed
     auto fetch_tokens = [&](int q) {
@@ -364,7 +373,8 @@ __global__ __launch_bounds__(TILE_THREADS, TM * TN > 8 ? 1 : 2) void tile_mxfp4_
         if (64 * wave >= BM) return;
         const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
             (void*)(p.a_rows + t.row0), (short)0, t.valid * 4, RSRC_WORD3);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)&s_tok[q & 1][64 * wave], 4, tid * 4, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(s_tok + (q & 1) * BM + 64 * wave), 4, tid * 4, 0,
+                                                 0, 0);
     };
     if (p.a_rows != nullptr) fetch_tokens(0);
     int lq = -1, lkt = p.KT;                             // before the first tile
@@ -391,12 +401,12 @@ __global__ __launch_bounds__(TILE_THREADS, TM * TN > 8 ? 1 : 2) void tile_mxfp4_
         else ra = {(uint64_t)(p.a + (int64_t)t.row0 * STEP_BYTES), some * t.valid * STEP_BYTES};
         ras = {(uint64_t)p.as, some * (int)p.a_total * 4};
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const int r = lrow + 64 * i;
+        for (int i = 0; i < AL; ++i) {
+            const int r = lrow + ROUND * i;
             if (p.a_rows == nullptr) aoff[i] = r * STEP_BYTES + lchunk;
-            else aoff[i] = r < t.valid ? s_tok[lq & 1][r] * STEP_BYTES + lchunk : A_OOB;
+            else aoff[i] = r < t.valid ? s_tok[(lq & 1) * BM + r] * STEP_BYTES + lchunk : A_OOB;
         }
-        asoff = (p.a_rows != nullptr ? s_tok[lq & 1][a_words + lane]
+        asoff = (p.a_rows != nullptr ? s_tok[(lq & 1) * BM + a_words + lane]
                                      : t.row0 + min(a_words + lane, t.valid - 1)) * 4;
         // weight rows past the matrix's, or of the gate half past its own, read as zero
         const int cols = __builtin_amdgcn_readfirstlane(some * max(min(BN_OUT, p.N - t.n0), 0));
@@ -409,16 +419,16 @@ __global__ __launch_bounds__(TILE_THREADS, TM * TN > 8 ? 1 : 2) void tile_mxfp4_
     };
     // direct load i of the stream's next step
     auto load1 = [&](char* st, int i) {
-        if (i < TM) {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(ra), (lds_void*)(st + wave * 1024 + i * 4096), 16,
-                                                     aoff[i], 0, 0, 0);
-        } else if (i < TM + TN) {
-            const int b = i - TM;
-            const bool up = SWIGLU && b >= TN / 2;
+        if (i < AL) {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                rsrc(up ? rhi : rlo), (lds_void*)(st + S::B_CODES + wave * 1024 + b * 4096), 16,
-                boff + (up ? b - TN / 2 : b) * 64 * STEP_BYTES, 0, 0, 0);
-        } else if (i == TM + TN) {
+                rsrc(ra), (lds_void*)(st + (ROUND * i + 16 * wave) * STEP_BYTES), 16, aoff[i], 0, 0, 0);
+        } else if (i < AL + BL) {
+            const int b = i - AL;
+            const bool up = SWIGLU && b >= BL / 2;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                rsrc(up ? rhi : rlo), (lds_void*)(st + S::B_CODES + (ROUND * b + 16 * wave) * STEP_BYTES),
+                16, boff + (up ? b - BL / 2 : b) * ROUND * STEP_BYTES, 0, 0, 0);
+        } else if (i == AL + BL && words_of_a) {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(ras), (lds_void*)(st + S::A_WORDS + a_words * 4),
                                                      4, asoff, 0, 0, 0);
         } else {
@@ -438,7 +448,7 @@ __global__ __launch_bounds__(TILE_THREADS, TM * TN > 8 ? 1 : 2) void tile_mxfp4_
 
     // the products' side: fragment addresses within a step (16-column halves of it by kk)
     const int swz = (r32 >> 2) & 3;
-    const int a_row = wm * (BM / 2) + r32;
+    const int a_row = wm * 32 * TM + r32;
     const int b_row = wn * (SWIGLU ? BN / 4 : BN / 2) + r32;
     auto b_tile = [](int j) { return SWIGLU && j >= TN / 2 ? BN / 2 + (j - TN / 2) * 32 : j * 32; };
     f32x16 acc[TM][TN];                                  // [token tile][weight tile]
@@ -489,20 +499,26 @@ __global__ __launch_bounds__(TILE_THREADS, TM * TN > 8 ? 1 : 2) void tile_mxfp4_
     constexpr std::integral_constant<int, 1> second{};
 
     unsigned step = 0;
+    // a step's loads are issued in two halves of a step of products each: the second of one
+    // step, once the slot is free, and the first of the next
+    constexpr int EARLY = (S::LOADS + 1) / 2;
     for (unsigned s = 0; s < RING; ++s) {
         if (lkt >= p.KT) next_tile();
 #pragma unroll
-        for (int i = 0; i < S::LOADS; ++i) load1(slot(s), i);
+        for (int i = 0; i < EARLY; ++i) load1(slot(s), i);
+        if (s == RING - 1) break;
+#pragma unroll
+        for (int i = EARLY; i < S::LOADS; ++i) load1(slot(s), i);
         next_step();
     }
-    wait_vm<(RING - 1) * S::LOADS>();
+    wait_vm<(RING - 2) * S::LOADS + EARLY>();
     asm volatile("s_barrier" ::: "memory");
 #pragma unroll
     for (int i = 0; i < TM + TN; ++i) {
         read1(slot(0), 0, i);
         read_word(slot(0), i);
     }
-    // stores of an epilogue, which the waits of the next three steps allow for
+    // stores of an epilogue: newer than the loads that the next RING - 2 waits are for
     constexpr int STORES = SWIGLU ? TM * TN / 2 + TM : 2 * TM * TN;
     int fresh = 0;
     for (int q = 0; q < n_list; ++q) {
@@ -517,10 +533,15 @@ __global__ __launch_bounds__(TILE_THREADS, TM * TN > 8 ? 1 : 2) void tile_mxfp4_
             take_words();
 #pragma unroll
             for (int i = 0; i < TM + TN; ++i) {
-                read1(slot(step), 1, i);
+                if (2 * i < TM + TN) {
+                    read1(slot(step), 1, 2 * i);
+                    read1(slot(step), 1, 2 * i + 1);
+                }
+                if (i >= TM + TN - (S::LOADS - EARLY)) load1(slot(step + RING - 1), S::LOADS - (TM + TN) + i);
                 multiply(first, i);
             }
             pin();
+            next_step();
             // the next step has landed: outstanding may be the two after it, and stores
             if (fresh > 0) {
                 wait_vm<(RING - 2) * S::LOADS + STORES>();
@@ -532,20 +553,22 @@ __global__ __launch_bounds__(TILE_THREADS, TM * TN > 8 ? 1 : 2) void tile_mxfp4_
             if (lkt >= p.KT) next_tile();
 #pragma unroll
             for (int i = 0; i < TM + TN; ++i) {
-                read1(slot(step + 1), 0, i);
-                read_word(slot(step + 1), i);
-                load1(slot(step), i);
-                if (i < 2) load1(slot(step), TM + TN + i);
+                if (2 * i < TM + TN) {
+                    read1(slot(step + 1), 0, 2 * i);
+                    read1(slot(step + 1), 0, 2 * i + 1);
+                    read_word(slot(step + 1), 2 * i);
+                    read_word(slot(step + 1), 2 * i + 1);
+                }
+                if (i >= TM + TN - EARLY) load1(slot(step), i - (TM + TN - EARLY));
                 multiply(second, i);
             }
             pin();
-            next_step();
         }
-        fresh = RING - 1;
+        fresh = RING - 2;
 
         // Every store is issued, those past the group's rows or the output's columns dropped
         // by the descriptor: the waits above count them.
-        const int lr = wm * (BM / 2) + r32;
+        const int lr = wm * 32 * TM + r32;
         if (SWIGLU) {
             const int col = cur.n0 + wn * (BN / 4);
             const __amdgpu_buffer_rsrc_t rh = __builtin_amdgcn_make_buffer_rsrc(
@@ -560,13 +583,10 @@ __global__ __launch_bounds__(TILE_THREADS, TM * TN > 8 ? 1 : 2) void tile_mxfp4_
 #pragma unroll
                 for (int j = 0; j < TN / 2; ++j) {
                     float v[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) v[e] = acc[m][j][e];
-                    silu(v);
                     uint32_t most = 0;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        v[e] *= acc[m][TN / 2 + j][e];
+                        v[e] = swiglu(acc[m][j][e], acc[m][TN / 2 + j][e]);
                         most = max(most, __float_as_uint(v[e]) & 0x7fffffffu);
                     }
                     most = max(most, (uint32_t)__shfl_xor((int)most, 32, 64));
@@ -604,14 +624,15 @@ __global__ __launch_bounds__(TILE_THREADS, TM * TN > 8 ? 1 : 2) void tile_mxfp4_
 #endif
 }
 
-template <bool SWIGLU, int TM, int TN, int RING>
+template <bool SWIGLU, int WM, int TM, int TN, int RING>
 int launch_tiles(const MxArgs& p, int cus, hipStream_t s) {
-    constexpr int lds = TileShape<TM, TN, RING>::LDS;
+    typedef TileShape<WM, TM, TN, RING> S;
     static LdsGrant grant;
-    const int st = allow_dynamic_lds((const void*)tile_mxfp4_kernel<SWIGLU, TM, TN, RING>, lds, grant);
+    const int st = allow_dynamic_lds((const void*)tile_mxfp4_kernel<SWIGLU, WM, TM, TN, RING>, S::LDS, grant);
     if (st != MOE_OK) return st;
-    const int grid = cus / NUM_XCD * NUM_XCD * (TM * TN > 8 ? 1 : 2);
-    hipLaunchKernelGGL((tile_mxfp4_kernel<SWIGLU, TM, TN, RING>), dim3(grid), dim3(TILE_THREADS), lds, s, p);
+    const int grid = cus / NUM_XCD * NUM_XCD * (S::PER_EU * 4 / S::WAVES);
+    hipLaunchKernelGGL((tile_mxfp4_kernel<SWIGLU, WM, TM, TN, RING>), dim3(grid), dim3(S::THREADS),
+                       S::LDS, s, p);
     return launch_status();
 }
 
@@ -686,7 +707,7 @@ int launch_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
     const int64_t max_rows = row_token ? T : rows;
     const int cus = num_cus();
     st = max_rows <= STRIP_MAX_ROWS ? launch_strips<true>(p, max_rows, s)
-         : rows * p.N >= LARGE_WORK ? launch_tiles<true, 4, 4, 4>(p, cus, s) : launch_tiles<true, 2, 2, 4>(p, cus, s);
+         : rows * p.N >= LARGE_WORK ? launch_tiles<true, 4, 2, 4, 3>(p, cus, s) : launch_tiles<true, 2, 2, 2, 4>(p, cus, s);
     if (st != MOE_OK) return st;
     for (int i = 0; i < n_groups; ++i) {
         p.w[i] = w2[i];
@@ -702,8 +723,8 @@ int launch_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
     p.y = (bf16_t*)y;
     p.strips = (int)ceil_div(d, STRIP_ROWS);
     return max_rows <= STRIP_MAX_ROWS ? launch_strips<false>(p, max_rows, s)
-           : rows * p.N >= LARGE_WORK ? launch_tiles<false, 4, 4, 4>(p, cus, s)
-                                      : launch_tiles<false, 2, 2, 4>(p, cus, s);
+           : rows * p.N >= LARGE_WORK ? launch_tiles<false, 4, 2, 4, 3>(p, cus, s)
+                                      : launch_tiles<false, 2, 2, 2, 4>(p, cus, s);
 }
 
 }  // namespace moe
