@@ -12,6 +12,7 @@
 // codes a row and then one word of scales a row, rows side by side.  What a product's step
 // needs of a row is then no part of a longer line, half of which the cache would fetch for
 // nothing (256 x 256 tiles over rows as a matrix has them, 128-byte lines: CHANGEME).
+#include <algorithm>
 #include <type_traits>
 
 #include "mxfp4.h"
@@ -45,6 +46,7 @@ struct MxArgs {
     int hp;                              // f padded to 128
     bf16_t* y;                           // down: [rows][d]
     int strips;                          // strips a group
+    int slots;                           // groups that can hold rows at once
 };
 
 __device__ __forceinline__ int first_row(const MxArgs& p, int g) {
@@ -62,153 +64,147 @@ __device__ __forceinline__ float swiglu(float a, float b) {
 }
 
 // ---------------------------------------------------------------------------
-// Strips: groups of few rows, bound by the weight bytes.  A workgroup holds 64 weight rows
-// of one group (32 gate rows and the same up rows: 32 hidden columns, one MXFP4 block) over
-// all of K, eight waves taking every eighth 128-column step: a weight byte goes from
-// memory to the registers of the one wave that multiplies it, no wave waits for another
-// before the end.  The waves' sums meet in LDS, in wave order.
-constexpr int STRIP_WAVES = 8;
-constexpr int STRIP_THREADS = STRIP_WAVES * 64;
-constexpr int STRIP_ROWS = 64;                           // weight rows
-constexpr int STRIP_TILES = STRIP_ROWS / 16;
-constexpr int RED_LD = STRIP_ROWS + 4;                   // floats a row of sums in LDS
-
+// Strips: groups of few rows, bound by the weight bytes.  A workgroup holds 16 TILES weight
+// rows of one group (of gate/up half gate rows, half the same up rows: TILES = 4 makes 32
+// hidden columns, one MXFP4 block) over all of K, its W waves taking every W-th step: a
+// weight byte goes from memory to the registers of the one wave that multiplies it, and no
+// wave waits for another before the end.  The waves' sums meet in LDS, in wave order.
 // MS: 16-row blocks of token rows held at once
-template <int MS>
+template <int MS, int TILES>
 struct StripStep {
-    i32x4 b[STRIP_TILES], a[MS];
-    uint32_t bs[STRIP_TILES], as[MS];
+    i32x4 b[TILES], a[MS];
+    uint32_t bs[TILES], as[MS];
 };
 
-template <bool SWIGLU, int MS>
-__global__ __launch_bounds__(STRIP_THREADS, 2) void strip_mxfp4_kernel(MxArgs p) {
-    constexpr int BM = 16 * MS;
-    constexpr int PARTS = MS == 4 ? 4 : STRIP_WAVES;     // sums in LDS at once (64 KB)
-    __shared__ float red[PARTS][BM][RED_LD];
-    const int g = blockIdx.x / p.strips, strip = blockIdx.x - g * p.strips;
-    const int row0 = first_row(p, g), rows = first_row(p, g + 1) - row0;
-    if (rows <= 0) return;
+// The rows of a group, 16 MS at a time; row0, rows: of the group.  D steps of loads are in
+// flight (past the end of K without traffic: every wait counts the same loads).
+template <bool SWIGLU, int W, int TILES, int MS, int D>
+__device__ __forceinline__ void strip_rows(const MxArgs& p, float* red, int g, int n0, int row0,
+                                           int rows) {
+#ifdef __HIP_DEVICE_COMPILE__
+    constexpr int ROWS = 16 * TILES, LD = ROWS + 4, BM = 16 * MS;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int i16 = lane & 15, quarter = lane >> 4;
-    const int n0 = strip * (SWIGLU ? STRIP_ROWS / 2 : STRIP_ROWS);
     // weight rows of the strip: past the matrix's (or, of the gate half, past its N)
-    // columns they read as zero; the scale words start at the strip's first row
-    const int valid = min(SWIGLU ? STRIP_ROWS / 2 : STRIP_ROWS, p.N - n0);
-    auto rsrc = [&](int t, int first) {
-        return __builtin_amdgcn_make_buffer_rsrc(
-            (void*)(p.w[g] + ((int64_t)t * p.w_rows + first) * STEP_BYTES), (short)0,
-            max(valid, 0) * STEP_BYTES, RSRC_WORD3);
-    };
-    const uint32_t* wsc = p.ws[g];
-    int boff[STRIP_TILES], bsrow[STRIP_TILES];
+    // columns they read as zero; their scales are some row's
+    const int valid = max(min(SWIGLU ? ROWS / 2 : ROWS, p.N - n0), 0);
+    int boff[TILES], bsoff[TILES];
 #pragma unroll
-    for (int j = 0; j < STRIP_TILES; ++j) {
-        const int r = (SWIGLU && j >= STRIP_TILES / 2 ? j - STRIP_TILES / 2 : j) * 16 + i16;
+    for (int j = 0; j < TILES; ++j) {
+        const bool up = SWIGLU && j >= TILES / 2;
+        const int r = (up ? j - TILES / 2 : j) * 16 + i16;
         boff[j] = r * STEP_BYTES + quarter * 16;
-        // a row past the end has zero codes: any scale of the matrix does
-        bsrow[j] = (SWIGLU && j >= STRIP_TILES / 2 ? p.N : 0) + min(n0 + r, p.N - 1);
+        bsoff[j] = ((up ? p.N : 0) + min(n0 + r, p.N - 1)) * 4;
     }
-
+    auto rsrc = [](const void* base, int bytes) {
+        return __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, bytes, RSRC_WORD3);
+    };
     for (int m0 = 0; m0 < rows; m0 += BM) {
         // rows past the group repeat its last one; their sums are not stored
-        const uint8_t* ap[MS];
-        int64_t arow[MS];
+        int aoff[MS], asoff[MS];
 #pragma unroll
         for (int m = 0; m < MS; ++m) {
-            const int r = row0 + min(m0 + 16 * m + i16, rows - 1);
-            arow[m] = p.a_rows ? p.a_rows[r] : r;
-            ap[m] = p.a + arow[m] * STEP_BYTES + quarter * 16;
+            const int r = min(m0 + 16 * m + i16, rows - 1);
+            const int row = p.a_rows ? p.a_rows[row0 + r] : r;
+            aoff[m] = row * STEP_BYTES + quarter * 16;
+            asoff[m] = row * 4;
         }
-        f32x4 acc[MS][STRIP_TILES];
+        const int64_t first = p.a_rows ? 0 : row0;
+        const int reach = p.a_rows ? (int)p.a_total : rows;
+        f32x4 acc[MS][TILES];
 #pragma unroll
         for (int m = 0; m < MS; ++m)
 #pragma unroll
-            for (int j = 0; j < STRIP_TILES; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        auto load = [&](StripStep<MS>& s, int t) {
-            const auto lo = rsrc(t, n0), hi = rsrc(t, SWIGLU ? p.N + n0 : n0);
+            for (int j = 0; j < TILES; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        auto load = [&](StripStep<MS, TILES>& s, int t) {
+            const int live = t < p.KT ? 1 : 0;
+            const int64_t brow = (int64_t)t * p.w_rows, arow = t * p.a_total + first;
+            const auto lo = rsrc(p.w[g] + (brow + n0) * STEP_BYTES, live * valid * STEP_BYTES);
+            const auto hi = rsrc(p.w[g] + (brow + (SWIGLU ? p.N + n0 : n0)) * STEP_BYTES,
+                                 live * valid * STEP_BYTES);
+            const auto bs = rsrc(p.ws[g] + brow, live * p.w_rows * 4);
+            const auto a = rsrc(p.a + arow * STEP_BYTES, live * reach * STEP_BYTES);
+            const auto as = rsrc(p.as + arow, live * reach * 4);
 #pragma unroll
-            for (int j = 0; j < STRIP_TILES; ++j) {
+            for (int j = 0; j < TILES; ++j)
                 s.b[j] = __builtin_bit_cast(
-                    i32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                               SWIGLU && j >= STRIP_TILES / 2 ? hi : lo, boff[j], 0, 0));
-                s.bs[j] = wsc[(int64_t)t * p.w_rows + bsrow[j]];
-            }
+                    i32x4, __builtin_amdgcn_raw_buffer_load_b128(SWIGLU && j >= TILES / 2 ? hi : lo,
+                                                                 boff[j], 0, 0));
+#pragma unroll
+            for (int j = 0; j < TILES; ++j)
+                s.bs[j] = __builtin_amdgcn_raw_buffer_load_b32(bs, bsoff[j], 0, 0);
 #pragma unroll
             for (int m = 0; m < MS; ++m) {
-                s.a[m] = *(const i32x4*)(ap[m] + t * p.a_total * STEP_BYTES);
-                s.as[m] = p.as[t * p.a_total + arow[m]];
+                s.a[m] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(a, aoff[m], 0, 0));
+                s.as[m] = __builtin_amdgcn_raw_buffer_load_b32(as, asoff[m], 0, 0);
             }
         };
         // the weights are the matrix instruction's first operand: a lane then holds four
         // consecutive output columns of one row.  A lane's block of 32 is the word's byte
         // `quarter`
-        auto multiply = [&](const StripStep<MS>& s) {
-            uint32_t sa[MS], sb[STRIP_TILES];
+        auto multiply = [&](const StripStep<MS, TILES>& s) {
+            uint32_t sa[MS];
 #pragma unroll
             for (int m = 0; m < MS; ++m) sa[m] = s.as[m] >> (8 * quarter);
 #pragma unroll
-            for (int j = 0; j < STRIP_TILES; ++j) sb[j] = s.bs[j] >> (8 * quarter);
-#pragma unroll
-            for (int j = 0; j < STRIP_TILES; ++j)
+            for (int j = 0; j < TILES; ++j) {
+                const uint32_t sb = s.bs[j] >> (8 * quarter);
 #pragma unroll
                 for (int m = 0; m < MS; ++m)
                     acc[m][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                        operand(s.b[j]), operand(s.a[m]), acc[m][j], 4, 4, 0, (int)sb[j], 0,
-                        (int)sa[m]);
-        };
-        // two steps of loads in flight
-        StripStep<MS> s0, s1;
-        int t = wave;
-        if (t < p.KT) load(s0, t);
-        if (t + STRIP_WAVES < p.KT) load(s1, t + STRIP_WAVES);
-        for (; t < p.KT; t += 2 * STRIP_WAVES) {
-            multiply(s0);
-            if (t + 2 * STRIP_WAVES < p.KT) load(s0, t + 2 * STRIP_WAVES);
-            if (t + STRIP_WAVES < p.KT) {
-                multiply(s1);
-                if (t + 3 * STRIP_WAVES < p.KT) load(s1, t + 3 * STRIP_WAVES);
+                        operand(s.b[j]), operand(s.a[m]), acc[m][j], 4, 4, 0, (int)sb, 0, (int)sa[m]);
             }
-        }
+        };
+        StripStep<MS, TILES> s[D];
+#pragma unroll
+        for (int i = 0; i < D; ++i) load(s[i], wave + i * W);
+        for (int t = wave; t < p.KT; t += D * W)
+#pragma unroll
+            for (int i = 0; i < D; ++i) {
+                multiply(s[i]);
+                load(s[i], t + (i + D) * W);
+            }
 
+        constexpr int PARTS = W * BM * LD * 4 > 70 * 1024 ? W / 2 : W;   // sums in LDS at once
         auto at = [&](int part, int m, int j) {
-            return (f32x4*)&red[part][16 * m + i16][16 * j + 4 * quarter];
+            return (f32x4*)&red[(part * BM + 16 * m + i16) * LD + 16 * j + 4 * quarter];
         };
         __syncthreads();                                 // the last row block's sums are read
-        if (PARTS < STRIP_WAVES) {
+        if (PARTS < W) {
             if (wave >= PARTS)
 #pragma unroll
                 for (int m = 0; m < MS; ++m)
 #pragma unroll
-                    for (int j = 0; j < STRIP_TILES; ++j) *at(wave - PARTS, m, j) = acc[m][j];
+                    for (int j = 0; j < TILES; ++j) *at(wave - PARTS, m, j) = acc[m][j];
             __syncthreads();
             if (wave < PARTS)
 #pragma unroll
                 for (int m = 0; m < MS; ++m)
 #pragma unroll
-                    for (int j = 0; j < STRIP_TILES; ++j) acc[m][j] += *at(wave, m, j);
+                    for (int j = 0; j < TILES; ++j) acc[m][j] += *at(wave, m, j);
             __syncthreads();
         }
         if (wave < PARTS)
 #pragma unroll
             for (int m = 0; m < MS; ++m)
 #pragma unroll
-                for (int j = 0; j < STRIP_TILES; ++j) *at(wave, m, j) = acc[m][j];
+                for (int j = 0; j < TILES; ++j) *at(wave, m, j) = acc[m][j];
         __syncthreads();
         // four output columns a thread
-        constexpr int PER_ROW = (SWIGLU ? STRIP_ROWS / 2 : STRIP_ROWS) / 4;
-        for (int i = tid; i < BM * PER_ROW; i += STRIP_THREADS) {
+        constexpr int PER_ROW = (SWIGLU ? ROWS / 2 : ROWS) / 4;
+        for (int i = tid; i < BM * PER_ROW; i += 64 * W) {
             const int r = i / PER_ROW, c = (i % PER_ROW) * 4;
             auto sum = [&](int col) {
-                f32x4 v = *(const f32x4*)&red[0][r][col];
+                f32x4 v = *(const f32x4*)&red[r * LD + col];
 #pragma unroll
-                for (int q = 1; q < PARTS; ++q) v += *(const f32x4*)&red[q][r][col];
+                for (int q = 1; q < PARTS; ++q) v += *(const f32x4*)&red[(q * BM + r) * LD + col];
                 return v;
             };
             const int row = row0 + m0 + r;
             const bool live = m0 + r < rows;
             if (SWIGLU) {
-                const f32x4 a = sum(c), b = sum(STRIP_ROWS / 2 + c);
+                const f32x4 a = sum(c), b = sum(ROWS / 2 + c);
                 float v[4];
                 uint32_t most = 0;
 #pragma unroll
@@ -220,10 +216,10 @@ __global__ __launch_bounds__(STRIP_THREADS, 2) void strip_mxfp4_kernel(MxArgs p)
                 most = quad_max(most);
                 most = max(most, (uint32_t)__shfl_xor((int)most, 4, 64));
                 const uint32_t byte = mx_byte(most);
-                const float s = mx_factor(byte);
+                const float f = mx_factor(byte);
                 uint32_t w = 0;
-                w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0] * s, v[1] * s, 1.0f, 0);
-                w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2] * s, v[3] * s, 1.0f, 1);
+                w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0] * f, v[1] * f, 1.0f, 0);
+                w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2] * f, v[3] * f, 1.0f, 1);
                 if (byte == 255u) w = 0;
                 if (live) {
                     *(uint16_t*)(p.h + ((int64_t)(n0 >> 7) * p.h_rows + row) * STEP_BYTES +
@@ -239,6 +235,46 @@ __global__ __launch_bounds__(STRIP_THREADS, 2) void strip_mxfp4_kernel(MxArgs p)
             }
         }
     }
+#endif
+}
+
+// The n-th group that holds rows, or -1 (a call of fewer rows than groups launches strips
+// for as many groups as it has rows: a single token's step over 64 experts of which it
+// takes 6 starts 264 workgroups, not 2816).
+__device__ __forceinline__ int nth_group(const MxArgs& p, int n) {
+    const int lane = threadIdx.x & 63;
+    for (int g0 = 0; g0 < p.n_groups; g0 += 64) {
+        const int g = g0 + lane;
+        const bool some = g < p.n_groups && first_row(p, g + 1) > first_row(p, g);
+        uint64_t mask = __ballot(some);
+        const int here = __popcll(mask);
+        if (n < here) {
+            for (; n > 0; --n) mask &= mask - 1;
+            return g0 + __builtin_ctzll(mask);
+        }
+        n -= here;
+    }
+    return -1;
+}
+
+// MAX_MS = 1: no group holds more than 16 rows, and the registers of one row block let
+// twice the waves in.  Otherwise each group takes the row blocks it needs.
+template <bool SWIGLU, int W, int TILES, int MAX_MS>
+__global__ __launch_bounds__(64 * W, MAX_MS == 1 ? 4 : 2) void strip_mxfp4_kernel(MxArgs p) {
+    constexpr int LD = 16 * TILES + 4;
+    constexpr int SUMS = W * 16 * MAX_MS * LD * 4 > 70 * 1024 ? W / 2 * 16 * MAX_MS * LD : W * 16 * MAX_MS * LD;
+    __shared__ __attribute__((aligned(16))) float red[SUMS];
+    const int slot = blockIdx.x / p.strips;
+    const int n0 = ((int)blockIdx.x - slot * p.strips) * 16 * TILES / (SWIGLU ? 2 : 1);
+    const int g = p.slots < p.n_groups ? nth_group(p, slot) : slot;
+    if (g < 0) return;
+    const int row0 = __builtin_amdgcn_readfirstlane(first_row(p, g));
+    const int rows = __builtin_amdgcn_readfirstlane(first_row(p, g + 1)) - row0;
+    if (rows <= 0) return;
+    constexpr int D1 = MAX_MS == 1 ? (TILES == 4 ? 3 : 4) : (TILES == 4 ? 3 : 4);
+    if (MAX_MS == 1 || rows <= 16) strip_rows<SWIGLU, W, TILES, 1, D1>(p, red, g, n0, row0, rows);
+    else if (rows <= 32) strip_rows<SWIGLU, W, TILES, 2, TILES == 4 ? 3 : 4>(p, red, g, n0, row0, rows);
+    else strip_rows<SWIGLU, W, TILES, 4, TILES == 4 ? 2 : 3>(p, red, g, n0, row0, rows);
 }
 
 // ---------------------------------------------------------------------------
@@ -636,19 +672,31 @@ int launch_tiles(const MxArgs& p, int cus, hipStream_t s) {
     return launch_status();
 }
 
-template <bool SWIGLU>
-int launch_strips(const MxArgs& p, int64_t max_rows, hipStream_t s) {
-    const dim3 grid((unsigned)(p.n_groups * p.strips)), block(STRIP_THREADS);
+template <bool SWIGLU, int W, int TILES>
+int launch_strips_of(MxArgs& p, int64_t max_rows, hipStream_t s) {
+    p.strips = (int)ceil_div(SWIGLU ? 2 * p.hp : p.N, 16 * TILES);
+    const dim3 grid((unsigned)(p.slots * p.strips)), block(64 * W);
     if (max_rows <= 16)
-        hipLaunchKernelGGL((strip_mxfp4_kernel<SWIGLU, 1>), grid, block, 0, s, p);
-    else if (max_rows <= 32)
-        hipLaunchKernelGGL((strip_mxfp4_kernel<SWIGLU, 2>), grid, block, 0, s, p);
+        hipLaunchKernelGGL((strip_mxfp4_kernel<SWIGLU, W, TILES, 1>), grid, block, 0, s, p);
     else
-        hipLaunchKernelGGL((strip_mxfp4_kernel<SWIGLU, 4>), grid, block, 0, s, p);
+        hipLaunchKernelGGL((strip_mxfp4_kernel<SWIGLU, W, TILES, 4>), grid, block, 0, s, p);
     return launch_status();
 }
 
-constexpr int64_t STRIP_MAX_ROWS = 64;
+// Two waves a strip where there are strips enough to fill the chip (64 DeepSeek-V2-Lite-
+// shaped experts, 64 tokens: FFN 63 us with four, 52 with two), else four (Mixtral-shaped
+// down product, 64 tokens, 128 strips: 31 us with two, 20 with four), of half the weight
+// rows where that still leaves CUs without one (17).
+template <bool SWIGLU>
+int launch_strips(MxArgs& p, int64_t max_rows, int cus, hipStream_t s) {
+    const int64_t n = p.slots * ceil_div(SWIGLU ? 2 * p.hp : p.N, 64);
+    if (n >= 4 * cus) return launch_strips_of<SWIGLU, 2, 4>(p, max_rows, s);
+    if constexpr (!SWIGLU)
+        if (n < 2 * cus) return launch_strips_of<false, 4, 2>(p, max_rows, s);
+    return launch_strips_of<SWIGLU, 4, 4>(p, max_rows, s);
+}
+
+constexpr int64_t STRIP_MAX_ROWS = 128;
 constexpr int64_t LARGE_WORK = (int64_t)256 * 256 * 256;
 
 int64_t align256(int64_t x) { return (x + 255) & ~(int64_t)255; }
@@ -688,6 +736,7 @@ int launch_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
     }
     p.offsets = offsets;
     p.n_groups = n_groups;
+    p.slots = (int)std::min<int64_t>(n_groups, rows);
     p.lead = lead;
     p.lead_rows = lead_rows;
     p.a = (const uint8_t*)base;
@@ -702,11 +751,10 @@ int launch_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
     p.h_rows = rows;
     p.hp = (int)mx_cols(f);
     p.y = nullptr;
-    p.strips = p.hp / (STRIP_ROWS / 2);
     // a token reaches an expert at most once
     const int64_t max_rows = row_token ? T : rows;
     const int cus = num_cus();
-    st = max_rows <= STRIP_MAX_ROWS ? launch_strips<true>(p, max_rows, s)
+    st = max_rows <= STRIP_MAX_ROWS ? launch_strips<true>(p, max_rows, cus, s)
          : rows * p.N >= LARGE_WORK ? launch_tiles<true, 4, 2, 4, 3>(p, cus, s) : launch_tiles<true, 2, 2, 2, 4>(p, cus, s);
     if (st != MOE_OK) return st;
     for (int i = 0; i < n_groups; ++i) {
@@ -721,8 +769,7 @@ int launch_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
     p.N = d;
     p.w_rows = d;
     p.y = (bf16_t*)y;
-    p.strips = (int)ceil_div(d, STRIP_ROWS);
-    return max_rows <= STRIP_MAX_ROWS ? launch_strips<false>(p, max_rows, s)
+    return max_rows <= STRIP_MAX_ROWS ? launch_strips<false>(p, max_rows, cus, s)
            : rows * p.N >= LARGE_WORK ? launch_tiles<false, 4, 2, 4, 3>(p, cus, s)
                                       : launch_tiles<false, 2, 2, 2, 4>(p, cus, s);
 }

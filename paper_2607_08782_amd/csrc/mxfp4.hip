@@ -75,14 +75,11 @@ struct Place {
     }
 };
 
-// STEPS: step-major codes and scale words (a word is the bytes of 16 lanes' pieces) rather
-// than row-major.
-template <typename T, Form F, bool STEPS>
+template <typename T, Form F>
 __global__ __launch_bounds__(MX_THREADS) void quantize_mxfp4_kernel(const T* __restrict__ x,
                                                                     int64_t pieces, int cols,
                                                                     uint32_t* __restrict__ codes,
-                                                                    uint8_t* __restrict__ scales,
-                                                                    int64_t rows) {
+                                                                    uint8_t* __restrict__ scales) {
     const int64_t base = (int64_t)blockIdx.x * MX_PIECES;
     const Place place(base, cols);
     float v[MX_UNROLL][8];
@@ -115,18 +112,29 @@ __global__ __launch_bounds__(MX_THREADS) void quantize_mxfp4_kernel(const T* __r
         const uint32_t most = quad_max(magnitude8(v[u]));
         const uint32_t w = mx_encode8(v[u], most, byte);
         if (i < pieces) {
-            if (!STEPS) {
-                codes[i] = w;
-                if ((threadIdx.x & 3) == 0) scales[i >> 2] = (uint8_t)byte;
-            } else {
-                const uint32_t o = place.first + u * MX_THREADS + threadIdx.x, r = o / place.per_row;
-                const uint32_t piece = o - r * place.per_row;
-                const int64_t at = (int64_t)(piece >> 4) * rows + place.row0 + r;
-                codes[at * 16 + (piece & 15)] = w;
-                if ((threadIdx.x & 3) == 0) scales[at * 4 + ((piece >> 2) & 3)] = (uint8_t)byte;
-            }
+            codes[i] = w;
+            if ((threadIdx.x & 3) == 0) scales[i >> 2] = (uint8_t)byte;
         }
     }
+}
+
+// Token rows, step-major: a row per workgroup (and 2048 columns of it), so that no piece
+// needs a division, and a short batch is spread over the chip.
+__global__ __launch_bounds__(MX_THREADS) void quantize_steps_kernel(const bf16_t* __restrict__ x,
+                                                                    int64_t rows, int cols,
+                                                                    uint32_t* __restrict__ codes,
+                                                                    uint8_t* __restrict__ scales) {
+    const int64_t row = blockIdx.x;
+    const int piece = blockIdx.y * MX_THREADS + threadIdx.x;
+    if (piece >= (int)(mx_cols(cols) / 8)) return;       // whole quads
+    float v[8] = {};
+    if (piece * 8 < cols) Elem<bf16_t>::load8(x + row * cols + piece * 8, v);
+    uint32_t byte;
+    const uint32_t most = quad_max(magnitude8(v));
+    const uint32_t w = mx_encode8(v, most, byte);
+    const int64_t at = (piece >> 4) * rows + row;
+    codes[at * 16 + (piece & 15)] = w;
+    if ((threadIdx.x & 3) == 0) scales[at * 4 + ((piece >> 2) & 3)] = (uint8_t)byte;
 }
 
 template <typename T, Form F>
@@ -210,13 +218,13 @@ Form form_of(const void* p, int cols) {
     return cols % 128 ? PADDED : DENSE;
 }
 
-template <bool STEPS, typename T>
+template <typename T>
 int quantize(const T* x, int64_t rows, int cols, uint8_t* codes, uint8_t* scales, hipStream_t s) {
     const int64_t pieces = rows * (mx_cols(cols) / 8);
     const dim3 grid((unsigned)ceil_div(pieces, MX_PIECES)), block(MX_THREADS);
 #define MOE_MXQ(F)                                                                             \
-    hipLaunchKernelGGL((quantize_mxfp4_kernel<T, F, STEPS>), grid, block, 0, s, x, pieces,     \
-                       cols, (uint32_t*)codes, scales, rows)
+    hipLaunchKernelGGL((quantize_mxfp4_kernel<T, F>), grid, block, 0, s, x, pieces,     \
+                       cols, (uint32_t*)codes, scales)
     switch (form_of(x, cols)) {
         case DENSE: MOE_MXQ(DENSE); break;
         case PADDED: MOE_MXQ(PADDED); break;
@@ -248,14 +256,17 @@ int dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int co
 int launch_quantize_mxfp4(const void* x, int dtype, int64_t rows, int cols, uint8_t* codes,
                           uint8_t* scales, hipStream_t s) {
     if (rows == 0) return MOE_OK;
-    return dtype == MOE_BF16 ? quantize<false>((const bf16_t*)x, rows, cols, codes, scales, s)
-                             : quantize<false>((const float*)x, rows, cols, codes, scales, s);
+    return dtype == MOE_BF16 ? quantize((const bf16_t*)x, rows, cols, codes, scales, s)
+                             : quantize((const float*)x, rows, cols, codes, scales, s);
 }
 
 int launch_quantize_mxfp4_steps(const bf16_t* x, int64_t rows, int cols, uint8_t* codes,
                                 uint32_t* words, hipStream_t s) {
     if (rows == 0) return MOE_OK;
-    return quantize<true>(x, rows, cols, codes, (uint8_t*)words, s);
+    const dim3 grid((unsigned)rows, (unsigned)ceil_div(mx_cols(cols) / 8, MX_THREADS));
+    hipLaunchKernelGGL(quantize_steps_kernel, grid, dim3(MX_THREADS), 0, s, x, rows, cols,
+                       (uint32_t*)codes, (uint8_t*)words);
+    return launch_status();
 }
 
 int launch_mxfp4_lay_out(const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols,
