@@ -238,23 +238,28 @@ __device__ __forceinline__ void strip_rows(const MxArgs& p, float* red, int g, i
 #endif
 }
 
-// The n-th group that holds rows, or -1 (a call of fewer rows than groups launches strips
-// for as many groups as it has rows: a single token's step over 64 experts of which it
-// takes 6 starts 264 workgroups, not 2816).
-__device__ __forceinline__ int nth_group(const MxArgs& p, int n) {
+// The n-th group that holds rows, its first row and their number (a call of fewer rows than
+// groups launches strips for as many groups as it has rows: a single token's step over 64
+// experts of which it takes 6 starts 264 workgroups, not 2816).
+struct Group {
+    int g, row0, rows;
+};
+
+__device__ __forceinline__ Group nth_group(const MxArgs& p, int n) {
     const int lane = threadIdx.x & 63;
     for (int g0 = 0; g0 < p.n_groups; g0 += 64) {
-        const int g = g0 + lane;
-        const bool some = g < p.n_groups && first_row(p, g + 1) > first_row(p, g);
-        uint64_t mask = __ballot(some);
+        const int g = min(g0 + lane, p.n_groups - 1);
+        const int row0 = first_row(p, g), rows = first_row(p, g + 1) - row0;
+        uint64_t mask = __ballot(g0 + lane < p.n_groups && rows > 0);
         const int here = __popcll(mask);
         if (n < here) {
             for (; n > 0; --n) mask &= mask - 1;
-            return g0 + __builtin_ctzll(mask);
+            const int l = __builtin_ctzll(mask);
+            return {g0 + l, __builtin_amdgcn_readlane(row0, l), __builtin_amdgcn_readlane(rows, l)};
         }
         n -= here;
     }
-    return -1;
+    return {0, 0, 0};
 }
 
 // MAX_MS = 1: no group holds more than 16 rows, and the registers of one row block let
@@ -266,15 +271,19 @@ __global__ __launch_bounds__(64 * W, MAX_MS == 1 ? 4 : 2) void strip_mxfp4_kerne
     __shared__ __attribute__((aligned(16))) float red[SUMS];
     const int slot = blockIdx.x / p.strips;
     const int n0 = ((int)blockIdx.x - slot * p.strips) * 16 * TILES / (SWIGLU ? 2 : 1);
-    const int g = p.slots < p.n_groups ? nth_group(p, slot) : slot;
-    if (g < 0) return;
-    const int row0 = __builtin_amdgcn_readfirstlane(first_row(p, g));
-    const int rows = __builtin_amdgcn_readfirstlane(first_row(p, g + 1)) - row0;
-    if (rows <= 0) return;
+    Group of;
+    if (p.slots < p.n_groups) {
+        of = nth_group(p, slot);
+    } else {
+        of.g = slot;
+        of.row0 = __builtin_amdgcn_readfirstlane(first_row(p, slot));
+        of.rows = __builtin_amdgcn_readfirstlane(first_row(p, slot + 1)) - of.row0;
+    }
+    if (of.rows <= 0) return;
     constexpr int D1 = MAX_MS == 1 ? (TILES == 4 ? 3 : 4) : (TILES == 4 ? 3 : 4);
-    if (MAX_MS == 1 || rows <= 16) strip_rows<SWIGLU, W, TILES, 1, D1>(p, red, g, n0, row0, rows);
-    else if (rows <= 32) strip_rows<SWIGLU, W, TILES, 2, TILES == 4 ? 3 : 4>(p, red, g, n0, row0, rows);
-    else strip_rows<SWIGLU, W, TILES, 4, TILES == 4 ? 2 : 3>(p, red, g, n0, row0, rows);
+    if (MAX_MS == 1 || of.rows <= 16) strip_rows<SWIGLU, W, TILES, 1, D1>(p, red, of.g, n0, of.row0, of.rows);
+    else if (of.rows <= 32) strip_rows<SWIGLU, W, TILES, 2, TILES == 4 ? 3 : 4>(p, red, of.g, n0, of.row0, of.rows);
+    else strip_rows<SWIGLU, W, TILES, 4, TILES == 4 ? 2 : 3>(p, red, of.g, n0, of.row0, of.rows);
 }
 
 // ---------------------------------------------------------------------------

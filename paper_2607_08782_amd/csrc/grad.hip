@@ -2,6 +2,8 @@
 // gates and gate scores (moe_route_topk_backward).  The gradient of the packaging is the
 // combine's sum with weights 1 (combine.hip).  Nothing is added by atomics: every sum has
 // one owner and a fixed order.
+#include <algorithm>
+
 #include "common.h"
 
 namespace moe {
@@ -174,22 +176,19 @@ int combine_backward(const void* dy, const void* y_perm, const int32_t* token_ro
 // ---------------------------------------------------------------------------
 // Gradient of the gates and gate scores.
 
-// dlogits of RT tokens a workgroup, a token per wave at a time; lane l holds experts l,
-// l + 64, ...  Beside the dense rows, the chosen experts' values [T][k] (sel) and the
-// workgroup's column sums (part).
+// dlogits, a token per wave at a time; lane l holds experts l, l + 64, ...  Beside the dense
+// rows, with MOE_RENORM, the chosen experts' values [T][k] (sel).
 constexpr int RB_THREADS = 256;
-constexpr int RT = 16;
+constexpr int RT = 16;                                   // tokens per workgroup
 constexpr int RJ = MOE_MAX_E / 64;
 
 template <bool RENORM>
 __global__ __launch_bounds__(RB_THREADS) void gate_backward_kernel(
     const float* __restrict__ dgate, const float* __restrict__ gate, const int32_t* __restrict__ idx,
     const float* __restrict__ logits, int64_t T, int E, int k, float* __restrict__ dlogits,
-    float* __restrict__ sel, float* __restrict__ part) {
-    __shared__ float sums[RB_THREADS / 64][MOE_MAX_E];
+    float* __restrict__ sel) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    float total[RJ] = {};
 #pragma unroll
     for (int i = 0; i < RT / (RB_THREADS / 64); ++i) {
         const int64_t t = (int64_t)blockIdx.x * RT + i * (RB_THREADS / 64) + wave;
@@ -243,112 +242,309 @@ __global__ __launch_bounds__(RB_THREADS) void gate_backward_kernel(
 #pragma unroll
         for (int j = 0; j < RJ; ++j) {
             if (dlogits && lane + 64 * j < E) dlogits[t * E + lane + 64 * j] = v[j];
-            total[j] += v[j];
         }
     }
-    if (!part) return;
-#pragma unroll
-    for (int j = 0; j < RJ; ++j) sums[wave][lane + 64 * j] = total[j];
-    __syncthreads();
-    for (int e = threadIdx.x; e < E; e += RB_THREADS) {
-        float v = sums[0][e];
-#pragma unroll
-        for (int q = 1; q < RB_THREADS / 64; ++q) v += sums[q][e];
-        part[(int64_t)blockIdx.x * E + e] = v;
-    }
 }
 
-// Four consecutive values of a row from column c on, zero past `cols`.
-template <typename Elem>
-__device__ __forceinline__ f32x4 load4(const Elem* row, int c, int cols);
-template <>
-__device__ __forceinline__ f32x4 load4<float>(const float* row, int c, int cols) {
-    f32x4 v;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = c + i < cols ? row[c + i] : 0.f;
-    return v;
-}
-template <>
-__device__ __forceinline__ f32x4 load4<bf16_t>(const bf16_t* row, int c, int cols) {
+// Four consecutive values of a row of scores from column e on, zero past E; VEC: E is a
+// multiple of 4 and rows are 16-byte aligned.
+template <bool VEC>
+__device__ __forceinline__ f32x4 scores4(const float* row, int e, int E) {
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (c < cols) {                                      // cols % 8 == 0
-        const uint2 u = *(const uint2*)(row + c);
-        v = f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u),
-                  __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u)};
+    if (VEC) {
+        if (e < E) v = *(const f32x4*)(row + e);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (e + i < E) v[i] = row[e + i];
     }
     return v;
 }
 
-// dw[e][c] = sum_t dlogits[t][e] x[t][c] by v_mfma_f32_16x16x4_f32: a wave holds 64 x 64
-// of it, the four values a lane loads of a row (experts 4 i .. of dlogits, columns 4 i ..
-// of x) being its elements of four operands, so both matrices are read as they lie.  A
-// workgroup takes one chunk of the tokens, a quarter of it per wave, summed in LDS.
-constexpr int GT = 64;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-template <typename Elem>
-__global__ __launch_bounds__(256) void router_grad_kernel(const float* __restrict__ dlogits,
-                                                          const Elem* __restrict__ x, int64_t T,
-                                                          int d, int E, int64_t chunk,
-                                                          float* __restrict__ out) {
-    __shared__ f32x4 red[3][4][4][64];
+// Eight fp32 values as N bf16 terms each (their sum: 8 N significant bits), packed.
+template <int N>
+__device__ __forceinline__ void split8(const float (&x)[8], u32x4 (&out)[N]) {
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = x[i];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = pack_bf16x2(r[2 * i], r[2 * i + 1]);
+            out[n][i] = w;
+            r[2 * i] -= __uint_as_float(w << 16);        // exact
+            r[2 * i + 1] -= __uint_as_float(w & 0xffff0000u);
+        }
+}
+
+// Column c (0..7) of eight rows of eight bf16 values: a matrix operand of eight
+// consecutive k, where the rows are k.
+__device__ __forceinline__ bf16x8 column(const u32x4 (&row)[8], int c) {
+    u32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        v[i] = __builtin_amdgcn_perm(row[2 * i + 1][c / 2], row[2 * i][c / 2],
+                                     c & 1 ? 0x07060302u : 0x05040100u);
+    return __builtin_bit_cast(bf16x8, v);
+}
+
+// dw[e][c] = sum_t dlogits[t][e] x[t][c], and dbias.  A wave holds 64 experts x 128 columns.
+// Lane (i, q) of it loads, for eight tokens 8 q .. 8 q + 7 of a step of 32, four experts 4 i
+// .. of dlogits and eight columns 8 i .. of x as they lie: its own elements, over eight
+// consecutive k, of four operands of the one side and eight of the other (a transpose within
+// the lane).  bf16 x: v_mfma_f32_16x16x32_bf16 over dlogits in three bf16 terms, which keep
+// all 24 bits, at a third of the rate of the bf16 instruction and five times that of the
+// fp32 one, which serves fp32 x.  Eight waves: blocks of 64 experts (one, two or four), and
+// tokens among the rest; a workgroup takes one chunk of the tokens, its waves' sums meet in
+// LDS in a fixed tree, and the chunks' in sum_parts_kernel in order.
+constexpr int DW_THREADS = 512;
+constexpr int DW_COLS = 128;
+constexpr int DW_STEP = 32;
+
+struct DwArgs {
+    const float* dl;
+    const void* x;
+    int64_t T, chunk;                                    // tokens, tokens per workgroup
+    int d, E, eb;                                        // eb: expert blocks of a workgroup
+    float* dw;                                           // [chunks][E][d], nullable
+    float* dbias;                                        // [chunks][E], nullable
+};
+
+template <typename Elem, bool VEC>
+__global__ __launch_bounds__(DW_THREADS, 2) void router_grad_kernel(DwArgs p) {
+    constexpr bool BF16 = sizeof(Elem) == 2;
+    __shared__ f32x4 red[4][4][4][64];
     const int lane = threadIdx.x & 63, i16 = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int c0 = blockIdx.x * GT + 4 * i16, e0 = blockIdx.y * GT + 4 * i16;
-    const int64_t begin = (int64_t)blockIdx.z * chunk, end = begin + chunk < T ? begin + chunk : T;
-    f32x4 acc[4][4];
+    const int ts_n = 8 / p.eb, block = wave / ts_n, ts = wave % ts_n;
+    const int e0 = block * 64 + 4 * i16, c0 = blockIdx.x * DW_COLS + 8 * i16;
+    const int64_t begin = (int64_t)blockIdx.y * p.chunk;
+    const int64_t end = begin + p.chunk < p.T ? begin + p.chunk : p.T;
+    const bool sums = p.dbias != nullptr && blockIdx.x == 0;
+    f32x4 acc[4][8], bias = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int m = 0; m < 4; ++m)
 #pragma unroll
-        for (int n = 0; n < 4; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // a step of four tokens, one per quarter
-    for (int64_t t0 = begin + 4 * wave; t0 < end; t0 += 16) {
-        const int64_t t = t0 + quarter;
-        f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
-        if (t < end) {
-            a = load4<float>(dlogits + t * E, e0, E);
-            b = load4<Elem>(x + t * d, c0, d);
+        for (int n = 0; n < 8; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int64_t t0 = begin + DW_STEP * ts; t0 < end; t0 += DW_STEP * ts_n) {
+        const int64_t t = t0 + 8 * quarter;
+        f32x4 a[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            a[j] = t + j < end ? scores4<VEC>(p.dl + (t + j) * p.E, e0, p.E) : f32x4{0.f, 0.f, 0.f, 0.f};
+        if (sums)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) bias += a[j];
+        if (p.dw == nullptr) continue;
+        const Elem* x = (const Elem*)p.x + t * p.d + c0;
+        if constexpr (BF16) {
+            u32x4 row[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                row[j] = t + j < end && c0 < p.d ? *(const u32x4*)(x + (int64_t)j * p.d) : u32x4{0, 0, 0, 0};
+            u32x4 w[4][3];
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = a[j][m];
+                split8<3>(v, w[m]);
+            }
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+                const bf16x8 b = column(row, n);
+                // the small terms first
+#pragma unroll
+                for (int term = 2; term >= 0; --term)
+#pragma unroll
+                    for (int m = 0; m < 4; ++m)
+                        acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            __builtin_bit_cast(bf16x8, w[m][term]), b, acc[m][n], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float b[8];
+#pragma unroll
+                for (int n = 0; n < 8; ++n)
+                    b[n] = t + j < end && c0 + n < p.d ? ((const float*)x)[(int64_t)j * p.d + n] : 0.f;
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+#pragma unroll
+                    for (int n = 0; n < 8; ++n)
+                        acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j][m], b[n], acc[m][n], 0, 0, 0);
+            }
         }
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-#pragma unroll
-            for (int n = 0; n < 4; ++n)
-                acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[m], b[n], acc[m][n], 0, 0, 0);
     }
-    if (wave > 0)
+    // token-split waves: the upper half's sums onto the lower half's, until one is left
+    for (int half = ts_n / 2; half >= 1; half /= 2) {
+        const int at = block * half + (ts >= half ? ts - half : ts);
 #pragma unroll
-        for (int m = 0; m < 4; ++m)
+        for (int part = 0; part < 2; ++part) {
+            __syncthreads();
+            if (ts >= half && ts < 2 * half)
 #pragma unroll
-            for (int n = 0; n < 4; ++n) red[wave - 1][m][n][lane] = acc[m][n];
-    __syncthreads();
-    if (wave > 0) return;
+                for (int m = 0; m < 4; ++m)
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) red[at][m][n][lane] = acc[m][4 * part + n];
+            __syncthreads();
+            if (ts < half)
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) acc[m][4 * part + n] += red[at][m][n][lane];
+        }
+    }
+    if (sums) {
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            bias[m] += __shfl_xor(bias[m], 16, 64);
+            bias[m] += __shfl_xor(bias[m], 32, 64);
+        }
+        // sixteen vectors of each of the eight waves: two rows of 64
+        __syncthreads();
+        if (quarter == 0) red[0][0][wave >> 2][(wave & 3) * 16 + i16] = bias;
+        __syncthreads();
+        if (ts == 0 && quarter == 0) {
+            f32x4 v = bias;
+            for (int q = 1; q < ts_n; ++q) {
+                const int from = wave + q;
+                v += red[0][0][from >> 2][(from & 3) * 16 + i16];
+            }
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+                if (e0 + m < p.E) p.dbias[(int64_t)blockIdx.y * p.E + e0 + m] = v[m];
+        }
+    }
+    if (ts > 0 || p.dw == nullptr || c0 >= p.d) return;
+    // element r of tile (m, n): expert 4 (4 quarter + r) + m of the block, column c0 + n
 #pragma unroll
     for (int m = 0; m < 4; ++m)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            // element r of tile (m, n): expert 4 (4 quarter + r) + m, column 4 i16 + n
-            const int e = blockIdx.y * GT + 4 * (4 * quarter + r) + m;
-            float* row = out + ((int64_t)blockIdx.z * E + e) * d;
+            const int e = block * 64 + 4 * (4 * quarter + r) + m;
+            if (e >= p.E) continue;
+            float* out = p.dw + ((int64_t)blockIdx.y * p.E + e) * p.d + c0;
+            if (BF16) {
+                ((f32x4*)out)[0] = f32x4{acc[m][0][r], acc[m][1][r], acc[m][2][r], acc[m][3][r]};
+                ((f32x4*)out)[1] = f32x4{acc[m][4][r], acc[m][5][r], acc[m][6][r], acc[m][7][r]};
+            } else {
 #pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const float v = ((acc[m][n][r] + red[0][m][n][lane][r]) + red[1][m][n][lane][r]) +
-                                red[2][m][n][lane][r];
-                if (e < E && c0 + n < d) row[c0 + n] = v;
+                for (int n = 0; n < 8; ++n)
+                    if (c0 + n < p.d) out[n] = acc[m][n][r];
             }
         }
 }
 
-// dx[t][c] = sum_e dlogits[t][e] w[e][c] by the same instruction: a wave holds 64 tokens x
-// 64 columns; sixteen experts a step, of which a lane has four consecutive ones of
-// dlogits' rows and the same four rows of w.
-template <typename Elem>
-__global__ __launch_bounds__(256) void scores_backward_kernel(const float* __restrict__ dlogits,
-                                                              const Elem* __restrict__ w, int64_t T,
-                                                              int d, int E, Elem* __restrict__ dx) {
+// out[i] = sum over n parts of parts[q][i], in order; two such sums in one launch.
+struct Parts {
+    const float* in;
+    float* out;
+    int64_t size;
+};
+
+__global__ __launch_bounds__(256) void sum_parts_kernel(Parts a, Parts b, int n) {
+    int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    Parts p = a;
+    if (i >= a.size) {
+        i -= a.size;
+        p = b;
+    }
+    if (i >= p.size) return;
+    float v = 0.f;
+    int q = 0;
+    for (; q + 8 <= n; q += 8) {
+        float w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = p.in[(q + j) * p.size + i];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v += w[j];
+    }
+    for (; q < n; ++q) v += p.in[q * p.size + i];
+    p.out[i] = v;
+}
+
+// dx[t][c] = sum_e dlogits[t][e] w[e][c] in bf16: a wave holds 64 tokens x 128 columns.  Of
+// a step of 32 experts lane (i, q) loads eight consecutive ones 8 q .. of four rows of
+// dlogits (in two bf16 terms, 16 bits for an output of 8), and the same eight rows of w,
+// eight columns 8 i .. each, transposed within the lane: its sums are eight consecutive
+// columns of a row, one 16-byte store.
+constexpr int DX_TOKENS = 64;
+
+template <bool VEC>
+__global__ __launch_bounds__(256, 2) void scores_backward_bf16_kernel(
+    const float* __restrict__ dlogits, const bf16_t* __restrict__ w, int64_t T, int d, int E,
+    bf16_t* __restrict__ dx) {
+    const int lane = threadIdx.x & 63, i16 = lane & 15, quarter = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int64_t t0 = ((int64_t)blockIdx.x * 4 + wave) * DX_TOKENS;
+    const int c0 = blockIdx.y * DW_COLS + 8 * i16;
+    if (t0 >= T) return;
+    f32x4 acc[4][8];
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int n = 0; n < 8; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int e0 = 0; e0 < E; e0 += 32) {
+        const int e = e0 + 8 * quarter;
+        u32x4 row[8], a[4][2];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            row[j] = e + j < E && c0 < d ? *(const u32x4*)(w + (int64_t)(e + j) * d + c0) : u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const int64_t t = t0 + 16 * m + i16;
+            f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+            if (t < T) {
+                lo = scores4<VEC>(dlogits + t * E, e, E);
+                hi = scores4<VEC>(dlogits + t * E, e + 4, E);
+            }
+            const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            split8<2>(v, a[m]);
+        }
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+            const bf16x8 b = column(row, n);
+#pragma unroll
+            for (int term = 1; term >= 0; --term)
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+                    acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        __builtin_bit_cast(bf16x8, a[m][term]), b, acc[m][n], 0, 0, 0);
+        }
+    }
+    if (c0 >= d) return;
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int64_t t = t0 + 16 * m + 4 * quarter + r;
+            if (t >= T) continue;
+            const float v[8] = {acc[m][0][r], acc[m][1][r], acc[m][2][r], acc[m][3][r],
+                                acc[m][4][r], acc[m][5][r], acc[m][6][r], acc[m][7][r]};
+            Chunk<bf16_t, 8>::store(dx + t * d + c0, v);
+        }
+}
+
+// The same in fp32 by v_mfma_f32_16x16x4_f32: 64 tokens x 64 columns a wave, sixteen
+// experts a step, of which a lane has four consecutive ones of dlogits' rows and the same
+// four rows of w.
+constexpr int GT = 64;
+
+template <bool VEC>
+__global__ __launch_bounds__(256) void scores_backward_f32_kernel(const float* __restrict__ dlogits,
+                                                                  const float* __restrict__ w,
+                                                                  int64_t T, int d, int E,
+                                                                  float* __restrict__ dx) {
     const int lane = threadIdx.x & 63, i16 = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int64_t t0 = ((int64_t)blockIdx.x * 4 + wave) * GT;
     const int c0 = blockIdx.y * GT + 4 * i16;
     if (t0 >= T) return;
+    const bool whole = d % 4 == 0;                       // rows of 16-byte chunks
     f32x4 acc[4][4];
 #pragma unroll
     for (int m = 0; m < 4; ++m)
@@ -360,11 +556,15 @@ __global__ __launch_bounds__(256) void scores_backward_kernel(const float* __res
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
             const int64_t t = t0 + 16 * m + i16;
-            a[m] = t < T ? load4<float>(dlogits + t * E, e, E) : f32x4{0.f, 0.f, 0.f, 0.f};
+            a[m] = t < T ? scores4<VEC>(dlogits + t * E, e, E) : f32x4{0.f, 0.f, 0.f, 0.f};
         }
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-            b[s] = e + s < E ? load4<Elem>(w + (int64_t)(e + s) * d, c0, d) : f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < 4; ++s) {
+            const float* row = w + (int64_t)(e + s) * d;
+            b[s] = e + s >= E ? f32x4{0.f, 0.f, 0.f, 0.f}
+                   : whole    ? scores4<true>(row, c0, d)
+                              : scores4<false>(row, c0, d);
+        }
 #pragma unroll
         for (int s = 0; s < 4; ++s)
 #pragma unroll
@@ -381,67 +581,92 @@ __global__ __launch_bounds__(256) void scores_backward_kernel(const float* __res
             if (t >= T) continue;
 #pragma unroll
             for (int n = 0; n < 4; ++n)
-                if (c0 + n < d) {
-                    const float v[1] = {acc[m][n][r]};
-                    Chunk<Elem, 1>::store(dx + t * d + c0 + n, v);
-                }
+                if (c0 + n < d) dx[t * d + c0 + n] = acc[m][n][r];
         }
-}
-
-// out[i] = sum over n parts of parts[q][i], in order.
-__global__ __launch_bounds__(256) void sum_parts_kernel(const float* __restrict__ parts, int n,
-                                                        int64_t size, float* __restrict__ out) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= size) return;
-    float v = 0.f;
-    for (int q = 0; q < n; ++q) v += parts[q * size + i];
-    out[i] = v;
 }
 
 int64_t align256(int64_t x) { return (x + 255) & ~(int64_t)255; }
 
-// Token chunks of dw: enough workgroups to fill the chip, 256 tokens each at least.
-int64_t grad_chunks(int64_t T, int d, int E) {
-    const int64_t tiles = ceil_div(d, GT) * ceil_div(E, GT);
-    const int64_t want = ceil_div(512, tiles), most = ceil_div(T, 256);
-    const int64_t n = want < most ? want : most;
-    return n < 1 ? 1 : n;
-}
+// Expert blocks of a dw workgroup (1, 2 or 4), and its chunks of the tokens: a workgroup per
+// CU, two steps per wave at least.
+int dw_blocks(int E) { return E <= 64 ? 1 : E <= 128 ? 2 : 4; }
 
-// workspace: [dlogits when not an output][the chosen experts' values][dw's chunks][dbias'
-// parts]
-struct RouteLayout {
-    int64_t sel, dw, dbias, total;
-    RouteLayout(int64_t T, int d, int E, int k) {
-        sel = align256(T * E * 4);
-        dw = sel + align256(T * k * 4);
-        dbias = dw + align256(grad_chunks(T, d, E) * E * d * 4);
-        total = dbias + align256(ceil_div(T, RT) * E * 4);
+struct DwPlan {
+    int64_t n, chunk;
+    DwPlan(int64_t T, int d, int E) {
+        const int64_t step = (int64_t)DW_STEP * (8 / dw_blocks(E));
+        const int64_t want = ceil_div(256, ceil_div(d, DW_COLS)), most = ceil_div(T, 2 * step);
+        n = std::max<int64_t>(std::min(want, most), 1);
+        chunk = ceil_div(ceil_div(T, n), step) * step;
+        n = std::max<int64_t>(chunk ? ceil_div(T, chunk) : 1, 1);
     }
 };
 
-template <typename Elem>
-int route_products(const float* dl, const float* sel, const int32_t* idx, const void* x, const void* w,
-                   int dtype, int64_t T, int d, int E, int k, void* dx, float* dw, float* parts,
-                   hipStream_t s) {
-    if (dx && sel) {
-        // only the chosen experts' scores have a gradient: their router rows, weighted
-        const int st = launch_combine(w, dtype, idx, sel, nullptr, 0, T, d, k, dx, s);
-        if (st != MOE_OK) return st;
-    } else if (dx) {
-        hipLaunchKernelGGL((scores_backward_kernel<Elem>),
-                           dim3((unsigned)ceil_div(T, 4 * GT), (unsigned)ceil_div(d, GT)), dim3(256),
-                           0, s, dl, (const Elem*)w, T, d, E, (Elem*)dx);
+// workspace: [dlogits when not an output][the chosen experts' values][dw's chunks][dbias']
+struct RouteLayout {
+    int64_t sel, dw, dbias, total;
+    RouteLayout(int64_t T, int d, int E, int k) {
+        const int64_t n = DwPlan(T, d, E).n;
+        sel = align256(T * E * 4);
+        dw = sel + align256(T * k * 4);
+        dbias = dw + align256(n * E * d * 4);
+        total = dbias + align256(n * E * 4);
     }
-    if (dw) {
-        const int64_t n = grad_chunks(T, d, E), chunk = ceil_div(ceil_div(T, n), 16) * 16;
-        hipLaunchKernelGGL((router_grad_kernel<Elem>),
-                           dim3((unsigned)ceil_div(d, GT), (unsigned)ceil_div(E, GT), (unsigned)n),
-                           dim3(256), 0, s, dl, (const Elem*)x, T, d, E, chunk, n > 1 ? parts : dw);
-        if (n > 1)
-            hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)ceil_div((int64_t)E * d, 256)),
-                               dim3(256), 0, s, parts, (int)n, (int64_t)E * d, dw);
+};
+
+int launch_router_grad(const float* dl, const void* x, int dtype, int64_t T, int d, int E, float* dw,
+                       float* dbias, float* dw_parts, float* dbias_parts, hipStream_t s) {
+    const DwPlan plan(T, d, E);
+    DwArgs p;
+    p.dl = dl;
+    p.x = x;
+    p.T = T;
+    p.chunk = plan.chunk;
+    p.d = d;
+    p.E = E;
+    p.eb = dw_blocks(E);
+    p.dw = !dw ? nullptr : plan.n > 1 ? dw_parts : dw;
+    p.dbias = !dbias ? nullptr : plan.n > 1 ? dbias_parts : dbias;
+    const dim3 grid(dw ? (unsigned)ceil_div(d, DW_COLS) : 1u, (unsigned)plan.n), block(DW_THREADS);
+    const bool vec = E % 4 == 0 && ((uintptr_t)dl & 15u) == 0;
+#define MOE_DW(T_)                                                                             \
+    do {                                                                                       \
+        if (vec) hipLaunchKernelGGL((router_grad_kernel<T_, true>), grid, block, 0, s, p);     \
+        else hipLaunchKernelGGL((router_grad_kernel<T_, false>), grid, block, 0, s, p);        \
+    } while (0)
+    if (dtype == MOE_BF16) MOE_DW(bf16_t);
+    else MOE_DW(float);
+#undef MOE_DW
+    if (plan.n > 1) {
+        const Parts a = {dw_parts, dw, dw ? (int64_t)E * d : 0}, b = {dbias_parts, dbias, dbias ? E : 0};
+        hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)ceil_div(a.size + b.size, 256)), dim3(256), 0,
+                           s, a, b, (int)plan.n);
     }
+    return launch_status();
+}
+
+int launch_scores_backward(const float* dl, const float* sel, const int32_t* idx, const void* w,
+                           int dtype, int64_t T, int d, int E, int k, void* dx, hipStream_t s) {
+    const bool vec = E % 4 == 0 && ((uintptr_t)dl & 15u) == 0;
+    if (dtype == MOE_BF16) {
+        const dim3 grid((unsigned)ceil_div(T, 4 * DX_TOKENS), (unsigned)ceil_div(d, DW_COLS));
+        if (vec)
+            hipLaunchKernelGGL(scores_backward_bf16_kernel<true>, grid, dim3(256), 0, s, dl,
+                               (const bf16_t*)w, T, d, E, (bf16_t*)dx);
+        else
+            hipLaunchKernelGGL(scores_backward_bf16_kernel<false>, grid, dim3(256), 0, s, dl,
+                               (const bf16_t*)w, T, d, E, (bf16_t*)dx);
+        return launch_status();
+    }
+    // only the chosen experts' scores have a gradient: their router rows, weighted
+    if (sel) return launch_combine(w, dtype, idx, sel, nullptr, 0, T, d, k, dx, s);
+    const dim3 grid((unsigned)ceil_div(T, 4 * GT), (unsigned)ceil_div(d, GT));
+    if (vec)
+        hipLaunchKernelGGL(scores_backward_f32_kernel<true>, grid, dim3(256), 0, s, dl, (const float*)w,
+                           T, d, E, (float*)dx);
+    else
+        hipLaunchKernelGGL(scores_backward_f32_kernel<false>, grid, dim3(256), 0, s, dl,
+                           (const float*)w, T, d, E, (float*)dx);
     return launch_status();
 }
 
@@ -470,28 +695,25 @@ int launch_route_backward(const float* dgate, const float* gate, const int32_t* 
     const bool renorm = (flags & MOE_RENORM) != 0;
     const RouteLayout at(T, d, E, k);
     char* base = (char*)ws;
-    float* dl = dlogits ? dlogits : dw || (dx && !renorm) ? (float*)base : nullptr;
-    float* sel = dx && renorm ? (float*)(base + at.sel) : nullptr;
-    float* part = dbias ? (float*)(base + at.dbias) : nullptr;
+    const bool sparse = dx && renorm && dtype == MOE_F32;
+    float* sel = sparse ? (float*)(base + at.sel) : nullptr;
+    float* dl = dlogits ? dlogits : dw || dbias || (dx && !sparse) ? (float*)base : nullptr;
     if (T > 0) {
         const dim3 grid((unsigned)ceil_div(T, RT)), block(RB_THREADS);
         if (renorm)
             hipLaunchKernelGGL(gate_backward_kernel<true>, grid, block, 0, s, dgate, gate, idx, logits,
-                               T, E, k, dl, sel, part);
+                               T, E, k, dl, sel);
         else
             hipLaunchKernelGGL(gate_backward_kernel<false>, grid, block, 0, s, dgate, gate, idx,
-                               logits, T, E, k, dl, sel, part);
+                               logits, T, E, k, dl, sel);
+        int st = launch_status();
+        if (st == MOE_OK && dx) st = launch_scores_backward(dl, sel, idx, w, dtype, T, d, E, k, dx, s);
+        if (st != MOE_OK) return st;
     }
-    if (dbias)
-        hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)ceil_div(E, 256)), dim3(256), 0, s, part,
-                           (int)ceil_div(T, RT), (int64_t)E, dbias);
-    if (T == 0) dx = nullptr;
-    float* parts = (float*)(base + at.dw);
-    if (dx || dw)
-        return dtype == MOE_BF16
-                   ? route_products<bf16_t>(dl, sel, idx, x, w, dtype, T, d, E, k, dx, dw, parts, s)
-                   : route_products<float>(dl, sel, idx, x, w, dtype, T, d, E, k, dx, dw, parts, s);
-    return launch_status();
+    if (dw || dbias)
+        return launch_router_grad(dl, x, dtype, T, d, E, dw, dbias, (float*)(base + at.dw),
+                                  (float*)(base + at.dbias), s);
+    return MOE_OK;
 }
 
 }  // namespace moe
