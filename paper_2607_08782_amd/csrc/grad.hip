@@ -263,6 +263,20 @@ __device__ __forceinline__ f32x4 scores4(const float* row, int e, int E) {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+// Workgroup b of `total` as (row, column) of a grid of `cols` columns, each XCD (workgroups
+// go round-robin over the eight) a contiguous range of it, columns first: the workgroups
+// that share rows share an L2, and write whole rows together.
+struct Cell {
+    int64_t row;
+    int col;
+};
+
+__device__ __forceinline__ Cell xcd_cell(unsigned b, unsigned total, unsigned cols) {
+    const unsigned x = b & 7, q = total >> 3, extra = total & 7;
+    const unsigned l = x * q + (x < extra ? x : extra) + (b >> 3);
+    return {(int64_t)(l / cols), (int)(l % cols)};
+}
+
 // Eight fp32 values as N bf16 terms each (their sum: 8 N significant bits), packed.
 template <int N>
 __device__ __forceinline__ void split8(const float (&x)[8], u32x4 (&out)[N]) {
@@ -291,24 +305,27 @@ __device__ __forceinline__ bf16x8 column(const u32x4 (&row)[8], int c) {
     return __builtin_bit_cast(bf16x8, v);
 }
 
-// dw[e][c] = sum_t dlogits[t][e] x[t][c], and dbias.  A wave holds 64 experts x 128 columns.
-// Lane (i, q) of it loads, for eight tokens 8 q .. 8 q + 7 of a step of 32, four experts 4 i
-// .. of dlogits and eight columns 8 i .. of x as they lie: its own elements, over eight
-// consecutive k, of four operands of the one side and eight of the other (a transpose within
-// the lane).  bf16 x: v_mfma_f32_16x16x32_bf16 over dlogits in three bf16 terms, which keep
-// all 24 bits, at a third of the rate of the bf16 instruction and five times that of the
-// fp32 one, which serves fp32 x.  Eight waves: blocks of 64 experts (one, two or four), and
-// tokens among the rest; a workgroup takes one chunk of the tokens, its waves' sums meet in
-// LDS in a fixed tree, and the chunks' in sum_parts_kernel in order.
+// dw[e][c] = sum_t dlogits[t][e] x[t][c], and dbias.  A wave holds 32 experts x 128 columns.
+// Lane (i, q) of it loads, for eight tokens 8 q .. 8 q + 7 of a step of 32, two experts 2 i
+// and 2 i + 1 of dlogits and eight columns 8 i .. of x as they lie: its own elements, over
+// eight consecutive k, of two operands of the one side and eight of the other (a transpose
+// within the lane).  bf16 x: v_mfma_f32_16x16x32_bf16 over dlogits in three bf16 terms, which
+// keep all 24 bits, at a third of the rate of the bf16 instruction and five times that of
+// the fp32 one, which serves fp32 x.  A step's operands come while the step before
+// multiplies.  Eight waves: all blocks of 32 experts (1 to 8), which read x's rows together,
+// and tokens among the rest; a workgroup takes one chunk of the tokens, its waves' sums meet
+// in LDS in a fixed tree, and the chunks' in sum_parts_kernel in order.
 constexpr int DW_THREADS = 512;
 constexpr int DW_COLS = 128;
 constexpr int DW_STEP = 32;
+constexpr int DW_EXPERTS = 32;
 
 struct DwArgs {
     const float* dl;
     const void* x;
     int64_t T, chunk;                                    // tokens, tokens per workgroup
-    int d, E, eb;                                        // eb: expert blocks of a workgroup
+    int d, E, eb;                                        // eb: expert blocks (1, 2, 4 or 8)
+    int cols;                                            // column tiles
     float* dw;                                           // [chunks][E][d], nullable
     float* dbias;                                        // [chunks][E], nullable
 };
@@ -316,118 +333,136 @@ struct DwArgs {
 template <typename Elem, bool VEC>
 __global__ __launch_bounds__(DW_THREADS, 2) void router_grad_kernel(DwArgs p) {
     constexpr bool BF16 = sizeof(Elem) == 2;
-    __shared__ f32x4 red[4][4][4][64];
+    __shared__ f32x4 red[4][2][8][64];
     const int lane = threadIdx.x & 63, i16 = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int ts_n = 8 / p.eb, block = wave / ts_n, ts = wave % ts_n;
-    const int e0 = block * 64 + 4 * i16, c0 = blockIdx.x * DW_COLS + 8 * i16;
-    const int64_t begin = (int64_t)blockIdx.y * p.chunk;
+    const Cell cell = xcd_cell(blockIdx.x, gridDim.x, p.cols);
+    const int e0 = block * DW_EXPERTS + 2 * i16, c0 = cell.col * DW_COLS + 8 * i16;
+    const int64_t begin = cell.row * p.chunk;
     const int64_t end = begin + p.chunk < p.T ? begin + p.chunk : p.T;
-    const bool sums = p.dbias != nullptr && blockIdx.x == 0;
-    f32x4 acc[4][8], bias = {0.f, 0.f, 0.f, 0.f};
+    const bool sums = p.dbias != nullptr && cell.col == 0;
+    f32x4 acc[2][8];
+    float bias[2] = {0.f, 0.f};
 #pragma unroll
-    for (int m = 0; m < 4; ++m)
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int n = 0; n < 8; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float2 a[8];
+    u32x4 row[8];
+    auto load = [&](int64_t t) {
+        const bf16_t* x = (const bf16_t*)p.x + t * p.d + c0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool live = t + j < end;
+            const float* s = p.dl + (t + j) * p.E + e0;
+            a[j] = make_float2(0.f, 0.f);
+            if (VEC) {
+                if (live && e0 < p.E) a[j] = *(const float2*)s;
+            } else {
+                if (live && e0 < p.E) a[j].x = s[0];
+                if (live && e0 + 1 < p.E) a[j].y = s[1];
+            }
+            if (BF16 && p.dw != nullptr)
+                row[j] = live && c0 < p.d ? *(const u32x4*)(x + (int64_t)j * p.d) : u32x4{0, 0, 0, 0};
+        }
+    };
+    load(begin + DW_STEP * ts + 8 * quarter);
     for (int64_t t0 = begin + DW_STEP * ts; t0 < end; t0 += DW_STEP * ts_n) {
         const int64_t t = t0 + 8 * quarter;
-        f32x4 a[8];
+        float v[2][8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            a[j] = t + j < end ? scores4<VEC>(p.dl + (t + j) * p.E, e0, p.E) : f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < 8; ++j) {
+            v[0][j] = a[j].x;
+            v[1][j] = a[j].y;
+        }
         if (sums)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) bias += a[j];
-        if (p.dw == nullptr) continue;
-        const Elem* x = (const Elem*)p.x + t * p.d + c0;
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) bias[m] += v[m][j];
         if constexpr (BF16) {
-            u32x4 row[8];
+            bf16x8 b[8];
+            u32x4 w[2][3];
+            if (p.dw != nullptr) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                row[j] = t + j < end && c0 < p.d ? *(const u32x4*)(x + (int64_t)j * p.d) : u32x4{0, 0, 0, 0};
-            u32x4 w[4][3];
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                float v[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = a[j][m];
-                split8<3>(v, w[m]);
+                for (int n = 0; n < 8; ++n) b[n] = column(row, n);
+                split8<3>(v[0], w[0]);
+                split8<3>(v[1], w[1]);
             }
+            load(t + DW_STEP * ts_n);
+            if (p.dw == nullptr) continue;
+            // the small terms first
 #pragma unroll
-            for (int n = 0; n < 8; ++n) {
-                const bf16x8 b = column(row, n);
-                // the small terms first
+            for (int term = 2; term >= 0; --term)
 #pragma unroll
-                for (int term = 2; term >= 0; --term)
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
-                    for (int m = 0; m < 4; ++m)
+                    for (int n = 0; n < 8; ++n)
                         acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            __builtin_bit_cast(bf16x8, w[m][term]), b, acc[m][n], 0, 0, 0);
-            }
+                            __builtin_bit_cast(bf16x8, w[m][term]), b[n], acc[m][n], 0, 0, 0);
         } else {
+            load(t + DW_STEP * ts_n);
+            if (p.dw == nullptr) continue;
+            const float* x = (const float*)p.x + t * p.d + c0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 float b[8];
 #pragma unroll
                 for (int n = 0; n < 8; ++n)
-                    b[n] = t + j < end && c0 + n < p.d ? ((const float*)x)[(int64_t)j * p.d + n] : 0.f;
+                    b[n] = t + j < end && c0 + n < p.d ? x[(int64_t)j * p.d + n] : 0.f;
 #pragma unroll
-                for (int m = 0; m < 4; ++m)
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int n = 0; n < 8; ++n)
-                        acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j][m], b[n], acc[m][n], 0, 0, 0);
+                        acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[m][j], b[n], acc[m][n], 0, 0, 0);
             }
         }
     }
     // token-split waves: the upper half's sums onto the lower half's, until one is left
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+        bias[m] += __shfl_xor(bias[m], 16, 64);
+        bias[m] += __shfl_xor(bias[m], 32, 64);
+    }
     for (int half = ts_n / 2; half >= 1; half /= 2) {
         const int at = block * half + (ts >= half ? ts - half : ts);
+        __syncthreads();
+        if (ts >= half && ts < 2 * half)
 #pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            __syncthreads();
-            if (ts >= half && ts < 2 * half)
+            for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int m = 0; m < 4; ++m)
+                for (int n = 0; n < 8; ++n) red[at][m][n][lane] = acc[m][n];
+        __syncthreads();
+        if (ts < half)
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) red[at][m][n][lane] = acc[m][4 * part + n];
-            __syncthreads();
-            if (ts < half)
+            for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int m = 0; m < 4; ++m)
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) acc[m][4 * part + n] += red[at][m][n][lane];
+                for (int n = 0; n < 8; ++n) acc[m][n] += red[at][m][n][lane];
+        if (!sums) continue;
+        float2* rb = (float2*)red;
+        __syncthreads();
+        if (ts >= half && ts < 2 * half && quarter == 0) rb[at * 16 + i16] = make_float2(bias[0], bias[1]);
+        __syncthreads();
+        if (ts < half) {
+            bias[0] += rb[at * 16 + i16].x;
+            bias[1] += rb[at * 16 + i16].y;
         }
     }
-    if (sums) {
+    if (ts > 0) return;
+    if (sums && quarter == 0)
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            bias[m] += __shfl_xor(bias[m], 16, 64);
-            bias[m] += __shfl_xor(bias[m], 32, 64);
-        }
-        // sixteen vectors of each of the eight waves: two rows of 64
-        __syncthreads();
-        if (quarter == 0) red[0][0][wave >> 2][(wave & 3) * 16 + i16] = bias;
-        __syncthreads();
-        if (ts == 0 && quarter == 0) {
-            f32x4 v = bias;
-            for (int q = 1; q < ts_n; ++q) {
-                const int from = wave + q;
-                v += red[0][0][from >> 2][(from & 3) * 16 + i16];
-            }
+        for (int m = 0; m < 2; ++m)
+            if (e0 + m < p.E) p.dbias[cell.row * p.E + e0 + m] = bias[m];
+    if (p.dw == nullptr || c0 >= p.d) return;
+    // element r of tile (m, n): expert 2 (4 quarter + r) + m of the block, column c0 + n
 #pragma unroll
-            for (int m = 0; m < 4; ++m)
-                if (e0 + m < p.E) p.dbias[(int64_t)blockIdx.y * p.E + e0 + m] = v[m];
-        }
-    }
-    if (ts > 0 || p.dw == nullptr || c0 >= p.d) return;
-    // element r of tile (m, n): expert 4 (4 quarter + r) + m of the block, column c0 + n
-#pragma unroll
-    for (int m = 0; m < 4; ++m)
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int e = block * 64 + 4 * (4 * quarter + r) + m;
+            const int e = block * DW_EXPERTS + 2 * (4 * quarter + r) + m;
             if (e >= p.E) continue;
-            float* out = p.dw + ((int64_t)blockIdx.y * p.E + e) * p.d + c0;
+            float* out = p.dw + (cell.row * p.E + e) * p.d + c0;
             if (BF16) {
                 ((f32x4*)out)[0] = f32x4{acc[m][0][r], acc[m][1][r], acc[m][2][r], acc[m][3][r]};
                 ((f32x4*)out)[1] = f32x4{acc[m][4][r], acc[m][5][r], acc[m][6][r], acc[m][7][r]};
@@ -467,12 +502,13 @@ __global__ __launch_bounds__(256) void sum_parts_kernel(Parts a, Parts b, int n)
     p.out[i] = v;
 }
 
-// dx[t][c] = sum_e dlogits[t][e] w[e][c] in bf16: a wave holds 64 tokens x 128 columns.  Of
-// a step of 32 experts lane (i, q) loads eight consecutive ones 8 q .. of four rows of
+// dx[t][c] = sum_e dlogits[t][e] w[e][c] in bf16: a wave holds 32 tokens x 128 columns.  Of
+// a step of 32 experts lane (i, q) loads eight consecutive ones 8 q .. of two rows of
 // dlogits (in two bf16 terms, 16 bits for an output of 8), and the same eight rows of w,
 // eight columns 8 i .. each, transposed within the lane: its sums are eight consecutive
-// columns of a row, one 16-byte store.
-constexpr int DX_TOKENS = 64;
+// columns of a row, one 16-byte store.  A step's operands come while the step before
+// multiplies.
+constexpr int DX_TOKENS = 32;
 
 template <bool VEC>
 __global__ __launch_bounds__(256, 2) void scores_backward_bf16_kernel(
@@ -480,45 +516,55 @@ __global__ __launch_bounds__(256, 2) void scores_backward_bf16_kernel(
     bf16_t* __restrict__ dx) {
     const int lane = threadIdx.x & 63, i16 = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int64_t t0 = ((int64_t)blockIdx.x * 4 + wave) * DX_TOKENS;
-    const int c0 = blockIdx.y * DW_COLS + 8 * i16;
+    const Cell cell = xcd_cell(blockIdx.x, gridDim.x, (unsigned)ceil_div(d, DW_COLS));
+    const int64_t t0 = (cell.row * 4 + wave) * DX_TOKENS;
+    const int c0 = cell.col * DW_COLS + 8 * i16;
     if (t0 >= T) return;
-    f32x4 acc[4][8];
+    f32x4 acc[2][8];
 #pragma unroll
-    for (int m = 0; m < 4; ++m)
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int n = 0; n < 8; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int e0 = 0; e0 < E; e0 += 32) {
-        const int e = e0 + 8 * quarter;
-        u32x4 row[8], a[4][2];
+    u32x4 row[8];
+    f32x4 lo[2], hi[2];
+    auto load = [&](int e) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const int64_t t = t0 + 16 * m + i16;
+            lo[m] = hi[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (t < T) {
+                lo[m] = scores4<VEC>(dlogits + t * E, e, E);
+                hi[m] = scores4<VEC>(dlogits + t * E, e + 4, E);
+            }
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             row[j] = e + j < E && c0 < d ? *(const u32x4*)(w + (int64_t)(e + j) * d + c0) : u32x4{0, 0, 0, 0};
+    };
+    load(8 * quarter);
+    for (int e0 = 0; e0 < E; e0 += 32) {
+        u32x4 a[2][2];
+        bf16x8 b[8];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const int64_t t = t0 + 16 * m + i16;
-            f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
-            if (t < T) {
-                lo = scores4<VEC>(dlogits + t * E, e, E);
-                hi = scores4<VEC>(dlogits + t * E, e + 4, E);
-            }
-            const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        for (int m = 0; m < 2; ++m) {
+            const float v[8] = {lo[m][0], lo[m][1], lo[m][2], lo[m][3], hi[m][0], hi[m][1], hi[m][2], hi[m][3]};
             split8<2>(v, a[m]);
         }
 #pragma unroll
-        for (int n = 0; n < 8; ++n) {
-            const bf16x8 b = column(row, n);
+        for (int n = 0; n < 8; ++n) b[n] = column(row, n);
+        if (e0 + 32 < E) load(e0 + 32 + 8 * quarter);
 #pragma unroll
-            for (int term = 1; term >= 0; --term)
+        for (int term = 1; term >= 0; --term)
 #pragma unroll
-                for (int m = 0; m < 4; ++m)
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int n = 0; n < 8; ++n)
                     acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        __builtin_bit_cast(bf16x8, a[m][term]), b, acc[m][n], 0, 0, 0);
-        }
+                        __builtin_bit_cast(bf16x8, a[m][term]), b[n], acc[m][n], 0, 0, 0);
     }
     if (c0 >= d) return;
 #pragma unroll
-    for (int m = 0; m < 4; ++m)
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int64_t t = t0 + 16 * m + 4 * quarter + r;
@@ -587,9 +633,9 @@ __global__ __launch_bounds__(256) void scores_backward_f32_kernel(const float* _
 
 int64_t align256(int64_t x) { return (x + 255) & ~(int64_t)255; }
 
-// Expert blocks of a dw workgroup (1, 2 or 4), and its chunks of the tokens: a workgroup per
-// CU, two steps per wave at least.
-int dw_blocks(int E) { return E <= 64 ? 1 : E <= 128 ? 2 : 4; }
+// Expert blocks of a dw workgroup, and the chunks of the tokens: a workgroup per CU, two
+// steps per wave at least.
+int dw_blocks(int E) { return E <= 32 ? 1 : E <= 64 ? 2 : E <= 128 ? 4 : 8; }
 
 struct DwPlan {
     int64_t n, chunk;
@@ -627,8 +673,9 @@ int launch_router_grad(const float* dl, const void* x, int dtype, int64_t T, int
     p.eb = dw_blocks(E);
     p.dw = !dw ? nullptr : plan.n > 1 ? dw_parts : dw;
     p.dbias = !dbias ? nullptr : plan.n > 1 ? dbias_parts : dbias;
-    const dim3 grid(dw ? (unsigned)ceil_div(d, DW_COLS) : 1u, (unsigned)plan.n), block(DW_THREADS);
-    const bool vec = E % 4 == 0 && ((uintptr_t)dl & 15u) == 0;
+    p.cols = dw ? (int)ceil_div(d, DW_COLS) : 1;
+    const dim3 grid((unsigned)(p.cols * plan.n)), block(DW_THREADS);
+    const bool vec = E % 2 == 0 && ((uintptr_t)dl & 7u) == 0;
 #define MOE_DW(T_)                                                                             \
     do {                                                                                       \
         if (vec) hipLaunchKernelGGL((router_grad_kernel<T_, true>), grid, block, 0, s, p);     \
@@ -649,7 +696,7 @@ int launch_scores_backward(const float* dl, const float* sel, const int32_t* idx
                            int dtype, int64_t T, int d, int E, int k, void* dx, hipStream_t s) {
     const bool vec = E % 4 == 0 && ((uintptr_t)dl & 15u) == 0;
     if (dtype == MOE_BF16) {
-        const dim3 grid((unsigned)ceil_div(T, 4 * DX_TOKENS), (unsigned)ceil_div(d, DW_COLS));
+        const dim3 grid((unsigned)(ceil_div(T, 4 * DX_TOKENS) * ceil_div(d, DW_COLS)));
         if (vec)
             hipLaunchKernelGGL(scores_backward_bf16_kernel<true>, grid, dim3(256), 0, s, dl,
                                (const bf16_t*)w, T, d, E, (bf16_t*)dx);
