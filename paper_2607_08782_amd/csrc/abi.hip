@@ -515,6 +515,8 @@ int moe_route_topk_backward(const float* dgate, const float* topk_gate, const in
         return MOE_ERR_ARG;
     if (T > 0 && ((dx && !w_router) || (dw && !x))) return MOE_ERR_ARG;
     if ((dtype == MOE_BF16 && d % 8) || d >= 1 << 22) return MOE_ERR_SHAPE;
+    // one grid covers the tiles of dx
+    if (ceil_div(T, 128) * ceil_div(d, 64) > 0x7fffffffLL) return MOE_ERR_SHAPE;
     if (d % (dtype == MOE_BF16 ? 8 : 4) == 0 &&
         (!aligned16(x) || !aligned16(w_router) || !aligned16(dx)))
         return MOE_ERR_ARG;

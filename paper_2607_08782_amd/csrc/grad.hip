@@ -333,7 +333,7 @@ struct DwArgs {
 template <typename Elem, bool VEC>
 __global__ __launch_bounds__(DW_THREADS, 2) void router_grad_kernel(DwArgs p) {
     constexpr bool BF16 = sizeof(Elem) == 2;
-    __shared__ f32x4 red[4][2][8][64];
+    __shared__ f32x4 red[4 * 16 * 64];
     const int lane = threadIdx.x & 63, i16 = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int ts_n = 8 / p.eb, block = wave / ts_n, ts = wave % ts_n;
@@ -432,13 +432,13 @@ __global__ __launch_bounds__(DW_THREADS, 2) void router_grad_kernel(DwArgs p) {
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int n = 0; n < 8; ++n) red[at][m][n][lane] = acc[m][n];
+                for (int n = 0; n < 8; ++n) red[(at * 16 + m * 8 + n) * 64 + lane] = acc[m][n];
         __syncthreads();
         if (ts < half)
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int n = 0; n < 8; ++n) acc[m][n] += red[at][m][n][lane];
+                for (int n = 0; n < 8; ++n) acc[m][n] += red[(at * 16 + m * 8 + n) * 64 + lane];
         if (!sums) continue;
         float2* rb = (float2*)red;
         __syncthreads();
@@ -502,77 +502,98 @@ __global__ __launch_bounds__(256) void sum_parts_kernel(Parts a, Parts b, int n)
     p.out[i] = v;
 }
 
-// dx[t][c] = sum_e dlogits[t][e] w[e][c] in bf16: a wave holds 32 tokens x 128 columns.  Of
-// a step of 32 experts lane (i, q) loads eight consecutive ones 8 q .. of two rows of
-// dlogits (in two bf16 terms, 16 bits for an output of 8), and the same eight rows of w,
-// eight columns 8 i .. each, transposed within the lane: its sums are eight consecutive
-// columns of a row, one 16-byte store.  A step's operands come while the step before
-// multiplies.
-constexpr int DX_TOKENS = 32;
-
-template <bool VEC>
+// dx[t][c] = sum_e dlogits[t][e] w[e][c] in bf16.  A wave keeps all experts' rows of w for
+// 16 NC columns in registers (KE steps of 32 experts: lane (i, q) loads eight experts 8 q ..
+// of a step, NC columns NC i .. each, and transposes them within the lane) and runs over
+// blocks of 16 tokens, whose dlogits come, in two bf16 terms (16 bits for an output of 8),
+// while the block before multiplies.  Its sums are NC consecutive columns of a row, stored
+// at once.
+template <int KE, int NC, bool VEC>
 __global__ __launch_bounds__(256, 2) void scores_backward_bf16_kernel(
-    const float* __restrict__ dlogits, const bf16_t* __restrict__ w, int64_t T, int d, int E,
+    const float* __restrict__ dlogits, const bf16_t* __restrict__ w, int64_t T, int d, int E, int runs,
     bf16_t* __restrict__ dx) {
+    typedef uint32_t words __attribute__((ext_vector_type(NC / 2)));
     const int lane = threadIdx.x & 63, i16 = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const Cell cell = xcd_cell(blockIdx.x, gridDim.x, (unsigned)ceil_div(d, DW_COLS));
-    const int64_t t0 = (cell.row * 4 + wave) * DX_TOKENS;
-    const int c0 = cell.col * DW_COLS + 8 * i16;
-    if (t0 >= T) return;
-    f32x4 acc[2][8];
+    const int cols = (d + 16 * NC - 1) / (16 * NC);
+    const Cell cell = xcd_cell(blockIdx.x, gridDim.x, cols);
+    const int c0 = cell.col * 16 * NC + NC * i16;
+    bf16x8 b[KE][NC];
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int s = 0; s < KE; ++s) {
+        words row[8];
 #pragma unroll
-        for (int n = 0; n < 8; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    u32x4 row[8];
-    f32x4 lo[2], hi[2];
-    auto load = [&](int e) {
+        for (int j = 0; j < 8; ++j) {
+            const int e = 32 * s + 8 * quarter + j;
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const int64_t t = t0 + 16 * m + i16;
-            lo[m] = hi[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < NC / 2; ++i) row[j][i] = 0;
+            if (e < E && c0 < d) row[j] = *(const words*)(w + (int64_t)e * d + c0);
+        }
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            u32x4 v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                v[i] = __builtin_amdgcn_perm(row[2 * i + 1][n / 2], row[2 * i][n / 2],
+                                             n & 1 ? 0x07060302u : 0x05040100u);
+            b[s][n] = __builtin_bit_cast(bf16x8, v);
+        }
+    }
+    // this wave's token blocks: every runs-th
+    const int64_t blocks = (T + 15) / 16;
+    f32x4 lo[KE], hi[KE];
+    auto load = [&](int64_t block) {
+        const int64_t t = block * 16 + i16;
+#pragma unroll
+        for (int s = 0; s < KE; ++s) {
+            lo[s] = hi[s] = f32x4{0.f, 0.f, 0.f, 0.f};
             if (t < T) {
-                lo[m] = scores4<VEC>(dlogits + t * E, e, E);
-                hi[m] = scores4<VEC>(dlogits + t * E, e + 4, E);
+                lo[s] = scores4<VEC>(dlogits + t * E, 32 * s + 8 * quarter, E);
+                hi[s] = scores4<VEC>(dlogits + t * E, 32 * s + 8 * quarter + 4, E);
             }
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            row[j] = e + j < E && c0 < d ? *(const u32x4*)(w + (int64_t)(e + j) * d + c0) : u32x4{0, 0, 0, 0};
     };
-    load(8 * quarter);
-    for (int e0 = 0; e0 < E; e0 += 32) {
-        u32x4 a[2][2];
-        bf16x8 b[8];
+    constexpr bool AHEAD = KE <= 4;                      // past 128 experts there is no room
+    int64_t block = cell.row * 4 + wave;
+    if (AHEAD && block < blocks) load(block);
+    for (; block < blocks; block += runs) {
+        u32x4 a[AHEAD ? KE : 1][2];
+        auto terms = [&](int s, u32x4 (&out)[2]) {
+            const float v[8] = {lo[s][0], lo[s][1], lo[s][2], lo[s][3], hi[s][0], hi[s][1], hi[s][2], hi[s][3]};
+            split8<2>(v, out);
+        };
+        if (AHEAD) {
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const float v[8] = {lo[m][0], lo[m][1], lo[m][2], lo[m][3], hi[m][0], hi[m][1], hi[m][2], hi[m][3]};
-            split8<2>(v, a[m]);
+            for (int s = 0; s < KE; ++s) terms(s, a[AHEAD ? s : 0]);
+            if (block + runs < blocks) load(block + runs);
+        } else {
+            load(block);
         }
+        f32x4 acc[NC];
 #pragma unroll
-        for (int n = 0; n < 8; ++n) b[n] = column(row, n);
-        if (e0 + 32 < E) load(e0 + 32 + 8 * quarter);
+        for (int n = 0; n < NC; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int term = 1; term >= 0; --term)
+        for (int s = 0; s < KE; ++s) {
+            if (!AHEAD) {
+                __builtin_amdgcn_sched_barrier(0);
+                terms(s, a[0]);
+            }
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+            for (int term = 1; term >= 0; --term)
 #pragma unroll
-                for (int n = 0; n < 8; ++n)
-                    acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        __builtin_bit_cast(bf16x8, a[m][term]), b[n], acc[m][n], 0, 0, 0);
-    }
-    if (c0 >= d) return;
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
+                for (int n = 0; n < NC; ++n)
+                    acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        __builtin_bit_cast(bf16x8, a[AHEAD ? s : 0][term]), b[s][n], acc[n], 0, 0, 0);
+        }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int64_t t = t0 + 16 * m + 4 * quarter + r;
-            if (t >= T) continue;
-            const float v[8] = {acc[m][0][r], acc[m][1][r], acc[m][2][r], acc[m][3][r],
-                                acc[m][4][r], acc[m][5][r], acc[m][6][r], acc[m][7][r]};
-            Chunk<bf16_t, 8>::store(dx + t * d + c0, v);
+            const int64_t t = block * 16 + 4 * quarter + r;
+            words v;
+#pragma unroll
+            for (int i = 0; i < NC / 2; ++i) v[i] = pack_bf16x2(acc[2 * i][r], acc[2 * i + 1][r]);
+            if (t < T && c0 < d) *(words*)(dx + t * d + c0) = v;
         }
+    }
 }
 
 // The same in fp32 by v_mfma_f32_16x16x4_f32: 64 tokens x 64 columns a wave, sixteen
@@ -696,13 +717,24 @@ int launch_scores_backward(const float* dl, const float* sel, const int32_t* idx
                            int dtype, int64_t T, int d, int E, int k, void* dx, hipStream_t s) {
     const bool vec = E % 4 == 0 && ((uintptr_t)dl & 15u) == 0;
     if (dtype == MOE_BF16) {
-        const dim3 grid((unsigned)(ceil_div(T, 4 * DX_TOKENS) * ceil_div(d, DW_COLS)));
-        if (vec)
-            hipLaunchKernelGGL(scores_backward_bf16_kernel<true>, grid, dim3(256), 0, s, dl,
-                               (const bf16_t*)w, T, d, E, (bf16_t*)dx);
-        else
-            hipLaunchKernelGGL(scores_backward_bf16_kernel<false>, grid, dim3(256), 0, s, dl,
-                               (const bf16_t*)w, T, d, E, (bf16_t*)dx);
+        // two workgroups of four waves a CU, a block of 16 tokens per wave at least
+        const int64_t cols = ceil_div(d, E > 128 ? 64 : 128), most = ceil_div(ceil_div(T, 16), 4);
+        const int64_t rows = std::max<int64_t>(std::min(most, ceil_div(512, cols)), 1);
+        const dim3 grid((unsigned)(rows * cols));
+#define MOE_DX(KE, NC, VEC)                                                                       \
+    hipLaunchKernelGGL((scores_backward_bf16_kernel<KE, NC, VEC>), grid, dim3(256), 0, s, dl,     \
+                       (const bf16_t*)w, T, d, E, (int)(4 * rows), (bf16_t*)dx)
+#define MOE_DX_E(VEC)                                                                             \
+    do {                                                                                          \
+        if (E <= 32) MOE_DX(1, 8, VEC);                                                           \
+        else if (E <= 64) MOE_DX(2, 8, VEC);                                                      \
+        else if (E <= 128) MOE_DX(4, 8, VEC);                                                     \
+        else MOE_DX(8, 4, VEC);                                                                   \
+    } while (0)
+        if (vec) MOE_DX_E(true);
+        else MOE_DX_E(false);
+#undef MOE_DX_E
+#undef MOE_DX
         return launch_status();
     }
     // only the chosen experts' scores have a gradient: their router rows, weighted

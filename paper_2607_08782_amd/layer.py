@@ -20,10 +20,16 @@ launches leave CUs idle) without holding CUs the routing launches wait for;
 the fork and join are stream events, so a graph capture of `run` holds both
 branches.  The expert placement can be swapped between batches
 (`set_placement`) by re-pointing the weight table; nothing is reallocated.
+
+With ``mxfp4=True`` the routed experts are held and multiplied in 4 bits
+(moe_grouped_ffn_mxfp4; a third of a decode step's weight bytes); shared experts
+keep bf16 and their own call.  `backward` and `backward_rows` are the gradient of
+the layer around its experts: from the loss gradient of y to the expert outputs'
+and the router's, and from the packaged rows' back to X.
 """
 from __future__ import annotations
 
-from typing import Optional, Sequence, Tuple
+from typing import Callable, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
@@ -88,7 +94,18 @@ class LayerShare:
                  w2: Sequence[torch.Tensor], shared=(), renorm: bool = True,
                  coact: bool = False, want_logits: bool = True, cap_rows: Optional[int] = None,
                  gather_in_ffn: Optional[bool] = None, overlap_shared: bool = True,
-                 fuse_combine: Optional[bool] = None, shared_in_ffn: Optional[bool] = None):
+                 fuse_combine: Optional[bool] = None, shared_in_ffn: Optional[bool] = None,
+                 mxfp4: bool = False):
+        if mxfp4:
+            # the 4-bit call reads rows through the row map, streams or tiles by itself,
+            # and leaves the shared experts to their own call
+            if X.dtype != torch.bfloat16:
+                raise ValueError("mxfp4 experts need bfloat16 activations")
+            if gather_in_ffn is False or fuse_combine or shared_in_ffn:
+                raise ValueError("mxfp4 experts gather their rows in the FFN call and take neither the "
+                                 "combine nor the shared experts into it")
+            gather_in_ffn, fuse_combine, shared_in_ffn = True, False, False
+        self.mxfp4 = mxfp4
         self.device = X.device
         self.X = X
         self.Wr = Wr
@@ -167,14 +184,18 @@ class LayerShare:
         self._y_perm_all = torch.empty((lead + cap, d), dtype=dt, device=dv)
         self.y_perm = self._y_perm_all[lead:]
         self.y_shared_slices = self._y_perm_all[:lead] if lead else None
-        self.weights = moe.WeightTable(w13, w2) if self.n_local else None
+        self.weights = self._table(w13, w2) if self.n_local else None
         self.f = self.weights.f if self.weights else f_routed
         dcode = moe.MOE_BF16 if dt == torch.bfloat16 else moe.MOE_F32
         self._blocks = blocks if self.shared_in_ffn else None
         self._ffn_weights = self._call_weights(w13, w2)
-        self.ws_ffn = moe.workspace(
-            moe.moe_grouped_ffn_ws_bytes(dcode, lead + self.cap_rows, d, max(self.f, 1),
-                                         max(self.n_shared_blocks + self.n_local, 1)), dv)
+        if mxfp4:
+            need = moe.moe_grouped_ffn_mxfp4_ws_bytes(T, self.cap_rows, d, max(self.f, 1),
+                                                      max(self.n_local, 1))
+        else:
+            need = moe.moe_grouped_ffn_ws_bytes(dcode, lead + self.cap_rows, d, max(self.f, 1),
+                                                max(self.n_shared_blocks + self.n_local, 1))
+        self.ws_ffn = moe.workspace(need, dv)
         sh = concat_shared(list(shared)) if not self.shared_in_ffn else None
         if sh is not None:
             self.shared_weights = moe.WeightTable([sh[0]], [sh[1]])
@@ -229,6 +250,10 @@ class LayerShare:
         if fuse_combine is None:
             fuse_combine = T <= 64 and k <= 2
         self.fused_combine = bool(fuse_combine) and can_fuse
+        self._grads = None
+
+    def _table(self, w13: Sequence[torch.Tensor], w2: Sequence[torch.Tensor]):
+        return moe.MxWeightTable.quantized(w13, w2) if self.mxfp4 else moe.WeightTable(w13, w2)
 
     def set_placement(self, placement: np.ndarray, w13: Sequence[torch.Tensor],
                       w2: Sequence[torch.Tensor]):
@@ -238,7 +263,7 @@ class LayerShare:
         if n_local != self.n_local:
             raise ValueError("the new placement must keep %d local slots" % self.n_local)
         self.placement = placement
-        self.weights = moe.WeightTable(w13, w2)
+        self.weights = self._table(w13, w2)
         self._ffn_weights = self._call_weights(w13, w2)
 
     def _call_weights(self, w13: Sequence[torch.Tensor], w2: Sequence[torch.Tensor]):
@@ -317,7 +342,7 @@ class LayerShare:
 
     def routed_ffn(self, fused: Optional[bool] = None):
         """Enqueue the routed experts' FFN call as `run` makes it: moe_grouped_ffn (or
-        moe_grouped_ffn_rows) into y_perm, or, when the share fuses the combine (fused
+        moe_grouped_ffn_rows, moe_grouped_ffn_mxfp4) into y_perm, or, when the share fuses the combine (fused
         None: as `run` does), moe_grouped_ffn_combine into y (which then reads y_shared:
         the shared experts' call must have completed on this stream)."""
         if self.shared_in_ffn:
@@ -327,6 +352,11 @@ class LayerShare:
                                             ws=self.ws_ffn, products=self.ffn_products)
             return
         if self.weights is None:
+            return
+        if self.mxfp4:
+            moe.moe_grouped_ffn_mxfp4(self.X, self.perm["group_offsets"], self.weights,
+                                      row_token=self.perm["row_token"], cap_rows=self.cap_rows,
+                                      y_perm=self.y_perm, ws=self.ws_ffn)
             return
         if self.fused_combine if fused is None else (fused and self.fused_combine):
             moe.moe_grouped_ffn_combine(self.perm["x_perm"], self.perm["group_offsets"],
@@ -378,3 +408,45 @@ class LayerShare:
             self._shared_ffn()
         self.combine()
         return self.y
+
+    def backward(self, dy: torch.Tensor, reduce_dgate: Optional[Callable] = None) -> dict:
+        """Enqueue the gradient of the last `run` from dy [T, d], the loss gradient of y, to
+        the experts and the router; returns device tensors, overwritten by the next call:
+            dy_perm  of every expert output row (rows past group_offsets' end unchanged)
+            dgate    [T, k] fp32, of topk_gate: 0 for experts on other GPUs
+            dx       [T, d], of X through the gate scores;  dw [E, d], dbias [E] fp32, of the
+                     router
+        (the shared experts' output has dy itself).  A token's gates depend on each other,
+        so where its experts are on several GPUs dgate has to be summed over them before it
+        goes on: reduce_dgate(dgate), in place, on the current stream."""
+        if self.fused_combine:
+            raise ValueError("the fused combine does not keep y_perm: backward needs fuse_combine=False")
+        if not self.renorm and self.logits is None:
+            raise ValueError("gates without renormalisation need want_logits=True for backward")
+        if tuple(dy.shape) != (self.T, self.d) or dy.dtype != self.X.dtype:
+            raise ValueError("dy must be %s [%d, %d]" % (self.X.dtype, self.T, self.d))
+        if self._grads is None:
+            f32 = dict(dtype=torch.float32, device=self.device)
+            dcode = moe.MOE_BF16 if self.X.dtype == torch.bfloat16 else moe.MOE_F32
+            need = moe.moe_route_topk_backward_ws_bytes(dcode, self.T, self.d, self.E, self.k,
+                                                        moe.MOE_RENORM if self.renorm else 0)
+            self._grads = {"dy_perm": torch.zeros_like(self.y_perm), "dgate": torch.empty((self.T, self.k), **f32),
+                           "dx": torch.empty_like(self.X), "dw": torch.empty((self.E, self.d), **f32),
+                           "dbias": torch.empty((self.E,), **f32)}
+            self._ws_grads = moe.workspace(need, self.device)
+        g = self._grads
+        moe.moe_combine_backward(dy, self.y_perm, self.perm["token_row"], self.topk_gate,
+                                 dy_perm=g["dy_perm"], dgate=g["dgate"])
+        if reduce_dgate is not None:
+            reduce_dgate(g["dgate"])
+        moe.moe_route_topk_backward(g["dgate"], self.topk_gate, self.topk_idx, self.X, self.Wr,
+                                    logits=self.logits, renorm=self.renorm, want_dlogits=False,
+                                    dx=g["dx"], dw=g["dw"], dbias=g["dbias"], ws=self._ws_grads)
+        return g
+
+    def backward_rows(self, dx_perm: torch.Tensor, dx: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Enqueue the gradient of the packaging: dx [T, d] (None: a new tensor) = the sum of
+        each token's rows of dx_perm, the gradient of the packaged rows, on top of the last
+        `backward`'s dx, if there was one."""
+        add = self._grads["dx"] if self._grads is not None else None
+        return moe.moe_permute_backward(dx_perm, self.perm["token_row"], dx_add=add, dx=dx)
