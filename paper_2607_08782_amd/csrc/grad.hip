@@ -350,38 +350,48 @@ __global__ __launch_bounds__(DW_THREADS, 2) void router_grad_kernel(DwArgs p) {
         for (int n = 0; n < 8; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
     float2 a[8];
     u32x4 row[8];
-    auto load = [&](int64_t t) {
-        const bf16_t* x = (const bf16_t*)p.x + t * p.d + c0;
+    f32x4 wide[BF16 ? 1 : 8][2];                         // fp32 x
+    const bool whole = p.d % 4 == 0;                     // rows of 16-byte chunks
+    auto load = [&](int64_t t, int j) {                  // token t + j
+        const bool live = t + j < end;
+        const float* s = p.dl + (t + j) * p.E + e0;
+        a[j] = make_float2(0.f, 0.f);
+        if (VEC) {
+            if (live && e0 < p.E) a[j] = *(const float2*)s;
+        } else {
+            if (live && e0 < p.E) a[j].x = s[0];
+            if (live && e0 + 1 < p.E) a[j].y = s[1];
+        }
+        if (p.dw == nullptr) return;
+        if (BF16) {
+            const bf16_t* x = (const bf16_t*)p.x + (t + j) * p.d + c0;
+            row[j] = live && c0 < p.d ? *(const u32x4*)x : u32x4{0, 0, 0, 0};
+        } else {
+            const float* x = (const float*)p.x + (t + j) * p.d;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const bool live = t + j < end;
-            const float* s = p.dl + (t + j) * p.E + e0;
-            a[j] = make_float2(0.f, 0.f);
-            if (VEC) {
-                if (live && e0 < p.E) a[j] = *(const float2*)s;
-            } else {
-                if (live && e0 < p.E) a[j].x = s[0];
-                if (live && e0 + 1 < p.E) a[j].y = s[1];
-            }
-            if (BF16 && p.dw != nullptr)
-                row[j] = live && c0 < p.d ? *(const u32x4*)(x + (int64_t)j * p.d) : u32x4{0, 0, 0, 0};
+            for (int h = 0; h < 2; ++h)
+                wide[BF16 ? 0 : j][h] = !live   ? f32x4{0.f, 0.f, 0.f, 0.f}
+                                        : whole ? scores4<true>(x, c0 + 4 * h, p.d)
+                                                : scores4<false>(x, c0 + 4 * h, p.d);
         }
     };
-    load(begin + DW_STEP * ts + 8 * quarter);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) load(begin + DW_STEP * ts + 8 * quarter, j);
     for (int64_t t0 = begin + DW_STEP * ts; t0 < end; t0 += DW_STEP * ts_n) {
         const int64_t t = t0 + 8 * quarter;
-        float v[2][8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            v[0][j] = a[j].x;
-            v[1][j] = a[j].y;
-        }
         if (sums)
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) bias[m] += v[m][j];
+            for (int j = 0; j < 8; ++j) {
+                bias[0] += a[j].x;
+                bias[1] += a[j].y;
+            }
         if constexpr (BF16) {
+            float v[2][8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[0][j] = a[j].x;
+                v[1][j] = a[j].y;
+            }
             bf16x8 b[8];
             u32x4 w[2][3];
             if (p.dw != nullptr) {
@@ -390,7 +400,8 @@ __global__ __launch_bounds__(DW_THREADS, 2) void router_grad_kernel(DwArgs p) {
                 split8<3>(v[0], w[0]);
                 split8<3>(v[1], w[1]);
             }
-            load(t + DW_STEP * ts_n);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) load(t + DW_STEP * ts_n, j);
             if (p.dw == nullptr) continue;
             // the small terms first
 #pragma unroll
@@ -402,20 +413,17 @@ __global__ __launch_bounds__(DW_THREADS, 2) void router_grad_kernel(DwArgs p) {
                         acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                             __builtin_bit_cast(bf16x8, w[m][term]), b[n], acc[m][n], 0, 0, 0);
         } else {
-            load(t + DW_STEP * ts_n);
-            if (p.dw == nullptr) continue;
-            const float* x = (const float*)p.x + t * p.d + c0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                float b[8];
+                if (p.dw != nullptr)
 #pragma unroll
-                for (int n = 0; n < 8; ++n)
-                    b[n] = t + j < end && c0 + n < p.d ? x[(int64_t)j * p.d + n] : 0.f;
+                    for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
-#pragma unroll
-                    for (int n = 0; n < 8; ++n)
-                        acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[m][j], b[n], acc[m][n], 0, 0, 0);
+                        for (int n = 0; n < 8; ++n)
+                            acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                                m ? a[j].y : a[j].x, wide[j][n / 4][n % 4], acc[m][n], 0, 0, 0);
+                load(t + DW_STEP * ts_n, j);             // into the registers just multiplied
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
     }
@@ -463,7 +471,7 @@ __global__ __launch_bounds__(DW_THREADS, 2) void router_grad_kernel(DwArgs p) {
             const int e = block * DW_EXPERTS + 2 * (4 * quarter + r) + m;
             if (e >= p.E) continue;
             float* out = p.dw + (cell.row * p.E + e) * p.d + c0;
-            if (BF16) {
+            if (BF16 || (whole && c0 + 4 < p.d)) {
                 ((f32x4*)out)[0] = f32x4{acc[m][0][r], acc[m][1][r], acc[m][2][r], acc[m][3][r]};
                 ((f32x4*)out)[1] = f32x4{acc[m][4][r], acc[m][5][r], acc[m][6][r], acc[m][7][r]};
             } else {
@@ -646,6 +654,11 @@ __global__ __launch_bounds__(256) void scores_backward_f32_kernel(const float* _
         for (int r = 0; r < 4; ++r) {
             const int64_t t = t0 + 16 * m + 4 * quarter + r;
             if (t >= T) continue;
+            if (whole) {
+                if (c0 < d)
+                    *(f32x4*)(dx + t * d + c0) = f32x4{acc[m][0][r], acc[m][1][r], acc[m][2][r], acc[m][3][r]};
+                continue;
+            }
 #pragma unroll
             for (int n = 0; n < 4; ++n)
                 if (c0 + n < d) dx[t * d + c0 + n] = acc[m][n][r];

@@ -157,8 +157,15 @@ def _holds(t: Optional[torch.Tensor], name: str, *shape: int):
         raise ValueError("%s must hold %s elements, got %s" % (name, tuple(shape), tuple(t.shape)))
 
 
+# the current stream's handle without the Stream object around it, which takes longer to
+# make (2.7 us) than the rest of a short call's marshalling
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> ctypes.c_void_p:
     if stream is None:
+        if _raw_stream is not None:
+            return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
         stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
