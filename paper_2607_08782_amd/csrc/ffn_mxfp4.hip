@@ -38,6 +38,7 @@ struct MxArgs {
     const int32_t* a_rows;               // row p of the product is row a_rows[p] of a, or p
     int64_t a_total;
     int KT;                              // 128-column steps of K
+    int segment;                         // steps that 32-bit offsets reach
     int N;                               // output columns: f (gate/up) or d
     int w_rows;                          // rows of a weight matrix: 2 f or d
     uint8_t* h;                          // gate/up: hidden codes [hp / 128][h_rows][64]
@@ -340,6 +341,27 @@ __device__ __forceinline__ int w_order(int r) {
     return (r & ~31) + 16 * ((r >> 2) & 1) + 4 * ((r >> 3) & 3) + (r & 3);
 }
 
+// Tiles come in two kinds: high ones, and those of at most half the rows (a group's last),
+// whose upper waves have nothing to multiply: half the time of a tile.
+template <int BM>
+__device__ __forceinline__ int high_tiles(int rows) {
+    return BM > 128 ? (rows + BM / 2 - 1) / BM : (int)ceil_div(rows, BM);
+}
+
+// start[g] = tiles of the groups before g, by count(rows) row tiles each; by one wave
+template <typename Count>
+__device__ __forceinline__ void starts(const int* s_off, int n_groups, int n_tiles, int* start, int lane,
+                                       Count count) {
+    int carry = 0;
+    for (int g0 = 0; g0 < n_groups; g0 += 64) {
+        const int g = g0 + lane;
+        const int incl = wave_incl_scan(g < n_groups ? count(s_off[g + 1] - s_off[g]) * n_tiles : 0);
+        if (g < n_groups) start[g + 1] = carry + incl;
+        carry += __shfl(incl, 63, 64);
+    }
+    if (lane == 0) start[0] = 0;
+}
+
 template <bool SWIGLU, int WM, int TM, int TN, int RING>
 __global__ __launch_bounds__(64 * 2 * WM, TM * TN > 8 ? 1 : 2) void tile_mxfp4_kernel(MxArgs p) {
 #ifdef __HIP_DEVICE_COMPILE__
@@ -347,38 +369,74 @@ __global__ __launch_bounds__(64 * 2 * WM, TM * TN > 8 ? 1 : 2) void tile_mxfp4_k
     constexpr int BM = S::BM, BN = S::BN, BN_OUT = SWIGLU ? BN / 2 : BN;
     constexpr int AL = S::AL, BL = S::BL, ROUND = 16 * S::WAVES;
     extern __shared__ __attribute__((aligned(1024))) char ring[];
-    __shared__ int s_off[MOE_MAX_GROUPS + 1], s_tstart[MOE_MAX_GROUPS + 1];
+    __shared__ int s_off[MOE_MAX_GROUPS + 1], s_high[MOE_MAX_GROUPS + 1], s_low[MOE_MAX_GROUPS + 1];
     __shared__ MxTile s_tile[TILE_LIST];
     int* const s_tok = (int*)(ring + RING * S::STAGE);   // [2][BM]
     const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave % WM, wn = wave / WM;
+    const int wm = wave / 2, wn = wave % 2;              // a SIMD's waves hold rows of both halves
     // of h, the padding columns too (as zeros)
     const int n_tiles = ((SWIGLU ? p.hp : p.N) + BN_OUT - 1) / BN_OUT;
     for (int g = tid; g <= p.n_groups; g += S::THREADS) s_off[g] = first_row(p, g);
     __syncthreads();
-    if (wave == 0) tile_starts<BM>(s_off, p.n_groups, 0, n_tiles, s_tstart, lane);
+    if (wave == 0) {
+        starts(s_off, p.n_groups, n_tiles, s_high, lane, [](int rows) { return high_tiles<BM>(rows); });
+        starts(s_off, p.n_groups, n_tiles, s_low, lane,
+               [](int rows) { return (int)ceil_div(rows, BM) - high_tiles<BM>(rows); });
+    }
     __syncthreads();
-    // each XCD takes a contiguous chunk of the tiles, its workgroups every nper-th of it
-    const int total = __builtin_amdgcn_readfirstlane(s_tstart[p.n_groups]);
+    // each XCD takes a contiguous chunk of the high tiles, then one of the low; its workgroups
+    // every nper-th of it, those from the end what is left after whole rounds, of which the
+    // high ones come as two halves if there are workgroups for all
     const int nper = gridDim.x / NUM_XCD, widx = blockIdx.x / NUM_XCD;
-    const int chunk = (total + NUM_XCD - 1) / NUM_XCD;
-    const int begin = min((int)(blockIdx.x % NUM_XCD) * chunk, total), end = min(begin + chunk, total);
-    const int n_list = (end - begin - widx + nper - 1) / nper;     // this workgroup's tiles
+    const int xcd = blockIdx.x % NUM_XCD;
+    auto share = [&](const int* start, int xcd, int& begin) {
+        const int total = __builtin_amdgcn_readfirstlane(start[p.n_groups]);
+        const int chunk = (total + NUM_XCD - 1) / NUM_XCD;
+        begin = min(xcd * chunk, total);
+        return min(chunk, total - begin);
+    };
+    int high0, low0;
+    const int high = share(s_high, xcd, high0), all = high + share(s_low, NUM_XCD - 1 - xcd, low0);
+    const int rounds = all / nper, whole = rounds * nper;
+    const int last_high = max(high - whole, 0);
+    const bool halves = BM > 128 && all - whole + last_high <= nper;
+    const int left = all - whole + (halves ? last_high : 0);
+    const int n_list = rounds + (nper - 1 - widx < left ? 1 : 0);  // this workgroup's tiles
     if (n_list <= 0) return;
-    // records of the half of the list that starts with tile q0
+    // records of the half of the list that starts with tile q0, half a list ahead of the
+    // products' tile (the loads' is RING ahead at most): the half's old ones are used up
     auto list_tiles = [&](int q0) {
         const int q = q0 + tid;
         if (tid >= TILE_LIST / 2 || q >= n_list) return;
-        const int L = begin + widx + q * nper;
-        const int g = last_le(s_tstart, p.n_groups, L);
+        int i = q * nper + (q < rounds ? widx : nper - 1 - widx), part = 0, parts = 1;
+        if (halves && i >= whole) {
+            if (i < whole + 2 * last_high) {
+                part = (i - whole) & 1;
+                parts = 2;
+                i = whole + (i - whole) / 2;
+            } else {
+                i -= last_high;
+            }
+        }
+        TilePos pos;
+        int g;
+        if (i < high) {
+            const int L = high0 + i;
+            g = last_le(s_high, p.n_groups, L);
+            pos = tile_pos(L - s_high[g], high_tiles<BM>(s_off[g + 1] - s_off[g]), n_tiles);
+        } else {
+            const int L = low0 + i - high;
+            g = last_le(s_low, p.n_groups, L);
+            pos = {high_tiles<BM>(s_off[g + 1] - s_off[g]), L - s_low[g]};
+        }
         const int rows = s_off[g + 1] - s_off[g];
-        const TilePos pos = tile_pos(L - s_tstart[g], (int)ceil_div(rows, BM), n_tiles);
         MxTile t;
         t.w = (uint64_t)p.w[g];
         t.ws = (uint64_t)p.ws[g];
-        t.row0 = s_off[g] + pos.m * BM;
-        t.valid = min(BM, rows - pos.m * BM);
+        const int m0 = pos.m * BM + part * (BM / 2);
+        t.row0 = s_off[g] + m0;
+        t.valid = min(BM / parts, rows - m0);
         t.n0 = pos.n * BN_OUT;
         s_tile[q % TILE_LIST] = t;
     };
@@ -392,25 +450,31 @@ __global__ __launch_bounds__(64 * 2 * WM, TM * TN > 8 ? 1 : 2) void tile_mxfp4_k
         return t;
     };
     list_tiles(0);
+    list_tiles(TILE_LIST / 2);
     __syncthreads();
 
     // the loads' side of the stream: tile, step of it, operand descriptors, row offsets
     // load i of a wave fills LDS rows ROUND i + 16 wave + lane / 4 of A or B, slot lane % 4
     const int lrow = 16 * wave + (lane >> 2);
     const int lchunk = ((lane & 3) ^ ((lane >> 4) & 3)) * 16;
-    const int boff = w_order(lrow) * STEP_BYTES + lchunk;
     const int a_words = 64 * (wave % (BM / 64)), b_words = 64 * (wave % (BN / 64));
-    const bool words_of_a = S::WL == 2 || wave < S::WAVES / 2;
-    // descriptors start at the step's first row: base and bytes of each, moved on by a step
-    struct Range {
-        uint64_t base;
-        int bytes;
+    // word load n: of A's rows or B's
+    auto of_a = [&](int n) { return S::WL == 2 ? n == 0 : wave < S::WAVES / 2; };
+    // Descriptors stay for up to p.segment steps, which an offset counts; rows past the
+    // group's or the matrix's repeat its last one.
+    auto rsrc = [](uint64_t base) {
+        return __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, -1, RSRC_WORD3);
     };
-    Range ra = {}, rlo = {}, rhi = {}, ras = {}, rbs = {};
-    auto rsrc = [](const Range& r) {
-        return __builtin_amdgcn_make_buffer_rsrc((void*)r.base, (short)0, r.bytes, RSRC_WORD3);
-    };
-    int aoff[AL], asoff = 0, bsoff = 0;
+    uint64_t base_a = 0, base_b = 0, base_w[S::WL];
+    __amdgpu_buffer_rsrc_t ra = rsrc(0), rb = ra, rw[S::WL] = {};
+    const uint32_t step_a = (uint32_t)p.a_total * STEP_BYTES, step_b = (uint32_t)p.w_rows * STEP_BYTES;
+    uint32_t at_a = 0, at_b = 0, at_w[S::WL], step_w[S::WL];
+    int aoff[AL], boff[BL], woff[S::WL], w_lds[S::WL];
+#pragma unroll
+    for (int n = 0; n < S::WL; ++n) {
+        w_lds[n] = of_a(n) ? S::A_WORDS + a_words * 4 : S::B_WORDS + b_words * 4;
+        step_w[n] = (of_a(n) ? step_a : step_b) / (STEP_BYTES / 4);
+    }
     // gather: the token rows of a tile's rows come into LDS a tile ahead, by a direct load
     // like the ring's (zero past the group): three steps later every wave's has landed
     auto fetch_tokens = [&](int q) {
@@ -422,74 +486,80 @@ __global__ __launch_bounds__(64 * 2 * WM, TM * TN > 8 ? 1 : 2) void tile_mxfp4_k
                                                  0, 0);
     };
     if (p.a_rows != nullptr) fetch_tokens(0);
-    int lq = -1, lkt = p.KT;                             // before the first tile
-    auto next_tile = [&]() {
-        ++lq;
-        lkt = 0;
-        const bool live = lq < n_list;
-        if ((lq + 1) % (TILE_LIST / 2) == 0 && lq + 1 < n_list) {
-            __syncthreads();                             // the half's old records are used up
-            list_tiles(lq + 1);
-            __syncthreads();
-        }
-        const MxTile t = tile_at(live ? lq : n_list - 1);
-        if (p.a_rows != nullptr) {
-            if (lq == 0 || p.KT < RING - 1) {            // no three steps since it was issued
-                wait_vm<0>();
-                asm volatile("s_barrier" ::: "memory");
-            }
-            if (lq + 1 < n_list) fetch_tokens(lq + 1);
-        }
-        // past the last tile: empty ranges, loads without traffic
-        const int some = live ? 1 : 0;
-        if (p.a_rows != nullptr) ra = {(uint64_t)p.a, some * (int)p.a_total * STEP_BYTES};
-        else ra = {(uint64_t)(p.a + (int64_t)t.row0 * STEP_BYTES), some * t.valid * STEP_BYTES};
-        ras = {(uint64_t)p.as, some * (int)p.a_total * 4};
+    int lq = -1, lkt = 0, left_steps = 0;                // before the first tile
+    // the next segment of the tile's steps, or the next tile
+    auto next_segment = [&]() {
+        if (lkt < p.KT && lq >= 0) {
+            base_a += (uint64_t)p.segment * p.a_total * STEP_BYTES;
+            base_b += (uint64_t)p.segment * p.w_rows * STEP_BYTES;
 #pragma unroll
-        for (int i = 0; i < AL; ++i) {
-            const int r = lrow + ROUND * i;
-            if (p.a_rows == nullptr) aoff[i] = r * STEP_BYTES + lchunk;
-            else aoff[i] = r < t.valid ? s_tok[(lq & 1) * BM + r] * STEP_BYTES + lchunk : A_OOB;
+            for (int n = 0; n < S::WL; ++n)
+                base_w[n] += (uint64_t)p.segment * (of_a(n) ? p.a_total : p.w_rows) * 4;
+        } else {
+            ++lq;
+            lkt = 0;
+            const bool live = lq < n_list;
+            const MxTile t = tile_at(live ? lq : n_list - 1);
+            if (p.a_rows != nullptr) {
+                if (lq == 0 || p.KT < RING - 1) {        // no three steps since it was issued
+                    wait_vm<0>();
+                    asm volatile("s_barrier" ::: "memory");
+                }
+                if (lq + 1 < n_list) fetch_tokens(lq + 1);
+            }
+            // past the last tile: all lanes on one row
+            auto row_a = [&](int r) {
+                return !live ? 0 : p.a_rows != nullptr ? s_tok[(lq & 1) * BM + r] : min(r, t.valid - 1);
+            };
+            auto row_b = [&](int r) {
+                const bool up = SWIGLU && r >= BN / 2;
+                return !live ? 0 : min(t.n0 + w_order(up ? r - BN / 2 : r), p.N - 1) + (up ? p.N : 0);
+            };
+            const int64_t first = p.a_rows != nullptr ? 0 : t.row0;
+            base_a = (uint64_t)p.a + first * STEP_BYTES;
+            base_b = t.w;
+#pragma unroll
+            for (int i = 0; i < AL; ++i) aoff[i] = row_a(lrow + ROUND * i) * STEP_BYTES + lchunk;
+#pragma unroll
+            for (int i = 0; i < BL; ++i) boff[i] = row_b(lrow + ROUND * i) * STEP_BYTES + lchunk;
+#pragma unroll
+            for (int n = 0; n < S::WL; ++n) {
+                base_w[n] = of_a(n) ? (uint64_t)p.as + first * 4 : t.ws;
+                woff[n] = (of_a(n) ? row_a(a_words + lane) : row_b(b_words + lane)) * 4;
+            }
         }
-        asoff = (p.a_rows != nullptr ? s_tok[(lq & 1) * BM + a_words + lane]
-                                     : t.row0 + min(a_words + lane, t.valid - 1)) * 4;
-        // weight rows past the matrix's, or of the gate half past its own, read as zero
-        const int cols = __builtin_amdgcn_readfirstlane(some * max(min(BN_OUT, p.N - t.n0), 0));
-        const int up = SWIGLU ? p.N + t.n0 : t.n0;
-        rlo = {t.w + (uint64_t)t.n0 * STEP_BYTES, cols * STEP_BYTES};
-        rhi = {t.w + (uint64_t)up * STEP_BYTES, cols * STEP_BYTES};
-        const int b = w_order(b_words + lane);
-        bsoff = (SWIGLU && b >= BN / 2 ? up + b - BN / 2 : t.n0 + b) * 4;
-        rbs = {t.ws, some * p.w_rows * 4};
+        ra = rsrc(base_a), rb = rsrc(base_b);
+        at_a = at_b = 0;
+#pragma unroll
+        for (int n = 0; n < S::WL; ++n) {
+            rw[n] = rsrc(base_w[n]);
+            at_w[n] = 0;
+        }
+        left_steps = min(p.segment, p.KT - lkt);
+        lkt += left_steps;
     };
     // direct load i of the stream's next step
     auto load1 = [&](char* st, int i) {
         if (i < AL) {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                rsrc(ra), (lds_void*)(st + (ROUND * i + 16 * wave) * STEP_BYTES), 16, aoff[i], 0, 0, 0);
+                ra, (lds_void*)(st + (ROUND * i + 16 * wave) * STEP_BYTES), 16, aoff[i], at_a, 0, 0);
         } else if (i < AL + BL) {
             const int b = i - AL;
-            const bool up = SWIGLU && b >= BL / 2;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                rsrc(up ? rhi : rlo), (lds_void*)(st + S::B_CODES + (ROUND * b + 16 * wave) * STEP_BYTES),
-                16, boff + (up ? b - BL / 2 : b) * ROUND * STEP_BYTES, 0, 0, 0);
-        } else if (i == AL + BL && words_of_a) {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(ras), (lds_void*)(st + S::A_WORDS + a_words * 4),
-                                                     4, asoff, 0, 0, 0);
+                rb, (lds_void*)(st + S::B_CODES + (ROUND * b + 16 * wave) * STEP_BYTES), 16, boff[b], at_b,
+                0, 0);
         } else {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(rbs), (lds_void*)(st + S::B_WORDS + b_words * 4),
-                                                     4, bsoff, 0, 0, 0);
+            const int n = i - AL - BL;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rw[n], (lds_void*)(st + w_lds[n]), 4, woff[n], at_w[n],
+                                                     0, 0);
         }
     };
     auto next_step = [&]() {
-        ++lkt;
-        ra.base += (uint64_t)p.a_total * STEP_BYTES;
-        ras.base += (uint64_t)p.a_total * 4;
-        rlo.base += (uint64_t)p.w_rows * STEP_BYTES;
-        rhi.base += (uint64_t)p.w_rows * STEP_BYTES;
-        rbs.base += (uint64_t)p.w_rows * 4;
+        --left_steps;
+        at_a += step_a, at_b += step_b;
+#pragma unroll
+        for (int n = 0; n < S::WL; ++n) at_w[n] += step_w[n];
     };
-    auto slot = [&](unsigned step) { return ring + (step % RING) * S::STAGE; };
 
     // the products' side: fragment addresses within a step (16-column halves of it by kk)
     const int swz = (r32 >> 2) & 3;
@@ -543,68 +613,100 @@ __global__ __launch_bounds__(64 * 2 * WM, TM * TN > 8 ? 1 : 2) void tile_mxfp4_k
     constexpr std::integral_constant<int, 0> first{};
     constexpr std::integral_constant<int, 1> second{};
 
-    unsigned step = 0;
     // a step's loads are issued in two halves of a step of products each: the second of one
     // step, once the slot is free, and the first of the next
     constexpr int EARLY = (S::LOADS + 1) / 2;
-    for (unsigned s = 0; s < RING; ++s) {
-        if (lkt >= p.KT) next_tile();
+    for (int r = 0; r < RING; ++r) {
+        char* const st = ring + r * S::STAGE;
+        if (left_steps == 0) next_segment();
 #pragma unroll
-        for (int i = 0; i < EARLY; ++i) load1(slot(s), i);
-        if (s == RING - 1) break;
+        for (int i = 0; i < EARLY; ++i) load1(st, i);
+        if (r == RING - 1) break;
 #pragma unroll
-        for (int i = EARLY; i < S::LOADS; ++i) load1(slot(s), i);
+        for (int i = EARLY; i < S::LOADS; ++i) load1(st, i);
         next_step();
     }
     wait_vm<(RING - 2) * S::LOADS + EARLY>();
     asm volatile("s_barrier" ::: "memory");
 #pragma unroll
     for (int i = 0; i < TM + TN; ++i) {
-        read1(slot(0), 0, i);
-        read_word(slot(0), i);
+        read1(ring, 0, i);
+        read_word(ring, i);
     }
+    // slots of this step, the next, and the one that loads go to (offsets in the ring)
+    unsigned here = 0, next = S::STAGE, fill = (RING - 1) * S::STAGE;
+    auto turn = [&]() {                                  // the step's slot is free
+        fill = here;
+        here = next;
+        next = next == (RING - 1) * S::STAGE ? 0 : next + S::STAGE;
+    };
     // stores of an epilogue: newer than the loads that the next RING - 2 waits are for
     constexpr int STORES = SWIGLU ? TM * TN / 2 + TM : 2 * TM * TN;
     int fresh = 0;
+    // the next step has landed: outstanding may be the two after it, and stores
+    auto landed = [&]() {
+        if (fresh > 0) {
+            wait_vm<(RING - 2) * S::LOADS + STORES>();
+            --fresh;
+        } else {
+            wait_vm<(RING - 2) * S::LOADS>();
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
     for (int q = 0; q < n_list; ++q) {
         const MxTile cur = tile_at(q);
+        if (q > 0 && q % (TILE_LIST / 2) == 0) list_tiles(q + TILE_LIST / 2);
+        if (wm * 32 * TM >= cur.valid) {                 // no row of this wave's: its loads only
+#pragma clang loop unroll(disable)
+            for (int t = 0; t < p.KT; ++t) {
+#pragma unroll
+                for (int i = EARLY; i < S::LOADS; ++i) load1(ring + fill, i);
+                next_step();
+                landed();
+                turn();
+                if (left_steps == 0) next_segment();
+#pragma unroll
+                for (int i = 0; i < EARLY; ++i) load1(ring + fill, i);
+            }
+#pragma unroll
+            for (int i = 0; i < TM + TN; ++i) {
+                read1(ring + here, 0, i);
+                read_word(ring + here, i);
+            }
+            continue;
+        }
 #pragma unroll
         for (int m = 0; m < TM; ++m)
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[m][j][e] = 0.f;
-        for (int t = 0; t < p.KT; ++t, ++step) {
+#pragma clang loop unroll(disable)
+        for (int t = 0; t < p.KT; ++t) {
             take_words();
 #pragma unroll
             for (int i = 0; i < TM + TN; ++i) {
                 if (2 * i < TM + TN) {
-                    read1(slot(step), 1, 2 * i);
-                    read1(slot(step), 1, 2 * i + 1);
+                    read1(ring + here, 1, 2 * i);
+                    read1(ring + here, 1, 2 * i + 1);
                 }
-                if (i >= TM + TN - (S::LOADS - EARLY)) load1(slot(step + RING - 1), S::LOADS - (TM + TN) + i);
+                if (i >= TM + TN - (S::LOADS - EARLY)) load1(ring + fill, S::LOADS - (TM + TN) + i);
                 multiply(first, i);
             }
             pin();
             next_step();
-            // the next step has landed: outstanding may be the two after it, and stores
-            if (fresh > 0) {
-                wait_vm<(RING - 2) * S::LOADS + STORES>();
-                --fresh;
-            } else {
-                wait_vm<(RING - 2) * S::LOADS>();
-            }
-            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            if (lkt >= p.KT) next_tile();
+            landed();
+            turn();
+            if (left_steps == 0) next_segment();
 #pragma unroll
             for (int i = 0; i < TM + TN; ++i) {
                 if (2 * i < TM + TN) {
-                    read1(slot(step + 1), 0, 2 * i);
-                    read1(slot(step + 1), 0, 2 * i + 1);
-                    read_word(slot(step + 1), 2 * i);
-                    read_word(slot(step + 1), 2 * i + 1);
+                    read1(ring + here, 0, 2 * i);
+                    read1(ring + here, 0, 2 * i + 1);
+                    read_word(ring + here, 2 * i);
+                    read_word(ring + here, 2 * i + 1);
                 }
-                if (i >= TM + TN - EARLY) load1(slot(step), i - (TM + TN - EARLY));
+                if (i >= TM + TN - EARLY) load1(ring + fill, i - (TM + TN - EARLY));
                 multiply(second, i);
             }
             pin();
@@ -632,6 +734,7 @@ __global__ __launch_bounds__(64 * 2 * WM, TM * TN > 8 ? 1 : 2) void tile_mxfp4_k
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         v[e] = swiglu(acc[m][j][e], acc[m][TN / 2 + j][e]);
+                        if (cur.n0 + BN_OUT > p.N && col + 32 * j + 16 * half + e >= p.N) v[e] = 0.f;
                         most = max(most, __float_as_uint(v[e]) & 0x7fffffffu);
                     }
                     most = max(most, (uint32_t)__shfl_xor((int)most, 32, 64));
@@ -708,6 +811,10 @@ int launch_strips(MxArgs& p, int64_t max_rows, int cus, hipStream_t s) {
 constexpr int64_t STRIP_MAX_ROWS = 128;
 constexpr int64_t LARGE_WORK = (int64_t)256 * 256 * 256;
 
+int segment_steps(int64_t a_rows, int64_t w_rows) {
+    return (int)std::max<int64_t>(0x7fffffff / (std::max(a_rows, w_rows) * STEP_BYTES), 1);
+}
+
 int64_t align256(int64_t x) { return (x + 255) & ~(int64_t)255; }
 
 // workspace: [x codes][x scale words][h codes][h scale words], step-major
@@ -753,6 +860,7 @@ int launch_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
     p.a_rows = row_token;
     p.a_total = T;
     p.KT = (int)(mx_cols(d) / 128);
+    p.segment = segment_steps(T, 2 * f);
     p.N = f;
     p.w_rows = 2 * f;
     p.h = (uint8_t*)base + at.h;
@@ -775,6 +883,7 @@ int launch_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
     p.a_rows = nullptr;
     p.a_total = rows;
     p.KT = p.hp / 128;
+    p.segment = segment_steps(rows, d);
     p.N = d;
     p.w_rows = d;
     p.y = (bf16_t*)y;
