@@ -37,6 +37,8 @@ struct MxArgs {
     const uint32_t* as;                  // and scale words [P / 128][a_total]
     const int32_t* a_rows;               // row p of the product is row a_rows[p] of a, or p
     int64_t a_total;
+    const bf16_t* x;                     // the rows before their quantization [a_total][d]
+    int d;
     int KT;                              // 128-column steps of K
     int segment;                         // steps that 32-bit offsets reach
     int N;                               // output columns: f (gate/up) or d
@@ -71,15 +73,36 @@ __device__ __forceinline__ float swiglu(float a, float b) {
 // weight byte goes from memory to the registers of the one wave that multiplies it, and no
 // wave waits for another before the end.  The waves' sums meet in LDS, in wave order.
 // MS: 16-row blocks of token rows held at once
-template <int MS, int TILES>
+template <int MS, int TILES, bool QUANT>
 struct StripStep {
-    i32x4 b[TILES], a[MS];
-    uint32_t bs[TILES], as[MS];
+    i32x4 b[TILES], a[QUANT ? 4 : MS];                   // QUANT: the lane's 32 bf16 values
+    uint32_t bs[TILES], as[QUANT ? 1 : MS];
 };
 
+// The MXFP4 block of a lane's 32 bf16 values: codes, scale byte.
+__device__ __forceinline__ i32x4 mx_block(const i32x4 (&x)[4], uint32_t& byte) {
+    float v[4][8];
+    uint32_t most = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[u][2 * i] = __uint_as_float((uint32_t)x[u][i] << 16);
+            v[u][2 * i + 1] = __uint_as_float((uint32_t)x[u][i] & 0xffff0000u);
+        }
+        most = max(most, magnitude8(v[u]));
+    }
+    i32x4 w;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) w[u] = (int)mx_encode8(v[u], most, byte);
+    return w;
+}
+
 // The rows of a group, 16 MS at a time; row0, rows: of the group.  D steps of loads are in
-// flight (past the end of K without traffic: every wait counts the same loads).
-template <bool SWIGLU, int W, int TILES, int MS, int D>
+// flight (past the end of K without traffic: every wait counts the same loads).  QUANT (one
+// row block): rows come as bf16 values, of which a lane holds just the 32 that are its block
+// of the step, and are quantized as they are multiplied.
+template <bool SWIGLU, int W, int TILES, int MS, int D, bool QUANT = false>
 __device__ __forceinline__ void strip_rows(const MxArgs& p, float* red, int g, int n0, int row0,
                                            int rows) {
 #ifdef __HIP_DEVICE_COMPILE__
@@ -108,7 +131,7 @@ __device__ __forceinline__ void strip_rows(const MxArgs& p, float* red, int g, i
         for (int m = 0; m < MS; ++m) {
             const int r = min(m0 + 16 * m + i16, rows - 1);
             const int row = p.a_rows ? p.a_rows[row0 + r] : r;
-            aoff[m] = row * STEP_BYTES + quarter * 16;
+            aoff[m] = QUANT ? (row * p.d + quarter * 32) * 2 : row * STEP_BYTES + quarter * 16;
             asoff[m] = row * 4;
         }
         const int64_t first = p.a_rows ? 0 : row0;
@@ -118,14 +141,15 @@ __device__ __forceinline__ void strip_rows(const MxArgs& p, float* red, int g, i
         for (int m = 0; m < MS; ++m)
 #pragma unroll
             for (int j = 0; j < TILES; ++j) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        auto load = [&](StripStep<MS, TILES>& s, int t) {
+        auto load = [&](StripStep<MS, TILES, QUANT>& s, int t) {
             const int live = t < p.KT ? 1 : 0;
             const int64_t brow = (int64_t)t * p.w_rows, arow = t * p.a_total + first;
             const auto lo = rsrc(p.w[g] + (brow + n0) * STEP_BYTES, live * valid * STEP_BYTES);
             const auto hi = rsrc(p.w[g] + (brow + (SWIGLU ? p.N + n0 : n0)) * STEP_BYTES,
                                  live * valid * STEP_BYTES);
             const auto bs = rsrc(p.ws[g] + brow, live * p.w_rows * 4);
-            const auto a = rsrc(p.a + arow * STEP_BYTES, live * reach * STEP_BYTES);
+            const auto a = QUANT ? rsrc(p.x + first * p.d, live * reach * p.d * 2)
+                                 : rsrc(p.a + arow * STEP_BYTES, live * reach * STEP_BYTES);
             const auto as = rsrc(p.as + arow, live * reach * 4);
 #pragma unroll
             for (int j = 0; j < TILES; ++j)
@@ -135,6 +159,15 @@ __device__ __forceinline__ void strip_rows(const MxArgs& p, float* red, int g, i
 #pragma unroll
             for (int j = 0; j < TILES; ++j)
                 s.bs[j] = __builtin_amdgcn_raw_buffer_load_b32(bs, bsoff[j], 0, 0);
+            if (QUANT) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u)              // columns past d: zeros
+                    s.a[u] = __builtin_bit_cast(
+                        i32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                   a, 128 * t + 32 * quarter + 8 * u < p.d ? aoff[0] + t * 256 + 16 * u : A_OOB,
+                                   0, 0));
+                return;
+            }
 #pragma unroll
             for (int m = 0; m < MS; ++m) {
                 s.a[m] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(a, aoff[m], 0, 0));
@@ -144,20 +177,28 @@ __device__ __forceinline__ void strip_rows(const MxArgs& p, float* red, int g, i
         // the weights are the matrix instruction's first operand: a lane then holds four
         // consecutive output columns of one row.  A lane's block of 32 is the word's byte
         // `quarter`
-        auto multiply = [&](const StripStep<MS, TILES>& s) {
+        auto multiply = [&](const StripStep<MS, TILES, QUANT>& s) {
             uint32_t sa[MS];
+            i32x4 a[MS];
 #pragma unroll
-            for (int m = 0; m < MS; ++m) sa[m] = s.as[m] >> (8 * quarter);
+            for (int m = 0; m < MS; ++m) {
+                if constexpr (QUANT) {
+                    a[m] = mx_block(s.a, sa[m]);
+                } else {
+                    a[m] = s.a[m];
+                    sa[m] = s.as[m] >> (8 * quarter);
+                }
+            }
 #pragma unroll
             for (int j = 0; j < TILES; ++j) {
                 const uint32_t sb = s.bs[j] >> (8 * quarter);
 #pragma unroll
                 for (int m = 0; m < MS; ++m)
                     acc[m][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                        operand(s.b[j]), operand(s.a[m]), acc[m][j], 4, 4, 0, (int)sb, 0, (int)sa[m]);
+                        operand(s.b[j]), operand(a[m]), acc[m][j], 4, 4, 0, (int)sb, 0, (int)sa[m]);
             }
         };
-        StripStep<MS, TILES> s[D];
+        StripStep<MS, TILES, QUANT> s[D];
 #pragma unroll
         for (int i = 0; i < D; ++i) load(s[i], wave + i * W);
         for (int t = wave; t < p.KT; t += D * W)
@@ -263,10 +304,16 @@ __device__ __forceinline__ Group nth_group(const MxArgs& p, int n) {
     return {0, 0, 0};
 }
 
+// Steps of a wave up to which two are in flight, not three or four: more are loads that a
+// wave issues before its first product and, past its last step, for nothing (a single token
+// through DeepSeek-V2-Lite's experts, whose down product gives a wave 3 steps: 14.8 us with
+// four, 13.7 with two; Mixtral's of 28 steps, 16 tokens: 41.8 and 42.5).
+constexpr int FEW_STEPS = 6;
+
 // MAX_MS = 1: no group holds more than 16 rows, and the registers of one row block let
 // twice the waves in.  Otherwise each group takes the row blocks it needs.
-template <bool SWIGLU, int W, int TILES, int MAX_MS>
-__global__ __launch_bounds__(64 * W, MAX_MS == 1 ? 4 : 2) void strip_mxfp4_kernel(MxArgs p) {
+template <bool SWIGLU, int W, int TILES, int MAX_MS, bool QUANT>
+__global__ __launch_bounds__(64 * W, QUANT ? 3 : MAX_MS == 1 ? 4 : 2) void strip_mxfp4_kernel(MxArgs p) {
     constexpr int LD = 16 * TILES + 4;
     constexpr int SUMS = W * 16 * MAX_MS * LD * 4 > 70 * 1024 ? W / 2 * 16 * MAX_MS * LD : W * 16 * MAX_MS * LD;
     __shared__ __attribute__((aligned(16))) float red[SUMS];
@@ -281,9 +328,12 @@ __global__ __launch_bounds__(64 * W, MAX_MS == 1 ? 4 : 2) void strip_mxfp4_kerne
         of.rows = __builtin_amdgcn_readfirstlane(first_row(p, slot + 1)) - of.row0;
     }
     if (of.rows <= 0) return;
-    constexpr int D1 = MAX_MS == 1 ? (TILES == 4 ? 3 : 4) : (TILES == 4 ? 3 : 4);
-    if (MAX_MS == 1 || of.rows <= 16) strip_rows<SWIGLU, W, TILES, 1, D1>(p, red, of.g, n0, of.row0, of.rows);
-    else if (of.rows <= 32) strip_rows<SWIGLU, W, TILES, 2, TILES == 4 ? 3 : 4>(p, red, of.g, n0, of.row0, of.rows);
+    constexpr int D = TILES == 4 ? 3 : 4;
+    if (QUANT || ((MAX_MS == 1 || of.rows <= 16) && p.KT <= FEW_STEPS * W))
+        strip_rows<SWIGLU, W, TILES, 1, 2, QUANT>(p, red, of.g, n0, of.row0, of.rows);
+    else if (MAX_MS == 1 || of.rows <= 16)
+        strip_rows<SWIGLU, W, TILES, 1, D>(p, red, of.g, n0, of.row0, of.rows);
+    else if (of.rows <= 32) strip_rows<SWIGLU, W, TILES, 2, D>(p, red, of.g, n0, of.row0, of.rows);
     else strip_rows<SWIGLU, W, TILES, 4, TILES == 4 ? 2 : 3>(p, red, of.g, n0, of.row0, of.rows);
 }
 
@@ -784,14 +834,24 @@ int launch_tiles(const MxArgs& p, int cus, hipStream_t s) {
     return launch_status();
 }
 
+// Whether gate/up strips quantize the token rows themselves: a launch less, but every strip
+// does it again (FFN, with the launch and without: one token, DeepSeek-V2-Lite 16.5 and
+// 14.8 us, Qwen3-30B-A3B 13.9 and 11.2; 16 tokens 34.1 and 33.0, 14.2 and 12.3; Mixtral-shaped,
+// twice the steps, 8 tokens 39.2 and 39.0, 16 tokens 40.0 and 41.8).
+bool strips_quantize(int64_t max_rows, int d) {
+    return max_rows <= 16 && max_rows * (mx_cols(d) / 128) <= 256;
+}
+
 template <bool SWIGLU, int W, int TILES>
 int launch_strips_of(MxArgs& p, int64_t max_rows, hipStream_t s) {
     p.strips = (int)ceil_div(SWIGLU ? 2 * p.hp : p.N, 16 * TILES);
     const dim3 grid((unsigned)(p.slots * p.strips)), block(64 * W);
-    if (max_rows <= 16)
-        hipLaunchKernelGGL((strip_mxfp4_kernel<SWIGLU, W, TILES, 1>), grid, block, 0, s, p);
+    if (SWIGLU && strips_quantize(max_rows, p.d))
+        hipLaunchKernelGGL((strip_mxfp4_kernel<SWIGLU, W, TILES, 1, SWIGLU>), grid, block, 0, s, p);
+    else if (max_rows <= 16)
+        hipLaunchKernelGGL((strip_mxfp4_kernel<SWIGLU, W, TILES, 1, false>), grid, block, 0, s, p);
     else
-        hipLaunchKernelGGL((strip_mxfp4_kernel<SWIGLU, W, TILES, 4>), grid, block, 0, s, p);
+        hipLaunchKernelGGL((strip_mxfp4_kernel<SWIGLU, W, TILES, 4, false>), grid, block, 0, s, p);
     return launch_status();
 }
 
@@ -842,9 +902,14 @@ int launch_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
     if (rows == 0 || T == 0) return MOE_OK;
     const Layout at(T, rows, d, f);
     char* base = (char*)ws;
-    int st = launch_quantize_mxfp4_steps((const bf16_t*)x, T, d, (uint8_t*)base,
+    // a token reaches an expert at most once
+    const int64_t max_rows = row_token ? T : rows;
+    int st = MOE_OK;
+    if (!strips_quantize(max_rows, d)) {
+        st = launch_quantize_mxfp4_steps((const bf16_t*)x, T, d, (uint8_t*)base,
                                          (uint32_t*)(base + at.xs), s);
-    if (st != MOE_OK) return st;
+        if (st != MOE_OK) return st;
+    }
     MxArgs p;
     for (int i = 0; i < MOE_MAX_GROUPS; ++i) {
         p.w[i] = i < n_groups ? w13[i] : nullptr;
@@ -859,6 +924,8 @@ int launch_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
     p.as = (const uint32_t*)(base + at.xs);
     p.a_rows = row_token;
     p.a_total = T;
+    p.x = (const bf16_t*)x;
+    p.d = d;
     p.KT = (int)(mx_cols(d) / 128);
     p.segment = segment_steps(T, 2 * f);
     p.N = f;
@@ -868,8 +935,6 @@ int launch_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
     p.h_rows = rows;
     p.hp = (int)mx_cols(f);
     p.y = nullptr;
-    // a token reaches an expert at most once
-    const int64_t max_rows = row_token ? T : rows;
     const int cus = num_cus();
     st = max_rows <= STRIP_MAX_ROWS ? launch_strips<true>(p, max_rows, cus, s)
          : rows * p.N >= LARGE_WORK ? launch_tiles<true, 4, 2, 4, 3>(p, cus, s) : launch_tiles<true, 2, 2, 2, 4>(p, cus, s);
