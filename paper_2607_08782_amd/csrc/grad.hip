@@ -5,6 +5,7 @@
 #include <algorithm>
 
 #include "common.h"
+#include "tiles.h"
 
 namespace moe {
 namespace {
@@ -176,10 +177,11 @@ int combine_backward(const void* dy, const void* y_perm, const int32_t* token_ro
 // ---------------------------------------------------------------------------
 // Gradient of the gates and gate scores.
 
-// dlogits, a token per wave at a time; lane l holds experts l, l + 64, ...  Beside the dense
-// rows, with MOE_RENORM, the chosen experts' values [T][k] (sel).
+// dlogits, a token per wave: four in turn took twice as long where there are few (777 of
+// DeepSeek-V2-Lite 7.7 us, this 3.8) and no less where there are many (16384 of Qwen3-30B-A3B
+// 9.1 and 8.6).  Lane l holds experts l, l + 64, ...  Beside the dense rows, with MOE_RENORM,
+// the chosen experts' values [T][k] (sel).
 constexpr int RB_THREADS = 256;
-constexpr int RT = 16;                                   // tokens per workgroup
 constexpr int RJ = MOE_MAX_E / 64;
 
 template <bool RENORM>
@@ -189,60 +191,57 @@ __global__ __launch_bounds__(RB_THREADS) void gate_backward_kernel(
     float* __restrict__ sel) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int64_t t = (int64_t)blockIdx.x * (RB_THREADS / 64) + wave;
+    if (t >= T) return;
+    const bool mine = lane < k;
+    const int e_r = mine ? idx[t * k + lane] : -1;
+    const float p_r = mine ? gate[t * k + lane] : 0.f;
+    const float dp_r = mine ? dgate[t * k + lane] : 0.f;
+    const float m = wave_sum(p_r * dp_r);
+    float v[RJ];
+    if (RENORM) {
+        const float dl = p_r * (dp_r - m);
+        if (sel && mine) sel[t * k + lane] = dl;
 #pragma unroll
-    for (int i = 0; i < RT / (RB_THREADS / 64); ++i) {
-        const int64_t t = (int64_t)blockIdx.x * RT + i * (RB_THREADS / 64) + wave;
-        if (t >= T) break;
-        const bool mine = lane < k;
-        const int e_r = mine ? idx[t * k + lane] : -1;
-        const float p_r = mine ? gate[t * k + lane] : 0.f;
-        const float dp_r = mine ? dgate[t * k + lane] : 0.f;
-        const float m = wave_sum(p_r * dp_r);
-        float v[RJ];
-        if (RENORM) {
-            const float dl = p_r * (dp_r - m);
-            if (sel && mine) sel[t * k + lane] = dl;
+        for (int j = 0; j < RJ; ++j) v[j] = 0.f;
+        for (int r = 0; r < k; ++r) {
+            const int e = __builtin_amdgcn_readlane(e_r, r);
+            const float x = __uint_as_float(
+                (uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(dl), r));
 #pragma unroll
-            for (int j = 0; j < RJ; ++j) v[j] = 0.f;
-            for (int r = 0; r < k; ++r) {
-                const int e = __builtin_amdgcn_readlane(e_r, r);
-                const float x = __uint_as_float(
-                    (uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(dl), r));
-#pragma unroll
-                for (int j = 0; j < RJ; ++j) v[j] = lane + 64 * j == e ? x : v[j];
-            }
-        } else {
-            float l[RJ], top = -INFINITY, z = 0.f;
-#pragma unroll
-            for (int j = 0; j < RJ; ++j) {
-                l[j] = lane + 64 * j < E ? logits[t * E + lane + 64 * j] : -INFINITY;
-                top = fmaxf(top, l[j]);
-            }
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-#pragma unroll
-            for (int j = 0; j < RJ; ++j) {
-                l[j] = expf(l[j] - top);
-                z += l[j];
-            }
-            z = 1.f / wave_sum(z);
-            float up[RJ];
-#pragma unroll
-            for (int j = 0; j < RJ; ++j) up[j] = 0.f;
-            for (int r = 0; r < k; ++r) {
-                const int e = __builtin_amdgcn_readlane(e_r, r);
-                const float x = __uint_as_float(
-                    (uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(dp_r), r));
-#pragma unroll
-                for (int j = 0; j < RJ; ++j) up[j] = lane + 64 * j == e ? x : up[j];
-            }
-#pragma unroll
-            for (int j = 0; j < RJ; ++j) v[j] = l[j] * z * (up[j] - m);
+            for (int j = 0; j < RJ; ++j) v[j] = lane + 64 * j == e ? x : v[j];
         }
+    } else {
+        float l[RJ], top = -INFINITY, z = 0.f;
 #pragma unroll
         for (int j = 0; j < RJ; ++j) {
-            if (dlogits && lane + 64 * j < E) dlogits[t * E + lane + 64 * j] = v[j];
+            l[j] = lane + 64 * j < E ? logits[t * E + lane + 64 * j] : -INFINITY;
+            top = fmaxf(top, l[j]);
         }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+#pragma unroll
+        for (int j = 0; j < RJ; ++j) {
+            l[j] = expf(l[j] - top);
+            z += l[j];
+        }
+        z = 1.f / wave_sum(z);
+        float up[RJ];
+#pragma unroll
+        for (int j = 0; j < RJ; ++j) up[j] = 0.f;
+        for (int r = 0; r < k; ++r) {
+            const int e = __builtin_amdgcn_readlane(e_r, r);
+            const float x = __uint_as_float(
+                (uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(dp_r), r));
+#pragma unroll
+            for (int j = 0; j < RJ; ++j) up[j] = lane + 64 * j == e ? x : up[j];
+        }
+#pragma unroll
+        for (int j = 0; j < RJ; ++j) v[j] = l[j] * z * (up[j] - m);
+    }
+#pragma unroll
+    for (int j = 0; j < RJ; ++j) {
+        if (dlogits && lane + 64 * j < E) dlogits[t * E + lane + 64 * j] = v[j];
     }
 }
 
@@ -352,33 +351,49 @@ __global__ __launch_bounds__(DW_THREADS, 2) void router_grad_kernel(DwArgs p) {
     u32x4 row[8];
     f32x4 wide[BF16 ? 1 : 8][2];                         // fp32 x
     const bool whole = p.d % 4 == 0;                     // rows of 16-byte chunks
-    auto load = [&](int64_t t, int j) {                  // token t + j
-        const bool live = t + j < end;
-        const float* s = p.dl + (t + j) * p.E + e0;
-        a[j] = make_float2(0.f, 0.f);
+    // A step's rows by descriptors that end with the chunk's last token: rows past it, and
+    // lanes past the last expert or column, read as zeros (fp32 x: by comparisons).
+    constexpr int SIZE = sizeof(Elem);
+    auto rsrc = [](const void* base, int bytes) {
+        return __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, bytes, RSRC_WORD3);
+    };
+    __amdgpu_buffer_rsrc_t ra = rsrc(nullptr, 0), rx = ra;
+    int64_t at = 0;
+    auto seek = [&](int64_t t0) {
+        const int rows = t0 < end ? (int)(end - t0 < DW_STEP ? end - t0 : DW_STEP) : 0;
+        ra = rsrc(p.dl + t0 * p.E, rows * p.E * 4);
+        rx = rsrc((const Elem*)p.x + t0 * p.d, rows * p.d * SIZE);
+        at = t0;
+    };
+    const uint32_t e_stride = (uint32_t)p.E * 4, x_stride = (uint32_t)p.d * SIZE;
+    const uint32_t e_off = e0 < p.E ? 8 * quarter * e_stride + 4 * e0 : A_OOB;
+    const uint32_t e_off1 = e0 + 1 < p.E ? 8 * quarter * e_stride + 4 * e0 + 4 : A_OOB;
+    const uint32_t x_off = c0 < p.d ? 8 * quarter * x_stride + SIZE * c0 : A_OOB;
+    auto load = [&](int j) {                             // token at + 8 quarter + j
         if (VEC) {
-            if (live && e0 < p.E) a[j] = *(const float2*)s;
+            a[j] = __builtin_bit_cast(float2, __builtin_amdgcn_raw_buffer_load_b64(ra, e_off + j * e_stride, 0, 0));
         } else {
-            if (live && e0 < p.E) a[j].x = s[0];
-            if (live && e0 + 1 < p.E) a[j].y = s[1];
+            a[j].x = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(ra, e_off + j * e_stride, 0, 0));
+            a[j].y = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(ra, e_off1 + j * e_stride, 0, 0));
         }
         if (p.dw == nullptr) return;
-        if (BF16) {
-            const bf16_t* x = (const bf16_t*)p.x + (t + j) * p.d + c0;
-            row[j] = live && c0 < p.d ? *(const u32x4*)x : u32x4{0, 0, 0, 0};
+        if constexpr (BF16) {
+            row[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, x_off + j * x_stride, 0, 0));
         } else {
-            const float* x = (const float*)p.x + (t + j) * p.d;
+            const bool live = at + 8 * quarter + j < end;
+            const float* x = (const float*)p.x + (at + 8 * quarter + j) * p.d;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                wide[BF16 ? 0 : j][h] = !live   ? f32x4{0.f, 0.f, 0.f, 0.f}
-                                        : whole ? scores4<true>(x, c0 + 4 * h, p.d)
-                                                : scores4<false>(x, c0 + 4 * h, p.d);
+                wide[j][h] = !live   ? f32x4{0.f, 0.f, 0.f, 0.f}
+                             : whole ? scores4<true>(x, c0 + 4 * h, p.d)
+                                     : scores4<false>(x, c0 + 4 * h, p.d);
         }
     };
+    seek(begin + DW_STEP * ts);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) load(begin + DW_STEP * ts + 8 * quarter, j);
+    for (int j = 0; j < 8; ++j) load(j);
     for (int64_t t0 = begin + DW_STEP * ts; t0 < end; t0 += DW_STEP * ts_n) {
-        const int64_t t = t0 + 8 * quarter;
+        seek(t0 + DW_STEP * ts_n);
         if (sums)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -401,7 +416,7 @@ __global__ __launch_bounds__(DW_THREADS, 2) void router_grad_kernel(DwArgs p) {
                 split8<3>(v[1], w[1]);
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) load(t + DW_STEP * ts_n, j);
+            for (int j = 0; j < 8; ++j) load(j);
             if (p.dw == nullptr) continue;
             // the small terms first
 #pragma unroll
@@ -422,7 +437,7 @@ __global__ __launch_bounds__(DW_THREADS, 2) void router_grad_kernel(DwArgs p) {
                         for (int n = 0; n < 8; ++n)
                             acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(
                                 m ? a[j].y : a[j].x, wide[j][n / 4][n % 4], acc[m][n], 0, 0, 0);
-                load(t + DW_STEP * ts_n, j);             // into the registers just multiplied
+                load(j);                                 // into the registers just multiplied
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -547,23 +562,40 @@ __global__ __launch_bounds__(256, 2) void scores_backward_bf16_kernel(
             b[s][n] = __builtin_bit_cast(bf16x8, v);
         }
     }
-    // this wave's token blocks: every runs-th
+    // this wave's token blocks: every runs-th.  Descriptors of a block's rows: rows past T
+    // read as zeros and are not stored, nor are columns past d
     const int64_t blocks = (T + 15) / 16;
+    auto rsrc = [&](const void* base, int64_t block, int row_bytes) {
+        const int rows = block < blocks ? (int)(T - block * 16 < 16 ? T - block * 16 : 16) : 0;
+        return __builtin_amdgcn_make_buffer_rsrc((char*)base + block * 16 * row_bytes, (short)0,
+                                                 rows * row_bytes, RSRC_WORD3);
+    };
     f32x4 lo[KE], hi[KE];
+    const int a_off = (i16 * E + 8 * quarter) * 4;
     auto load = [&](int64_t block) {
-        const int64_t t = block * 16 + i16;
+        const auto r = rsrc(dlogits, block, E * 4);
 #pragma unroll
         for (int s = 0; s < KE; ++s) {
-            lo[s] = hi[s] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (t < T) {
-                lo[s] = scores4<VEC>(dlogits + t * E, 32 * s + 8 * quarter, E);
-                hi[s] = scores4<VEC>(dlogits + t * E, 32 * s + 8 * quarter + 4, E);
+            const int e = 32 * s + 8 * quarter;
+            if (VEC) {
+                lo[s] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                      r, e < E ? a_off + 128 * s : A_OOB, 0, 0));
+                hi[s] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                      r, e + 4 < E ? a_off + 128 * s + 16 : A_OOB, 0, 0));
+            } else {
+                const int64_t t = block * 16 + i16;
+                lo[s] = hi[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (t < T) {
+                    lo[s] = scores4<false>(dlogits + t * E, e, E);
+                    hi[s] = scores4<false>(dlogits + t * E, e + 4, E);
+                }
             }
         }
     };
     constexpr bool AHEAD = KE <= 4;                      // past 128 experts there is no room
+    const int y_off = c0 < d ? (4 * quarter * d + c0) * 2 : A_OOB;
     int64_t block = cell.row * 4 + wave;
-    if (AHEAD && block < blocks) load(block);
+    if (AHEAD) load(block);
     for (; block < blocks; block += runs) {
         u32x4 a[AHEAD ? KE : 1][2];
         auto terms = [&](int s, u32x4 (&out)[2]) {
@@ -573,13 +605,11 @@ __global__ __launch_bounds__(256, 2) void scores_backward_bf16_kernel(
         if (AHEAD) {
 #pragma unroll
             for (int s = 0; s < KE; ++s) terms(s, a[AHEAD ? s : 0]);
-            if (block + runs < blocks) load(block + runs);
+            load(block + runs);
         } else {
             load(block);
         }
         f32x4 acc[NC];
-#pragma unroll
-        for (int n = 0; n < NC; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < KE; ++s) {
             if (!AHEAD) {
@@ -591,15 +621,17 @@ __global__ __launch_bounds__(256, 2) void scores_backward_bf16_kernel(
 #pragma unroll
                 for (int n = 0; n < NC; ++n)
                     acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        __builtin_bit_cast(bf16x8, a[AHEAD ? s : 0][term]), b[s][n], acc[n], 0, 0, 0);
+                        __builtin_bit_cast(bf16x8, a[AHEAD ? s : 0][term]), b[s][n],
+                        s == 0 && term == 1 ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[n], 0, 0, 0);
         }
+        const auto ry = rsrc(dx, block, d * 2);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int64_t t = block * 16 + 4 * quarter + r;
             words v;
 #pragma unroll
             for (int i = 0; i < NC / 2; ++i) v[i] = pack_bf16x2(acc[2 * i][r], acc[2 * i + 1][r]);
-            if (t < T && c0 < d) *(words*)(dx + t * d + c0) = v;
+            if constexpr (NC == 8) __builtin_amdgcn_raw_buffer_store_b128(v, ry, y_off + r * d * 2, 0, 0);
+            else __builtin_amdgcn_raw_buffer_store_b64(v, ry, y_off + r * d * 2, 0, 0);
         }
     }
 }
@@ -791,7 +823,7 @@ int launch_route_backward(const float* dgate, const float* gate, const int32_t* 
     float* sel = sparse ? (float*)(base + at.sel) : nullptr;
     float* dl = dlogits ? dlogits : dw || dbias || (dx && !sparse) ? (float*)base : nullptr;
     if (T > 0) {
-        const dim3 grid((unsigned)ceil_div(T, RT)), block(RB_THREADS);
+        const dim3 grid((unsigned)ceil_div(T, RB_THREADS / 64)), block(RB_THREADS);
         if (renorm)
             hipLaunchKernelGGL(gate_backward_kernel<true>, grid, block, 0, s, dgate, gate, idx, logits,
                                T, E, k, dl, sel);
