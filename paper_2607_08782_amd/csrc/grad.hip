@@ -329,14 +329,15 @@ struct DwArgs {
     float* dbias;                                        // [chunks][E], nullable
 };
 
+typedef f32x4 DwSums[4 * 16 * 64];
+
 template <typename Elem, bool VEC>
-__global__ __launch_bounds__(DW_THREADS, 2) void router_grad_kernel(DwArgs p) {
+__device__ __forceinline__ void router_grad(const DwArgs& p, DwSums& red, unsigned index, unsigned total) {
     constexpr bool BF16 = sizeof(Elem) == 2;
-    __shared__ f32x4 red[4 * 16 * 64];
     const int lane = threadIdx.x & 63, i16 = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int ts_n = 8 / p.eb, block = wave / ts_n, ts = wave % ts_n;
-    const Cell cell = xcd_cell(blockIdx.x, gridDim.x, p.cols);
+    const Cell cell = xcd_cell(index, total, p.cols);
     const int e0 = block * DW_EXPERTS + 2 * i16, c0 = cell.col * DW_COLS + 8 * i16;
     const int64_t begin = cell.row * p.chunk;
     const int64_t end = begin + p.chunk < p.T ? begin + p.chunk : p.T;
@@ -497,6 +498,12 @@ __global__ __launch_bounds__(DW_THREADS, 2) void router_grad_kernel(DwArgs p) {
         }
 }
 
+template <bool VEC>
+__global__ __launch_bounds__(DW_THREADS, 2) void router_grad_f32_kernel(DwArgs p) {
+    __shared__ DwSums red;
+    router_grad<float, VEC>(p, red, blockIdx.x, gridDim.x);
+}
+
 // out[i] = sum over n parts of parts[q][i], in order; two such sums in one launch.
 struct Parts {
     const float* in;
@@ -531,15 +538,26 @@ __global__ __launch_bounds__(256) void sum_parts_kernel(Parts a, Parts b, int n)
 // blocks of 16 tokens, whose dlogits come, in two bf16 terms (16 bits for an output of 8),
 // while the block before multiplies.  Its sums are NC consecutive columns of a row, stored
 // at once.
+struct DxArgs {
+    const float* dlogits;
+    const bf16_t* w;
+    int64_t T;
+    int d, E, runs;                                      // runs: waves side by side over the tokens
+    bf16_t* dx;
+};
+
 template <int KE, int NC, bool VEC>
-__global__ __launch_bounds__(256, 2) void scores_backward_bf16_kernel(
-    const float* __restrict__ dlogits, const bf16_t* __restrict__ w, int64_t T, int d, int E, int runs,
-    bf16_t* __restrict__ dx) {
+__device__ __forceinline__ void scores_backward_bf16(const DxArgs& p, unsigned index, unsigned total) {
+    const float* __restrict__ dlogits = p.dlogits;
+    const bf16_t* __restrict__ w = p.w;
+    bf16_t* __restrict__ dx = p.dx;
+    const int64_t T = p.T;
+    const int d = p.d, E = p.E, runs = p.runs;
     typedef uint32_t words __attribute__((ext_vector_type(NC / 2)));
     const int lane = threadIdx.x & 63, i16 = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int cols = (d + 16 * NC - 1) / (16 * NC);
-    const Cell cell = xcd_cell(blockIdx.x, gridDim.x, cols);
+    const Cell cell = xcd_cell(index, total, cols);
     const int c0 = cell.col * 16 * NC + NC * i16;
     bf16x8 b[KE][NC];
 #pragma unroll
@@ -594,7 +612,7 @@ __global__ __launch_bounds__(256, 2) void scores_backward_bf16_kernel(
     };
     constexpr bool AHEAD = KE <= 4;                      // past 128 experts there is no room
     const int y_off = c0 < d ? (4 * quarter * d + c0) * 2 : A_OOB;
-    int64_t block = cell.row * 4 + wave;
+    int64_t block = cell.row * (DW_THREADS / 64) + wave;
     if (AHEAD) load(block);
     for (; block < blocks; block += runs) {
         u32x4 a[AHEAD ? KE : 1][2];
@@ -634,6 +652,18 @@ __global__ __launch_bounds__(256, 2) void scores_backward_bf16_kernel(
             else __builtin_amdgcn_raw_buffer_store_b64(v, ry, y_off + r * d * 2, 0, 0);
         }
     }
+}
+
+// Both in one launch, dw's workgroups first: what a short batch saves is a launch (777 tokens
+// of DeepSeek-V2-Lite: CHANGE1).
+template <int KE, int NC, bool VEC>
+__global__ __launch_bounds__(DW_THREADS, 2) void router_backward_kernel(DwArgs p, DxArgs q, unsigned dw_groups,
+                                                                        unsigned dw_slots) {
+    __shared__ DwSums red;
+    if (blockIdx.x >= dw_slots)
+        scores_backward_bf16<KE, NC, VEC>(q, blockIdx.x - dw_slots, gridDim.x - dw_slots);
+    else if (blockIdx.x < dw_groups)
+        router_grad<bf16_t, VEC>(p, red, blockIdx.x, dw_groups);
 }
 
 // The same in fp32 by v_mfma_f32_16x16x4_f32: 64 tokens x 64 columns a wave, sixteen
@@ -726,9 +756,12 @@ struct RouteLayout {
     }
 };
 
-int launch_router_grad(const float* dl, const void* x, int dtype, int64_t T, int d, int E, float* dw,
-                       float* dbias, float* dw_parts, float* dbias_parts, hipStream_t s) {
+// dw, dbias (their chunks' sums with plan.n > 1) and dx in bf16; dlogits' rows are those of dl
+int launch_router_backward(const float* dl, const float* sel, const int32_t* idx, const void* x, const void* w,
+                           int dtype, int64_t T, int d, int E, int k, void* dx, float* dw, float* dbias,
+                           float* dw_parts, float* dbias_parts, hipStream_t s) {
     const DwPlan plan(T, d, E);
+    const bool sums = dw || dbias;
     DwArgs p;
     p.dl = dl;
     p.x = x;
@@ -740,58 +773,59 @@ int launch_router_grad(const float* dl, const void* x, int dtype, int64_t T, int
     p.dw = !dw ? nullptr : plan.n > 1 ? dw_parts : dw;
     p.dbias = !dbias ? nullptr : plan.n > 1 ? dbias_parts : dbias;
     p.cols = dw ? (int)ceil_div(d, DW_COLS) : 1;
-    const dim3 grid((unsigned)(p.cols * plan.n)), block(DW_THREADS);
-    const bool vec = E % 2 == 0 && ((uintptr_t)dl & 7u) == 0;
-#define MOE_DW(T_)                                                                             \
-    do {                                                                                       \
-        if (vec) hipLaunchKernelGGL((router_grad_kernel<T_, true>), grid, block, 0, s, p);     \
-        else hipLaunchKernelGGL((router_grad_kernel<T_, false>), grid, block, 0, s, p);        \
+    const unsigned groups = sums ? (unsigned)(p.cols * plan.n) : 0;
+    const dim3 block(DW_THREADS);
+    const bool vec = E % 4 == 0 && ((uintptr_t)dl & 15u) == 0;
+    int st = MOE_OK;
+    if (dtype == MOE_BF16) {
+        // a workgroup a CU, a block of 16 tokens per wave at least; dw's are rounded to whole
+        // rounds over the XCDs
+        const unsigned slots = (groups + 7) & ~7u;
+        const int64_t cols = ceil_div(d, E > 128 ? 64 : 128), most = ceil_div(ceil_div(T, 16), DW_THREADS / 64);
+        const int64_t rows = dx ? std::max<int64_t>(std::min(most, ceil_div(256, cols)), 1) : 0;
+        const DxArgs q = {dl, (const bf16_t*)w, T, d, E, (int)(DW_THREADS / 64 * rows), (bf16_t*)dx};
+        const dim3 grid((unsigned)(slots + rows * cols));
+        if (grid.x == 0) return MOE_OK;
+#define MOE_RB(KE, NC, VEC) \
+    hipLaunchKernelGGL((router_backward_kernel<KE, NC, VEC>), grid, block, 0, s, p, q, groups, slots)
+#define MOE_RB_E(VEC)                   \
+    do {                                \
+        if (E <= 32) MOE_RB(1, 8, VEC); \
+        else if (E <= 64) MOE_RB(2, 8, VEC);  \
+        else if (E <= 128) MOE_RB(4, 8, VEC); \
+        else MOE_RB(8, 4, VEC);         \
     } while (0)
-    if (dtype == MOE_BF16) MOE_DW(bf16_t);
-    else MOE_DW(float);
-#undef MOE_DW
-    if (plan.n > 1) {
+        if (vec) MOE_RB_E(true);
+        else MOE_RB_E(false);
+#undef MOE_RB_E
+#undef MOE_RB
+        st = launch_status();
+    } else {
+        if (dx && sel) {
+            // only the chosen experts' scores have a gradient: their router rows, weighted
+            st = launch_combine(w, dtype, idx, sel, nullptr, 0, T, d, k, dx, s);
+        } else if (dx) {
+            const dim3 grid((unsigned)ceil_div(T, 4 * GT), (unsigned)ceil_div(d, GT));
+            if (vec)
+                hipLaunchKernelGGL(scores_backward_f32_kernel<true>, grid, dim3(256), 0, s, dl,
+                                   (const float*)w, T, d, E, (float*)dx);
+            else
+                hipLaunchKernelGGL(scores_backward_f32_kernel<false>, grid, dim3(256), 0, s, dl,
+                                   (const float*)w, T, d, E, (float*)dx);
+            st = launch_status();
+        }
+        if (st != MOE_OK || !sums) return st;
+        if (vec) hipLaunchKernelGGL(router_grad_f32_kernel<true>, dim3(groups), block, 0, s, p);
+        else hipLaunchKernelGGL(router_grad_f32_kernel<false>, dim3(groups), block, 0, s, p);
+        st = launch_status();
+    }
+    if (st == MOE_OK && sums && plan.n > 1) {
         const Parts a = {dw_parts, dw, dw ? (int64_t)E * d : 0}, b = {dbias_parts, dbias, dbias ? E : 0};
         hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)ceil_div(a.size + b.size, 256)), dim3(256), 0,
                            s, a, b, (int)plan.n);
+        st = launch_status();
     }
-    return launch_status();
-}
-
-int launch_scores_backward(const float* dl, const float* sel, const int32_t* idx, const void* w,
-                           int dtype, int64_t T, int d, int E, int k, void* dx, hipStream_t s) {
-    const bool vec = E % 4 == 0 && ((uintptr_t)dl & 15u) == 0;
-    if (dtype == MOE_BF16) {
-        // two workgroups of four waves a CU, a block of 16 tokens per wave at least
-        const int64_t cols = ceil_div(d, E > 128 ? 64 : 128), most = ceil_div(ceil_div(T, 16), 4);
-        const int64_t rows = std::max<int64_t>(std::min(most, ceil_div(512, cols)), 1);
-        const dim3 grid((unsigned)(rows * cols));
-#define MOE_DX(KE, NC, VEC)                                                                       \
-    hipLaunchKernelGGL((scores_backward_bf16_kernel<KE, NC, VEC>), grid, dim3(256), 0, s, dl,     \
-                       (const bf16_t*)w, T, d, E, (int)(4 * rows), (bf16_t*)dx)
-#define MOE_DX_E(VEC)                                                                             \
-    do {                                                                                          \
-        if (E <= 32) MOE_DX(1, 8, VEC);                                                           \
-        else if (E <= 64) MOE_DX(2, 8, VEC);                                                      \
-        else if (E <= 128) MOE_DX(4, 8, VEC);                                                     \
-        else MOE_DX(8, 4, VEC);                                                                   \
-    } while (0)
-        if (vec) MOE_DX_E(true);
-        else MOE_DX_E(false);
-#undef MOE_DX_E
-#undef MOE_DX
-        return launch_status();
-    }
-    // only the chosen experts' scores have a gradient: their router rows, weighted
-    if (sel) return launch_combine(w, dtype, idx, sel, nullptr, 0, T, d, k, dx, s);
-    const dim3 grid((unsigned)ceil_div(T, 4 * GT), (unsigned)ceil_div(d, GT));
-    if (vec)
-        hipLaunchKernelGGL(scores_backward_f32_kernel<true>, grid, dim3(256), 0, s, dl, (const float*)w,
-                           T, d, E, (float*)dx);
-    else
-        hipLaunchKernelGGL(scores_backward_f32_kernel<false>, grid, dim3(256), 0, s, dl,
-                           (const float*)w, T, d, E, (float*)dx);
-    return launch_status();
+    return st;
 }
 
 }  // namespace
@@ -830,14 +864,11 @@ int launch_route_backward(const float* dgate, const float* gate, const int32_t* 
         else
             hipLaunchKernelGGL(gate_backward_kernel<false>, grid, block, 0, s, dgate, gate, idx,
                                logits, T, E, k, dl, sel);
-        int st = launch_status();
-        if (st == MOE_OK && dx) st = launch_scores_backward(dl, sel, idx, w, dtype, T, d, E, k, dx, s);
+        const int st = launch_status();
         if (st != MOE_OK) return st;
     }
-    if (dw || dbias)
-        return launch_router_grad(dl, x, dtype, T, d, E, dw, dbias, (float*)(base + at.dw),
-                                  (float*)(base + at.dbias), s);
-    return MOE_OK;
+    return launch_router_backward(dl, sel, idx, x, w, dtype, T, d, E, k, T > 0 ? dx : nullptr, dw, dbias,
+                                  (float*)(base + at.dw), (float*)(base + at.dbias), s);
 }
 
 }  // namespace moe

@@ -145,7 +145,7 @@ def _dev(t: Optional[torch.Tensor], name: str, dtype=None):
         raise ValueError("%s must be contiguous" % name)
     if dtype is not None and t.dtype != dtype:
         raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _holds(t: Optional[torch.Tensor], name: str, *shape: int):
@@ -162,10 +162,10 @@ def _holds(t: Optional[torch.Tensor], name: str, *shape: int):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream(stream) -> ctypes.c_void_p:
+def _stream(stream):
     if stream is None:
         if _raw_stream is not None:
-            return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
+            return _raw_stream(torch.cuda.current_device())
         stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
@@ -730,7 +730,7 @@ def moe_grouped_ffn_mxfp4(x: torch.Tensor, group_offsets: torch.Tensor, weights:
 
 def _same(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, *shape: int):
     """t (None passes) is of this type and shape."""
-    if t is not None and (t.dtype != dtype or tuple(t.shape) != shape):
+    if t is not None and (t.dtype != dtype or t.shape != shape):
         raise ValueError("%s must be %s %s, got %s %s" % (name, dtype, shape, t.dtype, tuple(t.shape)))
 
 
