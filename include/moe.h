@@ -527,8 +527,8 @@ size_t moe_grouped_ffn_mxfp4_ws_bytes(int64_t T, int64_t cap_rows, int d, int f,
 
 /*
  * moe_grouped_ffn_mxfp4 -- moe_grouped_ffn of experts whose weights are MXFP4
- * matrices.  The rows of x are quantized to MXFP4 once, and the hidden rows between
- * the products, so both products multiply 4-bit operands (the matrix cores do so
+ * matrices.  The rows of x are quantized to MXFP4, and the hidden rows between the
+ * products, so both products multiply 4-bit operands (the matrix cores do so
  * natively, block scales included):
  *
  *   for each group s and row p of it, with Q(.) = the values moe_quantize_mxfp4 keeps:
@@ -619,10 +619,11 @@ size_t moe_route_topk_backward_ws_bytes(int dtype, int64_t T, int d, int E, int 
  * dbias      device [E] float: outputs, each nullable (then not computed)
  * ws         moe_route_topk_backward_ws_bytes(...) bytes, 256-byte aligned
  * flags      MOE_RENORM or 0
- * Products and sums are fp32 in a fixed order (deterministic).  Requires T >= 0,
- * 1 <= E <= MOE_MAX_E, 1 <= k <= min(E, MOE_MAX_K), 1 <= d < 2^22 and, for MOE_BF16,
- * d % 8 == 0 (else MOE_ERR_SHAPE); 16-byte aligned matrices where a row is a multiple of
- * 16 bytes.
+ * Products and sums are fp32 in a fixed order (deterministic); with MOE_BF16, dlogits
+ * enter dw with all 24 bits and dx, which keeps 8, with 16.  Outputs must not overlap
+ * inputs or each other.  Requires T >= 0, 1 <= E <= MOE_MAX_E,
+ * 1 <= k <= min(E, MOE_MAX_K), 1 <= d < 2^22 and, for MOE_BF16, d % 8 == 0 (else
+ * MOE_ERR_SHAPE); 16-byte aligned matrices where a row is a multiple of 16 bytes.
  */
 int moe_route_topk_backward(const float* dgate, const float* topk_gate, const int32_t* topk_idx,
                             const float* logits, const void* x, const void* w_router, int dtype,
