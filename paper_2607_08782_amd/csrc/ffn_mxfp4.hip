@@ -3,7 +3,7 @@
 // rows and hidden rows quantized to it, both products on the matrix cores' block-scaled
 // 4-bit instructions, which take the E8M0 scales as operands.
 //
-//   0. xq = MXFP4(x), every token once
+//   0. xq = MXFP4(x), every token once (in few rows, by the strips of 1)
 //   1. h = SiLU(W1 xq) * (W3 xq), quantized in the epilogue (a strip or tile of it holds
 //      whole blocks of 32 columns, so h is written once, in 4 bits)
 //   2. y = W2 h
@@ -11,7 +11,8 @@
 // All operands lie step-major (moe_mxfp4_lay_out): per step of 128 columns, 64 bytes of
 // codes a row and then one word of scales a row, rows side by side.  What a product's step
 // needs of a row is then no part of a longer line, half of which the cache would fetch for
-// nothing (256 x 256 tiles over rows as a matrix has them, 128-byte lines: CHANGEME).
+// nothing (Mixtral-shaped chunk of 777 tokens, the first tiles: 141 us over rows as a matrix
+// has them, 125 step-major; 1500 tokens 218 and 190).
 #include <algorithm>
 #include <type_traits>
 
@@ -67,7 +68,8 @@ __device__ __forceinline__ float swiglu(float a, float b) {
 }
 
 // ---------------------------------------------------------------------------
-// Strips: groups of few rows, bound by the weight bytes.  A workgroup holds 16 TILES weight
+// Strips: groups of few rows, bound by the weight bytes (64 Mixtral-shaped tokens, the FFN of
+// two experts: 52 us, 188 MB at 3.6 TB/s; of that gate/up 30 us at 4.2).  A workgroup holds 16 TILES weight
 // rows of one group (of gate/up half gate rows, half the same up rows: TILES = 4 makes 32
 // hidden columns, one MXFP4 block) over all of K, its W waves taking every W-th step: a
 // weight byte goes from memory to the registers of the one wave that multiplies it, and no
@@ -164,8 +166,8 @@ __device__ __forceinline__ void strip_rows(const MxArgs& p, float* red, int g, i
                 for (int u = 0; u < 4; ++u)              // columns past d: zeros
                     s.a[u] = __builtin_bit_cast(
                         i32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                                   a, 128 * t + 32 * quarter + 8 * u < p.d ? aoff[0] + t * 256 + 16 * u : A_OOB,
-                                   0, 0));
+                                   a, 128 * t + 32 * quarter + 8 * u < p.d ? aoff[0] + t * 256 + 16 * u
+                                                                           : A_OOB, 0, 0));
                 return;
             }
 #pragma unroll
@@ -315,7 +317,7 @@ constexpr int FEW_STEPS = 6;
 template <bool SWIGLU, int W, int TILES, int MAX_MS, bool QUANT>
 __global__ __launch_bounds__(64 * W, QUANT ? 3 : MAX_MS == 1 ? 4 : 2) void strip_mxfp4_kernel(MxArgs p) {
     constexpr int LD = 16 * TILES + 4;
-    constexpr int SUMS = W * 16 * MAX_MS * LD * 4 > 70 * 1024 ? W / 2 * 16 * MAX_MS * LD : W * 16 * MAX_MS * LD;
+    constexpr int ALL = W * 16 * MAX_MS * LD, SUMS = ALL * 4 > 70 * 1024 ? ALL / 2 : ALL;
     __shared__ __attribute__((aligned(16))) float red[SUMS];
     const int slot = blockIdx.x / p.strips;
     const int n0 = ((int)blockIdx.x - slot * p.strips) * 16 * TILES / (SWIGLU ? 2 : 1);
@@ -338,26 +340,32 @@ __global__ __launch_bounds__(64 * W, QUANT ? 3 : MAX_MS == 1 ? 4 : 2) void strip
 }
 
 // ---------------------------------------------------------------------------
-// Tiles: groups of many rows, bound by the matrix rate.  A persistent grid of four-wave
-// workgroups, one 32 x 32 accumulator tile per v_mfma_scale_f32_32x32x64_f8f6f4; TM x TN of
-// them a side per wave, so 256 x 256 (TW = 4) or 128 x 128 (TW = 2) a workgroup.  A wave
-// alone on its SIMD keeps 32x32x64 at 6.5 PFLOP/s (random operands, the board's power
+// Tiles: groups of many rows, bound by the matrix rate.  A persistent grid of workgroups of
+// WM x 2 waves, each TM x TN accumulator tiles of v_mfma_scale_f32_32x32x64_f8f6f4: 256 x 256
+// by eight waves (two a SIMD) or, for few tiles, 128 x 128 by four (two workgroups a CU).  A
+// wave alone on its SIMD keeps 32x32x64 at 6.5 PFLOP/s (random operands, the board's power
 // limit) but 16x16x128 only at 4.4: the larger one halves the instructions to issue.
 //
 // Both operands go straight from memory into a ring of RING steps of 128 columns in LDS,
-// the row's codes (64 bytes) and its scale word, RING - 1 steps in flight: a step's loads
-// have that many steps of products to arrive.  The steps of all of a workgroup's tiles are
-// one stream: loads run four steps ahead of the products whatever tile these belong to, so
-// a tile starts without waiting for its first operands.  One barrier per step, in its
-// middle: there every wave holds its second half's fragments in registers, so the step's
-// ring slot is free, and the next step has landed, so the fragments of its first half are
-// read during the second half's products.
+// the row's codes (64 bytes) and its scale word: a step's loads have RING - 2 to RING - 1
+// steps of products to arrive.  The steps of all of a workgroup's tiles are one stream:
+// loads run ahead of the products whatever tile these belong to, so a tile starts without
+// waiting for its first operands.  One barrier per step, in its middle: there every wave
+// holds its second half's fragments in registers, so the step's ring slot is free, and the
+// next step has landed, so the fragments of its first half are read during the second
+// half's products.  Descriptors stay over a tile and offsets count its steps: with
+// descriptors made anew every step the scalar unit issued 120 instructions for 16 products.
 //
-// LDS rows are 64 bytes; 16-byte chunk c of row r sits at c ^ ((r >> 1) & 3), free of bank
-// conflicts for the reads of 32 rows.  The weights are the instruction's first operand; the
-// weight rows of a 32-row block are laid out in LDS so that a lane's sixteen accumulators
-// are sixteen consecutive output columns of one token row (w_order): half an MXFP4 block
-// of h, or two 16-byte stores of y.
+// LDS rows are 64 bytes; 16-byte chunk c of row r sits at c ^ ((r >> 2) & 3), free of bank
+// conflicts for the reads of 32 rows (none counted).  The weights are the instruction's first
+// operand; the weight rows of a 32-row block are laid out in LDS so that a lane's sixteen
+// accumulators are sixteen consecutive output columns of one token row (w_order): half an
+// MXFP4 block of h, or two 16-byte stores of y.
+//
+// 4096 Mixtral-shaped tokens (3254 rows of two experts): gate/up 206 us, down 100, 3.7 and 3.8
+// PFLOP/s; the matrix units are busy 47 % of the clocks, and the clock falls to 1.9 GHz under
+// the power limit: runs with half the scalar instructions, or with a seventh fewer waits, took
+// the same time at another clock.
 constexpr int TILE_LIST = 32;                            // tile records kept, in two halves
 
 // TM x TN accumulator tiles per wave, WM x 2 waves, R steps in the ring
@@ -391,8 +399,11 @@ __device__ __forceinline__ int w_order(int r) {
     return (r & ~31) + 16 * ((r >> 2) & 1) + 4 * ((r >> 3) & 3) + (r & 3);
 }
 
-// Tiles come in two kinds: high ones, and those of at most half the rows (a group's last),
-// whose upper waves have nothing to multiply: half the time of a tile.
+// Tiles of 256 rows come in two kinds: high ones, and those of at most half the rows (a
+// group's last), whose upper waves have nothing to multiply.  These come last, where a round
+// is partly filled (4096 Mixtral-shaped tokens, 5.7 rounds of the one and 0.4 of the other:
+// gate/up 220 us in 7 rounds, 206 so).  The smaller tiles stay in order: a group's tiles apart
+// read its weights twice (1024 tokens of DeepSeek-V2-Lite 106 and 112 us).
 template <int BM>
 __device__ __forceinline__ int high_tiles(int rows) {
     return BM > 128 ? (rows + BM / 2 - 1) / BM : (int)ceil_div(rows, BM);
@@ -532,8 +543,8 @@ __global__ __launch_bounds__(64 * 2 * WM, TM * TN > 8 ? 1 : 2) void tile_mxfp4_k
         if (64 * wave >= BM) return;
         const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
             (void*)(p.a_rows + t.row0), (short)0, t.valid * 4, RSRC_WORD3);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(s_tok + (q & 1) * BM + 64 * wave), 4, tid * 4, 0,
-                                                 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(s_tok + (q & 1) * BM + 64 * wave), 4,
+                                                 tid * 4, 0, 0, 0);
     };
     if (p.a_rows != nullptr) fetch_tokens(0);
     int lq = -1, lkt = 0, left_steps = 0;                // before the first tile
@@ -868,9 +879,20 @@ int launch_strips(MxArgs& p, int64_t max_rows, int cus, hipStream_t s) {
     return launch_strips_of<SWIGLU, 4, 4>(p, max_rows, s);
 }
 
+// Strips while no group can hold more rows than this, tiles past it (FFN, strips and tiles:
+// Mixtral-shaped, 40 tokens 47 and 64 us, 96 tokens 67 and 68, 128 tokens 75 and 71, 200 tokens
+// 94 and 78; 64 DeepSeek-V2-Lite experts, 128 tokens 63 and 68, 200 tokens 72 and 76; an eighth
+// of them, 256 tokens 40 and 22; Qwen3-30B-A3B, 128 tokens 23 and 20).
 constexpr int64_t STRIP_MAX_ROWS = 128;
+
+// Tiles of 256 x 256 from this many outputs of a product (a round of them over the chip), of
+// 128 x 128 below (FFN, all of one size: Mixtral-shaped, 400 tokens 103 and 87 us, 1500 tokens
+// 162 and 194; DeepSeek-V2-Lite on one of eight, 512 tokens 29 and 24, 2048 tokens 38 and 41,
+// 8192 tokens 90 and 114.  777 Mixtral-shaped tokens, where the products differ: 124 and 121,
+// by the rule 104).
 constexpr int64_t LARGE_WORK = (int64_t)256 * 256 * 256;
 
+// steps whose offsets from the first one's stay below 2^31
 int segment_steps(int64_t a_rows, int64_t w_rows) {
     return (int)std::max<int64_t>(0x7fffffff / (std::max(a_rows, w_rows) * STEP_BYTES), 1);
 }
@@ -937,7 +959,8 @@ int launch_grouped_ffn_mxfp4(const void* x, int64_t T, const int32_t* row_token,
     p.y = nullptr;
     const int cus = num_cus();
     st = max_rows <= STRIP_MAX_ROWS ? launch_strips<true>(p, max_rows, cus, s)
-         : rows * p.N >= LARGE_WORK ? launch_tiles<true, 4, 2, 4, 3>(p, cus, s) : launch_tiles<true, 2, 2, 2, 4>(p, cus, s);
+         : rows * p.N >= LARGE_WORK   ? launch_tiles<true, 4, 2, 4, 3>(p, cus, s)
+                                      : launch_tiles<true, 2, 2, 2, 4>(p, cus, s);
     if (st != MOE_OK) return st;
     for (int i = 0; i < n_groups; ++i) {
         p.w[i] = w2[i];
