@@ -751,9 +751,9 @@ def moe_combine_backward(dy: torch.Tensor, y_perm: Optional[torch.Tensor], token
     if want_dy_perm and dy_perm is None:
         if y_perm is None:
             raise ValueError("dy_perm's rows are y_perm's: give one of them")
-        dy_perm = _empty(y_perm.shape, dy.dtype, dy.device)
+        dy_perm = torch.empty_like(y_perm)               # (quicker than by a shape)
     if want_dgate and dgate is None:
-        dgate = _empty((T, k), torch.float32, dy.device)
+        dgate = dy.new_empty(T, k, dtype=torch.float32) if topk_gate is None else torch.empty_like(topk_gate)
     if dy_perm is not None and (dy_perm.dtype != dy.dtype or dy_perm.dim() != 2 or dy_perm.shape[1] != d):
         raise ValueError("dy_perm must be [rows, d] of dy's dtype")
     if dy_perm is not None and y_perm is not None and dy_perm.shape[0] < y_perm.shape[0]:
@@ -774,7 +774,7 @@ def moe_permute_backward(dx_perm: torch.Tensor, token_row: torch.Tensor, *,
     d = dx_perm.shape[1]
     T, k = token_row.shape
     if dx is None:
-        dx = _empty((T, d), dx_perm.dtype, dx_perm.device)
+        dx = dx_perm.new_empty(T, d) if dx_add is None else torch.empty_like(dx_add)
     _same(dx_add, "dx_add", dx_perm.dtype, T, d)
     _same(dx, "dx", dx_perm.dtype, T, d)
     st = lib.moe_permute_backward(_dev(dx_perm, "dx_perm"), _dtype_code(dx_perm),
@@ -811,13 +811,13 @@ def moe_route_topk_backward(dgate: torch.Tensor, topk_gate: torch.Tensor, topk_i
     _same(topk_idx, "topk_idx", torch.int32, T, k)
     _same(logits, "logits", f32, T, E)
     if want_dlogits and dlogits is None:
-        dlogits = _empty((T, E), f32, x.device)
+        dlogits = dgate.new_empty(T, E)
     if want_dx and dx is None:
-        dx = _empty((T, d), x.dtype, x.device)
+        dx = torch.empty_like(x)
     if want_dw and dw is None:
-        dw = _empty((E, d), f32, x.device)
+        dw = torch.empty_like(w_router, dtype=f32)
     if want_dbias and dbias is None:
-        dbias = _empty((E,), f32, x.device)
+        dbias = dgate.new_empty(E)
     _same(dlogits, "dlogits", f32, T, E)
     _same(dx, "dx", x.dtype, T, d)
     _same(dw, "dw", f32, E, d)
