@@ -537,7 +537,7 @@ __global__ __launch_bounds__(64 * 2 * WM, TM * TN > 8 ? 1 : 2) void tile_mxfp4_k
         step_w[n] = (of_a(n) ? step_a : step_b) / (STEP_BYTES / 4);
     }
     // gather: the token rows of a tile's rows come into LDS a tile ahead, by a direct load
-    // like the ring's (zero past the group): three steps later every wave's has landed
+    // like the ring's (zero past the group)
     auto fetch_tokens = [&](int q) {
         const MxTile t = tile_at(q);
         if (64 * wave >= BM) return;
@@ -562,7 +562,9 @@ __global__ __launch_bounds__(64 * 2 * WM, TM * TN > 8 ? 1 : 2) void tile_mxfp4_k
             const bool live = lq < n_list;
             const MxTile t = tile_at(live ? lq : n_list - 1);
             if (p.a_rows != nullptr) {
-                if (lq == 0 || p.KT < RING - 1) {        // no three steps since it was issued
+                // Issued a tile ago.  The waits of the loop are for older loads than a step's,
+                // but a tile of fewer steps than the ring ends before the first of them.
+                if (lq == 0 || p.KT < RING) {
                     wait_vm<0>();
                     asm volatile("s_barrier" ::: "memory");
                 }

@@ -619,7 +619,7 @@ __device__ __forceinline__ void scores_backward_bf16(const DxArgs& p, unsigned i
         }
     };
     constexpr bool AHEAD = KE <= 4;                      // past 128 experts there is no room
-    const int y_off = c0 < d ? (4 * quarter * d + c0) * 2 : A_OOB;
+    const uint32_t y_off = c0 < d ? (4 * quarter * d + c0) * 2 : A_OOB;
     int64_t block = cell.row * (DW_THREADS / 64) + wave;
     if (AHEAD) load(block);
     for (; block < blocks; block += runs) {

@@ -47,6 +47,14 @@ def test_large_tiles(sizes, d, f, T):
     _run(sizes, d, f, T, seed=13)
 
 
+@pytest.mark.parametrize("d,f,cap", [(128, 8192, 1500), (256, 8192, 1500), (384, 8192, 1500), (512, 8192, 1500),
+                                     (128, 16640, 1500), (256, 16640, 1500), (384, 16640, 1500)])
+def test_products_of_fewer_steps_than_the_ring(d, f, cap):
+    """Token rows of the next tile, several tiles a workgroup, 1 to 4 steps a tile."""
+    say("[ffn mxfp4 short products]", d, f)
+    _run([700, 130, 601], d, f, 900, cap=cap, seed=17)
+
+
 def test_a_buffer_much_longer_than_the_rows():
     say("[ffn mxfp4 long buffer]")
     _run([768], 128, 12544, 900, cap=1400, seed=14)
