@@ -330,13 +330,16 @@ __global__ __launch_bounds__(64 * W, QUANT ? 3 : MAX_MS == 1 ? 4 : 2) void strip
         of.rows = __builtin_amdgcn_readfirstlane(first_row(p, slot + 1)) - of.row0;
     }
     if (of.rows <= 0) return;
+    // steps of loads in flight that the registers of the row blocks leave room for, four in
+    // narrow strips whatever these (128 Mixtral-shaped tokens, whose down product takes them:
+    // 75.6 us with three for 33 rows and more, 73.9 so; 64 tokens 51.4 and 50.5)
     constexpr int D = TILES == 4 ? 3 : 4;
     if (QUANT || ((MAX_MS == 1 || of.rows <= 16) && p.KT <= FEW_STEPS * W))
         strip_rows<SWIGLU, W, TILES, 1, 2, QUANT>(p, red, of.g, n0, of.row0, of.rows);
     else if (MAX_MS == 1 || of.rows <= 16)
         strip_rows<SWIGLU, W, TILES, 1, D>(p, red, of.g, n0, of.row0, of.rows);
     else if (of.rows <= 32) strip_rows<SWIGLU, W, TILES, 2, D>(p, red, of.g, n0, of.row0, of.rows);
-    else strip_rows<SWIGLU, W, TILES, 4, TILES == 4 ? 2 : 3>(p, red, of.g, n0, of.row0, of.rows);
+    else strip_rows<SWIGLU, W, TILES, 4, TILES == 4 ? 2 : 4>(p, red, of.g, n0, of.row0, of.rows);
 }
 
 // ---------------------------------------------------------------------------
