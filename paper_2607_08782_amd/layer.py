@@ -250,6 +250,7 @@ class LayerShare:
         if fuse_combine is None:
             fuse_combine = T <= 64 and k <= 2
         self.fused_combine = bool(fuse_combine) and can_fuse
+        self._packaged = False                           # the row maps are written
         self._grads = None
 
     def _table(self, w13: Sequence[torch.Tensor], w2: Sequence[torch.Tensor]):
@@ -328,6 +329,7 @@ class LayerShare:
         moe.moe_permute(self.X, self.topk_idx, self.topk_gate, self.counts, self.placement,
                         self.dev, E=self.E, cap_rows=self.cap_rows, out=self.perm, ws=self.ws_perm,
                         copy_rows=not self.gather_in_ffn)
+        self._packaged = True
 
     def _route_package(self, logits_in: Optional[torch.Tensor] = None):
         """Enqueue routing, counts and packaging as one call: `route`, the histogram and
@@ -339,6 +341,7 @@ class LayerShare:
                               out=self.perm, ws_perm=self.ws_perm, cap_rows=self.cap_rows,
                               renorm=self.renorm, logits_in=logits_in is not None,
                               copy_rows=not self.gather_in_ffn)
+        self._packaged = True
 
     def routed_ffn(self, fused: Optional[bool] = None):
         """Enqueue the routed experts' FFN call as `run` makes it: moe_grouped_ffn (or
@@ -409,6 +412,12 @@ class LayerShare:
         self.combine()
         return self.y
 
+    def _needs_row_maps(self, name: str):
+        """Refuse what reads rows by the row maps before a step has written these: until then
+        they hold any row numbers."""
+        if not self._packaged:
+            raise ValueError("%s goes back through a run, and none was made" % name)
+
     def backward(self, dy: torch.Tensor, reduce_dgate: Optional[Callable] = None) -> dict:
         """Enqueue the gradient of the last `run` from dy [T, d], the loss gradient of y, to
         the experts and the router; returns device tensors, overwritten by the next call:
@@ -425,6 +434,7 @@ class LayerShare:
             raise ValueError("gates without renormalisation need want_logits=True for backward")
         if tuple(dy.shape) != (self.T, self.d) or dy.dtype != self.X.dtype:
             raise ValueError("dy must be %s [%d, %d]" % (self.X.dtype, self.T, self.d))
+        self._needs_row_maps("backward")
         if self._grads is None:
             f32 = dict(dtype=torch.float32, device=self.device)
             dcode = moe.MOE_BF16 if self.X.dtype == torch.bfloat16 else moe.MOE_F32
@@ -448,5 +458,6 @@ class LayerShare:
         """Enqueue the gradient of the packaging: dx [T, d] (None: a new tensor) = the sum of
         each token's rows of dx_perm, the gradient of the packaged rows, on top of the last
         `backward`'s dx, if there was one."""
+        self._needs_row_maps("backward_rows")
         add = self._grads["dx"] if self._grads is not None else None
         return moe.moe_permute_backward(dx_perm, self.perm["token_row"], dx_add=add, dx=dx)
