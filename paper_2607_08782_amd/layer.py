@@ -251,6 +251,7 @@ class LayerShare:
             fuse_combine = T <= 64 and k <= 2
         self.fused_combine = bool(fuse_combine) and can_fuse
         self._packaged = False                           # the row maps are written
+        self._scores = self.logits                       # the last routing's, which backward goes through
         self._grads = None
 
     def _table(self, w13: Sequence[torch.Tensor], w2: Sequence[torch.Tensor]):
@@ -291,6 +292,7 @@ class LayerShare:
             moe.moe_route_topk(self.X, self.Wr, self.bias, self.k, renorm=self.renorm,
                                logits=self.logits, want_logits=self.logits is not None,
                                topk_idx=self.topk_idx, topk_gate=self.topk_gate, ws=self.ws_route)
+        self._scores = self.logits if logits_in is None else logits_in
 
     def _shared_ffn(self, stream=None):
         """The shared experts' call of their own (nothing when they share the routed
@@ -341,6 +343,7 @@ class LayerShare:
                               out=self.perm, ws_perm=self.ws_perm, cap_rows=self.cap_rows,
                               renorm=self.renorm, logits_in=logits_in is not None,
                               copy_rows=not self.gather_in_ffn)
+        self._scores = self.logits if logits_in is None else logits_in
         self._packaged = True
 
     def routed_ffn(self, fused: Optional[bool] = None):
@@ -427,10 +430,13 @@ class LayerShare:
                      router
         (the shared experts' output has dy itself).  A token's gates depend on each other,
         so where its experts are on several GPUs dgate has to be summed over them before it
-        goes on: reduce_dgate(dgate), in place, on the current stream."""
+        goes on: reduce_dgate(dgate), in place, on the current stream.
+
+        After a run(logits_in=...) the gates' gradient is taken at those scores (keep them until
+        then where gates are not renormalised), and the router's as of scores X Wr^T + bias."""
         if self.fused_combine:
             raise ValueError("the fused combine does not keep y_perm: backward needs fuse_combine=False")
-        if not self.renorm and self.logits is None:
+        if not self.renorm and self._scores is None:
             raise ValueError("gates without renormalisation need want_logits=True for backward")
         if tuple(dy.shape) != (self.T, self.d) or dy.dtype != self.X.dtype:
             raise ValueError("dy must be %s [%d, %d]" % (self.X.dtype, self.T, self.d))
@@ -450,7 +456,7 @@ class LayerShare:
         if reduce_dgate is not None:
             reduce_dgate(g["dgate"])
         moe.moe_route_topk_backward(g["dgate"], self.topk_gate, self.topk_idx, self.X, self.Wr,
-                                    logits=self.logits, renorm=self.renorm, want_dlogits=False,
+                                    logits=self._scores, renorm=self.renorm, want_dlogits=False,
                                     dx=g["dx"], dw=g["dw"], dbias=g["dbias"], ws=self._ws_grads)
         return g
 

@@ -1,9 +1,17 @@
-"""What a share's gradient goes back through (marked `gpu`): the last run."""
+"""What a share's gradient goes back through (marked `gpu`): the scores and token rows of the
+last routing, whatever the share was given since.
+
+Tolerances: an fp32 sum of n products is within (n + 4) 2^-24 of the sum of its terms'
+magnitudes, a softmax gradient within (E + 16) 2^-24 + 2^-19 of its own."""
+import numpy as np
 import pytest
 import torch
 
 from paper_2607_08782_amd import moe, synth
 from paper_2607_08782_amd.layer import LayerShare
+
+from parity import say
+from test_gpu_grad import _np, _want_route
 
 pytestmark = pytest.mark.gpu
 
@@ -29,6 +37,19 @@ def _normal(seed, *shape):
     return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).cuda()
 
 
+def _check_router(share, g, X, logits, renorm):
+    """dx, dw and dbias of a share's backward against the formulas on X and these scores."""
+    dl, size, dx, dx_size, dw, dw_size = _want_route(logits, share.topk_idx, share.topk_gate, g["dgate"], X,
+                                                     share.Wr, renorm)
+    E = share.E
+    rel = (E + 16) * 2.0 ** -24 + 2.0 ** -19
+    for name, want, tol in (("dx", dx, (rel + (E + 4) * 2.0 ** -24) * dx_size),
+                            ("dw", dw, (rel + (T + 4) * 2.0 ** -24) * dw_size),
+                            ("dbias", dl.sum(0), (rel + (T + 4) * 2.0 ** -24) * size.sum(0))):
+        off = np.abs(_np(g[name]) - want)
+        assert (off <= tol + 2.0 ** -24 * np.abs(want)).all(), (name, off.max(), np.abs(want).max())
+
+
 def test_gradients_without_a_run_are_refused():
     """The row maps hold no rows yet: nothing is read by them."""
     _, share = _share()
@@ -36,3 +57,37 @@ def test_gradients_without_a_run_are_refused():
         share.backward(_normal(5, T, share.d))
     with pytest.raises(ValueError, match="run"):
         share.backward_rows(_normal(6, *share.y_perm.shape))
+
+
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("phases", [False, True])
+def test_backward_takes_the_scores_that_were_handed_in(renorm, phases):
+    """run(logits_in=...) and route(logits_in=...) choose by the caller's scores; the share's
+    own hold an earlier batch's."""
+    say("[backward of given scores]", renorm, phases)
+    _, share = _share(renorm=renorm)
+    share.run()
+    given = _normal(1, T, share.E)
+    if phases:
+        share.route(logits_in=given)
+        share.package()
+        share.routed_ffn()
+        share.combine()
+    else:
+        share.run(logits_in=given)
+    g = share.backward(_normal(2, T, share.d))
+    _check_router(share, g, share.X, given, renorm)
+    share.run()                                      # and its own again
+    g = share.backward(_normal(3, T, share.d))
+    _check_router(share, g, share.X, share.logits, renorm)
+
+
+def test_given_scores_need_none_of_the_share_s_own():
+    _, share = _share(renorm=False, want_logits=False)
+    dy = _normal(2, T, share.d)
+    given = _normal(1, T, share.E)
+    share.run(logits_in=given)
+    _check_router(share, share.backward(dy), share.X, given, False)
+    share.run()
+    with pytest.raises(ValueError, match="want_logits"):
+        share.backward(dy)
