@@ -251,7 +251,8 @@ class LayerShare:
             fuse_combine = T <= 64 and k <= 2
         self.fused_combine = bool(fuse_combine) and can_fuse
         self._packaged = False                           # the row maps are written
-        self._scores = self.logits                       # the last routing's, which backward goes through
+        # the last routing's token rows and scores, which backward goes through
+        self._rows, self._scores = self.X, self.logits
         self._grads = None
 
     def _table(self, w13: Sequence[torch.Tensor], w2: Sequence[torch.Tensor]):
@@ -292,7 +293,7 @@ class LayerShare:
             moe.moe_route_topk(self.X, self.Wr, self.bias, self.k, renorm=self.renorm,
                                logits=self.logits, want_logits=self.logits is not None,
                                topk_idx=self.topk_idx, topk_gate=self.topk_gate, ws=self.ws_route)
-        self._scores = self.logits if logits_in is None else logits_in
+        self._rows, self._scores = self.X, self.logits if logits_in is None else logits_in
 
     def _shared_ffn(self, stream=None):
         """The shared experts' call of their own (nothing when they share the routed
@@ -343,7 +344,7 @@ class LayerShare:
                               out=self.perm, ws_perm=self.ws_perm, cap_rows=self.cap_rows,
                               renorm=self.renorm, logits_in=logits_in is not None,
                               copy_rows=not self.gather_in_ffn)
-        self._scores = self.logits if logits_in is None else logits_in
+        self._rows, self._scores = self.X, self.logits if logits_in is None else logits_in
         self._packaged = True
 
     def routed_ffn(self, fused: Optional[bool] = None):
@@ -426,8 +427,8 @@ class LayerShare:
         the experts and the router; returns device tensors, overwritten by the next call:
             dy_perm  of every expert output row (rows past group_offsets' end unchanged)
             dgate    [T, k] fp32, of topk_gate: 0 for experts on other GPUs
-            dx       [T, d], of X through the gate scores;  dw [E, d], dbias [E] fp32, of the
-                     router
+            dx       [T, d], of that run's X through the gate scores;  dw [E, d], dbias [E]
+                     fp32, of the router
         (the shared experts' output has dy itself).  A token's gates depend on each other,
         so where its experts are on several GPUs dgate has to be summed over them before it
         goes on: reduce_dgate(dgate), in place, on the current stream.
@@ -455,7 +456,7 @@ class LayerShare:
                                  dy_perm=g["dy_perm"], dgate=g["dgate"])
         if reduce_dgate is not None:
             reduce_dgate(g["dgate"])
-        moe.moe_route_topk_backward(g["dgate"], self.topk_gate, self.topk_idx, self.X, self.Wr,
+        moe.moe_route_topk_backward(g["dgate"], self.topk_gate, self.topk_idx, self._rows, self.Wr,
                                     logits=self._scores, renorm=self.renorm, want_dlogits=False,
                                     dx=g["dx"], dw=g["dw"], dbias=g["dbias"], ws=self._ws_grads)
         return g

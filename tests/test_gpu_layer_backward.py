@@ -91,3 +91,11 @@ def test_given_scores_need_none_of_the_share_s_own():
     share.run()
     with pytest.raises(ValueError, match="want_logits"):
         share.backward(dy)
+
+
+def test_backward_after_the_next_batch_s_inputs_are_set():
+    """set_inputs for the next batch between run and backward: the gradient is the run's."""
+    i, share = _share()
+    share.run()
+    share.set_inputs(_normal(4, T, share.d))
+    _check_router(share, share.backward(_normal(5, T, share.d)), i.X, share.logits, True)
