@@ -254,6 +254,7 @@ class LayerShare:
         # the last routing's token rows and scores, which backward goes through
         self._rows, self._scores = self.X, self.logits
         self._grads = None
+        self._grads_current = False                      # they are the last routing's
 
     def _table(self, w13: Sequence[torch.Tensor], w2: Sequence[torch.Tensor]):
         return moe.MxWeightTable.quantized(w13, w2) if self.mxfp4 else moe.WeightTable(w13, w2)
@@ -293,7 +294,12 @@ class LayerShare:
             moe.moe_route_topk(self.X, self.Wr, self.bias, self.k, renorm=self.renorm,
                                logits=self.logits, want_logits=self.logits is not None,
                                topk_idx=self.topk_idx, topk_gate=self.topk_gate, ws=self.ws_route)
+        self._routed(logits_in)
+
+    def _routed(self, logits_in: Optional[torch.Tensor]):
+        """What `backward` goes through is this routing's now, and no gradient of it is there."""
         self._rows, self._scores = self.X, self.logits if logits_in is None else logits_in
+        self._grads_current = False
 
     def _shared_ffn(self, stream=None):
         """The shared experts' call of their own (nothing when they share the routed
@@ -344,7 +350,7 @@ class LayerShare:
                               out=self.perm, ws_perm=self.ws_perm, cap_rows=self.cap_rows,
                               renorm=self.renorm, logits_in=logits_in is not None,
                               copy_rows=not self.gather_in_ffn)
-        self._rows, self._scores = self.X, self.logits if logits_in is None else logits_in
+        self._routed(logits_in)
         self._packaged = True
 
     def routed_ffn(self, fused: Optional[bool] = None):
@@ -459,12 +465,14 @@ class LayerShare:
         moe.moe_route_topk_backward(g["dgate"], self.topk_gate, self.topk_idx, self._rows, self.Wr,
                                     logits=self._scores, renorm=self.renorm, want_dlogits=False,
                                     dx=g["dx"], dw=g["dw"], dbias=g["dbias"], ws=self._ws_grads)
+        self._grads_current = True
         return g
 
     def backward_rows(self, dx_perm: torch.Tensor, dx: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Enqueue the gradient of the packaging: dx [T, d] (None: a new tensor) = the sum of
-        each token's rows of dx_perm, the gradient of the packaged rows, on top of the last
-        `backward`'s dx, if there was one."""
+        each token's rows of dx_perm, the gradient of the packaged rows, on top of `backward`'s
+        dx, if there was one since the last run (by the calls made or captured last: a graph's
+        replays are not seen here)."""
         self._needs_row_maps("backward_rows")
-        add = self._grads["dx"] if self._grads is not None else None
+        add = self._grads["dx"] if self._grads_current else None
         return moe.moe_permute_backward(dx_perm, self.perm["token_row"], dx_add=add, dx=dx)

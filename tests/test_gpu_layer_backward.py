@@ -99,3 +99,23 @@ def test_backward_after_the_next_batch_s_inputs_are_set():
     share.run()
     share.set_inputs(_normal(4, T, share.d))
     _check_router(share, share.backward(_normal(5, T, share.d)), i.X, share.logits, True)
+
+
+def test_backward_rows_adds_no_earlier_batch_s_gradient():
+    """run, backward, run, backward_rows: dx is the rows' alone; after a backward of the same
+    run it is on top of that one's."""
+    _, share = _share()
+    dx_perm = _normal(6, *share.y_perm.shape)
+    rows = lambda: moe.moe_permute_backward(dx_perm, share.perm["token_row"])
+    share.run()
+    dx = share.backward(_normal(7, T, share.d))["dx"]
+    both = moe.moe_permute_backward(dx_perm, share.perm["token_row"], dx_add=dx)
+    assert torch.equal(share.backward_rows(dx_perm), both) and not torch.equal(both, rows())
+    share.set_inputs(_normal(8, T, share.d))
+    assert torch.equal(share.backward_rows(dx_perm), both)           # still the last run's
+    share.run()
+    assert torch.equal(share.backward_rows(dx_perm), rows())
+    share.backward(_normal(9, T, share.d))
+    assert not torch.equal(share.backward_rows(dx_perm), rows())
+    share.route()
+    assert torch.equal(share.backward_rows(dx_perm), rows())
