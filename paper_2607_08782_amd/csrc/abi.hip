@@ -518,7 +518,7 @@ int moe_route_topk_backward(const float* dgate, const float* topk_gate, const in
     // one grid covers the tiles of dx
     if (ceil_div(T, 128) * ceil_div(d, 64) > 0x7fffffffLL) return MOE_ERR_SHAPE;
     if (d % (dtype == MOE_BF16 ? 8 : 4) == 0 &&
-        (!aligned16(x) || !aligned16(w_router) || !aligned16(dx)))
+        (!aligned16(x) || !aligned16(w_router) || !aligned16(dx) || !aligned16(dw)))
         return MOE_ERR_ARG;
     if (!ws || ws_bytes < route_backward_ws_bytes(dtype, T, d, E, k, flags) || ((uintptr_t)ws & 255u))
         return MOE_ERR_SHAPE;
