@@ -245,7 +245,7 @@ int mx_check(const void* m, int dtype, int64_t rows, int cols, const uint8_t* co
              const uint8_t* scales) {
     if (dtype != MOE_F32 && dtype != MOE_BF16) return MOE_ERR_ARG;
     if (rows < 0 || cols < 1) return MOE_ERR_ARG;
-    // a piece's place in its row is a 32-bit number, and the grid's size another
+    // a piece's place in its row is a 32-bit number; 2^44 values lie past any memory
     if (cols >= 1 << 28 || rows > (int64_t)0x7fffffff * 8192 / mx_cols(cols)) return MOE_ERR_SHAPE;
     if (rows > 0 && (!m || !codes || !scales)) return MOE_ERR_ARG;
     if (((uintptr_t)m & (dtype == MOE_BF16 ? 1u : 3u)) || !aligned16(codes) || !aligned4(scales))

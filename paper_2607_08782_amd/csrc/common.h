@@ -95,6 +95,20 @@ __host__ __device__ constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a
     return e == hipSuccess ? MOE_OK : MOE_ERR_DEVICE;
 }
 
+// A launch of `groups` workgroups of `threads` threads as launch(first, n) of n of them from
+// `first` on: one, or several where they are more than a grid holds (below 2^32 work-items a
+// dimension).
+template <typename Launch>
+[[nodiscard]] int launch_groups(int64_t groups, int threads, const Launch& launch) {
+    const int64_t most = 0xffffffffLL / threads;
+    for (int64_t first = 0; first < groups; first += most) {
+        launch(first, (unsigned)(groups - first < most ? groups - first : most));
+        const int st = launch_status();
+        if (st != MOE_OK) return st;
+    }
+    return MOE_OK;
+}
+
 // Raise a kernel's dynamic-LDS limit to `bytes` on the current device.  The
 // setting persists, so each device is configured once per size increase and
 // later launches skip the runtime call.  The check, the runtime call and the

@@ -76,11 +76,11 @@ struct Place {
 };
 
 template <typename T, Form F>
-__global__ __launch_bounds__(MX_THREADS) void quantize_mxfp4_kernel(const T* __restrict__ x,
+__global__ __launch_bounds__(MX_THREADS) void quantize_mxfp4_kernel(const T* __restrict__ x, int64_t first,
                                                                     int64_t pieces, int cols,
                                                                     uint32_t* __restrict__ codes,
                                                                     uint8_t* __restrict__ scales) {
-    const int64_t base = (int64_t)blockIdx.x * MX_PIECES;
+    const int64_t base = (first + blockIdx.x) * MX_PIECES;
     const Place place(base, cols);
     float v[MX_UNROLL][8];
 #pragma unroll
@@ -121,10 +121,10 @@ __global__ __launch_bounds__(MX_THREADS) void quantize_mxfp4_kernel(const T* __r
 // Token rows, step-major: a row per workgroup (and 2048 columns of it), so that no piece
 // needs a division, and a short batch is spread over the chip.
 __global__ __launch_bounds__(MX_THREADS) void quantize_steps_kernel(const bf16_t* __restrict__ x,
-                                                                    int64_t rows, int cols,
+                                                                    int64_t first, int64_t rows, int cols,
                                                                     uint32_t* __restrict__ codes,
                                                                     uint8_t* __restrict__ scales) {
-    const int64_t row = blockIdx.x;
+    const int64_t row = first + blockIdx.x;
     const int piece = blockIdx.y * MX_THREADS + threadIdx.x;
     if (piece >= (int)(mx_cols(cols) / 8)) return;       // whole quads
     float v[8] = {};
@@ -139,9 +139,9 @@ __global__ __launch_bounds__(MX_THREADS) void quantize_steps_kernel(const bf16_t
 
 template <typename T, Form F>
 __global__ __launch_bounds__(MX_THREADS) void dequantize_mxfp4_kernel(
-    const uint32_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t pieces,
-    int cols, T* __restrict__ y) {
-    const int64_t base = (int64_t)blockIdx.x * MX_PIECES;
+    const uint32_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t first,
+    int64_t pieces, int cols, T* __restrict__ y) {
+    const int64_t base = (first + blockIdx.x) * MX_PIECES;
     const Place place(base, cols);
     uint32_t w[MX_UNROLL], byte[MX_UNROLL];
 #pragma unroll
@@ -180,18 +180,19 @@ __global__ __launch_bounds__(MX_THREADS) void dequantize_mxfp4_kernel(
 
 // [rows][steps] -> [steps][rows], of 64-byte code pieces and of scale words: blocks of 32
 // rows x 8 steps, so that reads are 512 contiguous bytes and writes 2 KB.
-constexpr int LAY_ROWS = 32, LAY_STEPS = 8;
+constexpr int LAY_ROWS = 32, LAY_STEPS = 8, LAY_THREADS = 256;
 
-__global__ __launch_bounds__(256) void lay_out_kernel(const uint4* __restrict__ codes,
+__global__ __launch_bounds__(LAY_THREADS) void lay_out_kernel(const uint4* __restrict__ codes,
                                                       const uint32_t* __restrict__ scales,
-                                                      int64_t rows, int n, uint4* __restrict__ steps,
+                                                      int64_t first, int64_t rows, int n,
+                                                      uint4* __restrict__ steps,
                                                       uint32_t* __restrict__ words) {
     __shared__ uint4 piece[LAY_ROWS][LAY_STEPS * 4 + 1];
     __shared__ uint32_t word[LAY_ROWS][LAY_STEPS + 1];
-    const int64_t r0 = (int64_t)blockIdx.x * LAY_ROWS;
+    const int64_t r0 = (first + blockIdx.x) * LAY_ROWS;
     const int tid = threadIdx.x;
     for (int s0 = blockIdx.y * LAY_STEPS; s0 < n; s0 += gridDim.y * LAY_STEPS) {
-        for (int i = tid; i < LAY_ROWS * LAY_STEPS * 4; i += 256) {
+        for (int i = tid; i < LAY_ROWS * LAY_STEPS * 4; i += LAY_THREADS) {
             const int r = i / (LAY_STEPS * 4), c = i % (LAY_STEPS * 4);
             if (r0 + r < rows && s0 + c / 4 < n) piece[r][c] = codes[(r0 + r) * n * 4 + s0 * 4 + c];
         }
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(256) void lay_out_kernel(const uint4* __restrict__ 
             if (r0 + r < rows && s0 + c < n) word[r][c] = scales[(r0 + r) * n + s0 + c];
         }
         __syncthreads();
-        for (int i = tid; i < LAY_ROWS * LAY_STEPS * 4; i += 256) {
+        for (int i = tid; i < LAY_ROWS * LAY_STEPS * 4; i += LAY_THREADS) {
             const int c = i / (LAY_ROWS * 4), r = i % (LAY_ROWS * 4) / 4, q = i % 4;
             if (r0 + r < rows && s0 + c < n)
                 steps[((int64_t)(s0 + c) * rows + r0 + r) * 4 + q] = piece[r][c * 4 + q];
@@ -221,34 +222,36 @@ Form form_of(const void* p, int cols) {
 template <typename T>
 int quantize(const T* x, int64_t rows, int cols, uint8_t* codes, uint8_t* scales, hipStream_t s) {
     const int64_t pieces = rows * (mx_cols(cols) / 8);
-    const dim3 grid((unsigned)ceil_div(pieces, MX_PIECES)), block(MX_THREADS);
+    const Form form = form_of(x, cols);
+    return launch_groups(ceil_div(pieces, MX_PIECES), MX_THREADS, [&](int64_t first, unsigned groups) {
 #define MOE_MXQ(F)                                                                             \
-    hipLaunchKernelGGL((quantize_mxfp4_kernel<T, F>), grid, block, 0, s, x, pieces,     \
-                       cols, (uint32_t*)codes, scales)
-    switch (form_of(x, cols)) {
-        case DENSE: MOE_MXQ(DENSE); break;
-        case PADDED: MOE_MXQ(PADDED); break;
-        default: MOE_MXQ(ELEMENTS); break;
-    }
+    hipLaunchKernelGGL((quantize_mxfp4_kernel<T, F>), dim3(groups), dim3(MX_THREADS), 0, s, x, \
+                       first, pieces, cols, (uint32_t*)codes, scales)
+        switch (form) {
+            case DENSE: MOE_MXQ(DENSE); break;
+            case PADDED: MOE_MXQ(PADDED); break;
+            default: MOE_MXQ(ELEMENTS); break;
+        }
 #undef MOE_MXQ
-    return launch_status();
+    });
 }
 
 template <typename T>
 int dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols, T* y,
                hipStream_t s) {
     const int64_t pieces = rows * (mx_cols(cols) / 8);
-    const dim3 grid((unsigned)ceil_div(pieces, MX_PIECES)), block(MX_THREADS);
-#define MOE_MXD(F)                                                                             \
-    hipLaunchKernelGGL((dequantize_mxfp4_kernel<T, F>), grid, block, 0, s,                     \
-                       (const uint32_t*)codes, scales, pieces, cols, y)
-    switch (form_of(y, cols)) {
-        case DENSE: MOE_MXD(DENSE); break;
-        case PADDED: MOE_MXD(PADDED); break;
-        default: MOE_MXD(ELEMENTS); break;
-    }
+    const Form form = form_of(y, cols);
+    return launch_groups(ceil_div(pieces, MX_PIECES), MX_THREADS, [&](int64_t first, unsigned groups) {
+#define MOE_MXD(F)                                                                          \
+    hipLaunchKernelGGL((dequantize_mxfp4_kernel<T, F>), dim3(groups), dim3(MX_THREADS), 0,  \
+                       s, (const uint32_t*)codes, scales, first, pieces, cols, y)
+        switch (form) {
+            case DENSE: MOE_MXD(DENSE); break;
+            case PADDED: MOE_MXD(PADDED); break;
+            default: MOE_MXD(ELEMENTS); break;
+        }
 #undef MOE_MXD
-    return launch_status();
+    });
 }
 
 }  // namespace
@@ -263,20 +266,22 @@ int launch_quantize_mxfp4(const void* x, int dtype, int64_t rows, int cols, uint
 int launch_quantize_mxfp4_steps(const bf16_t* x, int64_t rows, int cols, uint8_t* codes,
                                 uint32_t* words, hipStream_t s) {
     if (rows == 0) return MOE_OK;
-    const dim3 grid((unsigned)rows, (unsigned)ceil_div(mx_cols(cols) / 8, MX_THREADS));
-    hipLaunchKernelGGL(quantize_steps_kernel, grid, dim3(MX_THREADS), 0, s, x, rows, cols,
-                       (uint32_t*)codes, (uint8_t*)words);
-    return launch_status();
+    const unsigned along = (unsigned)ceil_div(mx_cols(cols) / 8, MX_THREADS);
+    return launch_groups(rows, MX_THREADS, [&](int64_t first, unsigned groups) {
+        hipLaunchKernelGGL(quantize_steps_kernel, dim3(groups, along), dim3(MX_THREADS), 0, s, x, first, rows,
+                           cols, (uint32_t*)codes, (uint8_t*)words);
+    });
 }
 
 int launch_mxfp4_lay_out(const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols,
                          uint8_t* steps, uint32_t* words, hipStream_t s) {
     if (rows == 0) return MOE_OK;
     const int n = (int)(mx_cols(cols) / 128);
-    const dim3 grid((unsigned)ceil_div(rows, LAY_ROWS), (unsigned)std::min(ceil_div(n, LAY_STEPS), (int64_t)65535));
-    hipLaunchKernelGGL(lay_out_kernel, grid, dim3(256), 0, s, (const uint4*)codes,
-                       (const uint32_t*)scales, rows, n, (uint4*)steps, words);
-    return launch_status();
+    const unsigned along = (unsigned)std::min(ceil_div(n, LAY_STEPS), (int64_t)65535);
+    return launch_groups(ceil_div(rows, LAY_ROWS), LAY_THREADS, [&](int64_t first, unsigned groups) {
+        hipLaunchKernelGGL(lay_out_kernel, dim3(groups, along), dim3(LAY_THREADS), 0, s, (const uint4*)codes,
+                           (const uint32_t*)scales, first, rows, n, (uint4*)steps, words);
+    });
 }
 
 int launch_dequantize_mxfp4(const uint8_t* codes, const uint8_t* scales, int64_t rows, int cols,

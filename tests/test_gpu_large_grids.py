@@ -1,0 +1,61 @@
+"""Calls of more workgroups than one grid holds (marked `gpu`): every row is there, and the
+rows around the end of the first launch and the last ones are right."""
+import pytest
+import torch
+
+from oracle import mxfp4 as om
+from paper_2607_08782_amd import moe
+
+from parity import say
+from test_gpu_ffn_mxfp4 import _expected, _experts, _values
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    moe.load_library()
+    yield
+    torch.cuda.empty_cache()
+
+
+def test_4_bit_ffn_of_a_long_batch():
+    """2^24 token rows and some: the first ones, those around the end of a launch, the last."""
+    say("[ffn mxfp4 long batch]")
+    d, f, T = 8, 96, (1 << 24) + 100
+    (w13,), (w2,) = _experts(1, d, f, 21)
+    table = moe.MxWeightTable([w13], [w2], d, f)
+    x = torch.randn(T, d, generator=torch.Generator(device="cuda").manual_seed(21), device="cuda").bfloat16()
+    token = torch.cat([torch.arange(0, 40), torch.arange((1 << 24) - 60, T)]).int().cuda()
+    n = len(token)
+    off = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    ws = torch.full((moe.moe_grouped_ffn_mxfp4_ws_bytes(T, n, d, f, 1),), 0xFF, dtype=torch.uint8, device="cuda")
+    got = moe.moe_grouped_ffn_mxfp4(x, off, table, row_token=token, cap_rows=n, ws=ws)
+    want, tol = _expected(om.rounded(x[token.long()].float().cpu().numpy()), _values(w13, d), _values(w2, f), f)
+    assert (abs(got[:n].double().cpu().numpy() - want) <= tol).all()
+
+
+def test_conversions_of_many_rows():
+    """Rows of one value that 4 bits hold exactly: to MXFP4, step-major (of one step: in the
+    same order) and back."""
+    say("[mxfp4 many rows]")
+    rows, part = (1 << 30) + 37, 1 << 26
+    values = torch.tensor([0.0, 0.5, 1.0, 1.5, 3.0, 6.0, -0.75, -48.0, 2.0 ** 100, -2.0 ** -90], device="cuda")
+    order = torch.randint(0, len(values), (9973,), generator=torch.Generator().manual_seed(1)).cuda()
+    x = torch.empty(rows, 1, dtype=torch.bfloat16, device="cuda")
+    for r in range(0, rows, part):
+        at = torch.arange(r, min(r + part, rows), device="cuda") % len(order)
+        x[r:r + part, 0] = values[order[at]]
+    q = torch.full((rows, 64), 0xA5, dtype=torch.uint8, device="cuda")
+    scales = torch.full((rows, 4), 0xA5, dtype=torch.uint8, device="cuda")
+    moe.moe_quantize_mxfp4(x, q=q, scales=scales)
+    y = torch.full((rows, 1), 7.0, dtype=torch.bfloat16, device="cuda")
+    moe.moe_dequantize_mxfp4(q, scales, 1, out=y)
+    steps, words = moe.moe_mxfp4_lay_out(q, scales, 1)
+    for r in range(0, rows, part):
+        e = min(r + part, rows)
+        assert torch.equal(x[r:e], y[r:e]), r
+        assert torch.equal(steps[0, r:e].view(torch.int64), q[r:e].view(torch.int64)), r
+        assert torch.equal(words[0, r:e], scales[r:e].view(torch.int32)[:, 0]), r
+        assert not q[r:e, 1:].view(torch.uint8).any() and not scales[r:e, 1:].any(), r
