@@ -95,9 +95,9 @@ __device__ __forceinline__ void add_shared(const Elem* __restrict__ y_shared, in
 template <typename Elem, int V, int KM>
 __global__ __launch_bounds__(COMBINE_THREADS) void combine_kernel(
     const Elem* __restrict__ y_perm, const int32_t* __restrict__ token_row,
-    const float* __restrict__ gate, const Elem* __restrict__ y_shared, int n_shared, int64_t T,
-    int d, int k, int chunks_per_row, Elem* __restrict__ y) {
-    const int64_t gid = (int64_t)blockIdx.x * COMBINE_THREADS + threadIdx.x;
+    const float* __restrict__ gate, const Elem* __restrict__ y_shared, int n_shared, int64_t first,
+    int64_t T, int d, int k, int chunks_per_row, Elem* __restrict__ y) {
+    const int64_t gid = (first + blockIdx.x) * COMBINE_THREADS + threadIdx.x;
     const int64_t t = gid / chunks_per_row;
     const int c = (int)(gid - t * chunks_per_row);
     if (t >= T) return;
@@ -114,17 +114,17 @@ __global__ __launch_bounds__(COMBINE_THREADS) void combine_kernel(
         p[r] = r < k ? token_row[t * k + rr] : -1;
         g[r] = gate ? gate[t * k + rr] : 1.f;
     }
-    int32_t first = -1;
+    int32_t local = -1;
 #pragma unroll
-    for (int r = KM - 1; r >= 0; --r) first = p[r] >= 0 ? p[r] : first;
+    for (int r = KM - 1; r >= 0; --r) local = p[r] >= 0 ? p[r] : local;
     float acc[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = 0.f;
-    if (first >= 0) {
+    if (local >= 0) {
         float v[KM][V];
 #pragma unroll
         for (int r = 0; r < KM; ++r)
-            Vec<Elem, V>::load(y_perm + (int64_t)(p[r] >= 0 ? p[r] : first) * d + col, v[r]);
+            Vec<Elem, V>::load(y_perm + (int64_t)(p[r] >= 0 ? p[r] : local) * d + col, v[r]);
 #pragma unroll
         for (int r = 0; r < KM; ++r)
 #pragma unroll
@@ -169,10 +169,10 @@ __device__ __forceinline__ void combine_rows(const Elem* __restrict__ y_perm, in
 template <typename Elem, int V>
 __global__ __launch_bounds__(COMBINE_THREADS) void combine_wave_kernel(
     const Elem* __restrict__ y_perm, const int32_t* __restrict__ token_row,
-    const float* __restrict__ gate, const Elem* __restrict__ y_shared, int n_shared, int T,
-    int d, int k, int parts, Elem* __restrict__ y) {
+    const float* __restrict__ gate, const Elem* __restrict__ y_shared, int n_shared, int first,
+    int T, int d, int k, int parts, Elem* __restrict__ y) {
     // wave w: token w / parts, its chunks from (w % parts) * 64
-    const int w = __builtin_amdgcn_readfirstlane((int)blockIdx.x * (COMBINE_THREADS / 64) +
+    const int w = __builtin_amdgcn_readfirstlane((first + (int)blockIdx.x) * (COMBINE_THREADS / 64) +
                                                  (int)(threadIdx.x >> 6));
     const int t = parts == 1 ? w : (int)((unsigned)w / (unsigned)parts);
     if (t >= T) return;
@@ -203,17 +203,19 @@ int launch_k(const void* y_perm, const int32_t* token_row, const float* gate, co
     const int chunks = d / V;
     if (V > 1 && chunks % 64 == 0 && T * (chunks / 64) < ((int64_t)1 << 30)) {
         const int parts = chunks / 64;
-        hipLaunchKernelGGL((combine_wave_kernel<Elem, V>),
-                           dim3((unsigned)ceil_div(T * parts, COMBINE_THREADS / 64)),
-                           dim3(COMBINE_THREADS), 0, s, (const Elem*)y_perm, token_row, gate,
-                           (const Elem*)y_shared, n_shared, (int)T, d, k, parts, (Elem*)y);
-        return launch_status();
+        return launch_groups(ceil_div(T * parts, COMBINE_THREADS / 64), COMBINE_THREADS,
+                             [&](int64_t first, unsigned groups) {
+            hipLaunchKernelGGL((combine_wave_kernel<Elem, V>), dim3(groups), dim3(COMBINE_THREADS), 0, s,
+                               (const Elem*)y_perm, token_row, gate, (const Elem*)y_shared, n_shared,
+                               (int)first, (int)T, d, k, parts, (Elem*)y);
+        });
     }
-    const int64_t blocks = ceil_div(T * chunks, COMBINE_THREADS);
-    hipLaunchKernelGGL((combine_kernel<Elem, V, KM>), dim3((unsigned)blocks), dim3(COMBINE_THREADS),
-                       0, s, (const Elem*)y_perm, token_row, gate, (const Elem*)y_shared, n_shared,
-                       T, d, k, chunks, (Elem*)y);
-    return launch_status();
+    return launch_groups(ceil_div(T * chunks, COMBINE_THREADS), COMBINE_THREADS,
+                         [&](int64_t first, unsigned groups) {
+        hipLaunchKernelGGL((combine_kernel<Elem, V, KM>), dim3(groups), dim3(COMBINE_THREADS), 0, s,
+                           (const Elem*)y_perm, token_row, gate, (const Elem*)y_shared, n_shared, first,
+                           T, d, k, chunks, (Elem*)y);
+    });
 }
 
 template <typename Elem, int V>

@@ -59,3 +59,20 @@ def test_conversions_of_many_rows():
         assert torch.equal(steps[0, r:e].view(torch.int64), q[r:e].view(torch.int64)), r
         assert torch.equal(words[0, r:e], scales[r:e].view(torch.int32)[:, 0]), r
         assert not q[r:e, 1:].view(torch.uint8).any() and not scales[r:e, 1:].any(), r
+
+
+@pytest.mark.parametrize("T,d", [((1 << 20) + 900, 4097), ((1 << 23) + 900, 4096)])
+def test_packaging_gradient_of_a_long_batch(T, d):
+    """More elements than work-items of a grid, by either of the kernels: each token's row is
+    one of few, its number tells which."""
+    say("[permute grad long batch]", T, d)
+    n = 97
+    rows = torch.randn(n, d, generator=torch.Generator().manual_seed(5)).bfloat16().cuda()
+    row = (torch.arange(T, device="cuda") % n).int().view(T, 1)
+    dx = torch.full((T, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    moe.moe_permute_backward(rows, row, dx=dx)
+    part = n * 10000
+    want = rows.repeat(10000, 1)
+    for t in range(0, T, part):
+        got = dx[t:t + part]
+        assert torch.equal(got, want[:len(got)]), t
