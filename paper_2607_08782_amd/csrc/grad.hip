@@ -74,12 +74,12 @@ constexpr int CB_THREADS = 256;
 template <typename Elem, int V, int W, int NC>
 __global__ __launch_bounds__(CB_THREADS) void combine_backward_kernel(
     const Elem* __restrict__ dy, const Elem* __restrict__ y_perm,
-    const int32_t* __restrict__ token_row, const float* __restrict__ gate, int64_t T, int d, int k,
-    Elem* __restrict__ dy_perm, float* __restrict__ dgate) {
+    const int32_t* __restrict__ token_row, const float* __restrict__ gate, int64_t first, int64_t T,
+    int d, int k, Elem* __restrict__ dy_perm, float* __restrict__ dgate) {
     __shared__ float part[W > 1 ? MOE_MAX_K : 1][W];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int64_t t = (int64_t)blockIdx.x * (CB_THREADS / 64 / W) + wave / W;
+    const int64_t t = (first + blockIdx.x) * (CB_THREADS / 64 / W) + wave / W;
     if (t >= T) return;                                  // whole workgroups where W > 1
     const int sub = wave % W;
     const int chunks = d / V;
@@ -155,23 +155,24 @@ int combine_backward(const void* dy, const void* y_perm, const int32_t* token_ro
     // a wave per token where that fills the chip and a row fits its registers, else four
     const int chunks = d / V;
     const bool wide = T < 4096 || chunks > 64 * 8;
-#define MOE_CB(W, NC)                                                                            \
-    hipLaunchKernelGGL((combine_backward_kernel<Elem, V, W, NC>),                                \
-                       dim3((unsigned)ceil_div(T, CB_THREADS / 64 / W)), dim3(CB_THREADS), 0, s, \
-                       (const Elem*)dy, (const Elem*)y_perm, token_row, gate, T, d, k,           \
-                       (Elem*)dy_perm, dgate)
-    if (wide) {
-        if (chunks <= 256) MOE_CB(4, 1);
-        else if (chunks <= 512) MOE_CB(4, 2);
-        else MOE_CB(4, 4);
-    } else {
-        if (chunks <= 64) MOE_CB(1, 1);
-        else if (chunks <= 128) MOE_CB(1, 2);
-        else if (chunks <= 256) MOE_CB(1, 4);
-        else MOE_CB(1, 8);
-    }
+    const int tokens = wide ? 1 : CB_THREADS / 64;       // a workgroup's
+    return launch_groups(ceil_div(T, tokens), CB_THREADS, [&](int64_t first, unsigned groups) {
+#define MOE_CB(W, NC)                                                                             \
+    hipLaunchKernelGGL((combine_backward_kernel<Elem, V, W, NC>), dim3(groups), dim3(CB_THREADS), \
+                       0, s, (const Elem*)dy, (const Elem*)y_perm, token_row, gate, first, T, d,  \
+                       k, (Elem*)dy_perm, dgate)
+        if (wide) {
+            if (chunks <= 256) MOE_CB(4, 1);
+            else if (chunks <= 512) MOE_CB(4, 2);
+            else MOE_CB(4, 4);
+        } else {
+            if (chunks <= 64) MOE_CB(1, 1);
+            else if (chunks <= 128) MOE_CB(1, 2);
+            else if (chunks <= 256) MOE_CB(1, 4);
+            else MOE_CB(1, 8);
+        }
 #undef MOE_CB
-    return launch_status();
+    });
 }
 
 // ---------------------------------------------------------------------------
@@ -187,11 +188,11 @@ constexpr int RJ = MOE_MAX_E / 64;
 template <bool RENORM>
 __global__ __launch_bounds__(RB_THREADS) void gate_backward_kernel(
     const float* __restrict__ dgate, const float* __restrict__ gate, const int32_t* __restrict__ idx,
-    const float* __restrict__ logits, int64_t T, int E, int k, float* __restrict__ dlogits,
-    float* __restrict__ sel) {
+    const float* __restrict__ logits, int64_t first, int64_t T, int E, int k,
+    float* __restrict__ dlogits, float* __restrict__ sel) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int64_t t = (int64_t)blockIdx.x * (RB_THREADS / 64) + wave;
+    const int64_t t = (first + blockIdx.x) * (RB_THREADS / 64) + wave;
     if (t >= T) return;
     const bool mine = lane < k;
     const int e_r = mine ? idx[t * k + lane] : -1;
@@ -684,12 +685,12 @@ constexpr int GT = 64;
 template <bool VEC>
 __global__ __launch_bounds__(256) void scores_backward_f32_kernel(const float* __restrict__ dlogits,
                                                                   const float* __restrict__ w,
-                                                                  int64_t T, int d, int E,
+                                                                  int first, int64_t T, int d, int E,
                                                                   float* __restrict__ dx) {
     const int lane = threadIdx.x & 63, i16 = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int64_t t0 = ((int64_t)blockIdx.x * 4 + wave) * GT;
-    const int c0 = blockIdx.y * GT + 4 * i16;
+    const int c0 = (first + (int)blockIdx.y) * GT + 4 * i16;
     if (t0 >= T) return;
     const bool whole = d % 4 == 0;                       // rows of 16-byte chunks
     f32x4 acc[4][4];
@@ -816,14 +817,17 @@ int launch_router_backward(const float* dl, const float* sel, const int32_t* idx
             // only the chosen experts' scores have a gradient: their router rows, weighted
             st = launch_combine(w, dtype, idx, sel, nullptr, 0, T, d, k, dx, s);
         } else if (dx) {
-            const dim3 grid((unsigned)ceil_div(T, 4 * GT), (unsigned)ceil_div(d, GT));
-            if (vec)
-                hipLaunchKernelGGL(scores_backward_f32_kernel<true>, grid, dim3(256), 0, s, dl,
-                                   (const float*)w, T, d, E, (float*)dx);
-            else
-                hipLaunchKernelGGL(scores_backward_f32_kernel<false>, grid, dim3(256), 0, s, dl,
-                                   (const float*)w, T, d, E, (float*)dx);
-            st = launch_status();
+            const int cols = (int)ceil_div(d, GT), most = 65535;     // the latter: of a grid
+            for (int first = 0; first < cols && st == MOE_OK; first += most) {
+                const dim3 grid((unsigned)ceil_div(T, 4 * GT), (unsigned)std::min(cols - first, most));
+                if (vec)
+                    hipLaunchKernelGGL(scores_backward_f32_kernel<true>, grid, dim3(256), 0, s, dl,
+                                       (const float*)w, first, T, d, E, (float*)dx);
+                else
+                    hipLaunchKernelGGL(scores_backward_f32_kernel<false>, grid, dim3(256), 0, s, dl,
+                                       (const float*)w, first, T, d, E, (float*)dx);
+                st = launch_status();
+            }
         }
         if (st != MOE_OK || !sums) return st;
         if (vec) hipLaunchKernelGGL(router_grad_f32_kernel<true>, dim3(groups), block, 0, s, p);
@@ -868,14 +872,15 @@ int launch_route_backward(const float* dgate, const float* gate, const int32_t* 
     float* sel = sparse ? (float*)(base + at.sel) : nullptr;
     float* dl = dlogits ? dlogits : dw || dbias || (dx && !sparse) ? (float*)base : nullptr;
     if (T > 0) {
-        const dim3 grid((unsigned)ceil_div(T, RB_THREADS / 64)), block(RB_THREADS);
-        if (renorm)
-            hipLaunchKernelGGL(gate_backward_kernel<true>, grid, block, 0, s, dgate, gate, idx, logits,
-                               T, E, k, dl, sel);
-        else
-            hipLaunchKernelGGL(gate_backward_kernel<false>, grid, block, 0, s, dgate, gate, idx,
-                               logits, T, E, k, dl, sel);
-        const int st = launch_status();
+        const int64_t groups = ceil_div(T, RB_THREADS / 64);
+        const int st = launch_groups(groups, RB_THREADS, [&](int64_t first, unsigned n) {
+            if (renorm)
+                hipLaunchKernelGGL(gate_backward_kernel<true>, dim3(n), dim3(RB_THREADS), 0, s, dgate, gate,
+                                   idx, logits, first, T, E, k, dl, sel);
+            else
+                hipLaunchKernelGGL(gate_backward_kernel<false>, dim3(n), dim3(RB_THREADS), 0, s, dgate, gate,
+                                   idx, logits, first, T, E, k, dl, sel);
+        });
         if (st != MOE_OK) return st;
     }
     return launch_router_backward(dl, sel, idx, x, w, dtype, T, d, E, k, T > 0 ? dx : nullptr, dw, dbias,

@@ -76,3 +76,53 @@ def test_packaging_gradient_of_a_long_batch(T, d):
     for t in range(0, T, part):
         got = dx[t:t + part]
         assert torch.equal(got, want[:len(got)]), t
+
+
+def test_combine_and_gate_gradients_of_a_long_batch():
+    """2^26 tokens and some, of one column each: dy_perm and dgate of the last token of every
+    2^20 and of those around the end of a launch; dlogits of all."""
+    say("[combine grad long batch]")
+    T, n = (1 << 26) + 77, 200
+    tokens = torch.cat([torch.arange((1 << 20) - 1, T, 1 << 20), torch.arange((1 << 26) - 60, (1 << 26) - 1),
+                        torch.arange(T - 60, T)]).cuda()
+    m = len(tokens)
+    assert m <= n and len(tokens.unique()) == m
+    row = torch.full((T, 1), -1, dtype=torch.int32, device="cuda")
+    row[tokens, 0] = torch.arange(m, dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(6)
+    # products of bf16 values are exact in 32 bits
+    dy = torch.randn(T, 1, generator=g, device="cuda").bfloat16()
+    y = torch.randn(n, 1, generator=g, device="cuda").bfloat16()
+    gate = torch.rand(T, 1, generator=g, device="cuda")
+    out = torch.full((n, 1), 7.0, dtype=torch.bfloat16, device="cuda")
+    dgate = torch.full((T, 1), 7.0, device="cuda")
+    moe.moe_combine_backward(dy, y, row, gate, dy_perm=out, dgate=dgate)
+    want = torch.zeros(T, 1, device="cuda")
+    want[tokens, 0] = dy[tokens, 0].float() * y[:m, 0].float()
+    assert torch.equal(dgate, want)
+    assert torch.equal(out[:m], (gate[tokens] * dy[tokens].float()).bfloat16()) and bool((out[m:] == 7.0).all())
+    # one expert, not renormalised: the softmax is 1 and its gradient 0; two, one half each
+    zeros = torch.zeros(T, 2, device="cuda")
+    idx = torch.zeros(T, 1, dtype=torch.int32, device="cuda")
+    x, w = torch.empty(T, 1, device="cuda"), torch.empty(2, 1, device="cuda")
+    dl = torch.full((T, 2), 7.0, device="cuda")
+    moe.moe_route_topk_backward(gate, torch.full_like(gate, 0.5), idx, x, w, logits=zeros, renorm=False,
+                                want_dx=False, want_dw=False, want_dbias=False, dlogits=dl)
+    assert torch.equal(dl[:, :1], 0.25 * gate) and torch.equal(dl[:, 1:], -0.25 * gate)
+
+
+def test_router_gradient_of_the_longest_rows():
+    """fp32 dx over more column tiles than a grid has along its second dimension."""
+    say("[route grad long rows]")
+    T, E, d = 3, 2, (1 << 22) - 5
+    g = torch.Generator(device="cuda").manual_seed(7)
+    w = torch.randn(E, d, generator=g, device="cuda")
+    x = torch.empty(T, d, device="cuda")
+    dgate, gate = torch.randn(T, 1, generator=g, device="cuda"), torch.full((T, 1), 0.5, device="cuda")
+    idx = torch.tensor([[0], [1], [0]], dtype=torch.int32, device="cuda")
+    dl, dx, _, _ = moe.moe_route_topk_backward(dgate, gate, idx, x, w, logits=torch.zeros(T, E, device="cuda"),
+                                               renorm=False, want_dw=False, want_dbias=False,
+                                               dx=torch.full_like(x, 7.0))
+    want = (dl.double()[:, :, None] * w.double()).sum(1)
+    size = (dl.double()[:, :, None] * w.double()).abs().sum(1)
+    assert bool(((dx.double() - want).abs() <= (E + 4) * 2.0 ** -24 * size).all())

@@ -13,7 +13,7 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
-@pytest.mark.parametrize("group", ["mxfp4", "packaging"])
+@pytest.mark.parametrize("group", ["mxfp4", "packaging", "gradients"])
 def test_every_launch_fits_a_grid(tmp_path, group):
     if not os.path.exists(moe.LIB_PATH):
         from paper_2607_08782_amd import build
