@@ -8,7 +8,8 @@
 // (loads issued together; assignments placed on other GPUs are skipped), accumulates in
 // fp32 in ascending r, and stores once.  A wave serves one token where rows are whole
 // wave widths (combine_wave_kernel).  Without gates every row has weight 1: the gradient
-// of the packaging (moe_permute_backward), whose dx_add stands where y_shared does.
+// of the packaging (moe_permute_backward), whose dx_add stands where y_shared does and may be
+// the output itself: a thread adds the chunk that it then stores.
 #include "common.h"
 
 namespace moe {
@@ -68,7 +69,7 @@ struct Vec<float, 1> {
 // elements), in slice order; more than one slice: four loads at a time, a slice
 // past the last re-reading the last and dropped by a select.
 template <typename Elem, int V>
-__device__ __forceinline__ void add_shared(const Elem* __restrict__ y_shared, int n_shared,
+__device__ __forceinline__ void add_shared(const Elem* y_shared, int n_shared,
                                            int64_t stride, int64_t off, float* acc) {
     if (n_shared == 1) {
         float w[V];
@@ -95,8 +96,8 @@ __device__ __forceinline__ void add_shared(const Elem* __restrict__ y_shared, in
 template <typename Elem, int V, int KM>
 __global__ __launch_bounds__(COMBINE_THREADS) void combine_kernel(
     const Elem* __restrict__ y_perm, const int32_t* __restrict__ token_row,
-    const float* __restrict__ gate, const Elem* __restrict__ y_shared, int n_shared, int64_t first,
-    int64_t T, int d, int k, int chunks_per_row, Elem* __restrict__ y) {
+    const float* __restrict__ gate, const Elem* y_shared, int n_shared, int64_t first,
+    int64_t T, int d, int k, int chunks_per_row, Elem* y) {
     const int64_t gid = (first + blockIdx.x) * COMBINE_THREADS + threadIdx.x;
     const int64_t t = gid / chunks_per_row;
     const int c = (int)(gid - t * chunks_per_row);
@@ -169,8 +170,8 @@ __device__ __forceinline__ void combine_rows(const Elem* __restrict__ y_perm, in
 template <typename Elem, int V>
 __global__ __launch_bounds__(COMBINE_THREADS) void combine_wave_kernel(
     const Elem* __restrict__ y_perm, const int32_t* __restrict__ token_row,
-    const float* __restrict__ gate, const Elem* __restrict__ y_shared, int n_shared, int first,
-    int T, int d, int k, int parts, Elem* __restrict__ y) {
+    const float* __restrict__ gate, const Elem* y_shared, int n_shared, int first,
+    int T, int d, int k, int parts, Elem* y) {
     // wave w: token w / parts, its chunks from (w % parts) * 64
     const int w = __builtin_amdgcn_readfirstlane((first + (int)blockIdx.x) * (COMBINE_THREADS / 64) +
                                                  (int)(threadIdx.x >> 6));
