@@ -620,10 +620,12 @@ size_t moe_route_topk_backward_ws_bytes(int dtype, int64_t T, int d, int E, int 
  * ws         moe_route_topk_backward_ws_bytes(...) bytes, 256-byte aligned
  * flags      MOE_RENORM or 0
  * Products and sums are fp32 in a fixed order (deterministic); with MOE_BF16, dlogits
- * enter dw with all 24 bits and dx, which keeps 8, with 16.  Outputs must not overlap
- * inputs or each other.  Requires T >= 0, 1 <= E <= MOE_MAX_E,
- * 1 <= k <= min(E, MOE_MAX_K), 1 <= d < 2^22 and, for MOE_BF16, d % 8 == 0 (else
- * MOE_ERR_SHAPE); 16-byte aligned matrices where a row is a multiple of 16 bytes.
+ * enter dw with all 24 bits and dx, which keeps 8, with 16.  Infinite dlogits give infinite
+ * sums; an infinity in x (w_router) gives infinities or, with MOE_BF16, NaN in the sums of dw
+ * (dx) that it enters, and in no others.  Outputs must not overlap inputs or each other.
+ * Requires T >= 0, 1 <= E <= MOE_MAX_E, 1 <= k <= min(E, MOE_MAX_K), 1 <= d < 2^22 and, for
+ * MOE_BF16, d % 8 == 0 (else MOE_ERR_SHAPE); 16-byte aligned matrices where a row is a
+ * multiple of 16 bytes.
  */
 int moe_route_topk_backward(const float* dgate, const float* topk_gate, const int32_t* topk_idx,
                             const float* logits, const void* x, const void* w_router, int dtype,

@@ -277,7 +277,12 @@ __device__ __forceinline__ Cell xcd_cell(unsigned b, unsigned total, unsigned co
     return {(int64_t)(l / cols), (int)(l % cols)};
 }
 
-// Eight fp32 values as N bf16 terms each (their sum: 8 N significant bits), packed.
+// Eight fp32 values as N bf16 terms each (their sum: 8 N significant bits), packed.  What
+// remains after a term is exact, and so no term but the last takes more than bf16's largest
+// finite value: an infinity, and what would round to one, stays whole in what remains (an
+// infinity less itself would make it NaN).
+constexpr float BF16_MOST = 0x1.fep127f;
+
 template <int N>
 __device__ __forceinline__ void split8(const float (&x)[8], u32x4 (&out)[N]) {
     float r[8];
@@ -287,7 +292,12 @@ __device__ __forceinline__ void split8(const float (&x)[8], u32x4 (&out)[N]) {
     for (int n = 0; n < N; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t w = pack_bf16x2(r[2 * i], r[2 * i + 1]);
+            float a = r[2 * i], b = r[2 * i + 1];
+            if (n + 1 < N) {
+                a = __builtin_amdgcn_fmed3f(a, -BF16_MOST, BF16_MOST);
+                b = __builtin_amdgcn_fmed3f(b, -BF16_MOST, BF16_MOST);
+            }
+            const uint32_t w = pack_bf16x2(a, b);
             out[n][i] = w;
             r[2 * i] -= __uint_as_float(w << 16);        // exact
             r[2 * i + 1] -= __uint_as_float(w & 0xffff0000u);
