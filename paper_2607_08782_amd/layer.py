@@ -19,7 +19,8 @@ joined back before the combine, overlapping the routed experts' FFN (whose
 launches leave CUs idle) without holding CUs the routing launches wait for;
 the fork and join are stream events, so a graph capture of `run` holds both
 branches.  The expert placement can be swapped between batches
-(`set_placement`) by re-pointing the weight table; nothing is reallocated.
+(`set_placement`) by re-pointing the weight table; nothing is reallocated (but
+with 4-bit experts, whose table is made anew).
 
 With ``mxfp4=True`` the routed experts are held and multiplied in 4 bits
 (moe_grouped_ffn_mxfp4; a third of a decode step's weight bytes); shared experts
@@ -261,13 +262,18 @@ class LayerShare:
 
     def set_placement(self, placement: np.ndarray, w13: Sequence[torch.Tensor],
                       w2: Sequence[torch.Tensor]):
-        """Swap the expert placement between batches (same number of local slots)."""
+        """Swap the expert placement between batches (same number of local slots).  With mxfp4
+        every expert given is quantized and laid out, into new memory and on the current
+        stream; the call then waits for the GPU, so that runs on any stream find the new table
+        whole, and the old one's memory goes back with no kernel still reading it."""
         placement = np.ascontiguousarray(placement, dtype=np.uint8)
         n_local = int(placement[:, self.dev].sum())
         if n_local != self.n_local:
             raise ValueError("the new placement must keep %d local slots" % self.n_local)
-        self.placement = placement
-        self.weights = self._table(w13, w2)
+        table = self._table(w13, w2)
+        if self.mxfp4:
+            torch.cuda.synchronize(self.device)
+        self.placement, self.weights = placement, table
         self._ffn_weights = self._call_weights(w13, w2)
 
     def _call_weights(self, w13: Sequence[torch.Tensor], w2: Sequence[torch.Tensor]):
