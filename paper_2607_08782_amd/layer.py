@@ -190,6 +190,7 @@ class LayerShare:
         dcode = moe.MOE_BF16 if dt == torch.bfloat16 else moe.MOE_F32
         self._blocks = blocks if self.shared_in_ffn else None
         self._ffn_weights = self._call_weights(w13, w2)
+        self.captured_tables = []
         if mxfp4:
             need = moe.moe_grouped_ffn_mxfp4_ws_bytes(T, self.cap_rows, d, max(self.f, 1),
                                                       max(self.n_local, 1))
@@ -265,7 +266,9 @@ class LayerShare:
         """Swap the expert placement between batches (same number of local slots).  With mxfp4
         every expert given is quantized and laid out, into new memory and on the current
         stream; the call then waits for the GPU, so that runs on any stream find the new table
-        whole, and the old one's memory goes back with no kernel still reading it."""
+        whole, and the old one's memory goes back with no kernel still reading it.  A table that
+        a captured run reads stays in `captured_tables`, since the graph's replays go on reading
+        it: clear that list when the graphs captured before a swap are gone."""
         placement = np.ascontiguousarray(placement, dtype=np.uint8)
         n_local = int(placement[:, self.dev].sum())
         if n_local != self.n_local:
@@ -373,6 +376,9 @@ class LayerShare:
         if self.weights is None:
             return
         if self.mxfp4:
+            if torch.cuda.is_current_stream_capturing() and not any(t is self.weights
+                                                                    for t in self.captured_tables):
+                self.captured_tables.append(self.weights)
             moe.moe_grouped_ffn_mxfp4(self.X, self.perm["group_offsets"], self.weights,
                                       row_token=self.perm["row_token"], cap_rows=self.cap_rows,
                                       y_perm=self.y_perm, ws=self.ws_ffn)

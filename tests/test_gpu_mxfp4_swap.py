@@ -58,3 +58,31 @@ def test_runs_on_another_stream_around_a_swap(T):
     torch.cuda.synchronize()
     assert torch.equal(first, old) and torch.equal(second, new)
     del keep
+
+
+@pytest.mark.parametrize("T", [16, 300])
+def test_a_captured_run_replays_with_its_experts_after_swaps(T):
+    """As with experts in bf16, which belong to the caller: a graph from before a swap computes
+    what it did, whatever the memory that is free by then holds."""
+    say("[mxfp4 swap graph]", T)
+    i, other, share, (old, new) = _layers(T)
+    share.run()
+    torch.cuda.synchronize()
+    graphs = []
+    for e, want in ((i, old), (other, new)):
+        share.set_placement(i.placement, e.w13, e.w2)
+        graphs.append((torch.cuda.CUDAGraph(), want))
+        with torch.cuda.graph(graphs[-1][0]):
+            share.run()
+            share.run()
+    assert len(share.captured_tables) == 2 and share.captured_tables[1] is share.weights
+    share.set_placement(i.placement, i.w13, i.w2)
+    keep = _overwrite_free_memory(share.weights)
+    for _ in range(3):
+        for g, want in graphs:
+            g.replay()
+            assert torch.equal(share.y, want)
+        assert torch.equal(share.run(), old)
+        torch.cuda.synchronize()
+    del keep
+    assert len(share.captured_tables) == 2               # eager runs add none
