@@ -210,30 +210,12 @@ __device__ __forceinline__ void strip_rows(const MxArgs& p, float* red, int g, i
                 load(s[i], t + (i + D) * W);
             }
 
-        constexpr int PARTS = W * BM * LD * 4 > 70 * 1024 ? W / 2 : W;   // sums in LDS at once
-        auto at = [&](int part, int m, int j) {
-            return (f32x4*)&red[(part * BM + 16 * m + i16) * LD + 16 * j + 4 * quarter];
-        };
         __syncthreads();                                 // the last row block's sums are read
-        if (PARTS < W) {
-            if (wave >= PARTS)
 #pragma unroll
-                for (int m = 0; m < MS; ++m)
+        for (int m = 0; m < MS; ++m)
 #pragma unroll
-                    for (int j = 0; j < TILES; ++j) *at(wave - PARTS, m, j) = acc[m][j];
-            __syncthreads();
-            if (wave < PARTS)
-#pragma unroll
-                for (int m = 0; m < MS; ++m)
-#pragma unroll
-                    for (int j = 0; j < TILES; ++j) acc[m][j] += *at(wave, m, j);
-            __syncthreads();
-        }
-        if (wave < PARTS)
-#pragma unroll
-            for (int m = 0; m < MS; ++m)
-#pragma unroll
-                for (int j = 0; j < TILES; ++j) *at(wave, m, j) = acc[m][j];
+            for (int j = 0; j < TILES; ++j)
+                *(f32x4*)&red[(wave * BM + 16 * m + i16) * LD + 16 * j + 4 * quarter] = acc[m][j];
         __syncthreads();
         // four output columns a thread
         constexpr int PER_ROW = (SWIGLU ? ROWS / 2 : ROWS) / 4;
@@ -242,7 +224,7 @@ __device__ __forceinline__ void strip_rows(const MxArgs& p, float* red, int g, i
             auto sum = [&](int col) {
                 f32x4 v = *(const f32x4*)&red[r * LD + col];
 #pragma unroll
-                for (int q = 1; q < PARTS; ++q) v += *(const f32x4*)&red[(q * BM + r) * LD + col];
+                for (int q = 1; q < W; ++q) v += *(const f32x4*)&red[(q * BM + r) * LD + col];
                 return v;
             };
             const int row = row0 + m0 + r;
@@ -316,8 +298,8 @@ constexpr int FEW_STEPS = 6;
 // twice the waves in.  Otherwise each group takes the row blocks it needs.
 template <bool SWIGLU, int W, int TILES, int MAX_MS, bool QUANT>
 __global__ __launch_bounds__(64 * W, QUANT ? 3 : MAX_MS == 1 ? 4 : 2) void strip_mxfp4_kernel(MxArgs p) {
-    constexpr int LD = 16 * TILES + 4;
-    constexpr int ALL = W * 16 * MAX_MS * LD, SUMS = ALL * 4 > 70 * 1024 ? ALL / 2 : ALL;
+    constexpr int SUMS = W * 16 * MAX_MS * (16 * TILES + 4);
+    static_assert(SUMS * 4 <= 80 * 1024, "two workgroups share a CU's LDS");
     __shared__ __attribute__((aligned(16))) float red[SUMS];
     const int slot = blockIdx.x / p.strips;
     const int n0 = ((int)blockIdx.x - slot * p.strips) * 16 * TILES / (SWIGLU ? 2 : 1);
@@ -383,11 +365,12 @@ struct TileShape {
     // one operand a wave where there are eight, else of both)
     static constexpr int AL = BM / 16 / WAVES, BL = BN / 16 / WAVES, WL = WAVES == 8 ? 1 : 2;
     static constexpr int LOADS = AL + BL + WL;
-    static constexpr int PER_EU = TM * TN > 8 ? 1 : 2;   // waves a SIMD holds
+    static constexpr int PER_EU = 2;                     // waves a SIMD holds
+    static_assert(TM * TN <= 8, "the accumulators of two waves a SIMD");
 };
 
 struct MxTile {
-    int row0, valid, n0, none;
+    int row0, valid, n0;
     uint64_t w, ws;                                      // its group's weight codes and scale words
 };
 
@@ -427,7 +410,7 @@ __device__ __forceinline__ void starts(const int* s_off, int n_groups, int n_til
 }
 
 template <bool SWIGLU, int WM, int TM, int TN, int RING>
-__global__ __launch_bounds__(64 * 2 * WM, TM * TN > 8 ? 1 : 2) void tile_mxfp4_kernel(MxArgs p) {
+__global__ __launch_bounds__(64 * 2 * WM, 2) void tile_mxfp4_kernel(MxArgs p) {
 #ifdef __HIP_DEVICE_COMPILE__
     typedef TileShape<WM, TM, TN, RING> S;
     constexpr int BM = S::BM, BN = S::BN, BN_OUT = SWIGLU ? BN / 2 : BN;
@@ -671,10 +654,7 @@ __global__ __launch_bounds__(64 * 2 * WM, TM * TN > 8 ? 1 : 2) void tile_mxfp4_k
 #pragma unroll
         for (int m = 0; m < TM; ++m)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                if constexpr (TM * TN > 8) asm volatile("" : "+a"(acc[m][j]));
-                else asm volatile("" : "+v"(acc[m][j]));
-            }
+            for (int j = 0; j < TN; ++j) asm volatile("" : "+v"(acc[m][j]));
     };
     constexpr std::integral_constant<int, 0> first{};
     constexpr std::integral_constant<int, 1> second{};
