@@ -273,7 +273,7 @@ class LayerShare:
         n_local = int(placement[:, self.dev].sum())
         if n_local != self.n_local:
             raise ValueError("the new placement must keep %d local slots" % self.n_local)
-        table = self._table(w13, w2)
+        table = self._table(w13, w2) if n_local else None
         if self.mxfp4:
             torch.cuda.synchronize(self.device)
         self.placement, self.weights = placement, table

@@ -1,5 +1,6 @@
 """Swaps of the placement of a share with 4-bit experts (marked `gpu`) beside runs on other
 streams and captured ones."""
+import numpy as np
 import pytest
 import torch
 
@@ -86,3 +87,13 @@ def test_a_captured_run_replays_with_its_experts_after_swaps(T):
         torch.cuda.synchronize()
     del keep
     assert len(share.captured_tables) == 2               # eager runs add none
+
+
+@pytest.mark.parametrize("mxfp4", [False, True])
+def test_a_share_without_experts_takes_a_swap(mxfp4):
+    cfg = synth.custom_config(**CFG)
+    i = synth.make_layer(cfg, 20, device="cuda")
+    nothing = np.concatenate([i.placement, np.zeros_like(i.placement[:, :1])], 1)    # on one GPU more
+    share = LayerShare(i.X, i.Wr, i.bias, cfg.k, nothing, cfg.G, [], [], mxfp4=mxfp4)
+    share.set_placement(nothing, [], [])
+    assert not share.run().any()
