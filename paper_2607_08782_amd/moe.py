@@ -170,8 +170,23 @@ def _stream(stream):
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
-def _empty(shape, dtype, device):
-    return torch.empty(shape, dtype=dtype, device=device)
+def _of(stream, make):
+    """`make`, which allocates a tensor, for a call on this stream (None: the current one): in
+    that stream's memory, so that nothing queued on another stream still uses it, and what the
+    call drops is used again only behind the call."""
+    if stream is None:
+        return make
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
+
+    def on_stream(*args, **kw):
+        with torch.cuda.stream(stream):
+            return make(*args, **kw)
+    return on_stream
+
+
+def _empty(shape, dtype, device, stream=None):
+    return _of(stream, torch.empty)(shape, dtype=dtype, device=device)
 
 
 def moe_route_topk(x: Optional[torch.Tensor], w_router: Optional[torch.Tensor],
@@ -198,17 +213,17 @@ def moe_route_topk(x: Optional[torch.Tensor], w_router: Optional[torch.Tensor],
             raise ValueError("w_router must be [E, d] of x's dtype")
         device = x.device
         if logits is None and want_logits:
-            logits = _empty((T, E_), torch.float32, device)
+            logits = _empty((T, E_), torch.float32, device, stream)
     if E is not None and E != E_:
         raise ValueError("E mismatch")
     if topk_idx is None:
-        topk_idx = _empty((T, k), torch.int32, device)
+        topk_idx = _empty((T, k), torch.int32, device, stream)
     if topk_gate is None:
-        topk_gate = _empty((T, k), torch.float32, device)
+        topk_gate = _empty((T, k), torch.float32, device, stream)
     flags = (MOE_RENORM if renorm else 0) | (MOE_LOGITS_IN if logits_in else 0)
     need = moe_route_topk_ws_bytes(dtype, T, d, E_, flags)
     if need and ws is None:
-        ws = workspace(need, device)
+        ws = workspace(need, device, stream)
     st = lib.moe_route_topk(_dev(x, "x"), dtype, _dev(w_router, "w_router"),
                             _dev(bias, "bias", torch.float32), T, d, E_, k, flags,
                             _dev(logits, "logits", torch.float32),
@@ -225,9 +240,9 @@ def moe_quantize_e4m3(x: torch.Tensor, *, q: Optional[torch.Tensor] = None,
     lib = load_library()
     rows, cols = x.shape
     if q is None:
-        q = _empty((rows, cols), torch.uint8, x.device)
+        q = _empty((rows, cols), torch.uint8, x.device, stream)
     if scales is None:
-        scales = _empty((rows,), torch.float32, x.device)
+        scales = _empty((rows,), torch.float32, x.device, stream)
     st = lib.moe_quantize_e4m3(_dev(x, "x"), _dtype_code(x), rows, cols, _dev(q, "q", torch.uint8),
                                _dev(scales, "scales", torch.float32), _stream(stream))
     _check("moe_quantize_e4m3", st)
@@ -246,11 +261,11 @@ def moe_route_topk_e4m3(xq: torch.Tensor, x_scale: torch.Tensor, wq: torch.Tenso
     if wq.shape[1] != d:
         raise ValueError("wq must be [E, d]")
     if logits is None:
-        logits = _empty((T, E), torch.float32, xq.device)
+        logits = _empty((T, E), torch.float32, xq.device, stream)
     if topk_idx is None:
-        topk_idx = _empty((T, k), torch.int32, xq.device)
+        topk_idx = _empty((T, k), torch.int32, xq.device, stream)
     if topk_gate is None:
-        topk_gate = _empty((T, k), torch.float32, xq.device)
+        topk_gate = _empty((T, k), torch.float32, xq.device, stream)
     st = lib.moe_route_topk_e4m3(_dev(xq, "xq", torch.uint8), _dev(x_scale, "x_scale", torch.float32),
                                  _dev(wq, "wq", torch.uint8), _dev(w_scale, "w_scale", torch.float32),
                                  _dev(bias, "bias", torch.float32), T, d, E, k,
@@ -273,9 +288,9 @@ def moe_expert_histogram(topk_idx: torch.Tensor, E: int, *, counts: Optional[tor
     lib = load_library()
     T, k = topk_idx.shape
     if counts is None:
-        counts = _empty((E,), torch.int32, topk_idx.device)
+        counts = _empty((E,), torch.int32, topk_idx.device, stream)
     if coact is None and want_coact:
-        coact = _empty((E, E), torch.int32, topk_idx.device)
+        coact = _empty((E, E), torch.int32, topk_idx.device, stream)
     st = lib.moe_expert_histogram(_dev(topk_idx, "topk_idx", torch.int32), T, k, E,
                                   _dev(counts, "counts", torch.int32),
                                   _dev(coact, "coact", torch.int32), _stream(stream))
@@ -291,9 +306,10 @@ def moe_grouped_ffn_ws_bytes(dtype: int, cap_rows: int, d: int, f: int, n_groups
     return int(load_library().moe_grouped_ffn_ws_bytes(dtype, cap_rows, d, f, n_groups))
 
 
-def workspace(nbytes: int, device) -> torch.Tensor:
-    """A 256-byte aligned device workspace (torch's caching allocator aligns to 512 B)."""
-    ws = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+def workspace(nbytes: int, device, stream=None) -> torch.Tensor:
+    """A 256-byte aligned device workspace (torch's caching allocator aligns to 512 B) for calls
+    on this stream (None: the current one)."""
+    ws = _empty((max(int(nbytes), 256),), torch.uint8, device, stream)
     assert ws.data_ptr() % 256 == 0
     return ws
 
@@ -322,12 +338,12 @@ def moe_permute(x: torch.Tensor, topk_idx: torch.Tensor, topk_gate: torch.Tensor
     o = {} if out is None else out
     if "group_offsets" not in o:
         if copy_rows:
-            o["x_perm"] = _empty((max(cap_rows, 1), d), x.dtype, device)
-        o["group_offsets"] = _empty((n_local + 1,), torch.int32, device)
-        o["row_token"] = _empty((max(cap_rows, 1),), torch.int32, device)
-        o["row_gate"] = _empty((max(cap_rows, 1),), torch.float32, device)
-        o["token_row"] = _empty((T, k), torch.int32, device)
-        o["send_counts"] = _empty((G,), torch.int32, device) if want_send_counts else None
+            o["x_perm"] = _empty((max(cap_rows, 1), d), x.dtype, device, stream)
+        o["group_offsets"] = _empty((n_local + 1,), torch.int32, device, stream)
+        o["row_token"] = _empty((max(cap_rows, 1),), torch.int32, device, stream)
+        o["row_gate"] = _empty((max(cap_rows, 1),), torch.float32, device, stream)
+        o["token_row"] = _empty((T, k), torch.int32, device, stream)
+        o["send_counts"] = _empty((G,), torch.int32, device, stream) if want_send_counts else None
     args = [_dev(x, "x") if copy_rows else None, _dtype_code(x),
             _dev(topk_idx, "topk_idx", torch.int32), _dev(topk_gate, "topk_gate", torch.float32),
             _dev(counts, "counts", torch.int32), T, d if copy_rows else 0, k, E,
@@ -342,7 +358,7 @@ def moe_permute(x: torch.Tensor, topk_idx: torch.Tensor, topk_gate: torch.Tensor
         _check("moe_permute_noalloc", lib.moe_permute_noalloc(*args, _stream(stream)))
         return o
     if ws is None:
-        ws = workspace(moe_permute_ws_bytes(T, k, E), device)
+        ws = workspace(moe_permute_ws_bytes(T, k, E), device, stream)
     _check("moe_permute", lib.moe_permute(*args, _dev(ws, "ws"), ws.numel(), _stream(stream)))
     return o
 
@@ -443,9 +459,9 @@ def moe_grouped_ffn(x_perm: torch.Tensor, group_offsets: torch.Tensor, weights: 
     if group_offsets.numel() != len(weights) + 1:
         raise ValueError("group_offsets must hold n_groups + 1 entries")
     if y_perm is None:
-        y_perm = _empty((max(cap_rows, 1), d), x_perm.dtype, x_perm.device)
+        y_perm = _empty((max(cap_rows, 1), d), x_perm.dtype, x_perm.device, stream)
     if ws is None:
-        ws = workspace(moe_grouped_ffn_ws_bytes(dtype, cap_rows, d, f, len(weights)), x_perm.device)
+        ws = workspace(moe_grouped_ffn_ws_bytes(dtype, cap_rows, d, f, len(weights)), x_perm.device, stream)
     args = [_dev(x_perm, "x_perm"), dtype, _dev(group_offsets, "group_offsets", torch.int32),
             len(weights), ctypes.cast(weights.p13, ctypes.c_void_p),
             ctypes.cast(weights.p2, ctypes.c_void_p), d, f, cap_rows,
@@ -472,9 +488,9 @@ def moe_grouped_ffn_combine(x_perm: torch.Tensor, group_offsets: torch.Tensor,
         raise ValueError("x_perm must be [rows, d] of the weights' dtype")
     k = token_row.shape[1]
     if y is None:
-        y = _empty((max(T, 1), d), x_perm.dtype, x_perm.device)
+        y = _empty((max(T, 1), d), x_perm.dtype, x_perm.device, stream)
     if ws is None:
-        ws = workspace(moe_grouped_ffn_ws_bytes(dtype, cap_rows, d, f, len(weights)), x_perm.device)
+        ws = workspace(moe_grouped_ffn_ws_bytes(dtype, cap_rows, d, f, len(weights)), x_perm.device, stream)
     st = lib.moe_grouped_ffn_combine(
         _dev(x_perm, "x_perm"), dtype, _dev(group_offsets, "group_offsets", torch.int32),
         len(weights), ctypes.cast(weights.p13, ctypes.c_void_p),
@@ -501,9 +517,9 @@ def moe_grouped_ffn_rows(x: torch.Tensor, row_token: torch.Tensor, group_offsets
     if group_offsets.numel() != len(weights) + 1:
         raise ValueError("group_offsets must hold n_groups + 1 entries")
     if y_perm is None:
-        y_perm = _empty((max(cap_rows, 1), d), x.dtype, x.device)
+        y_perm = _empty((max(cap_rows, 1), d), x.dtype, x.device, stream)
     if ws is None:
-        ws = workspace(moe_grouped_ffn_ws_bytes(dtype, cap_rows, d, f, len(weights)), x.device)
+        ws = workspace(moe_grouped_ffn_ws_bytes(dtype, cap_rows, d, f, len(weights)), x.device, stream)
     args = [_dev(x, "x"), T, _dev(row_token, "row_token", torch.int32), dtype,
             _dev(group_offsets, "group_offsets", torch.int32), len(weights),
             ctypes.cast(weights.p13, ctypes.c_void_p), ctypes.cast(weights.p2, ctypes.c_void_p), d, f,
@@ -537,9 +553,9 @@ def moe_grouped_ffn_rows_shared(x: torch.Tensor, row_token: torch.Tensor,
     if row_token.numel() < rows:
         raise ValueError("row_token must hold n_shared * T + cap_rows entries")
     if y_perm is None:
-        y_perm = _empty((max(rows, 1), d), x.dtype, x.device)
+        y_perm = _empty((max(rows, 1), d), x.dtype, x.device, stream)
     if ws is None:
-        ws = workspace(moe_grouped_ffn_ws_bytes(dtype, rows, d, f, len(weights)), x.device)
+        ws = workspace(moe_grouped_ffn_ws_bytes(dtype, rows, d, f, len(weights)), x.device, stream)
     st = lib.moe_grouped_ffn_rows_shared(
         _dev(x, "x"), T, _dev(row_token, "row_token", torch.int32), dtype,
         _dev(group_offsets, "group_offsets", torch.int32), n_groups, n_shared,
@@ -558,7 +574,7 @@ def moe_combine(y_perm: torch.Tensor, token_row: torch.Tensor, topk_gate: torch.
     k = token_row.shape[1] if token_row.dim() == 2 else 1
     dtype = _dtype_code(y_perm)
     if y is None:
-        y = _empty((T, d), y_perm.dtype, y_perm.device)
+        y = _empty((T, d), y_perm.dtype, y_perm.device, stream)
     st = lib.moe_combine(_dev(y_perm, "y_perm", y.dtype), dtype,
                          _dev(token_row, "token_row", torch.int32),
                          _dev(topk_gate, "topk_gate", torch.float32),
@@ -577,7 +593,7 @@ def moe_combine_shared(y_perm: torch.Tensor, token_row: torch.Tensor, topk_gate:
     k = token_row.shape[1] if token_row.dim() == 2 else 1
     dtype = _dtype_code(y_perm)
     if y is None:
-        y = _empty((T, d), y_perm.dtype, y_perm.device)
+        y = _empty((T, d), y_perm.dtype, y_perm.device, stream)
     if y_shared is not None and n_shared > 0 and y_shared.numel() < n_shared * T * d:
         raise ValueError("y_shared must hold n_shared slices of [T, d]")
     st = lib.moe_combine_shared(_dev(y_perm, "y_perm", y.dtype), dtype,
@@ -602,9 +618,9 @@ def moe_quantize_mxfp4(x: torch.Tensor, *, q: Optional[torch.Tensor] = None,
     rows, cols = x.shape
     P = mxfp4_cols(cols)
     if q is None:
-        q = _empty((rows, P // 2), torch.uint8, x.device)
+        q = _empty((rows, P // 2), torch.uint8, x.device, stream)
     if scales is None:
-        scales = _empty((rows, P // 32), torch.uint8, x.device)
+        scales = _empty((rows, P // 32), torch.uint8, x.device, stream)
     _holds(q, "q", rows, P // 2)
     _holds(scales, "scales", rows, P // 32)
     st = lib.moe_quantize_mxfp4(_dev(x, "x"), _dtype_code(x), rows, cols, _dev(q, "q", torch.uint8),
@@ -623,7 +639,7 @@ def moe_dequantize_mxfp4(q: torch.Tensor, scales: torch.Tensor, cols: int, *,
         raise ValueError("an MXFP4 matrix of %d columns has codes [rows, %d] and scales [rows, %d]"
                          % (cols, P // 2, P // 32))
     if out is None:
-        out = _empty((rows, cols), dtype, q.device)
+        out = _empty((rows, cols), dtype, q.device, stream)
     _holds(out, "out", rows, cols)
     st = lib.moe_dequantize_mxfp4(_dev(q, "q", torch.uint8), _dev(scales, "scales", torch.uint8),
                                   rows, cols, _dtype_code(out), _dev(out, "out", dtype),
@@ -641,8 +657,8 @@ def moe_mxfp4_lay_out(q: torch.Tensor, scales: torch.Tensor, cols: int, *, strea
     if cols < 1 or tuple(q.shape) != (rows, P // 2) or tuple(scales.shape) != (rows, P // 32):
         raise ValueError("an MXFP4 matrix of %d columns has codes [rows, %d] and scales [rows, %d]"
                          % (cols, P // 2, P // 32))
-    steps = _empty((P // 128, rows, 64), torch.uint8, q.device)
-    words = _empty((P // 128, rows), torch.int32, q.device)
+    steps = _empty((P // 128, rows, 64), torch.uint8, q.device, stream)
+    words = _empty((P // 128, rows), torch.int32, q.device, stream)
     st = lib.moe_mxfp4_lay_out(_dev(q, "q", torch.uint8), _dev(scales, "scales", torch.uint8), rows, cols,
                                _dev(steps, "step_codes"), _dev(words, "step_scales"), _stream(stream))
     _check("moe_mxfp4_lay_out", st)
@@ -715,10 +731,10 @@ def moe_grouped_ffn_mxfp4(x: torch.Tensor, group_offsets: torch.Tensor, weights:
     rows = n_shared * T + cap_rows
     _holds(row_token, "row_token", rows)
     if y_perm is None:
-        y_perm = _empty((max(rows, 1), d), x.dtype, x.device)
+        y_perm = _empty((max(rows, 1), d), x.dtype, x.device, stream)
     _holds(y_perm, "y_perm", rows, d)
     if ws is None:
-        ws = workspace(moe_grouped_ffn_mxfp4_ws_bytes(T, rows, d, f, len(weights)), x.device)
+        ws = workspace(moe_grouped_ffn_mxfp4_ws_bytes(T, rows, d, f, len(weights)), x.device, stream)
     st = lib.moe_grouped_ffn_mxfp4(
         _dev(x, "x"), T, _dev(row_token, "row_token", torch.int32),
         _dev(group_offsets, "group_offsets", torch.int32), n_groups, n_shared, *weights.pointers,
@@ -748,12 +764,13 @@ def moe_combine_backward(dy: torch.Tensor, y_perm: Optional[torch.Tensor], token
     _same(topk_gate, "topk_gate", torch.float32, T, k)
     if y_perm is not None and (y_perm.dtype != dy.dtype or y_perm.dim() != 2 or y_perm.shape[1] != d):
         raise ValueError("y_perm must be [rows, d] of dy's dtype")
+    like = _of(stream, torch.empty_like)                 # (quicker than by a shape)
     if want_dy_perm and dy_perm is None:
         if y_perm is None:
             raise ValueError("dy_perm's rows are y_perm's: give one of them")
-        dy_perm = torch.empty_like(y_perm)               # (quicker than by a shape)
+        dy_perm = like(y_perm)
     if want_dgate and dgate is None:
-        dgate = dy.new_empty(T, k, dtype=torch.float32) if topk_gate is None else torch.empty_like(topk_gate)
+        dgate = _empty((T, k), torch.float32, dy.device, stream) if topk_gate is None else like(topk_gate)
     if dy_perm is not None and (dy_perm.dtype != dy.dtype or dy_perm.dim() != 2 or dy_perm.shape[1] != d):
         raise ValueError("dy_perm must be [rows, d] of dy's dtype")
     if dy_perm is not None and y_perm is not None and dy_perm.shape[0] < y_perm.shape[0]:
@@ -774,7 +791,8 @@ def moe_permute_backward(dx_perm: torch.Tensor, token_row: torch.Tensor, *,
     d = dx_perm.shape[1]
     T, k = token_row.shape
     if dx is None:
-        dx = dx_perm.new_empty(T, d) if dx_add is None else torch.empty_like(dx_add)
+        dx = (_of(stream, dx_perm.new_empty)(T, d) if dx_add is None
+              else _of(stream, torch.empty_like)(dx_add))
     _same(dx_add, "dx_add", dx_perm.dtype, T, d)
     _same(dx, "dx", dx_perm.dtype, T, d)
     st = lib.moe_permute_backward(_dev(dx_perm, "dx_perm"), _dtype_code(dx_perm),
@@ -810,21 +828,22 @@ def moe_route_topk_backward(dgate: torch.Tensor, topk_gate: torch.Tensor, topk_i
     _same(topk_gate, "topk_gate", f32, T, k)
     _same(topk_idx, "topk_idx", torch.int32, T, k)
     _same(logits, "logits", f32, T, E)
+    like, new = _of(stream, torch.empty_like), _of(stream, dgate.new_empty)
     if want_dlogits and dlogits is None:
-        dlogits = dgate.new_empty(T, E)
+        dlogits = new(T, E)
     if want_dx and dx is None:
-        dx = torch.empty_like(x)
+        dx = like(x)
     if want_dw and dw is None:
-        dw = torch.empty_like(w_router, dtype=f32)
+        dw = like(w_router, dtype=f32)
     if want_dbias and dbias is None:
-        dbias = dgate.new_empty(E)
+        dbias = new(E)
     _same(dlogits, "dlogits", f32, T, E)
     _same(dx, "dx", x.dtype, T, d)
     _same(dw, "dw", f32, E, d)
     _same(dbias, "dbias", f32, E)
     dtype, flags = _dtype_code(x), MOE_RENORM if renorm else 0
     if ws is None:
-        ws = workspace(moe_route_topk_backward_ws_bytes(dtype, T, d, E, k, flags), x.device)
+        ws = workspace(moe_route_topk_backward_ws_bytes(dtype, T, d, E, k, flags), x.device, stream)
     st = lib.moe_route_topk_backward(
         _dev(dgate, "dgate"), _dev(topk_gate, "topk_gate"), _dev(topk_idx, "topk_idx"),
         None if renorm else _dev(logits, "logits"), _dev(x, "x"), _dev(w_router, "w_router"), dtype, T,
