@@ -171,11 +171,9 @@ def _stream(stream):
 
 
 def _of(stream, make):
-    """`make`, which allocates a tensor, for a call on this stream (None: the current one): in
-    that stream's memory, so that nothing queued on another stream still uses it, and what the
-    call drops is used again only behind the call."""
-    if stream is None:
-        return make
+    """`make`, which allocates a tensor, for a call on this stream: in that stream's memory, so
+    that nothing queued on another stream still uses it, and what the call drops is used again
+    only behind the call."""
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
@@ -186,7 +184,8 @@ def _of(stream, make):
 
 
 def _empty(shape, dtype, device, stream=None):
-    return _of(stream, torch.empty)(shape, dtype=dtype, device=device)
+    make = torch.empty if stream is None else _of(stream, torch.empty)
+    return make(shape, dtype=dtype, device=device)
 
 
 def moe_route_topk(x: Optional[torch.Tensor], w_router: Optional[torch.Tensor],
@@ -309,7 +308,8 @@ def moe_grouped_ffn_ws_bytes(dtype: int, cap_rows: int, d: int, f: int, n_groups
 def workspace(nbytes: int, device, stream=None) -> torch.Tensor:
     """A 256-byte aligned device workspace (torch's caching allocator aligns to 512 B) for calls
     on this stream (None: the current one)."""
-    ws = _empty((max(int(nbytes), 256),), torch.uint8, device, stream)
+    make = torch.empty if stream is None else _of(stream, torch.empty)
+    ws = make(max(int(nbytes), 256), dtype=torch.uint8, device=device)
     assert ws.data_ptr() % 256 == 0
     return ws
 
@@ -764,7 +764,8 @@ def moe_combine_backward(dy: torch.Tensor, y_perm: Optional[torch.Tensor], token
     _same(topk_gate, "topk_gate", torch.float32, T, k)
     if y_perm is not None and (y_perm.dtype != dy.dtype or y_perm.dim() != 2 or y_perm.shape[1] != d):
         raise ValueError("y_perm must be [rows, d] of dy's dtype")
-    like = _of(stream, torch.empty_like)                 # (quicker than by a shape)
+    # (quicker than by a shape)
+    like = torch.empty_like if stream is None else _of(stream, torch.empty_like)
     if want_dy_perm and dy_perm is None:
         if y_perm is None:
             raise ValueError("dy_perm's rows are y_perm's: give one of them")
@@ -791,8 +792,8 @@ def moe_permute_backward(dx_perm: torch.Tensor, token_row: torch.Tensor, *,
     d = dx_perm.shape[1]
     T, k = token_row.shape
     if dx is None:
-        dx = (_of(stream, dx_perm.new_empty)(T, d) if dx_add is None
-              else _of(stream, torch.empty_like)(dx_add))
+        like = torch.empty_like if stream is None else _of(stream, torch.empty_like)
+        dx = _empty((T, d), dx_perm.dtype, dx_perm.device, stream) if dx_add is None else like(dx_add)
     _same(dx_add, "dx_add", dx_perm.dtype, T, d)
     _same(dx, "dx", dx_perm.dtype, T, d)
     st = lib.moe_permute_backward(_dev(dx_perm, "dx_perm"), _dtype_code(dx_perm),
@@ -828,7 +829,9 @@ def moe_route_topk_backward(dgate: torch.Tensor, topk_gate: torch.Tensor, topk_i
     _same(topk_gate, "topk_gate", f32, T, k)
     _same(topk_idx, "topk_idx", torch.int32, T, k)
     _same(logits, "logits", f32, T, E)
-    like, new = _of(stream, torch.empty_like), _of(stream, dgate.new_empty)
+    like, new = torch.empty_like, dgate.new_empty
+    if stream is not None:
+        like, new = _of(stream, like), _of(stream, new)
     if want_dlogits and dlogits is None:
         dlogits = new(T, E)
     if want_dx and dx is None:
