@@ -498,7 +498,8 @@ int moe_quantize_mxfp4(const void* x, int dtype, int64_t rows, int cols, uint8_t
 /*
  * moe_dequantize_mxfp4 -- the values an MXFP4 matrix holds: y[r][c] = E2M1(code) *
  * 2^(b - 127), NaN where b = 255.  Exact in MOE_F32, and in MOE_BF16 for every value
- * above its subnormal range (rounded to nearest even there).
+ * above its subnormal range (rounded to nearest even there); values of 2^128 and more, which
+ * only scale bytes 253 and 254 reach and no quantization gives, are infinities.
  * codes, scales  device, as above;  y  device [rows][cols] of `dtype` output
  * Requirements as for moe_quantize_mxfp4.
  */
