@@ -69,7 +69,7 @@ __device__ __forceinline__ float swiglu(float a, float b) {
 
 // ---------------------------------------------------------------------------
 // Strips: groups of few rows, bound by the weight bytes (64 Mixtral-shaped tokens, the FFN of
-// two experts: 52 us, 188 MB at 3.6 TB/s; of that gate/up 30 us at 4.2).  A workgroup holds 16 TILES weight
+// two experts: 51 us, 188 MB at 3.7 TB/s; of that gate/up 30 us at 4.2).  A workgroup holds 16 TILES weight
 // rows of one group (of gate/up half gate rows, half the same up rows: TILES = 4 makes 32
 // hidden columns, one MXFP4 block) over all of K, its W waves taking every W-th step: a
 // weight byte goes from memory to the registers of the one wave that multiplies it, and no
@@ -348,8 +348,8 @@ __global__ __launch_bounds__(64 * W, QUANT ? 3 : MAX_MS == 1 ? 4 : 2) void strip
 // MXFP4 block of h, or two 16-byte stores of y.
 //
 // 4096 Mixtral-shaped tokens (3254 rows of two experts): gate/up 206 us, down 100, 3.7 and 3.8
-// PFLOP/s; the matrix units are busy 47 % of the clocks, and the clock falls to 1.9 GHz under
-// the power limit: runs with half the scalar instructions, or with a seventh fewer waits, took
+// PFLOP/s; the matrix units are busy 47 and 44 % of the clocks, and the clock falls to 1.9 and
+// 2.1 GHz under the power limit: runs with half the scalar instructions, or with a seventh fewer waits, took
 // the same time at another clock.
 constexpr int TILE_LIST = 32;                            // tile records kept, in two halves
 
@@ -871,7 +871,8 @@ int launch_strips(MxArgs& p, int64_t max_rows, int cus, hipStream_t s) {
 constexpr int64_t STRIP_MAX_ROWS = 128;
 
 // Tiles of 256 x 256 from this many outputs of a product (a round of them over the chip), of
-// 128 x 128 below (FFN, all of one size: Mixtral-shaped, 400 tokens 103 and 87 us, 1500 tokens
+// 128 x 128 below, counted over the rows that the call has room for: how many there are only
+// the GPU knows (FFN, all of one size: Mixtral-shaped, 400 tokens 103 and 87 us, 1500 tokens
 // 162 and 194; DeepSeek-V2-Lite on one of eight, 512 tokens 29 and 24, 2048 tokens 38 and 41,
 // 8192 tokens 90 and 114.  777 Mixtral-shaped tokens, where the products differ: 124 and 121,
 // by the rule 104).

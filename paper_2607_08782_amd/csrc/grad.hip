@@ -325,8 +325,9 @@ __device__ __forceinline__ bf16x8 column(const u32x4 (&row)[8], int c) {
 // multiplies.  Eight waves: all blocks of 32 experts (1 to 8), which read x's rows together,
 // and tokens among the rest; a workgroup takes one chunk of the tokens, its waves' sums meet
 // in LDS in a fixed tree, and the chunks' in sum_parts_kernel in order.  16384 tokens of
-// Qwen3-30B-A3B (d = 2048, 128 experts): 33 us and 4 for the sum, where x is 67 MB (13 us);
-// matrix units busy 30 %, vector units with the terms and transposes as much.  Not kept: x
+// Qwen3-30B-A3B (d = 2048, 128 experts): 31 us and 4 for the sum, where x is 67 MB (13 us);
+// with dx in the same launch the matrix units are busy 30 % of the clocks, and the terms and
+// transposes take 4.4 vector instructions a matrix one, about as long.  Not kept: x
 // through a ring in LDS (36 -> 39 us), a second step of operands in registers (33 -> 34).
 constexpr int DW_THREADS = 512;
 constexpr int DW_COLS = 128;
@@ -555,7 +556,7 @@ __global__ __launch_bounds__(256) void sum_parts_kernel(Parts a, Parts b, int n)
 // of a step, NC columns NC i .. each, and transposes them within the lane) and runs over
 // blocks of 16 tokens, whose dlogits come, in two bf16 terms (16 bits for an output of 8),
 // while the block before multiplies.  Its sums are NC consecutive columns of a row, stored
-// at once.  16384 tokens of Qwen3-30B-A3B: 25 us, of which writing dx takes 13 at the rate of
+// at once.  16384 tokens of Qwen3-30B-A3B: 26 us, of which writing dx takes 13 at the rate of
 // a copy.
 struct DxArgs {
     const float* dlogits;

@@ -23,7 +23,7 @@ branches.  The expert placement can be swapped between batches
 with 4-bit experts, whose table is made anew).
 
 With ``mxfp4=True`` the routed experts are held and multiplied in 4 bits
-(moe_grouped_ffn_mxfp4; a third of a decode step's weight bytes); shared experts
+(moe_grouped_ffn_mxfp4; 17/64 of a decode step's weight bytes); shared experts
 keep bf16 and their own call.  `backward` and `backward_rows` are the gradient of
 the layer around its experts: from the loss gradient of y to the expert outputs'
 and the router's, and from the packaged rows' back to X.
@@ -449,7 +449,8 @@ class LayerShare:
                      fp32, of the router
         (the shared experts' output has dy itself).  A token's gates depend on each other,
         so where its experts are on several GPUs dgate has to be summed over them before it
-        goes on: reduce_dgate(dgate), in place, on the current stream.
+        goes on: reduce_dgate(dgate), in place, on the current stream.  dx, dw and dbias are
+        then whole on each of them, not parts to be summed again.
 
         After a run(logits_in=...) the gates' gradient is taken at those scores (keep them until
         then where gates are not renormalised), and the router's as of scores X Wr^T + bias."""
@@ -484,7 +485,8 @@ class LayerShare:
         """Enqueue the gradient of the packaging: dx [T, d] (None: a new tensor) = the sum of
         each token's rows of dx_perm, the gradient of the packaged rows, on top of `backward`'s
         dx, if there was one since the last run (by the calls made or captured last: a graph's
-        replays are not seen here)."""
+        replays are not seen here).  Where experts are on several GPUs the rows' part is summed
+        over these, and that dx, whole on each, belongs to the sum once."""
         self._needs_row_maps("backward_rows")
         add = self._grads["dx"] if self._grads_current else None
         return moe.moe_permute_backward(dx_perm, self.perm["token_row"], dx_add=add, dx=dx)
