@@ -777,7 +777,9 @@ def moe_combine_backward(dy: torch.Tensor, y_perm: Optional[torch.Tensor], token
     if dy_perm is not None and y_perm is not None and dy_perm.shape[0] < y_perm.shape[0]:
         raise ValueError("dy_perm must hold y_perm's rows")
     _same(dgate, "dgate", torch.float32, T, k)
-    st = lib.moe_combine_backward(_dev(dy, "dy"), _dev(y_perm, "y_perm"), _dtype_code(dy),
+    # no rows have no address: any stands for one that no token_row leads to
+    at_rows = _dev(y_perm, "y_perm") or (None if y_perm is None else dy.data_ptr())
+    st = lib.moe_combine_backward(_dev(dy, "dy"), at_rows, _dtype_code(dy),
                                   _dev(token_row, "token_row", torch.int32), _dev(topk_gate, "topk_gate"),
                                   T, d, k, _dev(dy_perm, "dy_perm"), _dev(dgate, "dgate"), _stream(stream))
     _check("moe_combine_backward", st)
@@ -796,7 +798,8 @@ def moe_permute_backward(dx_perm: torch.Tensor, token_row: torch.Tensor, *,
         dx = _empty((T, d), dx_perm.dtype, dx_perm.device, stream) if dx_add is None else like(dx_add)
     _same(dx_add, "dx_add", dx_perm.dtype, T, d)
     _same(dx, "dx", dx_perm.dtype, T, d)
-    st = lib.moe_permute_backward(_dev(dx_perm, "dx_perm"), _dtype_code(dx_perm),
+    at_rows = _dev(dx_perm, "dx_perm") or dx.data_ptr()  # (as moe_combine_backward)
+    st = lib.moe_permute_backward(at_rows, _dtype_code(dx_perm),
                                   _dev(token_row, "token_row", torch.int32), _dev(dx_add, "dx_add"),
                                   T, d, k, _dev(dx, "dx"), _stream(stream))
     _check("moe_permute_backward", st)
