@@ -633,6 +633,203 @@ int moe_route_topk_backward(const float* dgate, const float* topk_gate, const in
                             int64_t T, int d, int E, int k, int flags, float* dlogits, void* dx,
                             float* dw, float* dbias, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * Rows in 8-bit integers: a matrix of `cols` columns as
+ *   q       int8 [rows][MOE_INT8_COLS(cols)]: codes -127 .. 127, the padding zero
+ *   scales  float [rows]: value = q * scale
+ * The scale belongs to a token where the rows are activations, to an output channel where they
+ * are a weight matrix's.
+ */
+#define MOE_INT8_COLS(cols) (((int64_t)(cols) + 127) / 128 * 128)
+
+/*
+ * moe_quantize_int8 -- a matrix to 8-bit rows.  For every row r:
+ *
+ *   scales[r] = max(max_i |x[r][i]| / 127, 2^-126)      (fp32 division)
+ *   q[r][i]   = x[r][i] / scales[r]                     (fp32 division, then rounded to a
+ *                                                        whole number, ties to even)
+ *
+ * A row that holds an infinity or a NaN gets scale NaN and zero codes: all of it reads as
+ * NaN, and no other row does.
+ * x       device [rows][cols] of `dtype` (MOE_F32 or MOE_BF16)
+ * q, scales  device outputs as above, q 16-byte and scales 4-byte aligned
+ * Requires rows >= 0, 1 <= cols < 2^28 (else MOE_ERR_SHAPE).  Results are exact (bitwise
+ * reproducible).
+ */
+int moe_quantize_int8(const void* x, int dtype, int64_t rows, int cols, int8_t* q, float* scales,
+                      void* stream);
+
+/*
+ * moe_dequantize_int8 -- the values that 8-bit rows hold: y[r][c] = q[r][c] * scales[r] (the
+ * fp32 product, rounded to `dtype`).
+ * q, scales  device, as above;  y  device [rows][cols] of `dtype` output
+ * Requirements as for moe_quantize_int8.
+ */
+int moe_dequantize_int8(const int8_t* q, const float* scales, int64_t rows, int cols, int dtype,
+                        void* y, void* stream);
+
+/* Workspace bytes moe_grouped_ffn_int8 needs (all groups together n_groups, rows of every group,
+ * shared ones included, at most cap_rows). */
+size_t moe_grouped_ffn_int8_ws_bytes(int64_t cap_rows, int d, int f, int n_groups);
+
+/*
+ * moe_grouped_ffn_int8 -- moe_grouped_ffn of experts whose weights are 8-bit rows, over token rows
+ * in 8 bits: both products multiply 8-bit integers, a scale for each token and each output
+ * channel, and the hidden rows are quantized between them:
+ *
+ *   for each group s and row p of it, with x the 8-bit row xq[row_token[p]] of scale sx:
+ *     a = (W1_s x) sx s13_s[.],  b = (W3_s x) sx s13_s[f + .]     (whole sums, then fp32)
+ *     h = SiLU(a) * b                                              (rounded to bf16)
+ *     hq, sh = h as moe_quantize_int8 keeps it
+ *     y_perm[p] = (W2_s hq) sh s2_s[.]                             (fp32, stored in bf16)
+ *
+ * xq, x_scale  device [T][MOE_INT8_COLS(d)] and [T]: token rows (moe_quantize_int8, moe_rmsnorm)
+ * row_token  device [n_shared T + cap_rows] int32, as for moe_grouped_ffn_rows_shared (entries of
+ *            rows that exist lie in [0, T)); NULL: row p reads xq[p]
+ * group_offsets, n_groups, n_shared, cap_rows, y_perm  as for moe_grouped_ffn_rows_shared:
+ *            n_shared leading groups of T rows each (0 without row_token); y_perm in bf16
+ * w13, s13   HOST arrays of n_shared + n_groups device pointers: codes [2f][MOE_INT8_COLS(d)] and
+ *            scales [2f], rows 0..f-1 W1 (gate), f..2f-1 W3 (up)
+ * w2, s2     the same of [d][MOE_INT8_COLS(f)] and [d]
+ * ws         moe_grouped_ffn_int8_ws_bytes(n_shared T + cap_rows, d, f, n_shared + n_groups)
+ *            bytes, 256-byte aligned
+ * The sums of products are exact.  A token whose scale is NaN makes its own rows of y_perm NaN and
+ * no other; so does a row whose h overflows bf16.  Codes may be any of -128 .. 127; padding
+ * columns must be zero in one of each product's operands.  Deterministic.
+ * Requires d % 8 == 0, d and f at most 2^17, and T * MOE_INT8_COLS(d), 2 f * MOE_INT8_COLS(d)
+ * and d * MOE_INT8_COLS(f) below 2^31 (else MOE_ERR_SHAPE), 1 <= n_shared + n_groups <=
+ * MOE_MAX_GROUPS, codes and y_perm 16-byte, scales 4-byte aligned.
+ */
+int moe_grouped_ffn_int8(const int8_t* xq, const float* x_scale, int64_t T, const int32_t* row_token,
+                         const int32_t* group_offsets, int n_groups, int n_shared,
+                         const int8_t* const* w13, const float* const* s13, const int8_t* const* w2,
+                         const float* const* s2, int d, int f, int64_t cap_rows, void* y_perm,
+                         void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * moe_rmsnorm -- the root-mean-square norm in front of a layer, with the residual's addition
+ * before and the normed rows in 8 bits beside:
+ *
+ *   h[t] = x[t] + residual[t]              (fp32, rounded to `dtype`; x[t] without residual)
+ *   rstd[t] = 1 / sqrt(mean_i h[t][i]^2 + eps)
+ *   y[t][i] = h[t][i] * rstd[t] * weight[i]              (fp32, rounded to `dtype`)
+ *   q[t], scales[t] = y[t], as rounded, as moe_quantize_int8 keeps it (bit for bit)
+ *
+ * x        device [T][d] of `dtype`;  residual  device [T][d] of `dtype`, nullable
+ * weight   device [d] of `dtype`
+ * h        device [T][d] of `dtype` output, required with a residual and not written without
+ *          one; may be x or residual
+ * y        device [T][d] of `dtype` output, nullable; may be x or residual, where h is not the same
+ * rstd     device [T] float output, nullable (moe_rmsnorm_backward reads it)
+ * q, scales  device [T][MOE_INT8_COLS(d)] and [T] outputs, nullable together
+ * Apart from these, outputs must not overlap inputs or each other.
+ * A row that is not finite makes its own outputs NaN or infinite, and no other row's.  A row of
+ * zeros gives zeros (with eps > 0).  Sums are fp32 in a fixed order (deterministic).
+ * Requires T >= 0, 1 <= d < 2^22 (else MOE_ERR_SHAPE), eps >= 0 and finite, q 16-byte aligned.
+ */
+int moe_rmsnorm(const void* x, const void* residual, int dtype, const void* weight, float eps, int64_t T,
+                int d, void* h, void* y, float* rstd, int8_t* q, float* scales, void* stream);
+
+/* Workspace bytes moe_rmsnorm_backward needs for dw. */
+size_t moe_rmsnorm_backward_ws_bytes(int dtype, int64_t T, int d);
+
+/*
+ * moe_rmsnorm_backward -- gradient of moe_rmsnorm's y: from dy, the loss gradient of y, to h (whose
+ * gradient is x's and the residual's alike) and to the weight, with n = h rstd:
+ *
+ *   dh[t][i] = rstd[t] (dy[t][i] weight[i] - n[t][i] mean_j(dy[t][j] weight[j] n[t][j])) + dh_add[t][i]
+ *   dw[i]    = sum_t dy[t][i] n[t][i]                     (fp32)
+ *
+ * dy, h    device [T][d] of `dtype`;  weight  device [d] of `dtype`;  rstd  device [T] float
+ * dh_add   device [T][d] of `dtype`, nullable: what reaches h another way (the residual stream)
+ * dh       device [T][d] of `dtype` output, nullable (fp32, then stored; may be dh_add)
+ * dw       device [d] float output, nullable (zeros when T = 0)
+ * ws       moe_rmsnorm_backward_ws_bytes(dtype, T, d) bytes, 256-byte aligned (may be NULL without dw)
+ * Apart from dh over dh_add, outputs must not overlap inputs or each other.  Sums are fp32 in a
+ * fixed order (deterministic).  Requires T >= 0, 1 <= d < 2^22 (else MOE_ERR_SHAPE).
+ */
+int moe_rmsnorm_backward(const void* dy, const void* h, int dtype, const void* weight, const float* rstd,
+                         const void* dh_add, int64_t T, int d, void* dh, float* dw, void* ws,
+                         size_t ws_bytes, void* stream);
+
+/* Workspace bytes moe_balance_loss needs. */
+size_t moe_balance_loss_ws_bytes(int64_t T, int E);
+
+/*
+ * moe_balance_loss -- how far a batch's routing is from even (the popularity skew of Sec. III,
+ * Finding 1, as the loss that training holds it down with), with the counts behind it: over the
+ * n tokens that count, p[t] = softmax(logits[t]),
+ *
+ *   n_tokens = #{t : mask[t] != 0}
+ *   counts[e] = #{(t, r) : mask[t] != 0, topk_idx[t][r] == e}
+ *   prob_sum[e] = sum_{t : mask[t] != 0} p[t][e]
+ *   loss = E sum_e (counts[e] / (k n_tokens)) (prob_sum[e] / n_tokens)      (1 when even)
+ *
+ * logits    device [T][E] float, as moe_route_topk leaves them
+ * topk_idx  device [T][k] int32, values in [0, E)
+ * mask      device [T] bytes, nullable (every token counts).  Where it is 0 (the padding of a
+ *           batch) logits and topk_idx are not read.
+ * counts    device [E] int32, prob_sum  device [E] float, n_tokens  device [1] int32,
+ * loss      device [1] float: outputs (all zero when no token counts).  counts, prob_sum and
+ *           n_tokens may be summed over GPUs for the loss, and its gradient, of all their tokens.
+ * ws        moe_balance_loss_ws_bytes(T, E) bytes, 256-byte aligned
+ * A score of -infinity leaves its expert out (p = 0); a counted token needs one finite score.
+ * Sums have a fixed order (deterministic).  Requires 0 <= T, T * k < 2^31, 1 <= E <= MOE_MAX_E,
+ * 1 <= k <= min(E, MOE_MAX_K).
+ */
+int moe_balance_loss(const float* logits, const int32_t* topk_idx, const uint8_t* mask, int64_t T, int E,
+                     int k, int32_t* counts, float* prob_sum, int32_t* n_tokens, float* loss, void* ws,
+                     size_t ws_bytes, void* stream);
+
+/*
+ * moe_balance_loss_backward -- gradient of moe_balance_loss to the gate scores (the counts are
+ * constants: the choice of experts has no gradient), times `scale`:
+ *
+ *   dlogits[t][e] = scale E / (k n_tokens^2) p[t][e] (counts[e] - sum_e' p[t][e'] counts[e'])
+ *
+ * and 0 where mask[t] is 0.
+ * logits, mask, counts, n_tokens  device, as above (counts and n_tokens this batch's, or the sums
+ *           over several GPUs' batches)
+ * dlogits   device [T][E] float output; may be logits
+ * Requirements as for moe_balance_loss.
+ */
+int moe_balance_loss_backward(const float* logits, const uint8_t* mask, const int32_t* counts,
+                              const int32_t* n_tokens, int64_t T, int E, int k, float scale,
+                              float* dlogits, void* stream);
+
+/* Workspace bytes moe_grad_norm needs (sizes: HOST [n], elements of each gradient). */
+size_t moe_grad_norm_ws_bytes(const int64_t* sizes, int n);
+
+/*
+ * moe_grad_norm -- the Euclidean norm over all elements of n tensors together:
+ *
+ *   norm = sqrt(sum_i sum_j grads[i][j]^2)
+ *
+ * grads     HOST array of n device pointers;  sizes  HOST [n], their elements (0 allowed)
+ * dtypes    HOST [n], MOE_F32 or MOE_BF16
+ * norm      device [1] float output (0 when there are no elements)
+ * ws        moe_grad_norm_ws_bytes(sizes, n) bytes, 256-byte aligned
+ * Squares and sums are in 64 bits, in a fixed order (deterministic).  An infinity gives an
+ * infinite norm, a NaN a NaN.
+ */
+int moe_grad_norm(const void* const* grads, const int64_t* sizes, const int* dtypes, int n, float* norm,
+                  void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * moe_clip_grads -- the same tensors scaled down to a largest norm:
+ *
+ *   factor = 1 if norm <= max_norm else max_norm / norm   (fp32 division)
+ *   out[i][j] = grads[i][j] * factor                      (fp32, rounded to the tensor's type)
+ *
+ * norm      device [1] float (moe_grad_norm's, or that over several GPUs' tensors)
+ * out       HOST array of n device pointers; out[i] may be grads[i], and then nothing is read or
+ *           written where the factor is 1.  No other overlap.
+ * A NaN norm makes every element NaN, an infinite one makes finite elements zero.
+ * Requires max_norm >= 0.
+ */
+int moe_clip_grads(const void* const* grads, const int64_t* sizes, const int* dtypes, int n,
+                   const float* norm, float max_norm, void* const* out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

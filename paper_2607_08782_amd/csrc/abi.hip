@@ -4,6 +4,7 @@
 #include <string.h>
 
 #include "common.h"
+#include "int8.h"
 #include "mxfp4.h"
 
 namespace {
@@ -524,6 +525,203 @@ int moe_route_topk_backward(const float* dgate, const float* topk_gate, const in
         return MOE_ERR_SHAPE;
     return launch_route_backward(dgate, topk_gate, topk_idx, logits, x, w_router, dtype, T, d, E, k,
                                  flags, dlogits, dx, dw, dbias, ws, (hipStream_t)stream);
+}
+
+}  // extern "C"
+
+namespace {
+
+// Validation of the two conversions between a matrix m and 8-bit rows.
+int int8_check(const void* m, int dtype, int64_t rows, int cols, const int8_t* q, const float* scales) {
+    if (dtype != MOE_F32 && dtype != MOE_BF16) return MOE_ERR_ARG;
+    if (rows < 0 || cols < 1) return MOE_ERR_ARG;
+    // a value's place in its row is a 32-bit number; 2^44 values lie past any memory
+    if (cols >= 1 << 28 || rows > (int64_t)0x7fffffff * 8192 / int8_cols(cols)) return MOE_ERR_SHAPE;
+    if (rows > 0 && (!m || !q || !scales)) return MOE_ERR_ARG;
+    if (((uintptr_t)m & (dtype == MOE_BF16 ? 1u : 3u)) || !aligned16(q) || !aligned4(scales))
+        return MOE_ERR_ARG;
+    return MOE_OK;
+}
+
+// Sizes of a call over rows of hidden values.
+int norm_check(int dtype, int64_t T, int d) {
+    if (dtype != MOE_F32 && dtype != MOE_BF16) return MOE_ERR_ARG;
+    if (T < 0 || d < 1) return MOE_ERR_ARG;
+    if (T > 0x7fffffff || d >= 1 << 22) return MOE_ERR_SHAPE;
+    return MOE_OK;
+}
+
+bool element_aligned(const void* p, int dtype) {
+    return ((uintptr_t)p & (dtype == MOE_BF16 ? 1u : 3u)) == 0;
+}
+
+// Sizes of a call over gate scores.
+int balance_check(int64_t T, int E, int k) {
+    if (T < 0 || E < 1 || E > MOE_MAX_E || k < 1 || k > MOE_MAX_K || k > E) return MOE_ERR_ARG;
+    return T * (int64_t)k > 0x7fffffff || T > 0x7fffffff ? MOE_ERR_ARG : MOE_OK;
+}
+
+// A list of gradients.
+int grads_check(const void* const* grads, const int64_t* sizes, const int* dtypes, int n) {
+    if (n < 0 || (n > 0 && (!grads || !sizes || !dtypes))) return MOE_ERR_ARG;
+    for (int i = 0; i < n; ++i) {
+        if (dtypes[i] != MOE_F32 && dtypes[i] != MOE_BF16) return MOE_ERR_ARG;
+        if (sizes[i] < 0 || (sizes[i] > 0 && !grads[i]) || !element_aligned(grads[i], dtypes[i]))
+            return MOE_ERR_ARG;
+        if (sizes[i] > (int64_t)1 << 44) return MOE_ERR_SHAPE;
+    }
+    return MOE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int moe_quantize_int8(const void* x, int dtype, int64_t rows, int cols, int8_t* q, float* scales,
+                      void* stream) {
+    const int st = int8_check(x, dtype, rows, cols, q, scales);
+    if (st != MOE_OK) return st;
+    return launch_quantize_int8(x, dtype, rows, cols, cols, q, scales, nullptr, 0, (hipStream_t)stream);
+}
+
+int moe_dequantize_int8(const int8_t* q, const float* scales, int64_t rows, int cols, int dtype,
+                        void* y, void* stream) {
+    const int st = int8_check(y, dtype, rows, cols, q, scales);
+    if (st != MOE_OK) return st;
+    return launch_dequantize_int8(q, scales, rows, cols, dtype, y, (hipStream_t)stream);
+}
+
+size_t moe_grouped_ffn_int8_ws_bytes(int64_t cap_rows, int d, int f, int n_groups) {
+    if (cap_rows < 0 || d < 1 || f < 1 || n_groups < 0) return 0;
+    return grouped_ffn_int8_ws_bytes(cap_rows, f);
+}
+
+int moe_grouped_ffn_int8(const int8_t* xq, const float* x_scale, int64_t T, const int32_t* row_token,
+                         const int32_t* group_offsets, int n_groups, int n_shared,
+                         const int8_t* const* w13, const float* const* s13, const int8_t* const* w2,
+                         const float* const* s2, int d, int f, int64_t cap_rows, void* y_perm,
+                         void* ws, size_t ws_bytes, void* stream) {
+    if (n_shared < 0 || n_groups < 0 || n_shared > MOE_MAX_GROUPS || n_groups > MOE_MAX_GROUPS)
+        return MOE_ERR_ARG;
+    const int groups = n_shared + n_groups;
+    if (T < 0 || groups < 1 || groups > MOE_MAX_GROUPS || d < 1 || f < 1 || cap_rows < 0)
+        return MOE_ERR_ARG;
+    if (n_shared > 0 && (T < 1 || !row_token)) return MOE_ERR_ARG;
+    // every row, shared and routed, has a 32-bit row index
+    if (T > 0x7fffffff || cap_rows > 0x7fffffff || (int64_t)n_shared * T > 0x7fffffffLL - cap_rows)
+        return MOE_ERR_ARG;
+    const int64_t rows = (int64_t)n_shared * T + cap_rows;
+    if (!group_offsets || !w13 || !s13 || !w2 || !s2) return MOE_ERR_ARG;
+    for (int g = 0; g < groups; ++g) {
+        if (!w13[g] || !s13[g] || !w2[g] || !s2[g]) return MOE_ERR_ARG;
+        if (!aligned16(w13[g]) || !aligned16(w2[g]) || !aligned4(s13[g]) || !aligned4(s2[g]))
+            return MOE_ERR_ARG;
+    }
+    if (rows > 0 && (!y_perm || (T > 0 && (!xq || !x_scale)))) return MOE_ERR_ARG;
+    if (!aligned16(xq) || !aligned4(x_scale) || !aligned16(y_perm)) return MOE_ERR_ARG;
+    // sums of 2^17 products are exact; rows of codes are reached through 32-bit offsets
+    if (d % 8 || d > INT8_MAX_K || f > INT8_MAX_K) return MOE_ERR_SHAPE;
+    const int64_t reach = 0x7fffffff;
+    if (T * int8_cols(d) > reach || 2 * (int64_t)f * int8_cols(d) > reach || d * int8_cols(f) > reach)
+        return MOE_ERR_SHAPE;
+    // without a row map the rows are xq's own
+    if (!row_token && T < cap_rows) return MOE_ERR_SHAPE;
+    if (rows > 0 && (!ws || ws_bytes < grouped_ffn_int8_ws_bytes(rows, f) || ((uintptr_t)ws & 255u)))
+        return MOE_ERR_SHAPE;
+    return launch_grouped_ffn_int8(xq, x_scale, T, row_token, group_offsets, groups, n_shared, (int)T, w13,
+                                   s13, w2, s2, d, f, rows, y_perm, ws, (hipStream_t)stream);
+}
+
+int moe_rmsnorm(const void* x, const void* residual, int dtype, const void* weight, float eps, int64_t T,
+                int d, void* h, void* y, float* rstd, int8_t* q, float* scales, void* stream) {
+    const int st = norm_check(dtype, T, d);
+    if (st != MOE_OK) return st;
+    if (!(eps >= 0.0f) || eps > 3.0e38f) return MOE_ERR_ARG;
+    if (T > 0 && (!x || !weight || (residual && !h))) return MOE_ERR_ARG;
+    if ((q == nullptr) != (scales == nullptr)) return MOE_ERR_ARG;
+    // y of a row would be read as its sum, or overwrite it
+    if (y && y == h) return MOE_ERR_ARG;
+    for (const void* p : {x, residual, weight, (const void*)h, (const void*)y})
+        if (!element_aligned(p, dtype)) return MOE_ERR_ARG;
+    if (!aligned4(rstd) || !aligned16(q) || !aligned4(scales)) return MOE_ERR_ARG;
+    return launch_rmsnorm(x, residual, dtype, weight, eps, T, d, h, y, rstd, q, scales, (hipStream_t)stream);
+}
+
+size_t moe_rmsnorm_backward_ws_bytes(int dtype, int64_t T, int d) {
+    if (T < 0 || d < 1) return 0;
+    return rmsnorm_backward_ws_bytes(dtype, T, d);
+}
+
+int moe_rmsnorm_backward(const void* dy, const void* h, int dtype, const void* weight, const float* rstd,
+                         const void* dh_add, int64_t T, int d, void* dh, float* dw, void* ws,
+                         size_t ws_bytes, void* stream) {
+    const int st = norm_check(dtype, T, d);
+    if (st != MOE_OK) return st;
+    if (T > 0 && (!dy || !h || !weight || !rstd)) return MOE_ERR_ARG;
+    for (const void* p : {dy, h, weight, dh_add, (const void*)dh})
+        if (!element_aligned(p, dtype)) return MOE_ERR_ARG;
+    if (!aligned4(rstd) || !aligned4(dw)) return MOE_ERR_ARG;
+    if (dw && (!ws || ws_bytes < rmsnorm_backward_ws_bytes(dtype, T, d) || ((uintptr_t)ws & 255u)))
+        return MOE_ERR_SHAPE;
+    return launch_rmsnorm_backward(dy, h, dtype, weight, rstd, dh_add, T, d, dh, dw, ws, (hipStream_t)stream);
+}
+
+size_t moe_balance_loss_ws_bytes(int64_t T, int E) {
+    if (T < 0 || E < 1) return 0;
+    return balance_loss_ws_bytes(T, E);
+}
+
+int moe_balance_loss(const float* logits, const int32_t* topk_idx, const uint8_t* mask, int64_t T, int E,
+                     int k, int32_t* counts, float* prob_sum, int32_t* n_tokens, float* loss, void* ws,
+                     size_t ws_bytes, void* stream) {
+    const int st = balance_check(T, E, k);
+    if (st != MOE_OK) return st;
+    if (!counts || !prob_sum || !n_tokens || !loss || (T > 0 && (!logits || !topk_idx))) return MOE_ERR_ARG;
+    for (const void* p : {(const void*)logits, (const void*)topk_idx, (const void*)counts,
+                          (const void*)prob_sum, (const void*)n_tokens, (const void*)loss})
+        if (!aligned4(p)) return MOE_ERR_ARG;
+    if (!ws || ws_bytes < balance_loss_ws_bytes(T, E) || ((uintptr_t)ws & 255u)) return MOE_ERR_SHAPE;
+    return launch_balance_loss(logits, topk_idx, mask, T, E, k, counts, prob_sum, n_tokens, loss, ws,
+                               (hipStream_t)stream);
+}
+
+int moe_balance_loss_backward(const float* logits, const uint8_t* mask, const int32_t* counts,
+                              const int32_t* n_tokens, int64_t T, int E, int k, float scale,
+                              float* dlogits, void* stream) {
+    const int st = balance_check(T, E, k);
+    if (st != MOE_OK) return st;
+    if (T > 0 && (!logits || !counts || !n_tokens || !dlogits)) return MOE_ERR_ARG;
+    if (!aligned4(logits) || !aligned4(counts) || !aligned4(n_tokens) || !aligned4(dlogits))
+        return MOE_ERR_ARG;
+    return launch_balance_loss_backward(logits, mask, counts, n_tokens, T, E, k, scale, dlogits,
+                                        (hipStream_t)stream);
+}
+
+size_t moe_grad_norm_ws_bytes(const int64_t* sizes, int n) {
+    if (n < 0 || (n > 0 && !sizes)) return 0;
+    for (int i = 0; i < n; ++i)
+        if (sizes[i] < 0) return 0;
+    return (size_t)grad_chunks(sizes, n) * 8 + 256;
+}
+
+int moe_grad_norm(const void* const* grads, const int64_t* sizes, const int* dtypes, int n, float* norm,
+                  void* ws, size_t ws_bytes, void* stream) {
+    const int st = grads_check(grads, sizes, dtypes, n);
+    if (st != MOE_OK) return st;
+    if (!norm || !aligned4(norm)) return MOE_ERR_ARG;
+    if (!ws || ws_bytes < moe_grad_norm_ws_bytes(sizes, n) || ((uintptr_t)ws & 255u)) return MOE_ERR_SHAPE;
+    return launch_grad_norm(grads, sizes, dtypes, n, norm, ws, (hipStream_t)stream);
+}
+
+int moe_clip_grads(const void* const* grads, const int64_t* sizes, const int* dtypes, int n,
+                   const float* norm, float max_norm, void* const* out, void* stream) {
+    const int st = grads_check(grads, sizes, dtypes, n);
+    if (st != MOE_OK) return st;
+    if (n > 0 && (!norm || !aligned4(norm) || !out)) return MOE_ERR_ARG;
+    if (!(max_norm >= 0.0f)) return MOE_ERR_ARG;
+    for (int i = 0; i < n; ++i)
+        if ((sizes[i] > 0 && !out[i]) || !element_aligned(out[i], dtypes[i])) return MOE_ERR_ARG;
+    return launch_clip_grads(grads, sizes, dtypes, n, norm, max_norm, out, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -36,7 +36,12 @@ EXPORTS = ("moe_status_string", "moe_route_topk", "moe_route_topk_ws_bytes",
            "moe_quantize_mxfp4", "moe_dequantize_mxfp4", "moe_mxfp4_lay_out",
            "moe_grouped_ffn_mxfp4_ws_bytes", "moe_grouped_ffn_mxfp4",
            "moe_combine_backward", "moe_permute_backward", "moe_route_topk_backward_ws_bytes",
-           "moe_route_topk_backward")
+           "moe_route_topk_backward",
+           "moe_quantize_int8", "moe_dequantize_int8",
+           "moe_grouped_ffn_int8_ws_bytes", "moe_grouped_ffn_int8",
+           "moe_rmsnorm", "moe_rmsnorm_backward_ws_bytes", "moe_rmsnorm_backward",
+           "moe_balance_loss_ws_bytes", "moe_balance_loss", "moe_balance_loss_backward",
+           "moe_grad_norm_ws_bytes", "moe_grad_norm", "moe_clip_grads")
 
 _lib = None
 
@@ -114,6 +119,33 @@ def load_library(path: str = LIB_PATH):
     lib.moe_route_topk_backward_ws_bytes.restype = S
     lib.moe_route_topk_backward.argtypes = [P, P, P, P, P, P, I, L, I, I, I, I, P, P, P, P, P, S, P]
     lib.moe_route_topk_backward.restype = I
+    F = ctypes.c_float
+    lib.moe_quantize_int8.argtypes = [P, I, L, I, P, P, P]
+    lib.moe_quantize_int8.restype = I
+    lib.moe_dequantize_int8.argtypes = [P, P, L, I, I, P, P]
+    lib.moe_dequantize_int8.restype = I
+    lib.moe_grouped_ffn_int8_ws_bytes.argtypes = [L, I, I, I]
+    lib.moe_grouped_ffn_int8_ws_bytes.restype = S
+    lib.moe_grouped_ffn_int8.argtypes = [P, P, L, P, P, I, I, P, P, P, P, I, I, L, P, P, S, P]
+    lib.moe_grouped_ffn_int8.restype = I
+    lib.moe_rmsnorm.argtypes = [P, P, I, P, F, L, I, P, P, P, P, P, P]
+    lib.moe_rmsnorm.restype = I
+    lib.moe_rmsnorm_backward_ws_bytes.argtypes = [I, L, I]
+    lib.moe_rmsnorm_backward_ws_bytes.restype = S
+    lib.moe_rmsnorm_backward.argtypes = [P, P, I, P, P, P, L, I, P, P, P, S, P]
+    lib.moe_rmsnorm_backward.restype = I
+    lib.moe_balance_loss_ws_bytes.argtypes = [L, I]
+    lib.moe_balance_loss_ws_bytes.restype = S
+    lib.moe_balance_loss.argtypes = [P, P, P, L, I, I, P, P, P, P, P, S, P]
+    lib.moe_balance_loss.restype = I
+    lib.moe_balance_loss_backward.argtypes = [P, P, P, P, L, I, I, F, P, P]
+    lib.moe_balance_loss_backward.restype = I
+    lib.moe_grad_norm_ws_bytes.argtypes = [P, I]
+    lib.moe_grad_norm_ws_bytes.restype = S
+    lib.moe_grad_norm.argtypes = [P, P, P, I, P, P, S, P]
+    lib.moe_grad_norm.restype = I
+    lib.moe_clip_grads.argtypes = [P, P, P, I, P, F, P, P]
+    lib.moe_clip_grads.restype = I
     _lib = lib
     return lib
 
@@ -857,3 +889,306 @@ def moe_route_topk_backward(dgate: torch.Tensor, topk_gate: torch.Tensor, topk_i
         _dev(ws, "ws"), ws.numel(), _stream(stream))
     _check("moe_route_topk_backward", st)
     return dlogits, dx, dw, dbias
+
+
+def int8_cols(cols: int) -> int:
+    """Columns of an 8-bit row: `cols` padded to a multiple of 128 (MOE_INT8_COLS)."""
+    return (int(cols) + 127) // 128 * 128
+
+
+def moe_quantize_int8(x: torch.Tensor, *, q: Optional[torch.Tensor] = None,
+                      scales: Optional[torch.Tensor] = None, stream=None):
+    """The rows of x [rows, cols] in 8 bits.  Returns (codes int8 [rows, int8_cols(cols)], scales
+    float32 [rows])."""
+    lib = load_library()
+    rows, cols = x.shape
+    if q is None:
+        q = _empty((rows, int8_cols(cols)), torch.int8, x.device, stream)
+    if scales is None:
+        scales = _empty((rows,), torch.float32, x.device, stream)
+    _same(q, "q", torch.int8, rows, int8_cols(cols))
+    _same(scales, "scales", torch.float32, rows)
+    st = lib.moe_quantize_int8(_dev(x, "x"), _dtype_code(x), rows, cols, _dev(q, "q"), _dev(scales, "scales"),
+                               _stream(stream))
+    _check("moe_quantize_int8", st)
+    return q, scales
+
+
+def moe_dequantize_int8(q: torch.Tensor, scales: torch.Tensor, cols: int, *,
+                        dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
+                        stream=None) -> torch.Tensor:
+    """The values [rows, cols] that 8-bit rows hold, in `dtype` (float32 or bfloat16)."""
+    lib = load_library()
+    rows = q.shape[0]
+    if cols < 1:
+        raise ValueError("cols must be positive")
+    _same(q, "q", torch.int8, rows, int8_cols(cols))
+    _same(scales, "scales", torch.float32, rows)
+    if out is None:
+        out = _empty((rows, cols), dtype, q.device, stream)
+    _same(out, "out", dtype, rows, cols)
+    st = lib.moe_dequantize_int8(_dev(q, "q"), _dev(scales, "scales"), rows, cols, _dtype_code(out),
+                                 _dev(out, "out"), _stream(stream))
+    _check("moe_dequantize_int8", st)
+    return out
+
+
+class Int8WeightTable:
+    """Experts whose weights are 8-bit rows, as moe_grouped_ffn_int8 takes them: w13 and w2 hold one
+    (codes, scales) pair per group, as moe_quantize_int8 gives them for [2f, d] and [d, f]."""
+
+    def __init__(self, w13: Sequence, w2: Sequence, d: int, f: int):
+        if len(w13) != len(w2) or not len(w13):
+            raise ValueError("need one (w13, w2) pair per group")
+        self.d, self.f = int(d), int(f)
+        self.w13, self.w2 = [tuple(p) for p in w13], [tuple(p) for p in w2]
+        for pairs, rows, cols, name in ((self.w13, 2 * self.f, self.d, "w13"), (self.w2, self.d, self.f, "w2")):
+            for q, s in pairs:
+                _same(q, name + " codes", torch.int8, rows, int8_cols(cols))
+                _same(s, name + " scales", torch.float32, rows)
+                _dev(q, name + " codes")
+                _dev(s, name + " scales")
+        n = len(self.w13)
+        self._arrays = [(ctypes.c_void_p * n)(*[p[i].data_ptr() for p in pairs])
+                        for pairs in (self.w13, self.w2) for i in (0, 1)]
+        self.pointers = [ctypes.cast(a, ctypes.c_void_p) for a in self._arrays]
+
+    @classmethod
+    def quantized(cls, w13: Sequence[torch.Tensor], w2: Sequence[torch.Tensor]) -> "Int8WeightTable":
+        """The experts of a WeightTable (w13 [2f, d], w2 [d, f], bf16 or fp32), quantized."""
+        if not len(w13):
+            raise ValueError("need one (w13, w2) pair per group")
+        return cls([moe_quantize_int8(w) for w in w13], [moe_quantize_int8(w) for w in w2],
+                   w13[0].shape[1], w13[0].shape[0] // 2)
+
+    def __len__(self):
+        return len(self.w13)
+
+
+def moe_grouped_ffn_int8_ws_bytes(cap_rows: int, d: int, f: int, n_groups: int) -> int:
+    return int(load_library().moe_grouped_ffn_int8_ws_bytes(cap_rows, d, f, n_groups))
+
+
+def moe_grouped_ffn_int8(xq: torch.Tensor, x_scale: torch.Tensor, group_offsets: torch.Tensor,
+                         weights: Int8WeightTable, *, row_token: Optional[torch.Tensor] = None,
+                         n_shared: int = 0, cap_rows: Optional[int] = None,
+                         y_perm: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                         stream=None) -> torch.Tensor:
+    """SwiGLU FFN of every group in 8-bit integers; xq [T, int8_cols(d)] with x_scale [T], read
+    through row_token (as moe_grouped_ffn_rows_shared's, n_shared leading groups included) or,
+    without it, the packaged rows.  Returns y_perm [n_shared * T + cap_rows, d] bf16."""
+    lib = load_library()
+    T = xq.shape[0]
+    d, f = weights.d, weights.f
+    _same(xq, "xq", torch.int8, T, int8_cols(d))
+    _same(x_scale, "x_scale", torch.float32, T)
+    if cap_rows is None:
+        if row_token is not None:
+            raise ValueError("row_token needs cap_rows")
+        cap_rows = T
+    n_groups = len(weights) - n_shared
+    if n_shared < 0 or n_groups < 0 or group_offsets.numel() != n_groups + 1:
+        raise ValueError("group_offsets must hold n_groups + 1 entries for the routed groups")
+    rows = n_shared * T + cap_rows
+    _holds(row_token, "row_token", rows)
+    if y_perm is None:
+        y_perm = _empty((max(rows, 1), d), torch.bfloat16, xq.device, stream)
+    _holds(y_perm, "y_perm", rows, d)
+    if ws is None:
+        ws = workspace(moe_grouped_ffn_int8_ws_bytes(rows, d, f, len(weights)), xq.device, stream)
+    st = lib.moe_grouped_ffn_int8(
+        _dev(xq, "xq"), _dev(x_scale, "x_scale"), T, _dev(row_token, "row_token", torch.int32),
+        _dev(group_offsets, "group_offsets", torch.int32), n_groups, n_shared, *weights.pointers,
+        d, f, cap_rows, _dev(y_perm, "y_perm", torch.bfloat16), _dev(ws, "ws"), ws.numel(),
+        _stream(stream))
+    _check("moe_grouped_ffn_int8", st)
+    return y_perm
+
+
+def moe_rmsnorm(x: torch.Tensor, weight: torch.Tensor, *, residual: Optional[torch.Tensor] = None,
+                eps: float = 1e-6, h: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+                want_y: bool = True, rstd: Optional[torch.Tensor] = None, want_rstd: bool = False,
+                q: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                want_q: bool = False, stream=None):
+    """Root-mean-square norm of the rows of x [T, d] (+ residual).  Returns (h = the sum, or x
+    itself without a residual; y; rstd [T]; q, scales: y in 8 bits), None for what is not wanted."""
+    lib = load_library()
+    T, d = x.shape
+    dtype = _dtype_code(x)
+    _same(weight, "weight", x.dtype, d)
+    _same(residual, "residual", x.dtype, T, d)
+    like, new = torch.empty_like, x.new_empty
+    if stream is not None:
+        like, new = _of(stream, like), _of(stream, new)
+    if residual is None:
+        if h is not None:
+            raise ValueError("h is x itself without a residual")
+    elif h is None:
+        h = like(x)
+    if want_y and y is None:
+        y = like(x)
+    if want_rstd and rstd is None:
+        rstd = new(T, dtype=torch.float32)
+    if (q is None) != (scales is None):
+        raise ValueError("q and scales go together")
+    if want_q and q is None:
+        q, scales = new((T, int8_cols(d)), dtype=torch.int8), new(T, dtype=torch.float32)
+    _same(h, "h", x.dtype, T, d)
+    _same(y, "y", x.dtype, T, d)
+    _same(rstd, "rstd", torch.float32, T)
+    _same(q, "q", torch.int8, T, int8_cols(d))
+    _same(scales, "scales", torch.float32, T)
+    st = lib.moe_rmsnorm(_dev(x, "x"), _dev(residual, "residual"), dtype, _dev(weight, "weight"), eps, T, d,
+                         _dev(h, "h"), _dev(y, "y"), _dev(rstd, "rstd"), _dev(q, "q"),
+                         _dev(scales, "scales"), _stream(stream))
+    _check("moe_rmsnorm", st)
+    return (x if residual is None else h), y, rstd, q, scales
+
+
+def moe_rmsnorm_backward_ws_bytes(dtype: int, T: int, d: int) -> int:
+    return int(load_library().moe_rmsnorm_backward_ws_bytes(dtype, T, d))
+
+
+def moe_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor, *,
+                         dh_add: Optional[torch.Tensor] = None, dh: Optional[torch.Tensor] = None,
+                         dw: Optional[torch.Tensor] = None, want_dh: bool = True, want_dw: bool = True,
+                         ws: Optional[torch.Tensor] = None, stream=None):
+    """Gradient of moe_rmsnorm's y, on top of dh_add.  Returns (dh [T, d], of x and of the residual;
+    dw [d] float32), None for what is not wanted."""
+    lib = load_library()
+    T, d = dy.shape
+    _same(h, "h", dy.dtype, T, d)
+    _same(weight, "weight", dy.dtype, d)
+    _same(rstd, "rstd", torch.float32, T)
+    _same(dh_add, "dh_add", dy.dtype, T, d)
+    dtype = _dtype_code(dy)
+    if want_dh and dh is None:
+        dh = (torch.empty_like if stream is None else _of(stream, torch.empty_like))(dy)
+    if want_dw and dw is None:
+        dw = _empty((d,), torch.float32, dy.device, stream)
+    _same(dh, "dh", dy.dtype, T, d)
+    _same(dw, "dw", torch.float32, d)
+    if dw is not None and ws is None:
+        ws = workspace(moe_rmsnorm_backward_ws_bytes(dtype, T, d), dy.device, stream)
+    st = lib.moe_rmsnorm_backward(_dev(dy, "dy"), _dev(h, "h"), dtype, _dev(weight, "weight"),
+                                  _dev(rstd, "rstd"), _dev(dh_add, "dh_add"), T, d, _dev(dh, "dh"),
+                                  _dev(dw, "dw"), _dev(ws, "ws"), 0 if ws is None else ws.numel(),
+                                  _stream(stream))
+    _check("moe_rmsnorm_backward", st)
+    return dh, dw
+
+
+def _mask(mask: Optional[torch.Tensor], T: int):
+    """Device pointer of a token mask (bool or uint8 [T]; None -> NULL)."""
+    if mask is not None and (mask.dtype not in (torch.bool, torch.uint8) or tuple(mask.shape) != (T,)):
+        raise ValueError("mask must be bool or uint8 [%d]" % T)
+    return _dev(mask, "mask")
+
+
+def moe_balance_loss_ws_bytes(T: int, E: int) -> int:
+    return int(load_library().moe_balance_loss_ws_bytes(T, E))
+
+
+def moe_balance_loss(logits: torch.Tensor, topk_idx: torch.Tensor, *, mask: Optional[torch.Tensor] = None,
+                     loss: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None,
+                     prob_sum: Optional[torch.Tensor] = None, n_tokens: Optional[torch.Tensor] = None,
+                     ws: Optional[torch.Tensor] = None, stream=None):
+    """Balance loss of a routing over the tokens where mask [T] is not 0.  Returns (loss [1],
+    counts [E] int32, prob_sum [E], n_tokens [1] int32), on the device."""
+    lib = load_library()
+    T, E = logits.shape
+    k = topk_idx.shape[1]
+    _same(logits, "logits", torch.float32, T, E)
+    _same(topk_idx, "topk_idx", torch.int32, T, k)
+    new = logits.new_empty if stream is None else _of(stream, logits.new_empty)
+    loss = new(1) if loss is None else loss
+    counts = new(E, dtype=torch.int32) if counts is None else counts
+    prob_sum = new(E) if prob_sum is None else prob_sum
+    n_tokens = new(1, dtype=torch.int32) if n_tokens is None else n_tokens
+    _same(loss, "loss", torch.float32, 1)
+    _same(counts, "counts", torch.int32, E)
+    _same(prob_sum, "prob_sum", torch.float32, E)
+    _same(n_tokens, "n_tokens", torch.int32, 1)
+    if ws is None:
+        ws = workspace(moe_balance_loss_ws_bytes(T, E), logits.device, stream)
+    st = lib.moe_balance_loss(_dev(logits, "logits"), _dev(topk_idx, "topk_idx"), _mask(mask, T), T, E, k,
+                              _dev(counts, "counts"), _dev(prob_sum, "prob_sum"),
+                              _dev(n_tokens, "n_tokens"), _dev(loss, "loss"), _dev(ws, "ws"), ws.numel(),
+                              _stream(stream))
+    _check("moe_balance_loss", st)
+    return loss, counts, prob_sum, n_tokens
+
+
+def moe_balance_loss_backward(logits: torch.Tensor, counts: torch.Tensor, n_tokens: torch.Tensor, k: int, *,
+                              scale: float = 1.0, mask: Optional[torch.Tensor] = None,
+                              dlogits: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Gradient of moe_balance_loss, times scale.  Returns dlogits [T, E]."""
+    lib = load_library()
+    T, E = logits.shape
+    _same(logits, "logits", torch.float32, T, E)
+    _same(counts, "counts", torch.int32, E)
+    _same(n_tokens, "n_tokens", torch.int32, 1)
+    if dlogits is None:
+        dlogits = (torch.empty_like if stream is None else _of(stream, torch.empty_like))(logits)
+    _same(dlogits, "dlogits", torch.float32, T, E)
+    st = lib.moe_balance_loss_backward(_dev(logits, "logits"), _mask(mask, T), _dev(counts, "counts"),
+                                       _dev(n_tokens, "n_tokens"), T, E, k, scale,
+                                       _dev(dlogits, "dlogits"), _stream(stream))
+    _check("moe_balance_loss_backward", st)
+    return dlogits
+
+
+class GradTable:
+    """Host arrays of a step's gradients (float32 or bfloat16, any shapes), as moe_grad_norm and
+    moe_clip_grads take them; out (None: in place): where the clipped ones go."""
+
+    def __init__(self, grads: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]] = None):
+        self.grads = list(grads)
+        self.out = self.grads if out is None else list(out)
+        if len(self.out) != len(self.grads):
+            raise ValueError("need one output per gradient")
+        n = len(self.grads)
+        for g, o in zip(self.grads, self.out):
+            _dtype_code(g)
+            if o.dtype != g.dtype or o.shape != g.shape or o.device != g.device:
+                raise ValueError("outputs must be of the gradients' types and shapes, on their device")
+            if g.device != self.grads[0].device:
+                raise ValueError("gradients must be on one device")
+        self.pointers = (ctypes.c_void_p * n)(*[_dev(g, "grads") for g in self.grads])
+        self.outputs = (ctypes.c_void_p * n)(*[_dev(o, "out") for o in self.out])
+        self.sizes = (ctypes.c_int64 * n)(*[g.numel() for g in self.grads])
+        self.dtypes = (ctypes.c_int * n)(*[_dtype_code(g) for g in self.grads])
+
+    def __len__(self):
+        return len(self.grads)
+
+
+def moe_grad_norm_ws_bytes(table: GradTable) -> int:
+    return int(load_library().moe_grad_norm_ws_bytes(table.sizes, len(table)))
+
+
+def moe_grad_norm(table: GradTable, *, norm: Optional[torch.Tensor] = None,
+                  ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The norm over all gradients of a table.  Returns norm [1] float32, on the device."""
+    lib = load_library()
+    if norm is None:
+        if not len(table):
+            raise ValueError("a table without gradients needs norm")
+        norm = _empty((1,), torch.float32, table.grads[0].device, stream)
+    _same(norm, "norm", torch.float32, 1)
+    if ws is None:
+        ws = workspace(moe_grad_norm_ws_bytes(table), norm.device, stream)
+    st = lib.moe_grad_norm(table.pointers, table.sizes, table.dtypes, len(table), _dev(norm, "norm"),
+                           _dev(ws, "ws"), ws.numel(), _stream(stream))
+    _check("moe_grad_norm", st)
+    return norm
+
+
+def moe_clip_grads(table: GradTable, norm: torch.Tensor, max_norm: float, *, stream=None):
+    """Scale a table's gradients by max_norm / norm where that is below 1.  Returns its outputs."""
+    lib = load_library()
+    _same(norm, "norm", torch.float32, 1)
+    st = lib.moe_clip_grads(table.pointers, table.sizes, table.dtypes, len(table), _dev(norm, "norm"),
+                            max_norm, table.outputs, _stream(stream))
+    _check("moe_clip_grads", st)
+    return table.out
