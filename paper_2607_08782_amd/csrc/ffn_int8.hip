@@ -10,14 +10,17 @@
 //
 // Rows of codes are padded to whole steps of 128 columns, so no product has a last part of a step.
 #include <algorithm>
+#include <type_traits>
 
 #include "int8.h"
-#include "tiles.h"
+#include "stream_tiles.h"
 
 namespace moe {
 namespace {
 
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int STEP = 128;                                // columns (bytes) of a step
 
@@ -36,10 +39,6 @@ struct I8Args {
     int strips;                          // strips a group
     int slots;                           // groups that can hold rows at once
 };
-
-__device__ __forceinline__ int first_row(const I8Args& p, int g) {
-    return group_start(p.offsets, p.lead, p.lead_rows, g);
-}
 
 // ---------------------------------------------------------------------------
 // Strips: groups of few rows, bound by the weight bytes.  A workgroup holds 16 TILES weight rows
@@ -164,29 +163,6 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
 #endif
 }
 
-// The n-th group that holds rows, its first row and their number (a call of fewer rows than
-// groups launches strips for as many groups as it has rows).
-struct Group {
-    int g, row0, rows;
-};
-
-__device__ __forceinline__ Group nth_group(const I8Args& p, int n) {
-    const int lane = threadIdx.x & 63;
-    for (int g0 = 0; g0 < p.n_groups; g0 += 64) {
-        const int g = min(g0 + lane, p.n_groups - 1);
-        const int row0 = first_row(p, g), rows = first_row(p, g + 1) - row0;
-        uint64_t mask = __ballot(g0 + lane < p.n_groups && rows > 0);
-        const int here = __popcll(mask);
-        if (n < here) {
-            for (; n > 0; --n) mask &= mask - 1;
-            const int l = __builtin_ctzll(mask);
-            return {g0 + l, __builtin_amdgcn_readlane(row0, l), __builtin_amdgcn_readlane(rows, l)};
-        }
-        n -= here;
-    }
-    return {0, 0, 0};
-}
-
 // MAX_MS = 1: no group holds more than 16 rows.  Otherwise each group takes the row blocks it needs.
 template <bool SWIGLU, int W, int TILES, int MAX_MS>
 __global__ __launch_bounds__(64 * W, 2) void strip_int8_kernel(I8Args p) {
@@ -209,6 +185,362 @@ __global__ __launch_bounds__(64 * W, 2) void strip_int8_kernel(I8Args p) {
     else strip_rows<SWIGLU, W, TILES, 4, 2>(p, red, of.g, n0, of.row0, of.rows);
 }
 
+// ---------------------------------------------------------------------------
+// Tiles: groups of many rows, bound by the matrix rate.  A persistent grid of workgroups of
+// WM x 2 waves, each TM x TN accumulator tiles of v_mfma_i32_32x32x32_i8: 256 x 256 by eight waves
+// (two a SIMD) or, for few tiles, 128 x 128 by four (two workgroups a CU).
+//
+// Both operands go straight from memory into a ring of RING steps of 64 columns in LDS: a step's
+// loads have RING - 2 to RING - 1 steps of products to arrive.  The steps of all of a workgroup's
+// tiles are one stream: loads run ahead of the products whatever tile these belong to, so a tile
+// starts without waiting for its first operands.  One barrier per step, in its middle: there every
+// wave holds its second half's fragments in registers, so the step's ring slot is free, and the next
+// step has landed, so the fragments of its first half are read during the second half's products.
+//
+// LDS rows are 64 bytes; 16-byte chunk c of row r sits at c ^ ((r >> 2) & 3), free of bank conflicts
+// for the reads of 32 rows.  The weights are the instruction's first operand, laid out in LDS so that
+// a lane's sixteen accumulators are sixteen consecutive output columns of one token row (w_order).  A
+// tile's scales come into LDS like its operands, ahead of its first step.
+constexpr int HALF_LINE = 64;                            // columns (bytes) of a tile's step
+constexpr int SCALES = 8;                                // tiles whose scales are kept: the loads' and
+                                                         // the products' are RING steps apart, and a
+                                                         // tile has two steps at least
+
+// TM x TN accumulator tiles per wave, WM x 2 waves, R steps in the ring
+template <int WM, int TM, int TN, int R>
+struct TileShape {
+    static constexpr int WAVES = 2 * WM, THREADS = 64 * WAVES;
+    static constexpr int BM = 32 * WM * TM, BN = 64 * TN;          // token rows, weight rows
+    static constexpr int B_CODES = BM * HALF_LINE, STAGE = (BM + BN) * HALF_LINE;
+    static constexpr int AT_SX = R * STAGE, AT_SW = AT_SX + SCALES * BM * 4, AT_TOK = AT_SW + SCALES * BN * 4;
+    static constexpr int LDS = AT_TOK + 2 * BM * 4;      // the ring, scales, two tiles' token rows
+    // direct loads per wave and step: 16 rows each
+    static constexpr int AL = BM / 16 / WAVES, BL = BN / 16 / WAVES, LOADS = AL + BL;
+    static constexpr int PER_EU = 2;                     // waves a SIMD holds
+    static_assert(TM * TN <= 8, "the accumulators of two waves a SIMD");
+    static_assert(BM / 64 + BN / 64 == WAVES, "a wave loads 64 scales of a tile");
+};
+
+struct I8Tile {
+    int row0, valid, n0;
+    uint64_t w, ws;                                      // its group's weight codes and scales
+};
+
+template <bool SWIGLU, int WM, int TM, int TN, int RING>
+__global__ __launch_bounds__(64 * 2 * WM, 2) void tile_int8_kernel(I8Args p) {
+#ifdef __HIP_DEVICE_COMPILE__
+    typedef TileShape<WM, TM, TN, RING> S;
+    constexpr int BM = S::BM, BN = S::BN, BN_OUT = SWIGLU ? BN / 2 : BN;
+    constexpr int AL = S::AL, BL = S::BL, ROUND = 16 * S::WAVES;
+    extern __shared__ __attribute__((aligned(1024))) char ring[];
+    __shared__ int s_off[MOE_MAX_GROUPS + 1], s_high[MOE_MAX_GROUPS + 1], s_low[MOE_MAX_GROUPS + 1];
+    __shared__ I8Tile s_tile[TILE_LIST];
+    float* const s_sx = (float*)(ring + S::AT_SX);       // [SCALES][BM]
+    float* const s_sw = (float*)(ring + S::AT_SW);       // [SCALES][BN]
+    int* const s_tok = (int*)(ring + S::AT_TOK);         // [2][BM]
+    const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / 2, wn = wave % 2;              // a SIMD's waves hold rows of both halves
+    const int n_tiles = (p.N + BN_OUT - 1) / BN_OUT, KT = p.P / HALF_LINE;
+    for (int g = tid; g <= p.n_groups; g += S::THREADS) s_off[g] = first_row(p, g);
+    __syncthreads();
+    if (wave == 0) {
+        starts(s_off, p.n_groups, n_tiles, s_high, lane, [](int rows) { return high_tiles<BM>(rows); });
+        starts(s_off, p.n_groups, n_tiles, s_low, lane,
+               [](int rows) { return (int)ceil_div(rows, BM) - high_tiles<BM>(rows); });
+    }
+    __syncthreads();
+    const TileShare<BM> tiles(s_off, s_high, s_low, p.n_groups, n_tiles);
+    const int n_list = tiles.n_list;                     // this workgroup's tiles
+    if (n_list <= 0) return;
+    // records of the half of the list that starts with tile q0, half a list ahead of the
+    // products' tile (the loads' is RING ahead at most): the half's old ones are used up
+    auto list_tiles = [&](int q0) {
+        const int q = q0 + tid;
+        if (tid >= TILE_LIST / 2 || q >= n_list) return;
+        const auto at = tiles.at(q);
+        I8Tile t;
+        t.w = (uint64_t)p.w[at.g];
+        t.ws = (uint64_t)p.ws[at.g];
+        t.row0 = at.row0;
+        t.valid = at.valid;
+        t.n0 = at.n * BN_OUT;
+        s_tile[q % TILE_LIST] = t;
+    };
+    auto tile_at = [&](int q) {
+        I8Tile t = s_tile[q % TILE_LIST];
+        t.w = uniform(t.w);
+        t.ws = uniform(t.ws);
+        t.row0 = __builtin_amdgcn_readfirstlane(t.row0);
+        t.valid = __builtin_amdgcn_readfirstlane(t.valid);
+        t.n0 = __builtin_amdgcn_readfirstlane(t.n0);
+        return t;
+    };
+    list_tiles(0);
+    list_tiles(TILE_LIST / 2);
+    __syncthreads();
+
+    // the loads' side of the stream: tile, step of it, operand descriptors, row offsets
+    // load i of a wave fills LDS rows ROUND i + 16 wave + lane / 4 of A or B, slot lane % 4
+    const int lrow = 16 * wave + (lane >> 2);
+    const int lchunk = ((lane & 3) ^ ((lane >> 4) & 3)) * 16;
+    auto rsrc = [](uint64_t base) {
+        return __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, -1, RSRC_WORD3);
+    };
+    __amdgpu_buffer_rsrc_t ra = rsrc(0), rb = ra;
+    uint32_t at_k = 0;
+    int aoff[AL], boff[BL];
+    // gather: the token rows of a tile's rows come into LDS a tile ahead, by a direct load
+    // like the ring's (zero past the group)
+    auto fetch_tokens = [&](int q) {
+        const I8Tile t = tile_at(q);
+        if (64 * wave >= BM) return;
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)(p.a_rows + t.row0), (short)0, t.valid * 4, RSRC_WORD3);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(s_tok + (q & 1) * BM + 64 * wave), 4,
+                                                 tid * 4, 0, 0, 0);
+    };
+    if (p.a_rows != nullptr) fetch_tokens(0);
+    int lq = -1, left_steps = 0;                         // before the first tile
+    auto next_tile = [&]() {
+        ++lq;
+        const bool live = lq < n_list;
+        const I8Tile t = tile_at(live ? lq : n_list - 1);
+        if (p.a_rows != nullptr) {
+            // Issued a tile ago.  The waits of the loop are for older loads than a step's,
+            // but a tile of fewer steps than the ring ends before the first of them.
+            if (lq == 0 || KT < RING) {
+                wait_vm<0>();
+                asm volatile("s_barrier" ::: "memory");
+            }
+            if (lq + 1 < n_list) fetch_tokens(lq + 1);
+        }
+        // rows past the group's or the matrix's repeat its last one; past the last tile all lanes
+        // are on one row
+        auto row_a = [&](int r) {
+            return !live ? 0 : p.a_rows != nullptr ? s_tok[(lq & 1) * BM + r] : min(r, t.valid - 1);
+        };
+        auto row_b = [&](int r) {
+            const bool up = SWIGLU && r >= BN / 2;
+            return !live ? 0 : min(t.n0 + w_order(up ? r - BN / 2 : r), p.N - 1) + (up ? p.N : 0);
+        };
+        const int64_t first = p.a_rows != nullptr ? 0 : t.row0;
+        ra = rsrc((uint64_t)p.a + first * p.P);
+        rb = rsrc(t.w);
+#pragma unroll
+        for (int i = 0; i < AL; ++i) aoff[i] = row_a(lrow + ROUND * i) * p.P + lchunk;
+#pragma unroll
+        for (int i = 0; i < BL; ++i) boff[i] = row_b(lrow + ROUND * i) * p.P + lchunk;
+        // the tile's scales: its rows' by the first waves, its columns' by the others
+        constexpr int ROWS_BY = BM / 64;
+        if (live) {
+            const int slot = lq & (SCALES - 1);
+            if (wave < ROWS_BY) {
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc((uint64_t)(p.as + first)),
+                                                         (lds_void*)(s_sx + slot * BM + 64 * wave), 4,
+                                                         row_a(64 * wave + lane) * 4, 0, 0, 0);
+            } else {
+                const int c = 64 * (wave - ROWS_BY) + lane;
+                const bool up = SWIGLU && c >= BN / 2;
+                const int col = min(t.n0 + (up ? c - BN / 2 : c), p.N - 1) + (up ? p.N : 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(t.ws),
+                                                         (lds_void*)(s_sw + slot * BN + 64 * (wave - ROWS_BY)), 4,
+                                                         col * 4, 0, 0, 0);
+            }
+        }
+        at_k = 0;
+        left_steps = KT;
+    };
+    // direct load i of the stream's next step
+    auto load1 = [&](char* st, int i) {
+        if (i < AL)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                ra, (lds_void*)(st + (ROUND * i + 16 * wave) * HALF_LINE), 16, aoff[i], at_k, 0, 0);
+        else
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                rb, (lds_void*)(st + S::B_CODES + (ROUND * (i - AL) + 16 * wave) * HALF_LINE), 16, boff[i - AL],
+                at_k, 0, 0);
+    };
+    auto next_step = [&]() {
+        --left_steps;
+        at_k += HALF_LINE;
+    };
+
+    // the products' side: fragment addresses within a step (32-column halves of it by kk)
+    const int swz = (r32 >> 2) & 3;
+    const int a_row = wm * 32 * TM + r32;
+    const int b_row = wn * (SWIGLU ? BN / 4 : BN / 2) + r32;
+    auto b_tile = [](int j) { return SWIGLU && j >= TN / 2 ? BN / 2 + (j - TN / 2) * 32 : j * 32; };
+    i32x16 acc[TM][TN];                                  // [token tile][weight tile]
+    i32x4 fa[2][TM], fb[2][TN];                          // by half of a step
+    const int chunk0 = ((0 + half) ^ swz) * 16, chunk1 = ((2 + half) ^ swz) * 16;
+    // fragment i of a half of a step: the weights', then the rows'
+    auto read1 = [&](const char* st, int kk, int i) {
+        st += kk ? chunk1 : chunk0;
+        if (i < TN) fb[kk][i] = *(const i32x4*)(st + S::B_CODES + (b_row + b_tile(i)) * HALF_LINE);
+        else fa[kk][i - TN] = *(const i32x4*)(st + (a_row + 32 * (i - TN)) * HALF_LINE);
+    };
+    // the products of a half that follow its read i, behind what was issued before them: the
+    // order of reads, loads and products is the source's
+    auto multiply = [&](auto half_of, int i) {
+        constexpr int KK = decltype(half_of)::value;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = i * TM * TN / (TM + TN); u < (i + 1) * TM * TN / (TM + TN); ++u) {
+            const int m = u / TN, j = u % TN;
+            acc[m][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[KK][j], fa[KK][m], acc[m][j], 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // keeps a half's products from being moved past a wait
+    auto pin = [&]() {
+#pragma unroll
+        for (int m = 0; m < TM; ++m)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) asm volatile("" : "+v"(acc[m][j]));
+    };
+    constexpr std::integral_constant<int, 0> first{};
+    constexpr std::integral_constant<int, 1> second{};
+
+    // a step's loads are issued in two halves of a step of products each: the second of one
+    // step, once the slot is free, and the first of the next
+    constexpr int EARLY = (S::LOADS + 1) / 2;
+    for (int r = 0; r < RING; ++r) {
+        char* const st = ring + r * S::STAGE;
+        if (left_steps == 0) next_tile();
+#pragma unroll
+        for (int i = 0; i < EARLY; ++i) load1(st, i);
+        if (r == RING - 1) break;
+#pragma unroll
+        for (int i = EARLY; i < S::LOADS; ++i) load1(st, i);
+        next_step();
+    }
+    wait_vm<(RING - 2) * S::LOADS + EARLY>();
+    asm volatile("s_barrier" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < TM + TN; ++i) read1(ring, 0, i);
+    // slots of this step, the next, and the one that loads go to (offsets in the ring)
+    unsigned here = 0, next = S::STAGE, fill = (RING - 1) * S::STAGE;
+    auto turn = [&]() {                                  // the step's slot is free
+        fill = here;
+        here = next;
+        next = next == (RING - 1) * S::STAGE ? 0 : next + S::STAGE;
+    };
+    // stores of an epilogue: newer than the loads that the next RING - 2 waits are for
+    constexpr int STORES = SWIGLU ? TM * TN : 2 * TM * TN;
+    int fresh = 0;
+    // the next step has landed: outstanding may be the ones after it, and stores
+    auto landed = [&]() {
+        if (fresh > 0) {
+            wait_vm<(RING - 2) * S::LOADS + STORES>();
+            --fresh;
+        } else {
+            wait_vm<(RING - 2) * S::LOADS>();
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    for (int q = 0; q < n_list; ++q) {
+        const I8Tile cur = tile_at(q);
+        if (q > 0 && q % (TILE_LIST / 2) == 0) list_tiles(q + TILE_LIST / 2);
+        if (wm * 32 * TM >= cur.valid) {                 // no row of this wave's: its loads only
+#pragma clang loop unroll(disable)
+            for (int t = 0; t < KT; ++t) {
+#pragma unroll
+                for (int i = EARLY; i < S::LOADS; ++i) load1(ring + fill, i);
+                next_step();
+                landed();
+                turn();
+                if (left_steps == 0) next_tile();
+#pragma unroll
+                for (int i = 0; i < EARLY; ++i) load1(ring + fill, i);
+            }
+#pragma unroll
+            for (int i = 0; i < TM + TN; ++i) read1(ring + here, 0, i);
+            continue;
+        }
+#pragma unroll
+        for (int m = 0; m < TM; ++m)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[m][j][e] = 0;
+#pragma clang loop unroll(disable)
+        for (int t = 0; t < KT; ++t) {
+#pragma unroll
+            for (int i = 0; i < TM + TN; ++i) {
+                if (2 * i < TM + TN) {
+                    read1(ring + here, 1, 2 * i);
+                    read1(ring + here, 1, 2 * i + 1);
+                }
+                if (i >= TM + TN - (S::LOADS - EARLY)) load1(ring + fill, S::LOADS - (TM + TN) + i);
+                multiply(first, i);
+            }
+            pin();
+            next_step();
+            landed();
+            turn();
+            if (left_steps == 0) next_tile();
+#pragma unroll
+            for (int i = 0; i < TM + TN; ++i) {
+                if (2 * i < TM + TN) {
+                    read1(ring + here, 0, 2 * i);
+                    read1(ring + here, 0, 2 * i + 1);
+                }
+                if (i >= TM + TN - EARLY) load1(ring + fill, i - (TM + TN - EARLY));
+                multiply(second, i);
+            }
+            pin();
+        }
+        fresh = RING - 2;
+
+        // Every store is issued, those past the group's rows or the output's columns dropped
+        // by the descriptor: the waits above count them.
+        const int lr = wm * 32 * TM + r32, slot = q & (SCALES - 1);
+        const __amdgpu_buffer_rsrc_t ry = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)(p.out + (int64_t)cur.row0 * p.pitch), (short)0, cur.valid * (int)p.pitch * 2, RSRC_WORD3);
+        const int lc = wn * (SWIGLU ? BN / 4 : BN / 2) + 16 * half;        // column in the tile
+#pragma unroll
+        for (int m = 0; m < TM; ++m) {
+            const float sx = s_sx[slot * BM + lr + 32 * m];
+#pragma unroll
+            for (int j = 0; j < (SWIGLU ? TN / 2 : TN); ++j) {
+                const int c = lc + 32 * j;
+                const float* sw = s_sw + slot * BN + c;
+                float v[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] = (float)acc[m][j][e] * sx * sw[e];
+                if constexpr (SWIGLU) {
+                    silu(v);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) v[e] *= (float)acc[m][TN / 2 + j][e] * sx * sw[BN / 2 + e];
+                }
+#pragma unroll
+                for (int e = 0; e < 16; e += 8) {
+                    u32x4 w;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(v[e + 2 * i], v[e + 2 * i + 1]);
+                    const int col = cur.n0 + c + e;
+                    // (h's rows have room for whole tiles)
+                    __builtin_amdgcn_raw_buffer_store_b128(
+                        w, ry, SWIGLU || col < p.N ? ((lr + 32 * m) * (int)p.pitch + col) * 2 : A_OOB, 0, 0);
+                }
+            }
+        }
+    }
+#endif
+}
+
+template <bool SWIGLU, int WM, int TM, int TN, int RING>
+int launch_tiles(const I8Args& p, hipStream_t s) {
+    typedef TileShape<WM, TM, TN, RING> S;
+    static LdsGrant grant;
+    const int st = allow_dynamic_lds((const void*)tile_int8_kernel<SWIGLU, WM, TM, TN, RING>, S::LDS, grant);
+    if (st != MOE_OK) return st;
+    const int grid = num_cus() / NUM_XCD * NUM_XCD * (S::PER_EU * 4 / S::WAVES);
+    hipLaunchKernelGGL((tile_int8_kernel<SWIGLU, WM, TM, TN, RING>), dim3(grid), dim3(S::THREADS), S::LDS, s, p);
+    return launch_status();
+}
+
 template <bool SWIGLU>
 int launch_strips(I8Args& p, int64_t max_rows, hipStream_t s) {
     constexpr int W = 4, TILES = 4;
@@ -219,6 +551,19 @@ int launch_strips(I8Args& p, int64_t max_rows, hipStream_t s) {
     else
         hipLaunchKernelGGL((strip_int8_kernel<SWIGLU, W, TILES, 4>), grid, block, 0, s, p);
     return launch_status();
+}
+
+// Strips while no group can hold more rows than this, tiles past it.
+constexpr int64_t STRIP_MAX_ROWS = 128;
+
+// Tiles of 256 x 256 from this many outputs of a product (a round of them over the chip), of
+// 128 x 128 below, counted over the rows that the call has room for.
+constexpr int64_t LARGE_WORK = (int64_t)256 * 256 * 256;
+
+template <bool SWIGLU>
+int launch_product(I8Args& p, int64_t max_rows, int64_t rows, hipStream_t s) {
+    if (max_rows <= STRIP_MAX_ROWS) return launch_strips<SWIGLU>(p, max_rows, s);
+    return rows * p.N >= LARGE_WORK ? launch_tiles<SWIGLU, 4, 2, 4, 4>(p, s) : launch_tiles<SWIGLU, 2, 2, 2, 4>(p, s);
 }
 
 int64_t align256(int64_t x) { return (x + 255) & ~(int64_t)255; }
@@ -266,7 +611,7 @@ int launch_grouped_ffn_int8(const int8_t* xq, const float* x_scale, int64_t T,
     p.N = f;
     p.out = (bf16_t*)base;
     p.pitch = int8_cols(f);
-    int st = launch_strips<true>(p, max_rows, s);
+    int st = launch_product<true>(p, max_rows, rows, s);
     if (st != MOE_OK) return st;
     st = launch_quantize_int8(base, MOE_BF16, rows, f, p.pitch, hq, hs, offsets + n_groups - lead,
                               lead * lead_rows, s);
@@ -282,7 +627,7 @@ int launch_grouped_ffn_int8(const int8_t* xq, const float* x_scale, int64_t T,
     p.N = d;
     p.out = (bf16_t*)y;
     p.pitch = d;
-    return launch_strips<false>(p, max_rows, s);
+    return launch_product<false>(p, max_rows, rows, s);
 }
 
 }  // namespace moe

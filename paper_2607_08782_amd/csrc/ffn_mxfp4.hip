@@ -17,7 +17,7 @@
 #include <type_traits>
 
 #include "mxfp4.h"
-#include "tiles.h"
+#include "stream_tiles.h"
 
 namespace moe {
 namespace {
@@ -52,10 +52,6 @@ struct MxArgs {
     int strips;                          // strips a group
     int slots;                           // groups that can hold rows at once
 };
-
-__device__ __forceinline__ int first_row(const MxArgs& p, int g) {
-    return group_start(p.offsets, p.lead, p.lead_rows, g);
-}
 
 __device__ __forceinline__ i32x8 operand(const i32x4& v) {
     return i32x8{v[0], v[1], v[2], v[3], 0, 0, 0, 0};    // 4-bit operands use the lower half
@@ -264,30 +260,6 @@ __device__ __forceinline__ void strip_rows(const MxArgs& p, float* red, int g, i
 #endif
 }
 
-// The n-th group that holds rows, its first row and their number (a call of fewer rows than
-// groups launches strips for as many groups as it has rows: a single token's step over 64
-// experts of which it takes 6 starts 264 workgroups, not 2816).
-struct Group {
-    int g, row0, rows;
-};
-
-__device__ __forceinline__ Group nth_group(const MxArgs& p, int n) {
-    const int lane = threadIdx.x & 63;
-    for (int g0 = 0; g0 < p.n_groups; g0 += 64) {
-        const int g = min(g0 + lane, p.n_groups - 1);
-        const int row0 = first_row(p, g), rows = first_row(p, g + 1) - row0;
-        uint64_t mask = __ballot(g0 + lane < p.n_groups && rows > 0);
-        const int here = __popcll(mask);
-        if (n < here) {
-            for (; n > 0; --n) mask &= mask - 1;
-            const int l = __builtin_ctzll(mask);
-            return {g0 + l, __builtin_amdgcn_readlane(row0, l), __builtin_amdgcn_readlane(rows, l)};
-        }
-        n -= here;
-    }
-    return {0, 0, 0};
-}
-
 // Steps of a wave up to which two are in flight, not three or four: more are loads that a
 // wave issues before its first product and, past its last step, for nothing (a single token
 // through DeepSeek-V2-Lite's experts, whose down product gives a wave 3 steps: 14.8 us with
@@ -351,8 +323,6 @@ __global__ __launch_bounds__(64 * W, QUANT ? 3 : MAX_MS == 1 ? 4 : 2) void strip
 // PFLOP/s; the matrix units are busy 47 and 44 % of the clocks, and the clock falls to 1.9 and
 // 2.1 GHz under the power limit: runs with half the scalar instructions, or with a seventh fewer waits, took
 // the same time at another clock.
-constexpr int TILE_LIST = 32;                            // tile records kept, in two halves
-
 // TM x TN accumulator tiles per wave, WM x 2 waves, R steps in the ring
 template <int WM, int TM, int TN, int R>
 struct TileShape {
@@ -373,41 +343,6 @@ struct MxTile {
     int row0, valid, n0;
     uint64_t w, ws;                                      // its group's weight codes and scale words
 };
-
-__device__ __forceinline__ uint64_t uniform(uint64_t v) {
-    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 |
-           (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
-}
-
-// weight row, within its 32-row block, of LDS row r: the instruction's row 8 a + 4 h + b is
-// accumulator 4 a + b of half h of the wave, which holds columns 16 h + 0 .. 15
-__device__ __forceinline__ int w_order(int r) {
-    return (r & ~31) + 16 * ((r >> 2) & 1) + 4 * ((r >> 3) & 3) + (r & 3);
-}
-
-// Tiles of 256 rows come in two kinds: high ones, and those of at most half the rows (a
-// group's last), whose upper waves have nothing to multiply.  These come last, where a round
-// is partly filled (4096 Mixtral-shaped tokens, 5.7 rounds of the one and 0.4 of the other:
-// gate/up 220 us in 7 rounds, 206 so).  The smaller tiles stay in order: a group's tiles apart
-// read its weights twice (1024 tokens of DeepSeek-V2-Lite 106 and 112 us).
-template <int BM>
-__device__ __forceinline__ int high_tiles(int rows) {
-    return BM > 128 ? (rows + BM / 2 - 1) / BM : (int)ceil_div(rows, BM);
-}
-
-// start[g] = tiles of the groups before g, by count(rows) row tiles each; by one wave
-template <typename Count>
-__device__ __forceinline__ void starts(const int* s_off, int n_groups, int n_tiles, int* start, int lane,
-                                       Count count) {
-    int carry = 0;
-    for (int g0 = 0; g0 < n_groups; g0 += 64) {
-        const int g = g0 + lane;
-        const int incl = wave_incl_scan(g < n_groups ? count(s_off[g + 1] - s_off[g]) * n_tiles : 0);
-        if (g < n_groups) start[g + 1] = carry + incl;
-        carry += __shfl(incl, 63, 64);
-    }
-    if (lane == 0) start[0] = 0;
-}
 
 template <bool SWIGLU, int WM, int TM, int TN, int RING>
 __global__ __launch_bounds__(64 * 2 * WM, 2) void tile_mxfp4_kernel(MxArgs p) {
@@ -432,59 +367,21 @@ __global__ __launch_bounds__(64 * 2 * WM, 2) void tile_mxfp4_kernel(MxArgs p) {
                [](int rows) { return (int)ceil_div(rows, BM) - high_tiles<BM>(rows); });
     }
     __syncthreads();
-    // each XCD takes a contiguous chunk of the high tiles, then one of the low; its workgroups
-    // every nper-th of it, those from the end what is left after whole rounds, of which the
-    // high ones come as two halves if there are workgroups for all
-    const int nper = gridDim.x / NUM_XCD, widx = blockIdx.x / NUM_XCD;
-    const int xcd = blockIdx.x % NUM_XCD;
-    auto share = [&](const int* start, int xcd, int& begin) {
-        const int total = __builtin_amdgcn_readfirstlane(start[p.n_groups]);
-        const int chunk = (total + NUM_XCD - 1) / NUM_XCD;
-        begin = min(xcd * chunk, total);
-        return min(chunk, total - begin);
-    };
-    int high0, low0;
-    const int high = share(s_high, xcd, high0), all = high + share(s_low, NUM_XCD - 1 - xcd, low0);
-    const int rounds = all / nper, whole = rounds * nper;
-    const int last_high = max(high - whole, 0);
-    const bool halves = BM > 128 && all - whole + last_high <= nper;
-    const int left = all - whole + (halves ? last_high : 0);
-    const int n_list = rounds + (nper - 1 - widx < left ? 1 : 0);  // this workgroup's tiles
+    const TileShare<BM> tiles(s_off, s_high, s_low, p.n_groups, n_tiles);
+    const int n_list = tiles.n_list;                     // this workgroup's tiles
     if (n_list <= 0) return;
     // records of the half of the list that starts with tile q0, half a list ahead of the
     // products' tile (the loads' is RING ahead at most): the half's old ones are used up
     auto list_tiles = [&](int q0) {
         const int q = q0 + tid;
         if (tid >= TILE_LIST / 2 || q >= n_list) return;
-        int i = q * nper + (q < rounds ? widx : nper - 1 - widx), part = 0, parts = 1;
-        if (halves && i >= whole) {
-            if (i < whole + 2 * last_high) {
-                part = (i - whole) & 1;
-                parts = 2;
-                i = whole + (i - whole) / 2;
-            } else {
-                i -= last_high;
-            }
-        }
-        TilePos pos;
-        int g;
-        if (i < high) {
-            const int L = high0 + i;
-            g = last_le(s_high, p.n_groups, L);
-            pos = tile_pos(L - s_high[g], high_tiles<BM>(s_off[g + 1] - s_off[g]), n_tiles);
-        } else {
-            const int L = low0 + i - high;
-            g = last_le(s_low, p.n_groups, L);
-            pos = {high_tiles<BM>(s_off[g + 1] - s_off[g]), L - s_low[g]};
-        }
-        const int rows = s_off[g + 1] - s_off[g];
+        const auto at = tiles.at(q);
         MxTile t;
-        t.w = (uint64_t)p.w[g];
-        t.ws = (uint64_t)p.ws[g];
-        const int m0 = pos.m * BM + part * (BM / 2);
-        t.row0 = s_off[g] + m0;
-        t.valid = min(BM / parts, rows - m0);
-        t.n0 = pos.n * BN_OUT;
+        t.w = (uint64_t)p.w[at.g];
+        t.ws = (uint64_t)p.ws[at.g];
+        t.row0 = at.row0;
+        t.valid = at.valid;
+        t.n0 = at.n * BN_OUT;
         s_tile[q % TILE_LIST] = t;
     };
     auto tile_at = [&](int q) {
