@@ -581,7 +581,7 @@ int moe_quantize_int8(const void* x, int dtype, int64_t rows, int cols, int8_t* 
                       void* stream) {
     const int st = int8_check(x, dtype, rows, cols, q, scales);
     if (st != MOE_OK) return st;
-    return launch_quantize_int8(x, dtype, rows, cols, cols, q, scales, nullptr, 0, (hipStream_t)stream);
+    return launch_quantize_int8(x, dtype, rows, cols, q, scales, (hipStream_t)stream);
 }
 
 int moe_dequantize_int8(const int8_t* q, const float* scales, int64_t rows, int cols, int dtype,
@@ -593,7 +593,7 @@ int moe_dequantize_int8(const int8_t* q, const float* scales, int64_t rows, int 
 
 size_t moe_grouped_ffn_int8_ws_bytes(int64_t cap_rows, int d, int f, int n_groups) {
     if (cap_rows < 0 || d < 1 || f < 1 || n_groups < 0) return 0;
-    return grouped_ffn_int8_ws_bytes(cap_rows, f);
+    return grouped_ffn_int8_ws_bytes(cap_rows, d, f, n_groups);
 }
 
 int moe_grouped_ffn_int8(const int8_t* xq, const float* x_scale, int64_t T, const int32_t* row_token,
@@ -626,7 +626,7 @@ int moe_grouped_ffn_int8(const int8_t* xq, const float* x_scale, int64_t T, cons
         return MOE_ERR_SHAPE;
     // without a row map the rows are xq's own
     if (!row_token && T < cap_rows) return MOE_ERR_SHAPE;
-    if (rows > 0 && (!ws || ws_bytes < grouped_ffn_int8_ws_bytes(rows, f) || ((uintptr_t)ws & 255u)))
+    if (rows > 0 && (!ws || ws_bytes < grouped_ffn_int8_ws_bytes(rows, d, f, groups) || ((uintptr_t)ws & 255u)))
         return MOE_ERR_SHAPE;
     return launch_grouped_ffn_int8(xq, x_scale, T, row_token, group_offsets, groups, n_shared, (int)T, w13,
                                    s13, w2, s2, d, f, rows, y_perm, ws, (hipStream_t)stream);

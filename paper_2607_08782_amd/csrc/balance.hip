@@ -15,32 +15,66 @@ namespace moe {
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int MAX_GROUPS = 256;                          // parts of the batch
+constexpr int MAX_GROUPS = 512;                          // parts of the batch
 
-// A value over the L lanes of a token: the same order in each.
+// Lane o of the four steps of an exchange within 16 lanes: the quad's neighbour, its other half,
+// the other quad of eight lanes, the other eight (data moves within the vector unit; through LDS,
+// a shuffle each, the steps of a token took 1.3 us one after the other).
+template <int STEP>
+__device__ __forceinline__ float other(float v) {
+    constexpr int CTRL = STEP == 0 ? 0xb1 : STEP == 1 ? 0x4e : STEP == 2 ? 0x141 : 0x140;
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, false));
+}
+
+// A value over the L lanes of a token (2, 4, 8 or 16): the same order in each.
 template <int L>
 __device__ __forceinline__ float token_sum(float v) {
-#pragma unroll
-    for (int o = 1; o < L; o <<= 1) v += __shfl_xor(v, o, 64);
+    v += other<0>(v);
+    if (L >= 4) v += other<1>(v);
+    if (L >= 8) v += other<2>(v);
+    if (L >= 16) v += other<3>(v);
     return v;
 }
 
 template <int L>
 __device__ __forceinline__ float token_max(float v) {
-#pragma unroll
-    for (int o = 1; o < L; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    v = fmaxf(v, other<0>(v));
+    if (L >= 4) v = fmaxf(v, other<1>(v));
+    if (L >= 8) v = fmaxf(v, other<2>(v));
+    if (L >= 16) v = fmaxf(v, other<3>(v));
     return v;
 }
 
-// The softmax of a token's scores, J a lane: lane l of its L holds experts l, l + L, ...
-template <int L, int J>
-__device__ __forceinline__ void softmax(const float* row, int l, int E, float (&p)[J]) {
-    float top = -INFINITY, z = 0.f;
+// Expert of a lane's value j: four consecutive ones, then those 4 L further on.
+template <int L>
+__device__ __forceinline__ int expert_of(int l, int j) {
+    return 4 * (l + L * (j / 4)) + j % 4;
+}
+
+// A token's scores, 4 C a lane, -infinity past E.  VEC: rows are 16-byte aligned and E % 4 == 0.
+template <int L, int C, bool VEC>
+__device__ __forceinline__ void load_scores(const float* row, int l, int E, float (&p)[4 * C]) {
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-        p[j] = l + L * j < E ? row[l + L * j] : -INFINITY;
-        top = fmaxf(top, p[j]);
+    for (int c = 0; c < C; ++c) {
+        const int e = expert_of<L>(l, 4 * c);
+        if (VEC) {
+            f32x4 v = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            if (e < E) v = *(const f32x4*)(row + e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[4 * c + i] = v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[4 * c + i] = e + i < E ? row[e + i] : -INFINITY;
+        }
     }
+}
+
+// The softmax of a token's scores.
+template <int L, int J>
+__device__ __forceinline__ void softmax(float (&p)[J]) {
+    float top = p[0], z = 0.f;
+#pragma unroll
+    for (int j = 1; j < J; ++j) top = fmaxf(top, p[j]);
     top = token_max<L>(top);
 #pragma unroll
     for (int j = 0; j < J; ++j) {
@@ -52,26 +86,39 @@ __device__ __forceinline__ void softmax(const float* row, int l, int E, float (&
     for (int j = 0; j < J; ++j) p[j] *= z;
 }
 
-// A group's part of S, of the counts and of n: [groups][E] floats, then ints, then [groups] ints.
+// A group's part of S and of the counts, [groups][E], and of n; the experts' parts of the loss, a
+// number each for JOINT experts, and how many of these are there.
+struct Part {
+    float s;
+    int32_t c;
+};
+
+constexpr int JOINT = 16;
+
 struct BalanceParts {
-    float* s;
-    int32_t* c;
+    Part* e;
+    double* loss;
     int32_t* n;
+    uint32_t* ready;
 };
 
 BalanceParts parts_at(void* ws, int64_t groups, int E) {
-    float* s = (float*)ws;
-    int32_t* c = (int32_t*)(s + groups * E);
-    return {s, c, c + groups * E};
+    BalanceParts p;
+    p.e = (Part*)ws;
+    p.loss = (double*)(p.e + groups * E);
+    p.n = (int32_t*)(p.loss + MOE_MAX_E / JOINT);
+    p.ready = (uint32_t*)(p.n + groups);
+    return p;
 }
 
-template <int L, int J>
+template <int L, int C, bool VEC>
 __global__ __launch_bounds__(THREADS) void balance_parts_kernel(const float* __restrict__ logits,
                                                                 const int32_t* __restrict__ idx,
                                                                 const uint8_t* __restrict__ mask, int64_t T,
                                                                 int E, int k, int64_t per, BalanceParts out) {
-    constexpr int TOKENS = THREADS / L;                  // at a time
-    __shared__ float s[TOKENS][L * J];
+    constexpr int TOKENS = THREADS / L, J = 4 * C;       // tokens at a time
+    constexpr int JOINED = 16;                           // lanes whose tokens' sums meet in LDS
+    __shared__ float s[THREADS / JOINED][L * J];
     __shared__ int32_t c[MOE_MAX_E], n;
     const int l = threadIdx.x % L, sub = threadIdx.x / L;
     for (int e = threadIdx.x; e < E; e += THREADS) c[e] = 0;
@@ -85,29 +132,39 @@ __global__ __launch_bounds__(THREADS) void balance_parts_kernel(const float* __r
     for (int64_t t = begin + sub; t < end; t += TOKENS) {
         if (mask != nullptr && mask[t] == 0) continue;   // (all lanes of the token together)
         float p[J];
-        softmax<L, J>(logits + t * E, l, E, p);
-#pragma unroll
-        for (int j = 0; j < J; ++j) sum[j] += p[j];
+        load_scores<L, C, VEC>(logits + t * E, l, E, p);
         for (int r = l; r < k; r += L) {
             const int e = idx[t * k + r];
             if ((unsigned)e < (unsigned)E) atomicAdd(&c[e], 1);
         }
+        softmax<L>(p);
+#pragma unroll
+        for (int j = 0; j < J; ++j) sum[j] += p[j];
         ++mine;
     }
     if (l == 0 && mine) atomicAdd(&n, mine);
+    // tokens side by side in sixteen lanes first
 #pragma unroll
-    for (int j = 0; j < J; ++j) s[sub][l + L * j] = sum[j];
+    for (int j = 0; j < J; ++j) {
+        if (L <= 2) sum[j] += other<1>(sum[j]);
+        if (L <= 4) sum[j] += __shfl_xor(sum[j], 4, 64);
+        if (L <= 8) sum[j] += __shfl_xor(sum[j], 8, 64);
+        if (threadIdx.x % JOINED < L) s[threadIdx.x / JOINED][expert_of<L>(l, j)] = sum[j];
+    }
     __syncthreads();
     for (int e = threadIdx.x; e < E; e += THREADS) {
         float v = 0.f;
-        for (int q = 0; q < TOKENS; ++q) v += s[q][e];
-        out.s[(int64_t)blockIdx.x * E + e] = v;
-        out.c[(int64_t)blockIdx.x * E + e] = c[e];
+#pragma unroll
+        for (int q = 0; q < THREADS / JOINED; ++q) v += s[q][e];
+        out.e[(int64_t)blockIdx.x * E + e] = {v, c[e]};
     }
     if (threadIdx.x == 0) out.n[blockIdx.x] = n;
+    if (threadIdx.x == 0 && blockIdx.x == 0) *out.ready = 0;
 }
 
-// The parts' sums, and the loss, by one workgroup: 1024 / 256 slices of the parts for each expert.
+// The parts' sums, by a workgroup for JOINT experts: 64 slices of the parts for each, eight parts in
+// flight in a slice.  One workgroup for all experts would read every part through one CU (512 parts
+// of 128 experts: 24 us).  The last one to finish adds the experts' parts of the loss, in order.
 constexpr int JOIN = 1024;
 
 __global__ __launch_bounds__(JOIN) void balance_join_kernel(BalanceParts in, int groups, int E, int k,
@@ -115,86 +172,117 @@ __global__ __launch_bounds__(JOIN) void balance_join_kernel(BalanceParts in, int
                                                             float* __restrict__ prob_sum,
                                                             int32_t* __restrict__ n_tokens,
                                                             float* __restrict__ loss) {
-    __shared__ double s[JOIN / MOE_MAX_E][MOE_MAX_E], product[JOIN / 64];
-    __shared__ int32_t c[JOIN / MOE_MAX_E][MOE_MAX_E];
+    constexpr int SLICES = JOIN / JOINT, AHEAD = 8;
+    __shared__ double s[SLICES][JOINT];
+    __shared__ int32_t c[SLICES][JOINT];
     __shared__ int64_t tokens[JOIN / 64];
-    const int e = threadIdx.x % MOE_MAX_E, slice = threadIdx.x / MOE_MAX_E;
-    constexpr int SLICES = JOIN / MOE_MAX_E;
+    __shared__ bool last;
+    const int col = threadIdx.x % JOINT, e = blockIdx.x * JOINT + col, slice = threadIdx.x / JOINT;
+    int64_t n = 0;
+    for (int q = threadIdx.x; q < groups; q += JOIN) n += in.n[q];
     double v = 0.0;
     int32_t m = 0;
     if (e < E)
-        for (int q = slice; q < groups; q += SLICES) {
-            v += (double)in.s[(int64_t)q * E + e];
-            m += in.c[(int64_t)q * E + e];
+        for (int q0 = slice; q0 < groups; q0 += SLICES * AHEAD) {
+            Part a[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                a[i] = q0 + i * SLICES < groups ? in.e[(int64_t)(q0 + i * SLICES) * E + e] : Part{0.f, 0};
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                v += (double)a[i].s;
+                m += a[i].c;
+            }
         }
-    s[slice][e] = v;
-    c[slice][e] = m;
-    int64_t n = 0;
-    for (int q = threadIdx.x; q < groups; q += JOIN) n += in.n[q];
+    // slices side by side in a wave, then the waves'
+#pragma unroll
+    for (int o = JOINT; o < 64; o <<= 1) {
+        v += __shfl_xor(v, o, 64);
+        m += __shfl_xor(m, o, 64);
+    }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) n += __shfl_xor(n, o, 64);
-    if ((threadIdx.x & 63) == 0) tokens[threadIdx.x >> 6] = n;
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) < JOINT) {
+        s[wave][col] = v;
+        c[wave][col] = m;
+    }
+    if ((threadIdx.x & 63) == 0) tokens[wave] = n;
     __syncthreads();
-    if (slice == 0) {
-        for (int q = 1; q < SLICES; ++q) {
-            v += s[q][e];
-            m += c[q][e];
+    if (wave == 0) {
+        v = 0.0;
+        m = 0;
+#pragma unroll
+        for (int q = 0; q < JOIN / 64; ++q) {
+            v += s[q][col];
+            m += c[q][col];
         }
-        if (e < E) {
+        if (threadIdx.x < JOINT && e < E) {
             counts[e] = m;
             prob_sum[e] = (float)v;
         }
-    }
-    double x = slice == 0 && e < E ? (double)m * v : 0.0;
+        double x = e < E ? (double)m * v : 0.0;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o, 64);
-    if ((threadIdx.x & 63) == 0) product[threadIdx.x >> 6] = x;
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    n = 0;
-    x = 0.0;
-    for (int q = 0; q < JOIN / 64; ++q) {
-        n += tokens[q];
-        x += product[q];
+        for (int o = 1; o < JOINT; o <<= 1) x += __shfl_xor(x, o, 64);
+        if (threadIdx.x == 0) {
+            __hip_atomic_store(&in.loss[blockIdx.x], x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            last = __hip_atomic_fetch_add(in.ready, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1 == gridDim.x;
+        }
     }
+    __syncthreads();
+    if (!last || threadIdx.x != 0) return;
+    n = 0;
+    for (int q = 0; q < JOIN / 64; ++q) n += tokens[q];
+    double x = 0.0;
+    for (unsigned q = 0; q < gridDim.x; ++q)
+        x += __hip_atomic_load(&in.loss[q], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     n_tokens[0] = (int32_t)n;
     loss[0] = n > 0 ? (float)(x * E / ((double)k * (double)n * (double)n)) : 0.f;
 }
 
-template <int L, int J>
+template <int L, int C, bool VEC>
 __global__ __launch_bounds__(THREADS) void balance_backward_kernel(const float* logits,
                                                                    const uint8_t* __restrict__ mask,
                                                                    const int32_t* __restrict__ counts,
                                                                    const int32_t* __restrict__ n_tokens,
-                                                                   int64_t T, int E, int k, float scale,
-                                                                   float* dlogits) {
-    constexpr int TOKENS = THREADS / L;
-    const int l = threadIdx.x % L, sub = threadIdx.x / L;
-    const double n = (double)max(n_tokens[0], 1);
-    const float f = (float)((double)scale * E / ((double)k * n * n));
+                                                                   int64_t first, int64_t T, int E, int k,
+                                                                   float scale, float* dlogits) {
+    constexpr int TOKENS = THREADS / L, J = 4 * C;
+    const int l = threadIdx.x % L;
+    const int64_t t = (first + blockIdx.x) * TOKENS + threadIdx.x / L;
+    if (t >= T) return;                                  // (all lanes of the token together)
+    float p[J];
+    load_scores<L, C, VEC>(logits + t * E, l, E, p);
+    const bool live = mask == nullptr || mask[t] != 0;
+    const int64_t n = max(n_tokens[0], 1);
+    const float f = (float)((double)scale * E / ((double)k * (double)n * (double)n));
     // The counts less their mean: the gradient is the same (a token's p sum to 1) and its
     // rounding a matter of how far they spread, not of how large they are.
-    int64_t total = 0;
-    for (int e = 0; e < E; ++e) total += counts[e];
-    const int64_t mean = total / E;
+    const int64_t mean = k * n / E;
     float c[J];
 #pragma unroll
-    for (int j = 0; j < J; ++j) c[j] = l + L * j < E ? (float)(counts[l + L * j] - mean) : 0.f;
-    for (int64_t t = (int64_t)blockIdx.x * TOKENS + sub; t < T; t += (int64_t)gridDim.x * TOKENS) {
-        float p[J];
-        const bool live = mask == nullptr || mask[t] != 0;
-        if (live) {
-            softmax<L, J>(logits + t * E, l, E, p);
-            float dot = 0.f;
+    for (int j = 0; j < J; ++j) {
+        const int e = expert_of<L>(l, j);
+        c[j] = (float)((e < E ? counts[e] : 0) - mean);
+    }
+    softmax<L>(p);
+    float dot = 0.f;
 #pragma unroll
-            for (int j = 0; j < J; ++j) dot = fmaf(p[j], c[j], dot);
-            dot = token_sum<L>(dot);
+    for (int j = 0; j < J; ++j) dot = fmaf(p[j], c[j], dot);
+    dot = token_sum<L>(dot);
 #pragma unroll
-            for (int j = 0; j < J; ++j) p[j] = p[j] * (c[j] - dot) * f;
+    for (int j = 0; j < J; ++j) p[j] = live ? p[j] * (c[j] - dot) * f : 0.f;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        const int e = expert_of<L>(l, 4 * i);
+        float* out = dlogits + t * E + e;
+        if (VEC) {
+            if (e < E) *(f32x4*)out = f32x4{p[4 * i], p[4 * i + 1], p[4 * i + 2], p[4 * i + 3]};
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (e + j < E) out[j] = p[4 * i + j];
         }
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-            if (l + L * j < E) dlogits[t * E + l + L * j] = live ? p[j] : 0.f;
     }
 }
 
@@ -207,49 +295,56 @@ struct Split {
     }
 };
 
+bool aligned(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+
 }  // namespace
 
-// f(L, J) of E experts
-#define MOE_LANES(f)             \
-    do {                         \
-        if (E <= 8) f(8, 1);     \
-        else if (E <= 16) f(16, 1); \
-        else if (E <= 32) f(32, 1); \
-        else if (E <= 64) f(64, 1); \
-        else if (E <= 128) f(64, 2); \
-        else f(64, 4);           \
+// f(L, C, VEC) of E experts: lanes of a token, chunks of four experts in each
+#define MOE_LANES(f, VEC)                \
+    do {                                 \
+        if (E <= 8) f(2, 1, VEC);        \
+        else if (E <= 16) f(4, 1, VEC);  \
+        else if (E <= 32) f(8, 1, VEC);  \
+        else if (E <= 64) f(16, 1, VEC); \
+        else if (E <= 128) f(16, 2, VEC); \
+        else f(16, 4, VEC);              \
     } while (0)
 
-size_t balance_loss_ws_bytes(int64_t T, int E) { return (size_t)(Split(T).groups * (2 * E + 1) * 4) + 256; }
+size_t balance_loss_ws_bytes(int64_t T, int E) {
+    return (size_t)(Split(T).groups * (2 * E + 1) * 4) + MOE_MAX_E / JOINT * 8 + 256;
+}
 
 int launch_balance_loss(const float* logits, const int32_t* idx, const uint8_t* mask, int64_t T, int E,
                         int k, int32_t* counts, float* prob_sum, int32_t* n_tokens, float* loss,
                         void* ws, hipStream_t s) {
     const Split split(T);
     const BalanceParts parts = parts_at(ws, split.groups, E);
-#define MOE_BL(L, J)                                                                             \
-    hipLaunchKernelGGL((balance_parts_kernel<L, J>), dim3((unsigned)split.groups), dim3(THREADS), 0, s, \
+#define MOE_BL(L, C, VEC)                                                                               \
+    hipLaunchKernelGGL((balance_parts_kernel<L, C, VEC>), dim3((unsigned)split.groups), dim3(THREADS), 0, s, \
                        logits, idx, mask, T, E, k, split.per, parts)
-    MOE_LANES(MOE_BL);
+    if (E % 4 == 0 && aligned(logits)) MOE_LANES(MOE_BL, true);
+    else MOE_LANES(MOE_BL, false);
 #undef MOE_BL
     const int st = launch_status();
     if (st != MOE_OK) return st;
-    hipLaunchKernelGGL(balance_join_kernel, dim3(1), dim3(JOIN), 0, s, parts, (int)split.groups, E, k, counts,
-                       prob_sum, n_tokens, loss);
+    hipLaunchKernelGGL(balance_join_kernel, dim3((unsigned)ceil_div(E, JOINT)), dim3(JOIN), 0, s, parts,
+                       (int)split.groups, E, k, counts, prob_sum, n_tokens, loss);
     return launch_status();
 }
 
 int launch_balance_loss_backward(const float* logits, const uint8_t* mask, const int32_t* counts,
                                  const int32_t* n_tokens, int64_t T, int E, int k, float scale,
                                  float* dlogits, hipStream_t s) {
-    if (T == 0) return MOE_OK;
-#define MOE_BL(L, J)                                                                                  \
-    hipLaunchKernelGGL((balance_backward_kernel<L, J>),                                               \
-                       dim3((unsigned)std::min<int64_t>(ceil_div(T, THREADS / L), 2048)), dim3(THREADS), 0, s, \
-                       logits, mask, counts, n_tokens, T, E, k, scale, dlogits)
-    MOE_LANES(MOE_BL);
+    const bool vec = E % 4 == 0 && aligned(logits) && aligned(dlogits);
+    const int lanes = E <= 8 ? 2 : E <= 16 ? 4 : E <= 32 ? 8 : 16;
+    return launch_groups(ceil_div(T, THREADS / lanes), THREADS, [&](int64_t first, unsigned groups) {
+#define MOE_BL(L, C, VEC)                                                                               \
+    hipLaunchKernelGGL((balance_backward_kernel<L, C, VEC>), dim3(groups), dim3(THREADS), 0, s, logits, mask, \
+                       counts, n_tokens, first, T, E, k, scale, dlogits)
+        if (vec) MOE_LANES(MOE_BL, true);
+        else MOE_LANES(MOE_BL, false);
 #undef MOE_BL
-    return launch_status();
+    });
 }
 
 }  // namespace moe

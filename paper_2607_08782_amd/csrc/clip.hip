@@ -10,7 +10,7 @@ namespace moe {
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int CHUNK = 16384;
+constexpr int CHUNK = 8192;
 constexpr int TABLE = 96;                                // tensors a launch (kernel arguments: 4 KB)
 
 struct Tensors {
@@ -22,14 +22,15 @@ struct Tensors {
     int n;
 };
 
-// The tensor of a workgroup's chunk.
+// The tensor of a workgroup's chunk: the last that starts at or before it.  A wave compares the
+// whole table at once (a search's seven loads in turn are longer than a small tensor takes).
 __device__ __forceinline__ int tensor_of(const Tensors& t, uint32_t chunk) {
-    int lo = 0, hi = t.n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (t.first[mid] <= chunk) lo = mid; else hi = mid - 1;
-    }
-    return lo;
+    const int lane = threadIdx.x & 63;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < TABLE; i += 64)
+        n += __popcll(__ballot(i + lane < t.n && t.first[min(i + lane, TABLE - 1)] <= chunk));
+    return __builtin_amdgcn_readfirstlane(n - 1);
 }
 
 __device__ __forceinline__ double lanes_sum64(double v) {
@@ -38,23 +39,41 @@ __device__ __forceinline__ double lanes_sum64(double v) {
     return v;
 }
 
+// A chunk's pieces of a thread, AHEAD of them in flight: f(piece, its place).
+constexpr int AHEAD = 4;
+
+template <typename Elem, int V, typename F>
+__device__ __forceinline__ void pieces(const Elem* p, int n, const F& f) {
+    constexpr int ROUND = THREADS * V;
+    int c = threadIdx.x * V;
+    for (; c + (AHEAD - 1) * ROUND + V <= n; c += AHEAD * ROUND) {
+        Piece<Elem, V> a[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) a[i].load(p + c + i * ROUND);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) f(a[i], c + i * ROUND);
+    }
+    for (; c + V <= n; c += ROUND) {
+        Piece<Elem, V> a;
+        a.load(p + c);
+        f(a, c);
+    }
+}
+
 template <typename Elem, int V>
 __device__ __forceinline__ double squares(const Elem* p, int n) {
     double sum = 0.0;
-    for (int c = threadIdx.x * V; c + V <= n; c += THREADS * V) {
-        Piece<Elem, V> a;
-        float v[V];
-        a.load(p + c);
+    auto add = [&](const auto& a) {
+        float v[sizeof(a.u) / sizeof(Elem)];
         a.values(v);
 #pragma unroll
-        for (int j = 0; j < V; ++j) sum = fma((double)v[j], (double)v[j], sum);
-    }
+        for (float x : v) sum = fma((double)x, (double)x, sum);
+    };
+    pieces<Elem, V>(p, n, [&](const Piece<Elem, V>& a, int) { add(a); });
     if (V > 1 && (int)threadIdx.x < n % V) {             // the last few
         Piece<Elem, 1> a;
-        float v[1];
         a.load(p + n / V * V + threadIdx.x);
-        a.values(v);
-        sum = fma((double)v[0], (double)v[0], sum);
+        add(a);
     }
     return sum;
 }
@@ -98,24 +117,19 @@ __global__ __launch_bounds__(JOIN) void grad_norm_kernel(const double* __restric
 // p and out may be the same.
 template <typename Elem, int V>
 __device__ __forceinline__ void scaled(const Elem* p, Elem* out, int n, float factor) {
-    for (int c = threadIdx.x * V; c + V <= n; c += THREADS * V) {
-        Piece<Elem, V> a;
-        float v[V];
-        a.load(p + c);
+    auto put = [&](auto a, int c) {
+        float v[sizeof(a.u) / sizeof(Elem)];
         a.values(v);
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] *= factor;
+        for (float& x : v) x *= factor;
         a.set(v);
         a.store(out + c);
-    }
+    };
+    pieces<Elem, V>(p, n, [&](const Piece<Elem, V>& a, int c) { put(a, c); });
     if (V > 1 && (int)threadIdx.x < n % V) {
         Piece<Elem, 1> a;
-        float v[1];
         a.load(p + n / V * V + threadIdx.x);
-        a.values(v);
-        v[0] *= factor;
-        a.set(v);
-        a.store(out + n / V * V + threadIdx.x);
+        put(a, n / V * V + (int)threadIdx.x);
     }
 }
 

@@ -36,9 +36,23 @@ struct I8Args {
     int N;                               // output columns: f (gate/up) or d
     bf16_t* out;                         // h or y
     int64_t pitch;                       // its rows' elements
+    uint32_t* most;                      // bits of the largest |h| of a row's blocks [.][blocks]
+    int blocks;                          // (of 16 or 32 columns: a strip's, or half a wave's of a tile)
+    const bf16_t* h;                     // down, strips that quantize: h's rows [.][P]
+    int K;                               // and their columns
+    int32_t* part;                       // split: sums of the slices of K [slices][rows][N]
+    int64_t room;                        // sums that part holds
+    int32_t* split;                      // and how many slices there are (device)
+    int64_t rows;                        // rows of all groups at most
+    int slices;                          // strips: slices of K
     int strips;                          // strips a group
     int slots;                           // groups that can hold rows at once
 };
+
+// Bits (as a float) of the larger magnitude of two packed bf16 values.
+__device__ __forceinline__ uint32_t most_of2(uint32_t w) {
+    return max(w << 16 & 0x7fffffffu, w & 0x7fff0000u);
+}
 
 // ---------------------------------------------------------------------------
 // Strips: groups of few rows, bound by the weight bytes.  A workgroup holds 16 TILES weight rows
@@ -51,14 +65,23 @@ struct StripStep {
     i32x4 b[TILES][2], a[MS][2];
 };
 
-template <bool SWIGLU, int W, int TILES, int MS, int D>
-__device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int n0, int row0, int rows) {
+constexpr int QUANT_BYTES = 32 * 1024;                    // codes of a strip's rows in LDS, at most
+
+// QUANT (down): p.h's rows, as many as `codes` holds at a time, are quantized as the strip begins, by
+// all of its threads, and their scales go to `row_scale`.  SPLIT (down): the strip's slice of K, its
+// sums to p.part.
+template <bool SWIGLU, int W, int TILES, int MS, int D, bool QUANT = false, bool SPLIT = false>
+__device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int n0, int row0, int rows,
+                                           int8_t* codes = nullptr, float* row_scale = nullptr,
+                                           int slice = 0) {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int ROWS = 16 * TILES, LD = ROWS + 4, BM = 16 * MS;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int i16 = lane & 15, quarter = lane >> 4;
-    const int KT = p.P / STEP;
+    // steps of K, of a slice those of its own
+    const int per = SPLIT ? (p.P / STEP + p.slices - 1) / p.slices : 0;
+    const int begin = SPLIT ? slice * per : 0, KT = SPLIT ? min(begin + per, p.P / STEP) : p.P / STEP;
     // weight rows of the strip: past the matrix's columns (of the gate half, past its N) they
     // read as zero
     const int valid = max(min(SWIGLU ? ROWS / 2 : ROWS, p.N - n0), 0);
@@ -73,13 +96,16 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
     auto rsrc = [](const void* base, int bytes) {
         return __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, bytes, RSRC_WORD3);
     };
-    for (int m0 = 0; m0 < rows; m0 += BM) {
+    const int block = QUANT ? min(BM, QUANT_BYTES / (p.P + 16)) : BM;
+    for (int m0 = 0; m0 < rows; m0 += block) {
         // rows past the group repeat its last one; their sums are not stored
         const int8_t* at[MS];
+        const int here = min(rows - m0, block), pitch = p.P + 16;    // (the latter: of rows in LDS)
 #pragma unroll
         for (int m = 0; m < MS; ++m) {
             const int r = row0 + min(m0 + 16 * m + i16, rows - 1);
-            at[m] = p.a + (int64_t)(p.a_rows ? p.a_rows[r] : r) * p.P + quarter * 16;
+            if (QUANT) at[m] = codes + min(i16, here - 1) * pitch + quarter * 16;
+            else at[m] = p.a + (int64_t)(p.a_rows ? p.a_rows[r] : r) * p.P + quarter * 16;
         }
         i32x4 acc[MS][TILES];
 #pragma unroll
@@ -87,10 +113,9 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
 #pragma unroll
             for (int j = 0; j < TILES; ++j) acc[m][j] = i32x4{0, 0, 0, 0};
         // past the end of K: no traffic of the weights, and the last step's rows again
-        auto load = [&](StripStep<MS, TILES>& s, int t) {
+        auto load_b = [&](StripStep<MS, TILES>& s, int t) {
             const int bytes = t < KT ? valid * p.P - t * STEP : 0;
             const auto lo = rsrc(w_lo + (int64_t)t * STEP, bytes), hi = rsrc(w_hi + (int64_t)t * STEP, bytes);
-            const int ta = min(t, KT - 1) * STEP;
 #pragma unroll
             for (int j = 0; j < TILES; ++j)
 #pragma unroll
@@ -98,6 +123,9 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
                     s.b[j][u] = __builtin_bit_cast(
                         i32x4, __builtin_amdgcn_raw_buffer_load_b128(SWIGLU && j >= TILES / 2 ? hi : lo,
                                                                      boff[j], 64 * u, 0));
+        };
+        auto load_a = [&](StripStep<MS, TILES>& s, int t) {
+            const int ta = min(t, KT - 1) * STEP;
 #pragma unroll
             for (int m = 0; m < MS; ++m)
 #pragma unroll
@@ -116,13 +144,45 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
         };
         StripStep<MS, TILES> s[D];
 #pragma unroll
-        for (int i = 0; i < D; ++i) load(s[i], wave + i * W);
-        for (int t = wave; t < KT; t += D * W)
+        for (int i = 0; i < D; ++i) load_b(s[i], begin + wave + i * W);
+        if constexpr (QUANT) {
+            __syncthreads();                             // the last row block's codes are read
+            const bf16_t* const h = p.h + (int64_t)(row0 + m0) * p.P;
+            for (int r = wave; r < here; r += W) {
+                const uint32_t* const most = p.most + (int64_t)(row0 + m0 + r) * p.blocks;
+                uint32_t top = 0;
+                for (int b = lane; b < p.blocks; b += 64) top = max(top, most[b]);
+                top = lanes_max(top);
+                if (lane == 0) ((uint32_t*)row_scale)[r] = top;
+            }
+            __syncthreads();
+            const int chunks = p.P / 8;
+            for (int r = 0; r < here; ++r) {
+                const Int8Scale scale(((const uint32_t*)row_scale)[r]);
+                for (int c = tid; c < chunks; c += 64 * W) {
+                    Piece<bf16_t, 8> piece;
+                    float v[8];
+                    piece.load(h + (int64_t)r * p.P + c * 8);
+                    piece.values(v);
+                    if (c * 8 + 8 > p.K)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (c * 8 + e >= p.K) v[e] = 0.f;
+                    scale.template store<true>(v, codes + r * pitch + c * 8);
+                }
+            }
+            __syncthreads();
+            if (tid < here) row_scale[tid] = Int8Scale(((const uint32_t*)row_scale)[tid]).s;
+        }
+#pragma unroll
+        for (int i = 0; i < D; ++i) load_a(s[i], begin + wave + i * W);
+        for (int t = begin + wave; t < KT; t += D * W)
 #pragma unroll
             for (int i = 0; i < D; ++i) {
                 // (past the end: zero weights)
                 multiply(s[i]);
-                load(s[i], t + (i + D) * W);
+                load_b(s[i], t + (i + D) * W);
+                load_a(s[i], t + (i + D) * W);
             }
 
         __syncthreads();                                 // the last row block's sums are read
@@ -136,9 +196,16 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
         constexpr int PER_ROW = (SWIGLU ? ROWS / 2 : ROWS) / 4;
         for (int i = tid; i < BM * PER_ROW; i += 64 * W) {
             const int r = i / PER_ROW, c = (i % PER_ROW) * 4;
-            if (m0 + r >= rows || n0 + c >= p.N) continue;
-            const int row = row0 + m0 + r;
-            const float sx = p.as[p.a_rows ? p.a_rows[row] : row];
+            const bool live = r < here && n0 + c < p.N;
+            const int row = row0 + min(m0 + r, rows - 1);
+            if constexpr (SPLIT) {
+                i32x4 v = *(const i32x4*)&red[r * LD + c];
+#pragma unroll
+                for (int q = 1; q < W; ++q) v += *(const i32x4*)&red[(q * BM + r) * LD + c];
+                if (live) *(i32x4*)(p.part + (slice * (int64_t)first_row(p, p.n_groups) + row) * p.N + n0 + c) = v;
+                continue;
+            }
+            const float sx = QUANT ? row_scale[min(r, here - 1)] : p.as[p.a_rows ? p.a_rows[row] : row];
             // the sums of a column block at their scales; columns past N: some scale
             auto sum = [&](int col, int first, float (&out)[4]) {
                 i32x4 v = *(const i32x4*)&red[r * LD + col];
@@ -154,23 +221,35 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
                 sum(ROWS / 2 + c, p.N, b);
                 silu(y);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] *= b[e];
+                for (int e = 0; e < 4; ++e) y[e] = n0 + c + e < p.N ? y[e] * b[e] : 0.f;
             }
+            const uint2 w = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
             // (h's rows have room past N)
-            *(uint2*)(p.out + row * p.pitch + n0 + c) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+            if (live) *(uint2*)(p.out + row * p.pitch + n0 + c) = w;
+            if (SWIGLU) {
+                // the strip's columns of the row are the PER_ROW lanes side by side
+                uint32_t most = max(most_of2(w.x), most_of2(w.y));
+#pragma unroll
+                for (int o = 1; o < PER_ROW; o <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
+                if (c == 0 && live) p.most[(int64_t)row * p.blocks + n0 / (4 * PER_ROW)] = most;
+            }
         }
     }
 #endif
 }
 
 // MAX_MS = 1: no group holds more than 16 rows.  Otherwise each group takes the row blocks it needs.
-template <bool SWIGLU, int W, int TILES, int MAX_MS>
+template <bool SWIGLU, int W, int TILES, int MAX_MS, int D, bool QUANT, bool SPLIT>
 __global__ __launch_bounds__(64 * W, 2) void strip_int8_kernel(I8Args p) {
     constexpr int SUMS = W * 16 * MAX_MS * (16 * TILES + 4);
     static_assert(SUMS * 4 <= 80 * 1024, "two workgroups share a CU's LDS");
     __shared__ __attribute__((aligned(16))) int red[SUMS];
-    const int slot = blockIdx.x / p.strips;
-    const int n0 = ((int)blockIdx.x - slot * p.strips) * 16 * TILES / (SWIGLU ? 2 : 1);
+    __shared__ __attribute__((aligned(16))) int8_t codes[QUANT ? QUANT_BYTES : 16];
+    __shared__ float row_scale[16];
+    const int of_group = SPLIT ? p.strips * p.slices : p.strips, slot = blockIdx.x / of_group;
+    const int strip = (int)blockIdx.x - slot * of_group, slice = SPLIT ? strip / p.strips : 0;
+    const int n0 = (strip - slice * p.strips) * 16 * TILES / (SWIGLU ? 2 : 1);
+    if (SPLIT && blockIdx.x == 0 && threadIdx.x == 0) *p.split = p.slices;
     Group of;
     if (p.slots < p.n_groups) {
         of = nth_group(p, slot);
@@ -180,9 +259,17 @@ __global__ __launch_bounds__(64 * W, 2) void strip_int8_kernel(I8Args p) {
         of.rows = __builtin_amdgcn_readfirstlane(first_row(p, slot + 1)) - of.row0;
     }
     if (of.rows <= 0) return;
-    if (MAX_MS == 1 || of.rows <= 16) strip_rows<SWIGLU, W, TILES, 1, 2>(p, red, of.g, n0, of.row0, of.rows);
-    else if (of.rows <= 32) strip_rows<SWIGLU, W, TILES, 2, 2>(p, red, of.g, n0, of.row0, of.rows);
-    else strip_rows<SWIGLU, W, TILES, 4, 2>(p, red, of.g, n0, of.row0, of.rows);
+    if constexpr (QUANT) {
+        strip_rows<SWIGLU, W, TILES, 1, D, true>(p, red, of.g, n0, of.row0, of.rows, codes, row_scale);
+    } else {
+        auto rows = [&](auto blocks) {
+            strip_rows<SWIGLU, W, TILES, decltype(blocks)::value, D, false, SPLIT>(p, red, of.g, n0, of.row0,
+                                                                                  of.rows, nullptr, nullptr, slice);
+        };
+        if (MAX_MS == 1 || of.rows <= 16) rows(std::integral_constant<int, 1>{});
+        else if (of.rows <= 32) rows(std::integral_constant<int, 2>{});
+        else rows(std::integral_constant<int, MAX_MS>{});
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -222,11 +309,22 @@ struct TileShape {
 };
 
 struct I8Tile {
-    int row0, valid, n0;
+    int row0, valid, n0, slice;
     uint64_t w, ws;                                      // its group's weight codes and scales
 };
 
-template <bool SWIGLU, int WM, int TM, int TN, int RING>
+// Slices of K of a product whose tiles leave workgroups without one: as many, of one, two and four,
+// as there are workgroups for, of 2048 columns at least, as far as their sums have room.
+constexpr int SLICE_STEPS = 32, MAX_SLICES = 4;
+
+__device__ __forceinline__ int slices_of(int tiles, int steps, int64_t sums, int64_t room) {
+    int n = 1;
+    while (n < MAX_SLICES && 2 * n * tiles <= (int)gridDim.x && steps >= 2 * n * SLICE_STEPS && 2 * n * sums <= room)
+        n *= 2;
+    return n;
+}
+
+template <bool SWIGLU, int WM, int TM, int TN, int RING, bool SPLIT>
 __global__ __launch_bounds__(64 * 2 * WM, 2) void tile_int8_kernel(I8Args p) {
 #ifdef __HIP_DEVICE_COMPILE__
     typedef TileShape<WM, TM, TN, RING> S;
@@ -241,7 +339,8 @@ __global__ __launch_bounds__(64 * 2 * WM, 2) void tile_int8_kernel(I8Args p) {
     const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / 2, wn = wave % 2;              // a SIMD's waves hold rows of both halves
-    const int n_tiles = (p.N + BN_OUT - 1) / BN_OUT, KT = p.P / HALF_LINE;
+    int n_tiles = (p.N + BN_OUT - 1) / BN_OUT;
+    const int steps = p.P / HALF_LINE;
     for (int g = tid; g <= p.n_groups; g += S::THREADS) s_off[g] = first_row(p, g);
     __syncthreads();
     if (wave == 0) {
@@ -250,6 +349,24 @@ __global__ __launch_bounds__(64 * 2 * WM, 2) void tile_int8_kernel(I8Args p) {
                [](int rows) { return (int)ceil_div(rows, BM) - high_tiles<BM>(rows); });
     }
     __syncthreads();
+    // few tiles: slices of K, each a column tile of its own
+    int slices = 1;
+    if constexpr (SPLIT) {
+        slices = slices_of(__builtin_amdgcn_readfirstlane(s_high[p.n_groups] + s_low[p.n_groups]), steps,
+                           (int64_t)__builtin_amdgcn_readfirstlane(s_off[p.n_groups]) * p.N, p.room);
+        if (blockIdx.x == 0 && tid == 0) *p.split = slices;
+        if (slices > 1) {
+            __syncthreads();
+            for (int g = tid; g <= p.n_groups; g += S::THREADS) {
+                s_high[g] *= slices;
+                s_low[g] *= slices;
+            }
+            n_tiles *= slices;
+            __syncthreads();
+        }
+    }
+    const int per = (steps + slices - 1) / slices;
+    const int64_t slice_rows = SPLIT ? __builtin_amdgcn_readfirstlane(s_off[p.n_groups]) : 0;
     const TileShare<BM> tiles(s_off, s_high, s_low, p.n_groups, n_tiles);
     const int n_list = tiles.n_list;                     // this workgroup's tiles
     if (n_list <= 0) return;
@@ -264,7 +381,8 @@ __global__ __launch_bounds__(64 * 2 * WM, 2) void tile_int8_kernel(I8Args p) {
         t.ws = (uint64_t)p.ws[at.g];
         t.row0 = at.row0;
         t.valid = at.valid;
-        t.n0 = at.n * BN_OUT;
+        t.slice = SPLIT ? at.n % slices : 0;
+        t.n0 = (SPLIT ? at.n / slices : at.n) * BN_OUT;
         s_tile[q % TILE_LIST] = t;
     };
     auto tile_at = [&](int q) {
@@ -274,8 +392,10 @@ __global__ __launch_bounds__(64 * 2 * WM, 2) void tile_int8_kernel(I8Args p) {
         t.row0 = __builtin_amdgcn_readfirstlane(t.row0);
         t.valid = __builtin_amdgcn_readfirstlane(t.valid);
         t.n0 = __builtin_amdgcn_readfirstlane(t.n0);
+        t.slice = SPLIT ? __builtin_amdgcn_readfirstlane(t.slice) : 0;
         return t;
     };
+    auto steps_of = [&](const I8Tile& t) { return SPLIT ? min(per, steps - t.slice * per) : steps; };
     list_tiles(0);
     list_tiles(TILE_LIST / 2);
     __syncthreads();
@@ -309,7 +429,7 @@ __global__ __launch_bounds__(64 * 2 * WM, 2) void tile_int8_kernel(I8Args p) {
         if (p.a_rows != nullptr) {
             // Issued a tile ago.  The waits of the loop are for older loads than a step's,
             // but a tile of fewer steps than the ring ends before the first of them.
-            if (lq == 0 || KT < RING) {
+            if (lq == 0 || steps < RING) {
                 wait_vm<0>();
                 asm volatile("s_barrier" ::: "memory");
             }
@@ -348,8 +468,8 @@ __global__ __launch_bounds__(64 * 2 * WM, 2) void tile_int8_kernel(I8Args p) {
                                                          col * 4, 0, 0, 0);
             }
         }
-        at_k = 0;
-        left_steps = KT;
+        at_k = t.slice * per * HALF_LINE;
+        left_steps = steps_of(t);
     };
     // direct load i of the stream's next step
     auto load1 = [&](char* st, int i) {
@@ -427,7 +547,8 @@ __global__ __launch_bounds__(64 * 2 * WM, 2) void tile_int8_kernel(I8Args p) {
         next = next == (RING - 1) * S::STAGE ? 0 : next + S::STAGE;
     };
     // stores of an epilogue: newer than the loads that the next RING - 2 waits are for
-    constexpr int STORES = SWIGLU ? TM * TN : 2 * TM * TN;
+    // (of a split tile there are twice as many: its waits are stricter than they need be)
+    constexpr int STORES = SWIGLU ? TM * TN / 2 * 3 : 2 * TM * TN;
     int fresh = 0;
     // the next step has landed: outstanding may be the ones after it, and stores
     auto landed = [&]() {
@@ -441,6 +562,7 @@ __global__ __launch_bounds__(64 * 2 * WM, 2) void tile_int8_kernel(I8Args p) {
     };
     for (int q = 0; q < n_list; ++q) {
         const I8Tile cur = tile_at(q);
+        const int KT = steps_of(cur);
         if (q > 0 && q % (TILE_LIST / 2) == 0) list_tiles(q + TILE_LIST / 2);
         if (wm * 32 * TM >= cur.valid) {                 // no row of this wave's: its loads only
 #pragma clang loop unroll(disable)
@@ -496,8 +618,27 @@ __global__ __launch_bounds__(64 * 2 * WM, 2) void tile_int8_kernel(I8Args p) {
         // Every store is issued, those past the group's rows or the output's columns dropped
         // by the descriptor: the waits above count them.
         const int lr = wm * 32 * TM + r32, slot = q & (SCALES - 1);
+        if (SPLIT && slices > 1) {
+            const __amdgpu_buffer_rsrc_t rp = __builtin_amdgcn_make_buffer_rsrc(
+                (void*)(p.part + (cur.slice * slice_rows + cur.row0) * p.N), (short)0, cur.valid * p.N * 4, RSRC_WORD3);
+#pragma unroll
+            for (int m = 0; m < TM; ++m)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const int col = cur.n0 + wn * (BN / 2) + 32 * j + 16 * half + e;
+                        __builtin_amdgcn_raw_buffer_store_b128(
+                            u32x4{(uint32_t)acc[m][j][e], (uint32_t)acc[m][j][e + 1], (uint32_t)acc[m][j][e + 2],
+                                  (uint32_t)acc[m][j][e + 3]},
+                            rp, col < p.N ? ((lr + 32 * m) * p.N + col) * 4 : A_OOB, 0, 0);
+                    }
+            continue;
+        }
         const __amdgpu_buffer_rsrc_t ry = __builtin_amdgcn_make_buffer_rsrc(
             (void*)(p.out + (int64_t)cur.row0 * p.pitch), (short)0, cur.valid * (int)p.pitch * 2, RSRC_WORD3);
+        const __amdgpu_buffer_rsrc_t rm = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)(p.most + (int64_t)cur.row0 * p.blocks), (short)0, cur.valid * p.blocks * 4, RSRC_WORD3);
         const int lc = wn * (SWIGLU ? BN / 4 : BN / 2) + 16 * half;        // column in the tile
 #pragma unroll
         for (int m = 0; m < TM; ++m) {
@@ -513,16 +654,29 @@ __global__ __launch_bounds__(64 * 2 * WM, 2) void tile_int8_kernel(I8Args p) {
                     silu(v);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) v[e] *= (float)acc[m][TN / 2 + j][e] * sx * sw[BN / 2 + e];
+                    if (cur.n0 + BN_OUT > p.N)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (cur.n0 + c + e >= p.N) v[e] = 0.f;
                 }
+                uint32_t most = 0;
 #pragma unroll
                 for (int e = 0; e < 16; e += 8) {
                     u32x4 w;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(v[e + 2 * i], v[e + 2 * i + 1]);
+                    for (int i = 0; i < 4; ++i) {
+                        w[i] = pack_bf16x2(v[e + 2 * i], v[e + 2 * i + 1]);
+                        if (SWIGLU) most = max(most, most_of2(w[i]));
+                    }
                     const int col = cur.n0 + c + e;
                     // (h's rows have room for whole tiles)
                     __builtin_amdgcn_raw_buffer_store_b128(
                         w, ry, SWIGLU || col < p.N ? ((lr + 32 * m) * (int)p.pitch + col) * 2 : A_OOB, 0, 0);
+                }
+                if (SWIGLU) {
+                    most = max(most, (uint32_t)__shfl_xor((int)most, 32, 64));
+                    __builtin_amdgcn_raw_buffer_store_b32(
+                        most, rm, half || cur.n0 + c >= p.N ? A_OOB : ((lr + 32 * m) * p.blocks + (cur.n0 + c) / 32) * 4, 0, 0);
                 }
             }
         }
@@ -530,57 +684,208 @@ __global__ __launch_bounds__(64 * 2 * WM, 2) void tile_int8_kernel(I8Args p) {
 #endif
 }
 
-template <bool SWIGLU, int WM, int TM, int TN, int RING>
-int launch_tiles(const I8Args& p, hipStream_t s) {
+// y of the slices' sums: four columns a thread, a workgroup's threads in one row.
+__global__ __launch_bounds__(256) void join_slices_kernel(I8Args p, int64_t first) {
+    const int slices = *p.split;
+    if (slices == 1) return;                             // the tiles wrote y
+    const int wide = (int)ceil_div(p.N, 1024);
+    const int64_t total = first_row(p, p.n_groups);
+    const int64_t at = first + blockIdx.x, row = at / wide;
+    const int c = (int)(at - row * wide) * 1024 + 4 * threadIdx.x;
+    // the row's group: the last that starts at or before it
+    const int lane = threadIdx.x & 63;
+    int g = -1;
+    for (int g0 = 0; g0 <= p.n_groups; g0 += 64) {
+        const int mine = min(g0 + lane, p.n_groups);
+        g += __popcll(__ballot(g0 + lane <= p.n_groups && first_row(p, mine) <= row));
+    }
+    if (row >= total || c >= p.N) return;
+    i32x4 v = *(const i32x4*)(p.part + row * p.N + c);
+    for (int q = 1; q < slices; ++q) v += *(const i32x4*)(p.part + (q * total + row) * p.N + c);
+    const float* const sw = p.ws[g] + c;
+    const float sx = p.as[row];
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (float)v[e] * sx * sw[e];
+    *(uint2*)(p.out + row * p.pitch + c) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+}
+
+int launch_join_slices(const I8Args& p, hipStream_t s) {
+    return launch_groups(p.rows * ceil_div(p.N, 1024), 256, [&](int64_t first, unsigned n) {
+        hipLaunchKernelGGL(join_slices_kernel, dim3(n), dim3(256), 0, s, p, first);
+    });
+}
+
+template <bool SWIGLU, int WM, int TM, int TN, int RING, bool SPLIT>
+int launch_tiles_of(const I8Args& p, hipStream_t s) {
     typedef TileShape<WM, TM, TN, RING> S;
     static LdsGrant grant;
-    const int st = allow_dynamic_lds((const void*)tile_int8_kernel<SWIGLU, WM, TM, TN, RING>, S::LDS, grant);
+    const int st = allow_dynamic_lds((const void*)tile_int8_kernel<SWIGLU, WM, TM, TN, RING, SPLIT>, S::LDS, grant);
     if (st != MOE_OK) return st;
     const int grid = num_cus() / NUM_XCD * NUM_XCD * (S::PER_EU * 4 / S::WAVES);
-    hipLaunchKernelGGL((tile_int8_kernel<SWIGLU, WM, TM, TN, RING>), dim3(grid), dim3(S::THREADS), S::LDS, s, p);
+    hipLaunchKernelGGL((tile_int8_kernel<SWIGLU, WM, TM, TN, RING, SPLIT>), dim3(grid), dim3(S::THREADS), S::LDS, s, p);
     return launch_status();
 }
+
+template <bool SWIGLU, int WM, int TM, int TN, int RING>
+int launch_tiles(const I8Args& p, hipStream_t s) {
+    if constexpr (!SWIGLU)
+        if (p.room > 0) {
+            const int st = launch_tiles_of<false, WM, TM, TN, RING, true>(p, s);
+            return st != MOE_OK ? st : launch_join_slices(p, s);
+        }
+    return launch_tiles_of<SWIGLU, WM, TM, TN, RING, false>(p, s);
+}
+
+// Whether down strips quantize h's rows themselves: a launch less, but every strip does it again
+// (FFN, with the launch and without: one token of DeepSeek-V2-Lite 20.7 and 18.8 us, of
+// Qwen3-30B-A3B 10.9 and 9.5; two Mixtral-shaped tokens 60.7 and 59.8; eight tokens 41.0 and 43.2,
+// 14.3 and 17.1).
+bool strips_quantize(int64_t max_rows, int f) {
+    return max_rows <= 2 && max_rows * (int8_cols(f) + 16) <= QUANT_BYTES;
+}
+
+template <bool SWIGLU, int W, int TILES, int D>
+int launch_strips_of(I8Args& p, int64_t max_rows, hipStream_t s) {
+    p.strips = (int)ceil_div(SWIGLU ? 2 * (int64_t)p.N : p.N, 16 * TILES);
+    if (SWIGLU) p.blocks = p.strips;                     // a strip is a block
+    const dim3 grid((unsigned)(p.slots * p.strips)), block(64 * W);
+    const bool few = max_rows <= 16;
+    if constexpr (!SWIGLU) {
+        if (strips_quantize(max_rows, p.K)) {
+            hipLaunchKernelGGL((strip_int8_kernel<false, W, TILES, 1, D, true, false>), grid, block, 0, s, p);
+            return launch_status();
+        }
+        // two slices of K where the strips alone give a CU one workgroup at most (Mixtral-shaped down
+        // product, 256 strips of K = 14336: 64 tokens 108 and 105 us, 32 tokens 93 and 91)
+        if ((int64_t)grid.x <= num_cus() && p.P >= 2 * SLICE_STEPS * HALF_LINE && 2 * p.rows * p.N <= p.room) {
+            p.slices = 2;
+            const dim3 more(grid.x * p.slices);
+            if (few) hipLaunchKernelGGL((strip_int8_kernel<false, W, TILES, 1, D, false, true>), more, block, 0, s, p);
+            else hipLaunchKernelGGL((strip_int8_kernel<false, W, TILES, 4, D, false, true>), more, block, 0, s, p);
+            const int st = launch_status();
+            return st != MOE_OK ? st : launch_join_slices(p, s);
+        }
+    }
+    if (few) hipLaunchKernelGGL((strip_int8_kernel<SWIGLU, W, TILES, 1, D, false, false>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((strip_int8_kernel<SWIGLU, W, TILES, 4, D, false, false>), grid, block, 0, s, p);
+    return launch_status();
+}
+
+// A short K gives a strip's waves few steps, and what a strip waits for at its start and end is
+// hidden by other workgroups: narrow strips, one step of loads in flight and registers for more
+// waves (FFN of 64 tokens, wide and two steps, narrow and one: DeepSeek-V2-Lite 97.3 and 91.2 us,
+// Qwen3-30B-A3B 22.7 and 20.3).  A long K: wide strips of gate and up rows, so that token rows are read
+// half as often (Mixtral-shaped 107 and 113), and two steps in the down product, whose strips are
+// few (16 tokens 73.2, with one 76.2).
+constexpr int SHORT_K = 16 * STEP;
 
 template <bool SWIGLU>
 int launch_strips(I8Args& p, int64_t max_rows, hipStream_t s) {
-    constexpr int W = 4, TILES = 4;
-    p.strips = (int)ceil_div(SWIGLU ? 2 * (int64_t)p.N : p.N, 16 * TILES);
-    const dim3 grid((unsigned)(p.slots * p.strips)), block(64 * W);
-    if (max_rows <= 16)
-        hipLaunchKernelGGL((strip_int8_kernel<SWIGLU, W, TILES, 1>), grid, block, 0, s, p);
-    else
-        hipLaunchKernelGGL((strip_int8_kernel<SWIGLU, W, TILES, 4>), grid, block, 0, s, p);
-    return launch_status();
+    if (p.P <= SHORT_K) return launch_strips_of<SWIGLU, 4, 2, 1>(p, max_rows, s);
+    if constexpr (SWIGLU) return launch_strips_of<true, 4, 4, 1>(p, max_rows, s);
+    else return launch_strips_of<false, 4, 2, 2>(p, max_rows, s);
 }
 
-// Strips while no group can hold more rows than this, tiles past it.
-constexpr int64_t STRIP_MAX_ROWS = 128;
+// Strips while no group can hold more rows than this, tiles past it (FFN, strips and tiles:
+// Mixtral-shaped, 32 tokens 91 and 97 us, 64 tokens 105 and 102, 96 tokens 127 and 105; 64
+// DeepSeek-V2-Lite experts, 64 tokens 91 and 97, 128 tokens 125 and 125; Qwen3-30B-A3B, 64 tokens 20
+// and 25, 128 tokens 32 and 27).
+constexpr int64_t STRIP_MAX_ROWS = 64;
 
-// Tiles of 256 x 256 from this many outputs of a product (a round of them over the chip), of
-// 128 x 128 below, counted over the rows that the call has room for.
-constexpr int64_t LARGE_WORK = (int64_t)256 * 256 * 256;
+// Tiles of 256 x 256 from this many outputs of a product, of 128 x 128 below, counted over the rows
+// that the call has room for (how many there are only the GPU knows).  Gate/up (FFN with 128 x 128
+// and 256 x 256, by millions of outputs): 2.2 32 and 39 us, 4.3 163 and 151, 6.3 35.9 and 39.5 but
+// 43.8 and 42.2, 17 67 and 60, 23 91 and 79.  Down, K short: 9 42 and 47, 13 42.1 and 47.2, 25 even,
+// 34 79 and 75; K long, where slices fill the chip: 1.6 122 and 125, 4.1 176 and 174, 6.4 224 and 202.
+// Outputs of a down product from which none is cut into slices: of an eighth of the rows that
+// there is room for, 256 x 256 tiles still fill a quarter of the chip.
+constexpr int64_t FILLED = 1 << 25;
+constexpr int64_t LARGE_UP = 1 << 22, LARGE_DOWN = 1 << 24, LARGE_SLICED = 1 << 22;
 
 template <bool SWIGLU>
-int launch_product(I8Args& p, int64_t max_rows, int64_t rows, hipStream_t s) {
+int launch_product(I8Args& p, int64_t max_rows, hipStream_t s) {
     if (max_rows <= STRIP_MAX_ROWS) return launch_strips<SWIGLU>(p, max_rows, s);
-    return rows * p.N >= LARGE_WORK ? launch_tiles<SWIGLU, 4, 2, 4, 4>(p, s) : launch_tiles<SWIGLU, 2, 2, 2, 4>(p, s);
+    if (SWIGLU) p.blocks = (int)ceil_div(p.N, 32);
+    const int64_t large = SWIGLU ? LARGE_UP : p.room > 0 ? LARGE_SLICED : LARGE_DOWN;
+    return p.rows * p.N >= large ? launch_tiles<SWIGLU, 4, 2, 4, 4>(p, s) : launch_tiles<SWIGLU, 2, 2, 2, 4>(p, s);
+}
+
+// ---------------------------------------------------------------------------
+// The hidden rows in 8 bits: a row's largest magnitude is that of its blocks', which the first
+// product left, so a row needs no pass of its own for it and any number of waves share one: a wave
+// takes 64 SEG chunks of eight values.
+template <int SEG>
+__global__ __launch_bounds__(256) void quantize_hidden_kernel(const bf16_t* __restrict__ h, int64_t rows,
+                                                              int cols, const uint32_t* __restrict__ most,
+                                                              int blocks, const int32_t* __restrict__ end,
+                                                              int end_base, int units, int64_t first,
+                                                              int8_t* __restrict__ q,
+                                                              float* __restrict__ scales) {
+    const int lane = threadIdx.x & 63;
+    const int64_t unit = (first + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int64_t row = unit / units;
+    const int part = (int)(unit - row * units);
+    if (row >= min(rows, (int64_t)end_base + end[0])) return;
+    const int P = (int)int8_cols(cols), chunks = P / 8;
+    Piece<bf16_t, 8> held[SEG];
+    auto chunk = [&](int i) { return (part * SEG + i) * 64 + lane; };
+#pragma unroll
+    for (int i = 0; i < SEG; ++i) held[i].load(h + row * P + (int64_t)min(chunk(i), chunks - 1) * 8);
+    uint32_t top = 0;
+    for (int b = lane; b < blocks; b += 64) top = max(top, most[row * blocks + b]);
+    const Int8Scale scale(lanes_max(top));
+    if (part == 0 && lane == 0) scales[row] = scale.s;
+#pragma unroll
+    for (int i = 0; i < SEG; ++i) {
+        const int c = chunk(i);
+        float v[8];
+        held[i].values(v);
+        if (c * 8 + 8 > cols)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (c * 8 + j >= cols) v[j] = 0.f;
+        if (c < chunks) scale.template store<true>(v, q + row * P + (int64_t)c * 8);
+    }
+}
+
+int launch_quantize_hidden(const I8Args& p, int64_t rows, int cols, const int32_t* end, int end_base, int8_t* q,
+                           float* scales, hipStream_t s) {
+    const int64_t lanes = int8_cols(cols) / 8;
+    const int seg = rows >= 1024 ? 4 : 1, units = (int)ceil_div(lanes, 64 * seg);
+    return launch_groups(ceil_div(rows * units, 4), 256, [&](int64_t first, unsigned n) {
+        if (seg == 4)
+            hipLaunchKernelGGL(quantize_hidden_kernel<4>, dim3(n), dim3(256), 0, s, p.out, rows, cols, p.most,
+                               p.blocks, end, end_base, units, first, q, scales);
+        else
+            hipLaunchKernelGGL(quantize_hidden_kernel<1>, dim3(n), dim3(256), 0, s, p.out, rows, cols, p.most,
+                               p.blocks, end, end_base, units, first, q, scales);
+    });
 }
 
 int64_t align256(int64_t x) { return (x + 255) & ~(int64_t)255; }
 
-// workspace: [h in bf16][h codes][h scales]
+// workspace: [h in bf16][h codes][h scales][largest |h| of a row's blocks of 16 columns or more]
+// [how many slices][sums of slices of K]
 struct Layout {
-    int64_t hq, hs, total;
-    Layout(int64_t rows, int f) {
+    int64_t hq, hs, most, split, part, room, total;      // room: sums of slices
+    Layout(int64_t rows, int d, int f) {
         hq = align256(rows * int8_cols(f) * 2);
         hs = hq + align256(rows * int8_cols(f));
-        total = hs + align256(rows * 4);
+        most = hs + align256(rows * 4);
+        split = most + align256(rows * ceil_div(f, 16) * 4);
+        part = split + 256;
+        // slices only where each has SLICE_STEPS, and as many sums as fill the chip's tiles
+        room = int8_cols(f) / HALF_LINE >= 2 * SLICE_STEPS ? std::min<int64_t>(MAX_SLICES * rows * d, 1 << 24) : 0;
+        total = part + align256(room * 4);
     }
 };
 
 }  // namespace
 
-size_t grouped_ffn_int8_ws_bytes(int64_t rows, int f) { return (size_t)Layout(rows, f).total + 256; }
+size_t grouped_ffn_int8_ws_bytes(int64_t rows, int d, int f, int n_groups) {
+    return (size_t)Layout(rows, d, f).total + 256;
+}
 
 int launch_grouped_ffn_int8(const int8_t* xq, const float* x_scale, int64_t T,
                             const int32_t* row_token, const int32_t* offsets, int n_groups, int lead,
@@ -588,7 +893,7 @@ int launch_grouped_ffn_int8(const int8_t* xq, const float* x_scale, int64_t T,
                             const int8_t* const* w2, const float* const* s2, int d, int f,
                             int64_t rows, void* y, void* ws, hipStream_t s) {
     if (rows == 0 || T == 0) return MOE_OK;
-    const Layout at(rows, f);
+    const Layout at(rows, d, f);
     char* base = (char*)ws;
     int8_t* hq = (int8_t*)(base + at.hq);
     float* hs = (float*)(base + at.hs);
@@ -603,6 +908,8 @@ int launch_grouped_ffn_int8(const int8_t* xq, const float* x_scale, int64_t T,
     p.n_groups = n_groups;
     p.slots = (int)std::min<int64_t>(n_groups, rows);
     p.lead = lead;
+    p.slices = 1;
+    p.room = 0;
     p.lead_rows = lead_rows;
     p.a = xq;
     p.as = x_scale;
@@ -611,11 +918,16 @@ int launch_grouped_ffn_int8(const int8_t* xq, const float* x_scale, int64_t T,
     p.N = f;
     p.out = (bf16_t*)base;
     p.pitch = int8_cols(f);
-    int st = launch_product<true>(p, max_rows, rows, s);
+    p.most = (uint32_t*)(base + at.most);
+    p.rows = rows;
+    int st = launch_product<true>(p, max_rows, s);
     if (st != MOE_OK) return st;
-    st = launch_quantize_int8(base, MOE_BF16, rows, f, p.pitch, hq, hs, offsets + n_groups - lead,
-                              lead * lead_rows, s);
-    if (st != MOE_OK) return st;
+    p.h = p.out;
+    p.K = f;
+    if (!strips_quantize(max_rows, f)) {
+        st = launch_quantize_hidden(p, rows, f, offsets + n_groups - lead, lead * lead_rows, hq, hs, s);
+        if (st != MOE_OK) return st;
+    }
     for (int i = 0; i < n_groups; ++i) {
         p.w[i] = w2[i];
         p.ws[i] = s2[i];
@@ -627,7 +939,11 @@ int launch_grouped_ffn_int8(const int8_t* xq, const float* x_scale, int64_t T,
     p.N = d;
     p.out = (bf16_t*)y;
     p.pitch = d;
-    return launch_product<false>(p, max_rows, rows, s);
+    p.part = (int32_t*)(base + at.part);
+    // (with so many rows that the tiles fill the chip however the rows fall, none)
+    p.room = rows * d < FILLED ? at.room : 0;
+    p.split = (int32_t*)(base + at.split);
+    return launch_product<false>(p, max_rows, s);
 }
 
 }  // namespace moe

@@ -137,16 +137,14 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
     return v;
 }
 
-// Rows of x, `pitch` elements apart, as codes [rows][int8_cols(cols)] and scales.  end
-// (nullable): rows from end[0] + end_base on are left alone.
 [[nodiscard]]
-int launch_quantize_int8(const void* x, int dtype, int64_t rows, int cols, int64_t pitch, int8_t* q,
-                         float* scales, const int32_t* end, int end_base, hipStream_t s);
+int launch_quantize_int8(const void* x, int dtype, int64_t rows, int cols, int8_t* q, float* scales,
+                         hipStream_t s);
 [[nodiscard]]
 int launch_dequantize_int8(const int8_t* q, const float* scales, int64_t rows, int cols, int dtype,
                            void* y, hipStream_t s);
 
-size_t grouped_ffn_int8_ws_bytes(int64_t rows, int f);
+size_t grouped_ffn_int8_ws_bytes(int64_t rows, int d, int f, int n_groups);
 // n_groups groups in all, the first `lead` of lead_rows rows each; rows: of all groups at most
 [[nodiscard]]
 int launch_grouped_ffn_int8(const int8_t* xq, const float* x_scale, int64_t T,

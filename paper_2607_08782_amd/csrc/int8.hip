@@ -11,26 +11,16 @@ constexpr int THREADS = 256;
 // first CH of them stay in registers in between, later ones are read again.
 template <typename Elem, int V, int CH, int W>
 __global__ __launch_bounds__(THREADS) void quantize_int8_kernel(const Elem* __restrict__ x, int64_t rows,
-                                                                int cols, int64_t pitch,
-                                                                int8_t* __restrict__ q,
-                                                                float* __restrict__ scales,
-                                                                const int32_t* __restrict__ end,
-                                                                int end_base) {
+                                                                int cols, int8_t* __restrict__ q,
+                                                                float* __restrict__ scales) {
     __shared__ uint32_t red[THREADS / 64];
     constexpr int NT = 64 * W, PER = THREADS / NT;       // threads of a row, rows of a workgroup
     constexpr bool NARROW = sizeof(Elem) == 2;
     const int tid = threadIdx.x % NT;
-    const int chunks = (int)ceil_div(cols, V), P = (int)int8_cols(cols);
-    if (end != nullptr) rows = min(rows, (int64_t)end_base + end[0]);
+    const int chunks = cols / V, P = (int)int8_cols(cols);
     for (int64_t r = (int64_t)blockIdx.x * PER + threadIdx.x / NT; r < rows; r += (int64_t)gridDim.x * PER) {
-        const Elem* xr = x + r * pitch;
+        const Elem* xr = x + r * cols;
         Piece<Elem, V> held[CH];
-        auto values = [&](const Piece<Elem, V>& p, int c, float (&v)[V]) {
-            p.values(v);
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (V > 1 && c * V + i >= cols) v[i] = 0.f;
-        };
         uint32_t most = 0;
 #pragma unroll
         for (int i = 0; i < CH; ++i)
@@ -38,14 +28,14 @@ __global__ __launch_bounds__(THREADS) void quantize_int8_kernel(const Elem* __re
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             float v[V];
-            values(held[i], tid + i * NT < chunks ? tid + i * NT : 0, v);
+            held[i].values(v);
             most = max(most, magnitude(v));
         }
         for (int c = tid + CH * NT; c < chunks; c += NT) {
             Piece<Elem, V> p;
             float v[V];
             p.load(xr + (int64_t)c * V);
-            values(p, c, v);
+            p.values(v);
             most = max(most, magnitude(v));
         }
         most = lanes_max(most);
@@ -63,31 +53,29 @@ __global__ __launch_bounds__(THREADS) void quantize_int8_kernel(const Elem* __re
         for (int i = 0; i < CH; ++i) {
             const int c = tid + i * NT;
             float v[V];
-            values(held[i], c, v);
+            held[i].values(v);
             if (c < chunks) scale.template store<NARROW>(v, qr + (int64_t)c * V);
         }
         for (int c = tid + CH * NT; c < chunks; c += NT) {
             Piece<Elem, V> p;
             float v[V];
             p.load(xr + (int64_t)c * V);
-            values(p, c, v);
+            p.values(v);
             scale.template store<NARROW>(v, qr + (int64_t)c * V);
         }
-        // the padding: whole chunks of zeros (the last chunk's own are stored with it)
-        for (int c = chunks * V + tid; c < P; c += NT) qr[c] = 0;
+        for (int c = cols + tid; c < P; c += NT) qr[c] = 0;
     }
 }
 
 template <typename Elem, int V>
-int quantize(const Elem* x, int64_t rows, int cols, int64_t pitch, int8_t* q, float* scales,
-             const int32_t* end, int end_base, hipStream_t s) {
-    const int chunks = (int)ceil_div(cols, V);
+int quantize(const Elem* x, int64_t rows, int cols, int8_t* q, float* scales, hipStream_t s) {
+    const int chunks = cols / V;
     const bool wave = chunks <= 64 * 4 && rows >= 1024;
     const int64_t groups = wave ? ceil_div(rows, THREADS / 64) : rows;
     const dim3 grid((unsigned)(groups < 65536 ? groups : 65536));
 #define MOE_Q8(CH, W)                                                                               \
-    hipLaunchKernelGGL((quantize_int8_kernel<Elem, V, CH, W>), grid, dim3(THREADS), 0, s, x, rows, cols, \
-                       pitch, q, scales, end, end_base)
+    hipLaunchKernelGGL((quantize_int8_kernel<Elem, V, CH, W>), grid, dim3(THREADS), 0, s, x, rows, cols, q, \
+                       scales)
     if (wave) {
         if (chunks <= 64) MOE_Q8(1, 1);
         else if (chunks <= 128) MOE_Q8(2, 1);
@@ -142,16 +130,14 @@ bool aligned(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 }  // namespace
 
-int launch_quantize_int8(const void* x, int dtype, int64_t rows, int cols, int64_t pitch, int8_t* q,
-                         float* scales, const int32_t* end, int end_base, hipStream_t s) {
+int launch_quantize_int8(const void* x, int dtype, int64_t rows, int cols, int8_t* q, float* scales,
+                         hipStream_t s) {
     if (rows == 0) return MOE_OK;
     if (dtype == MOE_BF16)
-        return pitch % 8 == 0 && aligned(x)
-                   ? quantize<bf16_t, 8>((const bf16_t*)x, rows, cols, pitch, q, scales, end, end_base, s)
-                   : quantize<bf16_t, 1>((const bf16_t*)x, rows, cols, pitch, q, scales, end, end_base, s);
-    return pitch % 4 == 0 && aligned(x)
-               ? quantize<float, 4>((const float*)x, rows, cols, pitch, q, scales, end, end_base, s)
-               : quantize<float, 1>((const float*)x, rows, cols, pitch, q, scales, end, end_base, s);
+        return cols % 8 == 0 && aligned(x) ? quantize<bf16_t, 8>((const bf16_t*)x, rows, cols, q, scales, s)
+                                           : quantize<bf16_t, 1>((const bf16_t*)x, rows, cols, q, scales, s);
+    return cols % 4 == 0 && aligned(x) ? quantize<float, 4>((const float*)x, rows, cols, q, scales, s)
+                                       : quantize<float, 1>((const float*)x, rows, cols, q, scales, s);
 }
 
 int launch_dequantize_int8(const int8_t* q, const float* scales, int64_t rows, int cols, int dtype,

@@ -311,22 +311,29 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_backward_columns_kernel(
     parts[range * d + c] = sum;
 }
 
-// dw[c] = the sum of the ranges' parts, in order, by slices of them that are joined in order.
-constexpr int SLICES = 16;
+// dw[c] = the sum of the ranges' parts, by slices of them that are joined in order; eight of a
+// slice's parts in flight (2048 columns of 512 parts: 9.4 us one after the other by 16 slices).
+constexpr int JOIN = 1024, COLS = 32, SLICES = JOIN / COLS;
 
-__global__ __launch_bounds__(THREADS) void sum_ranges_kernel(const float* __restrict__ parts, int64_t n,
-                                                             int d, float* __restrict__ dw) {
-    constexpr int COLS = THREADS / SLICES;
+__global__ __launch_bounds__(JOIN) void sum_ranges_kernel(const float* __restrict__ parts, int64_t n, int d,
+                                                          float* __restrict__ dw) {
     __shared__ float s[SLICES][COLS];
     const int slice = threadIdx.x / COLS, col = threadIdx.x % COLS;
     const int64_t c = (int64_t)blockIdx.x * COLS + col;
-    const int64_t per = ceil_div(n, SLICES);
     float v = 0.f;
+    constexpr int AHEAD = 8;
     if (c < d)
-        for (int64_t q = slice * per; q < min(slice * per + per, n); ++q) v += parts[q * d + c];
+        for (int64_t q0 = slice; q0 < n; q0 += SLICES * AHEAD) {
+            float a[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) a[i] = q0 + i * SLICES < n ? parts[(q0 + i * SLICES) * d + c] : 0.f;
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) v += a[i];
+        }
     s[slice][col] = v;
     __syncthreads();
     if (slice > 0 || c >= d) return;
+#pragma unroll
     for (int q = 1; q < SLICES; ++q) v += s[q][col];
     dw[c] = v;
 }
@@ -387,8 +394,7 @@ int rmsnorm_backward(const Elem* dy, const Elem* h, const Elem* weight, const fl
         }
     }
     if (st != MOE_OK || dw == nullptr) return st;
-    hipLaunchKernelGGL(sum_ranges_kernel, dim3((unsigned)ceil_div(d, THREADS / SLICES)), dim3(THREADS), 0, s,
-                       parts, n, d, dw);
+    hipLaunchKernelGGL(sum_ranges_kernel, dim3((unsigned)ceil_div(d, COLS)), dim3(JOIN), 0, s, parts, n, d, dw);
     return launch_status();
 }
 

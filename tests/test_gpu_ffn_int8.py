@@ -109,6 +109,10 @@ def _run(sizes, d, f, T, *, gather=True, n_shared=0, seed=0, cap=None, x=None, s
     ([40, 7], 4096, 1024, 50), ([3, 2], 512, 4500, 5), ([65, 2, 128], 384, 257, 130), ([9, 1], 24, 131, 9),
     ([500, 115, 0, 260], 512, 640, 777), ([256, 257, 255, 1, 0, 513], 256, 384, 600),
     ([129], 1920, 72, 129), ([1000, 3], 640, 128, 1000), ([300] * 6, 128, 128, 300), ([700, 129], 40, 520, 700),
+    # few strips, and few tiles, over a long K: slices of it
+    ([20, 1], 264, 4100, 20), ([70, 0, 300, 1], 512, 4224, 310), ([650, 30], 264, 8200, 700),
+    # a token alone, two tokens: hidden rows quantized by the strips, also past what LDS holds
+    ([1, 0, 1, 1], 520, 1000, 1), ([2, 1], 64, 15000, 2), ([2, 2], 128, 20000, 2),
 ])
 def test_groups(sizes, d, f, T):
     say("[ffn int8]", sizes, d, f, T)
@@ -126,6 +130,40 @@ def test_packaged_rows(sizes, d, f):
 def test_shared_leading_groups(sizes, d, f, T, n_shared):
     say("[ffn int8 shared]", sizes, d, f, T, n_shared)
     _run(sizes, d, f, T, n_shared=n_shared, seed=5)
+
+
+@pytest.mark.parametrize("d,f", [(512, 1408), (1000, 328), (256, 4500)])
+def test_a_row_has_the_same_bits_in_every_batch(d, f):
+    """Whatever kernels a batch takes: alone (strips that quantize), in a few rows (strips), in many
+    (tiles of both sizes, slices of K)."""
+    say("[ffn int8 batches]", d, f)
+    g = torch.Generator().manual_seed(d)
+    xq, sx = moe.moe_quantize_int8(torch.randn(5000, d, generator=g).bfloat16().cuda())
+    w13, w2 = _experts(1, d, f, 3)
+    table = moe.Int8WeightTable(w13, w2, d, f)
+
+    def run(n):
+        off = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+        return moe.moe_grouped_ffn_int8(xq[:n], sx[:n], off, table)
+    want = run(5000)
+    for n in (1, 2, 3, 16, 17, 33, 64, 65, 300, 2000):
+        assert torch.equal(run(n), want[:n]), n
+
+
+@pytest.mark.parametrize("T,n", [(1, 40), (2, 21)])
+def test_a_group_that_names_a_token_more_than_once(T, n):
+    """More rows in a group than tokens: every one is computed."""
+    d, f = 256, 12000
+    xq, sx = moe.moe_quantize_int8(torch.randn(T, d, generator=torch.Generator().manual_seed(4)).cuda())
+    w13, w2 = _experts(2, d, f, 3)
+    table = moe.Int8WeightTable(w13, w2, d, f)
+    one = [moe.moe_grouped_ffn_int8(xq, sx, torch.tensor([0, T * (s == 0), T], dtype=torch.int32, device="cuda"), table)
+           for s in (0, 1)]
+    token = torch.tensor([i % T for i in range(n)] * 2, dtype=torch.int32, device="cuda")
+    off = torch.tensor([0, n, 2 * n], dtype=torch.int32, device="cuda")
+    y = moe.moe_grouped_ffn_int8(xq, sx, off, table, row_token=token, cap_rows=2 * n)
+    for s in (0, 1):
+        assert torch.equal(y[s * n:(s + 1) * n], one[s][token[:n].long()])
 
 
 @pytest.mark.parametrize("T,sizes", [(7, [3, 0, 7]), (40, [33, 40]), (300, [299, 10])])
