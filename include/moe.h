@@ -634,6 +634,20 @@ int moe_route_topk_backward(const float* dgate, const float* topk_gate, const in
                             float* dw, float* dbias, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * moe_route_topk_backward_aux -- moe_route_topk_backward with a gradient that reaches the gate
+ * scores another way (moe_balance_loss_backward's): dlogits_add is added to dlogits before dx, dw
+ * and dbias are taken of it.
+ *
+ * dlogits_add  device [T][E] float, nullable (then it is moe_route_topk_backward); may be dlogits
+ * Other arguments, requirements and errors as for moe_route_topk_backward.
+ */
+int moe_route_topk_backward_aux(const float* dgate, const float* topk_gate, const int32_t* topk_idx,
+                                const float* logits, const float* dlogits_add, const void* x,
+                                const void* w_router, int dtype, int64_t T, int d, int E, int k,
+                                int flags, float* dlogits, void* dx, float* dw, float* dbias, void* ws,
+                                size_t ws_bytes, void* stream);
+
+/*
  * Rows in 8-bit integers: a matrix of `cols` columns as
  *   q       int8 [rows][MOE_INT8_COLS(cols)]: codes -127 .. 127, the padding zero
  *   scales  float [rows]: value = q * scale

@@ -503,10 +503,11 @@ size_t moe_route_topk_backward_ws_bytes(int dtype, int64_t T, int d, int E, int 
     return route_backward_ws_bytes(dtype, T, d, E, k, flags);
 }
 
-int moe_route_topk_backward(const float* dgate, const float* topk_gate, const int32_t* topk_idx,
-                            const float* logits, const void* x, const void* w_router, int dtype,
-                            int64_t T, int d, int E, int k, int flags, float* dlogits, void* dx,
-                            float* dw, float* dbias, void* ws, size_t ws_bytes, void* stream) {
+int moe_route_topk_backward_aux(const float* dgate, const float* topk_gate, const int32_t* topk_idx,
+                                const float* logits, const float* dlogits_add, const void* x,
+                                const void* w_router, int dtype, int64_t T, int d, int E, int k,
+                                int flags, float* dlogits, void* dx, float* dw, float* dbias, void* ws,
+                                size_t ws_bytes, void* stream) {
     if (dtype != MOE_F32 && dtype != MOE_BF16) return MOE_ERR_ARG;
     if (T < 0 || d < 1 || E < 1 || E > MOE_MAX_E || k < 1 || k > MOE_MAX_K || k > E)
         return MOE_ERR_ARG;
@@ -515,6 +516,7 @@ int moe_route_topk_backward(const float* dgate, const float* topk_gate, const in
     if (T > 0 && (!dgate || !topk_gate || !topk_idx || (!(flags & MOE_RENORM) && !logits)))
         return MOE_ERR_ARG;
     if (T > 0 && ((dx && !w_router) || (dw && !x))) return MOE_ERR_ARG;
+    if (!aligned4(dlogits_add)) return MOE_ERR_ARG;
     if ((dtype == MOE_BF16 && d % 8) || d >= 1 << 22) return MOE_ERR_SHAPE;
     // one grid covers the tiles of dx
     if (ceil_div(T, 128) * ceil_div(d, 64) > 0x7fffffffLL) return MOE_ERR_SHAPE;
@@ -523,8 +525,16 @@ int moe_route_topk_backward(const float* dgate, const float* topk_gate, const in
         return MOE_ERR_ARG;
     if (!ws || ws_bytes < route_backward_ws_bytes(dtype, T, d, E, k, flags) || ((uintptr_t)ws & 255u))
         return MOE_ERR_SHAPE;
-    return launch_route_backward(dgate, topk_gate, topk_idx, logits, x, w_router, dtype, T, d, E, k,
-                                 flags, dlogits, dx, dw, dbias, ws, (hipStream_t)stream);
+    return launch_route_backward(dgate, topk_gate, topk_idx, logits, dlogits_add, x, w_router, dtype, T, d, E,
+                                 k, flags, dlogits, dx, dw, dbias, ws, (hipStream_t)stream);
+}
+
+int moe_route_topk_backward(const float* dgate, const float* topk_gate, const int32_t* topk_idx,
+                            const float* logits, const void* x, const void* w_router, int dtype,
+                            int64_t T, int d, int E, int k, int flags, float* dlogits, void* dx,
+                            float* dw, float* dbias, void* ws, size_t ws_bytes, void* stream) {
+    return moe_route_topk_backward_aux(dgate, topk_gate, topk_idx, logits, nullptr, x, w_router, dtype, T, d,
+                                       E, k, flags, dlogits, dx, dw, dbias, ws, ws_bytes, stream);
 }
 
 }  // extern "C"

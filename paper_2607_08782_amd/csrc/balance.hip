@@ -69,6 +69,22 @@ __device__ __forceinline__ void load_scores(const float* row, int l, int E, floa
     }
 }
 
+// A token's experts, those of a lane, -1 past k (k <= E: with few lanes E is small).
+template <int L>
+struct Chosen {
+    static constexpr int N = L >= 16 ? 1 : L == 8 ? 2 : 4;
+    int e[N];
+    __device__ __forceinline__ void load(const int32_t* row, int l, int k) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) e[i] = l + L * i < k ? row[l + L * i] : -1;
+    }
+    __device__ __forceinline__ void count(int32_t* c, int E) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if ((unsigned)e[i] < (unsigned)E) atomicAdd(&c[e[i]], 1);
+    }
+};
+
 // The softmax of a token's scores.
 template <int L, int J>
 __device__ __forceinline__ void softmax(float (&p)[J]) {
@@ -132,11 +148,10 @@ __global__ __launch_bounds__(THREADS) void balance_parts_kernel(const float* __r
     for (int64_t t = begin + sub; t < end; t += TOKENS) {
         if (mask != nullptr && mask[t] == 0) continue;   // (all lanes of the token together)
         float p[J];
+        Chosen<L> to;
+        to.load(idx + t * k, l, k);
         load_scores<L, C, VEC>(logits + t * E, l, E, p);
-        for (int r = l; r < k; r += L) {
-            const int e = idx[t * k + r];
-            if ((unsigned)e < (unsigned)E) atomicAdd(&c[e], 1);
-        }
+        to.count(c, E);
         softmax<L>(p);
 #pragma unroll
         for (int j = 0; j < J; ++j) sum[j] += p[j];
@@ -240,6 +255,83 @@ __global__ __launch_bounds__(JOIN) void balance_join_kernel(BalanceParts in, int
     loss[0] = n > 0 ? (float)(x * E / ((double)k * (double)n * (double)n)) : 0.f;
 }
 
+// A short batch by one workgroup in one launch: the parts are those of its slices, in LDS.  One CU's
+// exponentials bound it (loss and gradient of 100 tokens of 60 experts 8.2 us, of 273 10.4, of 777
+// 17.7; in two launches 777 take 11).
+constexpr int64_t SHORT = 1 << 14;                       // scores
+
+template <int L, int C, bool VEC>
+__global__ __launch_bounds__(JOIN) void balance_short_kernel(const float* __restrict__ logits,
+                                                             const int32_t* __restrict__ idx,
+                                                             const uint8_t* __restrict__ mask, int T, int E,
+                                                             int k, int32_t* __restrict__ counts,
+                                                             float* __restrict__ prob_sum,
+                                                             int32_t* __restrict__ n_tokens,
+                                                             float* __restrict__ loss) {
+    constexpr int TOKENS = JOIN / L, J = 4 * C, JOINED = 16, AHEAD = C == 1 ? 8 : C == 2 ? 4 : 2;
+    __shared__ float s[JOIN / JOINED][L * J];
+    __shared__ double product[JOIN / 64];
+    __shared__ int32_t c[MOE_MAX_E], n;
+    const int l = threadIdx.x % L, sub = threadIdx.x / L;
+    for (int e = threadIdx.x; e < E; e += JOIN) c[e] = 0;
+    if (threadIdx.x == 0) n = 0;
+    __syncthreads();
+    float sum[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) sum[j] = 0.f;
+    int mine = 0;
+    for (int t0 = sub; t0 < T; t0 += TOKENS * AHEAD) {   // (all lanes of a token together)
+        float p[AHEAD][J];
+        Chosen<L> to[AHEAD];
+        bool live[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int t = min(t0 + i * TOKENS, T - 1);
+            live[i] = t0 + i * TOKENS < T && (mask == nullptr || mask[t] != 0);
+            to[i].load(idx + (int64_t)t * k, l, k);
+            load_scores<L, C, VEC>(logits + (int64_t)t * E, l, E, p[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (!live[i]) continue;
+            to[i].count(c, E);
+            softmax<L>(p[i]);
+#pragma unroll
+            for (int j = 0; j < J; ++j) sum[j] += p[i][j];
+            ++mine;
+        }
+    }
+    if (l == 0 && mine) atomicAdd(&n, mine);
+    // tokens side by side in sixteen lanes first
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        if (L <= 2) sum[j] += other<1>(sum[j]);
+        if (L <= 4) sum[j] += __shfl_xor(sum[j], 4, 64);
+        if (L <= 8) sum[j] += __shfl_xor(sum[j], 8, 64);
+        if (threadIdx.x % JOINED < L) s[threadIdx.x / JOINED][expert_of<L>(l, j)] = sum[j];
+    }
+    __syncthreads();
+    const int e = threadIdx.x;
+    double x = 0.0;
+    if (e < E) {
+        double v = 0.0;
+#pragma unroll 8
+        for (int q = 0; q < JOIN / JOINED; ++q) v += (double)s[q][e];
+        counts[e] = c[e];
+        prob_sum[e] = (float)v;
+        x = (double)c[e] * v;
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o, 64);
+    if ((threadIdx.x & 63) == 0) product[threadIdx.x >> 6] = x;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    x = 0.0;
+    for (int q = 0; q < JOIN / 64; ++q) x += product[q];
+    n_tokens[0] = n;
+    loss[0] = n > 0 ? (float)(x * E / ((double)k * (double)n * (double)n)) : 0.f;
+}
+
 template <int L, int C, bool VEC>
 __global__ __launch_bounds__(THREADS) void balance_backward_kernel(const float* logits,
                                                                    const uint8_t* __restrict__ mask,
@@ -317,12 +409,22 @@ size_t balance_loss_ws_bytes(int64_t T, int E) {
 int launch_balance_loss(const float* logits, const int32_t* idx, const uint8_t* mask, int64_t T, int E,
                         int k, int32_t* counts, float* prob_sum, int32_t* n_tokens, float* loss,
                         void* ws, hipStream_t s) {
+    const bool vec = E % 4 == 0 && aligned(logits);
+    if (T * E <= SHORT) {
+#define MOE_BL(L, C, VEC)                                                                              \
+    hipLaunchKernelGGL((balance_short_kernel<L, C, VEC>), dim3(1), dim3(JOIN), 0, s, logits, idx, mask, (int)T, \
+                       E, k, counts, prob_sum, n_tokens, loss)
+        if (vec) MOE_LANES(MOE_BL, true);
+        else MOE_LANES(MOE_BL, false);
+#undef MOE_BL
+        return launch_status();
+    }
     const Split split(T);
     const BalanceParts parts = parts_at(ws, split.groups, E);
 #define MOE_BL(L, C, VEC)                                                                               \
     hipLaunchKernelGGL((balance_parts_kernel<L, C, VEC>), dim3((unsigned)split.groups), dim3(THREADS), 0, s, \
                        logits, idx, mask, T, E, k, split.per, parts)
-    if (E % 4 == 0 && aligned(logits)) MOE_LANES(MOE_BL, true);
+    if (vec) MOE_LANES(MOE_BL, true);
     else MOE_LANES(MOE_BL, false);
 #undef MOE_BL
     const int st = launch_status();

@@ -266,8 +266,8 @@ int launch_combine_backward(const void* dy, const void* y_perm, int dtype, const
 size_t route_backward_ws_bytes(int dtype, int64_t T, int d, int E, int k, int flags);
 [[nodiscard]]
 int launch_route_backward(const float* dgate, const float* gate, const int32_t* idx,
-                          const float* logits, const void* x, const void* w, int dtype, int64_t T,
-                          int d, int E, int k, int flags, float* dlogits, void* dx, float* dw,
-                          float* dbias, void* ws, hipStream_t s);
+                          const float* logits, const float* add, const void* x, const void* w,
+                          int dtype, int64_t T, int d, int E, int k, int flags, float* dlogits, void* dx,
+                          float* dw, float* dbias, void* ws, hipStream_t s);
 
 }  // namespace moe

@@ -181,15 +181,16 @@ int combine_backward(const void* dy, const void* y_perm, const int32_t* token_ro
 // dlogits, a token per wave: four in turn took twice as long where there are few (777 of
 // DeepSeek-V2-Lite 7.7 us, this 3.8) and no less where there are many (16384 of Qwen3-30B-A3B
 // 9.1 and 8.6).  Lane l holds experts l, l + 64, ...  Beside the dense rows, with MOE_RENORM,
-// the chosen experts' values [T][k] (sel).
+// the chosen experts' values [T][k] (sel).  add (nullable, may be dlogits): what reaches the scores
+// another way, added at the end.
 constexpr int RB_THREADS = 256;
 constexpr int RJ = MOE_MAX_E / 64;
 
 template <bool RENORM>
 __global__ __launch_bounds__(RB_THREADS) void gate_backward_kernel(
     const float* __restrict__ dgate, const float* __restrict__ gate, const int32_t* __restrict__ idx,
-    const float* __restrict__ logits, int64_t first, int64_t T, int E, int k,
-    float* __restrict__ dlogits, float* __restrict__ sel) {
+    const float* __restrict__ logits, const float* add, int64_t first, int64_t T, int E, int k,
+    float* dlogits, float* __restrict__ sel) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int64_t t = (first + blockIdx.x) * (RB_THREADS / 64) + wave;
@@ -242,7 +243,8 @@ __global__ __launch_bounds__(RB_THREADS) void gate_backward_kernel(
     }
 #pragma unroll
     for (int j = 0; j < RJ; ++j) {
-        if (dlogits && lane + 64 * j < E) dlogits[t * E + lane + 64 * j] = v[j];
+        if (dlogits && lane + 64 * j < E)
+            dlogits[t * E + lane + 64 * j] = add ? v[j] + add[t * E + lane + 64 * j] : v[j];
     }
 }
 
@@ -872,14 +874,14 @@ size_t route_backward_ws_bytes(int, int64_t T, int d, int E, int k, int) {
 }
 
 int launch_route_backward(const float* dgate, const float* gate, const int32_t* idx,
-                          const float* logits, const void* x, const void* w, int dtype, int64_t T,
-                          int d, int E, int k, int flags, float* dlogits, void* dx, float* dw,
-                          float* dbias, void* ws, hipStream_t s) {
+                          const float* logits, const float* add, const void* x, const void* w,
+                          int dtype, int64_t T, int d, int E, int k, int flags, float* dlogits, void* dx,
+                          float* dw, float* dbias, void* ws, hipStream_t s) {
     if (!dlogits && !dx && !dw && !dbias) return MOE_OK;
     const bool renorm = (flags & MOE_RENORM) != 0;
     const RouteLayout at(T, d, E, k);
     char* base = (char*)ws;
-    const bool sparse = dx && renorm && dtype == MOE_F32;
+    const bool sparse = dx && renorm && dtype == MOE_F32 && !add;
     float* sel = sparse ? (float*)(base + at.sel) : nullptr;
     float* dl = dlogits ? dlogits : dw || dbias || (dx && !sparse) ? (float*)base : nullptr;
     if (T > 0) {
@@ -887,10 +889,10 @@ int launch_route_backward(const float* dgate, const float* gate, const int32_t* 
         const int st = launch_groups(groups, RB_THREADS, [&](int64_t first, unsigned n) {
             if (renorm)
                 hipLaunchKernelGGL(gate_backward_kernel<true>, dim3(n), dim3(RB_THREADS), 0, s, dgate, gate,
-                                   idx, logits, first, T, E, k, dl, sel);
+                                   idx, logits, add, first, T, E, k, dl, sel);
             else
                 hipLaunchKernelGGL(gate_backward_kernel<false>, dim3(n), dim3(RB_THREADS), 0, s, dgate, gate,
-                                   idx, logits, first, T, E, k, dl, sel);
+                                   idx, logits, add, first, T, E, k, dl, sel);
         });
         if (st != MOE_OK) return st;
     }

@@ -24,9 +24,15 @@ with 4-bit experts, whose table is made anew).
 
 With ``mxfp4=True`` the routed experts are held and multiplied in 4 bits
 (moe_grouped_ffn_mxfp4; 17/64 of a decode step's weight bytes); shared experts
-keep bf16 and their own call.  `backward` and `backward_rows` are the gradient of
-the layer around its experts: from the loss gradient of y to the expert outputs'
-and the router's, and from the packaged rows' back to X.
+keep bf16 and their own call.  With ``int8=True`` they are held and multiplied in
+8-bit integers (moe_grouped_ffn_int8), over token rows that a step quantizes once.
+With ``norm`` the share begins at the residual stream: a step's rows are the
+root-mean-square norm of X (+ residual), in one launch with the addition and, for
+8-bit experts, their codes (moe_rmsnorm).
+
+`backward` and `backward_rows` are the gradient of the layer around its experts:
+from the loss gradient of y to the expert outputs' and the router's, and from the
+packaged rows' back to the rows; `backward_norm` takes these to the residual stream.
 """
 from __future__ import annotations
 
@@ -96,17 +102,28 @@ class LayerShare:
                  coact: bool = False, want_logits: bool = True, cap_rows: Optional[int] = None,
                  gather_in_ffn: Optional[bool] = None, overlap_shared: bool = True,
                  fuse_combine: Optional[bool] = None, shared_in_ffn: Optional[bool] = None,
-                 mxfp4: bool = False):
-        if mxfp4:
-            # the 4-bit call reads rows through the row map, streams or tiles by itself,
+                 mxfp4: bool = False, int8: bool = False, norm: Optional[torch.Tensor] = None,
+                 norm_eps: float = 1e-6, residual: Optional[torch.Tensor] = None):
+        if mxfp4 and int8:
+            raise ValueError("experts are held in 4 bits or in 8, not in both")
+        if mxfp4 or int8:
+            # the call reads rows through the row map, streams or tiles by itself,
             # and leaves the shared experts to their own call
+            name = "mxfp4" if mxfp4 else "int8"
             if X.dtype != torch.bfloat16:
-                raise ValueError("mxfp4 experts need bfloat16 activations")
+                raise ValueError("%s experts need bfloat16 activations" % name)
             if gather_in_ffn is False or fuse_combine or shared_in_ffn:
-                raise ValueError("mxfp4 experts gather their rows in the FFN call and take neither the "
-                                 "combine nor the shared experts into it")
+                raise ValueError("%s experts gather their rows in the FFN call and take neither the "
+                                 "combine nor the shared experts into it" % name)
             gather_in_ffn, fuse_combine, shared_in_ffn = True, False, False
-        self.mxfp4 = mxfp4
+        self.mxfp4, self.int8 = mxfp4, int8
+        # norm [d]: the rows that router and experts read are the norm of X (+ residual), made at a
+        # step's start into `normed`; the sum goes to `hidden` (X itself without a residual)
+        if norm is not None and (tuple(norm.shape) != (X.shape[1],) or norm.dtype != X.dtype):
+            raise ValueError("norm must be %s [%d]" % (X.dtype, X.shape[1]))
+        if residual is not None and norm is None:
+            raise ValueError("a residual is added in front of the norm: give its weight")
+        self.norm, self.norm_eps = norm, float(norm_eps)
         self.device = X.device
         self.X = X
         self.Wr = Wr
@@ -156,6 +173,15 @@ class LayerShare:
         self.cap_rows = cap_rows if cap_rows is not None else self.T * min(k, self.n_local)
         T, d, E, dt = self.T, self.d, self.E, X.dtype
         dv = self.device
+        self.residual = None
+        if norm is not None:
+            self.normed = torch.empty_like(X)
+            self.rstd = torch.empty((T,), dtype=torch.float32, device=dv)
+            self.hidden = X if residual is None else torch.empty_like(X)
+            self._set_residual(residual)
+        if int8:
+            self.xq = torch.empty((T, moe.int8_cols(d)), dtype=torch.int8, device=dv)
+            self.x_scale = torch.empty((T,), dtype=torch.float32, device=dv)
         self.logits = torch.empty((T, E), dtype=torch.float32, device=dv) if want_logits else None
         self.topk_idx = torch.empty((T, k), dtype=torch.int32, device=dv)
         self.topk_gate = torch.empty((T, k), dtype=torch.float32, device=dv)
@@ -194,6 +220,8 @@ class LayerShare:
         if mxfp4:
             need = moe.moe_grouped_ffn_mxfp4_ws_bytes(T, self.cap_rows, d, max(self.f, 1),
                                                       max(self.n_local, 1))
+        elif int8:
+            need = moe.moe_grouped_ffn_int8_ws_bytes(self.cap_rows, d, max(self.f, 1), max(self.n_local, 1))
         else:
             need = moe.moe_grouped_ffn_ws_bytes(dcode, lead + self.cap_rows, d, max(self.f, 1),
                                                 max(self.n_shared_blocks + self.n_local, 1))
@@ -254,17 +282,43 @@ class LayerShare:
         self.fused_combine = bool(fuse_combine) and can_fuse
         self._packaged = False                           # the row maps are written
         # the last routing's token rows and scores, which backward goes through
-        self._rows, self._scores = self.X, self.logits
+        self._rows, self._scores = self.rows, self.logits
         self._grads = None
         self._grads_current = False                      # they are the last routing's
+        self._balance = None                             # the balance loss's outputs and workspace
+        self._normed_of = None                           # the rows that the last norm was of
+
+    @property
+    def rows(self) -> torch.Tensor:
+        """The rows that router and experts read: X, or its norm."""
+        return self.X if self.norm is None else self.normed
+
+    def _set_residual(self, residual: Optional[torch.Tensor]):
+        if residual is not None and (tuple(residual.shape) != (self.T, self.d) or residual.dtype != self.X.dtype):
+            raise ValueError("residual must be %s [%d, %d]" % (self.X.dtype, self.T, self.d))
+        self.residual = residual
+
+    def prepare_rows(self):
+        """Enqueue what a step's rows need before the routing, as `run` does: the residual's addition
+        and the norm, the rows in 8 bits for 8-bit experts (nothing without either)."""
+        q = dict(q=self.xq, scales=self.x_scale) if self.int8 else {}
+        if self.norm is not None:
+            h = moe.moe_rmsnorm(self.X, self.norm, residual=self.residual, eps=self.norm_eps,
+                                h=None if self.residual is None else self.hidden, y=self.normed,
+                                rstd=self.rstd, **q)[0]
+            self.hidden = self._normed_of = h
+        elif self.int8:
+            moe.moe_quantize_int8(self.X, **q)
 
     def _table(self, w13: Sequence[torch.Tensor], w2: Sequence[torch.Tensor]):
-        return moe.MxWeightTable.quantized(w13, w2) if self.mxfp4 else moe.WeightTable(w13, w2)
+        if self.mxfp4:
+            return moe.MxWeightTable.quantized(w13, w2)
+        return moe.Int8WeightTable.quantized(w13, w2) if self.int8 else moe.WeightTable(w13, w2)
 
     def set_placement(self, placement: np.ndarray, w13: Sequence[torch.Tensor],
                       w2: Sequence[torch.Tensor]):
         """Swap the expert placement between batches (same number of local slots).  With mxfp4
-        every expert given is quantized and laid out, into new memory and on the current
+        or int8 every expert given is quantized and laid out, into new memory and on the current
         stream; the call then waits for the GPU, so that runs on any stream find the new table
         whole, and the old one's memory goes back with no kernel still reading it.  A table that
         a captured run reads stays in `captured_tables`, since the graph's replays go on reading
@@ -274,7 +328,7 @@ class LayerShare:
         if n_local != self.n_local:
             raise ValueError("the new placement must keep %d local slots" % self.n_local)
         table = self._table(w13, w2) if n_local else None
-        if self.mxfp4:
+        if self.mxfp4 or self.int8:
             torch.cuda.synchronize(self.device)
         self.placement, self.weights = placement, table
         self._ffn_weights = self._call_weights(w13, w2)
@@ -288,9 +342,15 @@ class LayerShare:
         w2 = list(w2)[:self.n_local]
         return moe.WeightTable(self._blocks[0] + w13, self._blocks[1] + w2)
 
-    def set_inputs(self, X: torch.Tensor, bias: Optional[torch.Tensor] = None):
+    def set_inputs(self, X: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                   residual: Optional[torch.Tensor] = None):
+        """The next batch (residual: of a share that was made with one; None keeps the last)."""
         if tuple(X.shape) != (self.T, self.d) or X.dtype != self.X.dtype:
             raise ValueError("X must keep shape and dtype")
+        if residual is not None:
+            if self.residual is None:
+                raise ValueError("the share was made without a residual")
+            self._set_residual(residual)
         self.X = X
         if bias is not None:
             self.bias = bias
@@ -300,14 +360,14 @@ class LayerShare:
             moe.moe_route_topk(None, None, None, self.k, renorm=self.renorm, logits=logits_in,
                                logits_in=True, topk_idx=self.topk_idx, topk_gate=self.topk_gate)
         else:
-            moe.moe_route_topk(self.X, self.Wr, self.bias, self.k, renorm=self.renorm,
+            moe.moe_route_topk(self.rows, self.Wr, self.bias, self.k, renorm=self.renorm,
                                logits=self.logits, want_logits=self.logits is not None,
                                topk_idx=self.topk_idx, topk_gate=self.topk_gate, ws=self.ws_route)
         self._routed(logits_in)
 
     def _routed(self, logits_in: Optional[torch.Tensor]):
         """What `backward` goes through is this routing's now, and no gradient of it is there."""
-        self._rows, self._scores = self.X, self.logits if logits_in is None else logits_in
+        self._rows, self._scores = self.rows, self.logits if logits_in is None else logits_in
         self._grads_current = False
 
     def _shared_ffn(self, stream=None):
@@ -315,7 +375,7 @@ class LayerShare:
         call, or there are none)."""
         if self.shared_weights is None:
             return
-        moe.moe_grouped_ffn(self.X, self.shared_offsets, self.shared_weights, cap_rows=self.T,
+        moe.moe_grouped_ffn(self.rows, self.shared_offsets, self.shared_weights, cap_rows=self.T,
                             y_perm=self.y_shared, ws=self.ws_shared, stream=stream,
                             products=self.shared_products)
 
@@ -344,7 +404,7 @@ class LayerShare:
     def package(self):
         """Enqueue the packaging step as `run` makes it (moe_permute; the row copy
         x_perm only when the FFN does not gather the rows itself)."""
-        moe.moe_permute(self.X, self.topk_idx, self.topk_gate, self.counts, self.placement,
+        moe.moe_permute(self.rows, self.topk_idx, self.topk_gate, self.counts, self.placement,
                         self.dev, E=self.E, cap_rows=self.cap_rows, out=self.perm, ws=self.ws_perm,
                         copy_rows=not self.gather_in_ffn)
         self._packaged = True
@@ -352,7 +412,7 @@ class LayerShare:
     def _route_package(self, logits_in: Optional[torch.Tensor] = None):
         """Enqueue routing, counts and packaging as one call: `route`, the histogram and
         `package`, the same outputs in fewer launches over short batches."""
-        moe.moe_route_package(self.X, self.Wr, self.bias, self.placement, self.dev,
+        moe.moe_route_package(self.rows, self.Wr, self.bias, self.placement, self.dev,
                               logits=self.logits if logits_in is None else logits_in,
                               topk_idx=self.topk_idx, topk_gate=self.topk_gate,
                               ws_route=self.ws_route, counts=self.counts, coact=self.coact,
@@ -364,24 +424,27 @@ class LayerShare:
 
     def routed_ffn(self, fused: Optional[bool] = None):
         """Enqueue the routed experts' FFN call as `run` makes it: moe_grouped_ffn (or
-        moe_grouped_ffn_rows, moe_grouped_ffn_mxfp4) into y_perm, or, when the share fuses the combine (fused
+        moe_grouped_ffn_rows, moe_grouped_ffn_mxfp4, moe_grouped_ffn_int8) into y_perm, or, when the share fuses the combine (fused
         None: as `run` does), moe_grouped_ffn_combine into y (which then reads y_shared:
         the shared experts' call must have completed on this stream)."""
         if self.shared_in_ffn:
-            moe.moe_grouped_ffn_rows_shared(self.X, self._row_token_all, self.perm["group_offsets"],
+            moe.moe_grouped_ffn_rows_shared(self.rows, self._row_token_all, self.perm["group_offsets"],
                                             self._ffn_weights, self.n_shared_blocks,
                                             cap_rows=self.cap_rows, y_perm=self._y_perm_all,
                                             ws=self.ws_ffn, products=self.ffn_products)
             return
         if self.weights is None:
             return
-        if self.mxfp4:
+        if self.mxfp4 or self.int8:
             if torch.cuda.is_current_stream_capturing() and not any(t is self.weights
                                                                     for t in self.captured_tables):
                 self.captured_tables.append(self.weights)
-            moe.moe_grouped_ffn_mxfp4(self.X, self.perm["group_offsets"], self.weights,
-                                      row_token=self.perm["row_token"], cap_rows=self.cap_rows,
-                                      y_perm=self.y_perm, ws=self.ws_ffn)
+            to = dict(row_token=self.perm["row_token"], cap_rows=self.cap_rows, y_perm=self.y_perm,
+                      ws=self.ws_ffn)
+            if self.mxfp4:
+                moe.moe_grouped_ffn_mxfp4(self.rows, self.perm["group_offsets"], self.weights, **to)
+            else:
+                moe.moe_grouped_ffn_int8(self.xq, self.x_scale, self.perm["group_offsets"], self.weights, **to)
             return
         if self.fused_combine if fused is None else (fused and self.fused_combine):
             moe.moe_grouped_ffn_combine(self.perm["x_perm"], self.perm["group_offsets"],
@@ -389,7 +452,7 @@ class LayerShare:
                                         self.y_shared, cap_rows=self.cap_rows, T=self.T, y=self.y,
                                         ws=self.ws_ffn)
         elif self.gather_in_ffn:
-            moe.moe_grouped_ffn_rows(self.X, self.perm["row_token"], self.perm["group_offsets"],
+            moe.moe_grouped_ffn_rows(self.rows, self.perm["row_token"], self.perm["group_offsets"],
                                      self.weights, cap_rows=self.cap_rows, y_perm=self.y_perm,
                                      ws=self.ws_ffn, products=self.ffn_products)
         else:
@@ -409,6 +472,7 @@ class LayerShare:
             self._shared_ffn(self._side)
             self._join.record(self._side)
 
+        self.prepare_rows()
         if self.fused_combine:
             # the fused call reads y_shared: the shared branch overlaps the routing
             if self._side is not None:
@@ -440,17 +504,41 @@ class LayerShare:
         if not self._packaged:
             raise ValueError("%s goes back through a run, and none was made" % name)
 
-    def backward(self, dy: torch.Tensor, reduce_dgate: Optional[Callable] = None) -> dict:
+    def balance_loss(self, scale: float = 1.0, mask: Optional[torch.Tensor] = None) -> dict:
+        """Enqueue the balance loss of the last routing over the tokens where mask [T] is not 0, and
+        its gradient times scale; returns device tensors, overwritten by the next call: loss [1],
+        counts [E], prob_sum [E], n_tokens [1], dlogits [T, E]."""
+        if self._scores is None:
+            raise ValueError("the balance loss is of the gate scores: it needs want_logits=True")
+        self._needs_row_maps("balance_loss")
+        if self._balance is None:
+            new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=self.device)
+            self._balance = {"loss": new(1), "counts": new(self.E, dtype=torch.int32), "prob_sum": new(self.E),
+                             "n_tokens": new(1, dtype=torch.int32), "dlogits": new(self.T, self.E)}
+            self._ws_balance = moe.workspace(moe.moe_balance_loss_ws_bytes(self.T, self.E), self.device)
+        b = self._balance
+        moe.moe_balance_loss(self._scores, self.topk_idx, mask=mask, loss=b["loss"], counts=b["counts"],
+                             prob_sum=b["prob_sum"], n_tokens=b["n_tokens"], ws=self._ws_balance)
+        moe.moe_balance_loss_backward(self._scores, b["counts"], b["n_tokens"], self.k, scale=scale, mask=mask,
+                                      dlogits=b["dlogits"])
+        return b
+
+    def backward(self, dy: torch.Tensor, reduce_dgate: Optional[Callable] = None, balance: float = 0.0,
+                 mask: Optional[torch.Tensor] = None) -> dict:
         """Enqueue the gradient of the last `run` from dy [T, d], the loss gradient of y, to
         the experts and the router; returns device tensors, overwritten by the next call:
             dy_perm  of every expert output row (rows past group_offsets' end unchanged)
             dgate    [T, k] fp32, of topk_gate: 0 for experts on other GPUs
-            dx       [T, d], of that run's X through the gate scores;  dw [E, d], dbias [E]
-                     fp32, of the router
+            dx       [T, d], of that run's rows (X, or its norm) through the gate scores;  dw
+                     [E, d], dbias [E] fp32, of the router
         (the shared experts' output has dy itself).  A token's gates depend on each other,
         so where its experts are on several GPUs dgate has to be summed over them before it
         goes on: reduce_dgate(dgate), in place, on the current stream.  dx, dw and dbias are
         then whole on each of them, not parts to be summed again.
+
+        balance adds that much times the balance loss of the routing (over the tokens where mask
+        [T] is not 0) to the loss whose gradient this is: through the scores to dx, dw and dbias;
+        its value is `balance_loss`'s, under "balance_loss" here.
 
         After a run(logits_in=...) the gates' gradient is taken at those scores (keep them until
         then where gates are not renormalised), and the router's as of scores X Wr^T + bias."""
@@ -460,6 +548,8 @@ class LayerShare:
             raise ValueError("gates without renormalisation need want_logits=True for backward")
         if tuple(dy.shape) != (self.T, self.d) or dy.dtype != self.X.dtype:
             raise ValueError("dy must be %s [%d, %d]" % (self.X.dtype, self.T, self.d))
+        if balance and self._scores is None:
+            raise ValueError("the balance loss is of the gate scores: it needs want_logits=True")
         self._needs_row_maps("backward")
         if self._grads is None:
             f32 = dict(dtype=torch.float32, device=self.device)
@@ -475,11 +565,13 @@ class LayerShare:
                                  dy_perm=g["dy_perm"], dgate=g["dgate"])
         if reduce_dgate is not None:
             reduce_dgate(g["dgate"])
+        b = self.balance_loss(balance, mask) if balance else None
         moe.moe_route_topk_backward(g["dgate"], self.topk_gate, self.topk_idx, self._rows, self.Wr,
                                     logits=self._scores, renorm=self.renorm, want_dlogits=False,
-                                    dx=g["dx"], dw=g["dw"], dbias=g["dbias"], ws=self._ws_grads)
+                                    dx=g["dx"], dw=g["dw"], dbias=g["dbias"], ws=self._ws_grads,
+                                    dlogits_add=None if b is None else b["dlogits"])
         self._grads_current = True
-        return g
+        return g if b is None else dict(g, balance_loss=b["loss"])
 
     def backward_rows(self, dx_perm: torch.Tensor, dx: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Enqueue the gradient of the packaging: dx [T, d] (None: a new tensor) = the sum of
@@ -490,3 +582,15 @@ class LayerShare:
         self._needs_row_maps("backward_rows")
         add = self._grads["dx"] if self._grads_current else None
         return moe.moe_permute_backward(dx_perm, self.perm["token_row"], dx_add=add, dx=dx)
+
+    def backward_norm(self, drows: torch.Tensor, dh_add: Optional[torch.Tensor] = None,
+                      dh: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None):
+        """Enqueue the gradient of the norm: from drows [T, d], the gradient of the last run's rows,
+        to (dh [T, d], of X and of the residual alike, on top of dh_add, what reaches the sum
+        through the residual stream; dw [d] fp32, of the norm's weight).  The sum that the norm was
+        of has to be as that run left it: `hidden`, or X where there is no residual."""
+        if self.norm is None:
+            raise ValueError("the share has no norm")
+        if self._normed_of is None:
+            raise ValueError("backward_norm goes back through a run, and none was made")
+        return moe.moe_rmsnorm_backward(drows, self._normed_of, self.norm, self.rstd, dh_add=dh_add, dh=dh, dw=dw)

@@ -36,7 +36,7 @@ EXPORTS = ("moe_status_string", "moe_route_topk", "moe_route_topk_ws_bytes",
            "moe_quantize_mxfp4", "moe_dequantize_mxfp4", "moe_mxfp4_lay_out",
            "moe_grouped_ffn_mxfp4_ws_bytes", "moe_grouped_ffn_mxfp4",
            "moe_combine_backward", "moe_permute_backward", "moe_route_topk_backward_ws_bytes",
-           "moe_route_topk_backward",
+           "moe_route_topk_backward", "moe_route_topk_backward_aux",
            "moe_quantize_int8", "moe_dequantize_int8",
            "moe_grouped_ffn_int8_ws_bytes", "moe_grouped_ffn_int8",
            "moe_rmsnorm", "moe_rmsnorm_backward_ws_bytes", "moe_rmsnorm_backward",
@@ -119,6 +119,8 @@ def load_library(path: str = LIB_PATH):
     lib.moe_route_topk_backward_ws_bytes.restype = S
     lib.moe_route_topk_backward.argtypes = [P, P, P, P, P, P, I, L, I, I, I, I, P, P, P, P, P, S, P]
     lib.moe_route_topk_backward.restype = I
+    lib.moe_route_topk_backward_aux.argtypes = [P, P, P, P, P, P, P, I, L, I, I, I, I, P, P, P, P, P, S, P]
+    lib.moe_route_topk_backward_aux.restype = I
     F = ctypes.c_float
     lib.moe_quantize_int8.argtypes = [P, I, L, I, P, P, P]
     lib.moe_quantize_int8.restype = I
@@ -849,9 +851,10 @@ def moe_route_topk_backward(dgate: torch.Tensor, topk_gate: torch.Tensor, topk_i
                             want_dbias: bool = True, dlogits: Optional[torch.Tensor] = None,
                             dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None,
                             dbias: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
-                            stream=None):
+                            dlogits_add: Optional[torch.Tensor] = None, stream=None):
     """Gradient of moe_route_topk.  Returns (dlogits [T, E], dx [T, d] of x's dtype, dw [E, d],
-    dbias [E]), float32 but dx, None for what is not wanted.  renorm=False needs logits."""
+    dbias [E]), float32 but dx, None for what is not wanted.  renorm=False needs logits.
+    dlogits_add [T, E] (moe_route_topk_backward_aux): what reaches the scores another way."""
     lib = load_library()
     T, d = x.shape
     E, k = w_router.shape[0], topk_idx.shape[1]
@@ -882,13 +885,29 @@ def moe_route_topk_backward(dgate: torch.Tensor, topk_gate: torch.Tensor, topk_i
     dtype, flags = _dtype_code(x), MOE_RENORM if renorm else 0
     if ws is None:
         ws = workspace(moe_route_topk_backward_ws_bytes(dtype, T, d, E, k, flags), x.device, stream)
-    st = lib.moe_route_topk_backward(
-        _dev(dgate, "dgate"), _dev(topk_gate, "topk_gate"), _dev(topk_idx, "topk_idx"),
-        None if renorm else _dev(logits, "logits"), _dev(x, "x"), _dev(w_router, "w_router"), dtype, T,
-        d, E, k, flags, _dev(dlogits, "dlogits"), _dev(dx, "dx"), _dev(dw, "dw"), _dev(dbias, "dbias"),
-        _dev(ws, "ws"), ws.numel(), _stream(stream))
+    _same(dlogits_add, "dlogits_add", f32, T, E)
+    scores = (None if renorm else _dev(logits, "logits"),)
+    if dlogits_add is not None:
+        scores += (_dev(dlogits_add, "dlogits_add"),)
+    call = lib.moe_route_topk_backward if dlogits_add is None else lib.moe_route_topk_backward_aux
+    st = call(_dev(dgate, "dgate"), _dev(topk_gate, "topk_gate"), _dev(topk_idx, "topk_idx"), *scores,
+              _dev(x, "x"), _dev(w_router, "w_router"), dtype, T, d, E, k, flags, _dev(dlogits, "dlogits"),
+              _dev(dx, "dx"), _dev(dw, "dw"), _dev(dbias, "dbias"), _dev(ws, "ws"), ws.numel(), _stream(stream))
     _check("moe_route_topk_backward", st)
     return dlogits, dx, dw, dbias
+
+
+def _arg(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, *shape: int):
+    """Device pointer of a contiguous GPU tensor of this type and shape (None -> NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError("%s must be %s %s, got %s %s" % (name, dtype, shape, t.dtype, tuple(t.shape)))
+    if not t.is_cuda:
+        raise ValueError("%s must be a GPU tensor" % name)
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return t.data_ptr()
 
 
 def int8_cols(cols: int) -> int:
@@ -906,10 +925,9 @@ def moe_quantize_int8(x: torch.Tensor, *, q: Optional[torch.Tensor] = None,
         q = _empty((rows, int8_cols(cols)), torch.int8, x.device, stream)
     if scales is None:
         scales = _empty((rows,), torch.float32, x.device, stream)
-    _same(q, "q", torch.int8, rows, int8_cols(cols))
-    _same(scales, "scales", torch.float32, rows)
-    st = lib.moe_quantize_int8(_dev(x, "x"), _dtype_code(x), rows, cols, _dev(q, "q"), _dev(scales, "scales"),
-                               _stream(stream))
+    st = lib.moe_quantize_int8(_dev(x, "x"), _dtype_code(x), rows, cols,
+                               _arg(q, "q", torch.int8, rows, int8_cols(cols)),
+                               _arg(scales, "scales", torch.float32, rows), _stream(stream))
     _check("moe_quantize_int8", st)
     return q, scales
 
@@ -922,13 +940,12 @@ def moe_dequantize_int8(q: torch.Tensor, scales: torch.Tensor, cols: int, *,
     rows = q.shape[0]
     if cols < 1:
         raise ValueError("cols must be positive")
-    _same(q, "q", torch.int8, rows, int8_cols(cols))
-    _same(scales, "scales", torch.float32, rows)
+    at_q, at_scales = _arg(q, "q", torch.int8, rows, int8_cols(cols)), _arg(scales, "scales", torch.float32, rows)
     if out is None:
-        out = _empty((rows, cols), dtype, q.device, stream)
-    _same(out, "out", dtype, rows, cols)
-    st = lib.moe_dequantize_int8(_dev(q, "q"), _dev(scales, "scales"), rows, cols, _dtype_code(out),
-                                 _dev(out, "out"), _stream(stream))
+        new = q.new_empty if stream is None else _of(stream, q.new_empty)
+        out = new((rows, cols), dtype=dtype)
+    st = lib.moe_dequantize_int8(at_q, at_scales, rows, cols, _dtype_code(out),
+                                 _arg(out, "out", dtype, rows, cols), _stream(stream))
     _check("moe_dequantize_int8", st)
     return out
 
@@ -944,10 +961,8 @@ class Int8WeightTable:
         self.w13, self.w2 = [tuple(p) for p in w13], [tuple(p) for p in w2]
         for pairs, rows, cols, name in ((self.w13, 2 * self.f, self.d, "w13"), (self.w2, self.d, self.f, "w2")):
             for q, s in pairs:
-                _same(q, name + " codes", torch.int8, rows, int8_cols(cols))
-                _same(s, name + " scales", torch.float32, rows)
-                _dev(q, name + " codes")
-                _dev(s, name + " scales")
+                _arg(q, name + " codes", torch.int8, rows, int8_cols(cols))
+                _arg(s, name + " scales", torch.float32, rows)
         n = len(self.w13)
         self._arrays = [(ctypes.c_void_p * n)(*[p[i].data_ptr() for p in pairs])
                         for pairs in (self.w13, self.w2) for i in (0, 1)]
@@ -980,8 +995,7 @@ def moe_grouped_ffn_int8(xq: torch.Tensor, x_scale: torch.Tensor, group_offsets:
     lib = load_library()
     T = xq.shape[0]
     d, f = weights.d, weights.f
-    _same(xq, "xq", torch.int8, T, int8_cols(d))
-    _same(x_scale, "x_scale", torch.float32, T)
+    at_x, at_scale = _arg(xq, "xq", torch.int8, T, int8_cols(d)), _arg(x_scale, "x_scale", torch.float32, T)
     if cap_rows is None:
         if row_token is not None:
             raise ValueError("row_token needs cap_rows")
@@ -997,7 +1011,7 @@ def moe_grouped_ffn_int8(xq: torch.Tensor, x_scale: torch.Tensor, group_offsets:
     if ws is None:
         ws = workspace(moe_grouped_ffn_int8_ws_bytes(rows, d, f, len(weights)), xq.device, stream)
     st = lib.moe_grouped_ffn_int8(
-        _dev(xq, "xq"), _dev(x_scale, "x_scale"), T, _dev(row_token, "row_token", torch.int32),
+        at_x, at_scale, T, _dev(row_token, "row_token", torch.int32),
         _dev(group_offsets, "group_offsets", torch.int32), n_groups, n_shared, *weights.pointers,
         d, f, cap_rows, _dev(y_perm, "y_perm", torch.bfloat16), _dev(ws, "ws"), ws.numel(),
         _stream(stream))
@@ -1014,9 +1028,8 @@ def moe_rmsnorm(x: torch.Tensor, weight: torch.Tensor, *, residual: Optional[tor
     itself without a residual; y; rstd [T]; q, scales: y in 8 bits), None for what is not wanted."""
     lib = load_library()
     T, d = x.shape
-    dtype = _dtype_code(x)
-    _same(weight, "weight", x.dtype, d)
-    _same(residual, "residual", x.dtype, T, d)
+    dt, f32 = x.dtype, torch.float32
+    at_weight, at_residual = _arg(weight, "weight", dt, d), _arg(residual, "residual", dt, T, d)
     like, new = torch.empty_like, x.new_empty
     if stream is not None:
         like, new = _of(stream, like), _of(stream, new)
@@ -1028,19 +1041,15 @@ def moe_rmsnorm(x: torch.Tensor, weight: torch.Tensor, *, residual: Optional[tor
     if want_y and y is None:
         y = like(x)
     if want_rstd and rstd is None:
-        rstd = new(T, dtype=torch.float32)
+        rstd = new(T, dtype=f32)
     if (q is None) != (scales is None):
         raise ValueError("q and scales go together")
     if want_q and q is None:
-        q, scales = new((T, int8_cols(d)), dtype=torch.int8), new(T, dtype=torch.float32)
-    _same(h, "h", x.dtype, T, d)
-    _same(y, "y", x.dtype, T, d)
-    _same(rstd, "rstd", torch.float32, T)
-    _same(q, "q", torch.int8, T, int8_cols(d))
-    _same(scales, "scales", torch.float32, T)
-    st = lib.moe_rmsnorm(_dev(x, "x"), _dev(residual, "residual"), dtype, _dev(weight, "weight"), eps, T, d,
-                         _dev(h, "h"), _dev(y, "y"), _dev(rstd, "rstd"), _dev(q, "q"),
-                         _dev(scales, "scales"), _stream(stream))
+        q, scales = new((T, int8_cols(d)), dtype=torch.int8), new(T, dtype=f32)
+    st = lib.moe_rmsnorm(_dev(x, "x"), at_residual, _dtype_code(x), at_weight, eps, T, d, _arg(h, "h", dt, T, d),
+                         _arg(y, "y", dt, T, d), _arg(rstd, "rstd", f32, T),
+                         _arg(q, "q", torch.int8, T, int8_cols(d)), _arg(scales, "scales", f32, T),
+                         _stream(stream))
     _check("moe_rmsnorm", st)
     return (x if residual is None else h), y, rstd, q, scales
 
@@ -1057,23 +1066,21 @@ def moe_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor
     dw [d] float32), None for what is not wanted."""
     lib = load_library()
     T, d = dy.shape
-    _same(h, "h", dy.dtype, T, d)
-    _same(weight, "weight", dy.dtype, d)
-    _same(rstd, "rstd", torch.float32, T)
-    _same(dh_add, "dh_add", dy.dtype, T, d)
-    dtype = _dtype_code(dy)
+    dt, dtype = dy.dtype, _dtype_code(dy)
+    at_h, at_weight = _arg(h, "h", dt, T, d), _arg(weight, "weight", dt, d)
+    at_rstd, at_add = _arg(rstd, "rstd", torch.float32, T), _arg(dh_add, "dh_add", dt, T, d)
+    like, new = torch.empty_like, dy.new_empty
+    if stream is not None:
+        like, new = _of(stream, like), _of(stream, new)
     if want_dh and dh is None:
-        dh = (torch.empty_like if stream is None else _of(stream, torch.empty_like))(dy)
+        dh = like(dy)
     if want_dw and dw is None:
-        dw = _empty((d,), torch.float32, dy.device, stream)
-    _same(dh, "dh", dy.dtype, T, d)
-    _same(dw, "dw", torch.float32, d)
+        dw = new(d, dtype=torch.float32)
     if dw is not None and ws is None:
-        ws = workspace(moe_rmsnorm_backward_ws_bytes(dtype, T, d), dy.device, stream)
-    st = lib.moe_rmsnorm_backward(_dev(dy, "dy"), _dev(h, "h"), dtype, _dev(weight, "weight"),
-                                  _dev(rstd, "rstd"), _dev(dh_add, "dh_add"), T, d, _dev(dh, "dh"),
-                                  _dev(dw, "dw"), _dev(ws, "ws"), 0 if ws is None else ws.numel(),
-                                  _stream(stream))
+        ws = new(moe_rmsnorm_backward_ws_bytes(dtype, T, d), dtype=torch.uint8)
+    st = lib.moe_rmsnorm_backward(_dev(dy, "dy"), at_h, dtype, at_weight, at_rstd, at_add, T, d,
+                                  _arg(dh, "dh", dt, T, d), _arg(dw, "dw", torch.float32, d),
+                                  _dev(ws, "ws"), 0 if ws is None else ws.numel(), _stream(stream))
     _check("moe_rmsnorm_backward", st)
     return dh, dw
 
@@ -1098,23 +1105,22 @@ def moe_balance_loss(logits: torch.Tensor, topk_idx: torch.Tensor, *, mask: Opti
     lib = load_library()
     T, E = logits.shape
     k = topk_idx.shape[1]
-    _same(logits, "logits", torch.float32, T, E)
-    _same(topk_idx, "topk_idx", torch.int32, T, k)
+    f32, i32 = torch.float32, torch.int32
+    at_logits, at_idx, at_mask = _arg(logits, "logits", f32, T, E), _arg(topk_idx, "topk_idx", i32, T, k), _mask(mask, T)
     new = logits.new_empty if stream is None else _of(stream, logits.new_empty)
-    loss = new(1) if loss is None else loss
-    counts = new(E, dtype=torch.int32) if counts is None else counts
-    prob_sum = new(E) if prob_sum is None else prob_sum
-    n_tokens = new(1, dtype=torch.int32) if n_tokens is None else n_tokens
-    _same(loss, "loss", torch.float32, 1)
-    _same(counts, "counts", torch.int32, E)
-    _same(prob_sum, "prob_sum", torch.float32, E)
-    _same(n_tokens, "n_tokens", torch.int32, 1)
+    if loss is None:
+        loss = new(1)
+    if counts is None:
+        counts = new(E, dtype=i32)
+    if prob_sum is None:
+        prob_sum = new(E)
+    if n_tokens is None:
+        n_tokens = new(1, dtype=i32)
     if ws is None:
-        ws = workspace(moe_balance_loss_ws_bytes(T, E), logits.device, stream)
-    st = lib.moe_balance_loss(_dev(logits, "logits"), _dev(topk_idx, "topk_idx"), _mask(mask, T), T, E, k,
-                              _dev(counts, "counts"), _dev(prob_sum, "prob_sum"),
-                              _dev(n_tokens, "n_tokens"), _dev(loss, "loss"), _dev(ws, "ws"), ws.numel(),
-                              _stream(stream))
+        ws = new(moe_balance_loss_ws_bytes(T, E), dtype=torch.uint8)
+    st = lib.moe_balance_loss(at_logits, at_idx, at_mask, T, E, k, _arg(counts, "counts", i32, E),
+                              _arg(prob_sum, "prob_sum", f32, E), _arg(n_tokens, "n_tokens", i32, 1),
+                              _arg(loss, "loss", f32, 1), _dev(ws, "ws"), ws.numel(), _stream(stream))
     _check("moe_balance_loss", st)
     return loss, counts, prob_sum, n_tokens
 
@@ -1125,15 +1131,12 @@ def moe_balance_loss_backward(logits: torch.Tensor, counts: torch.Tensor, n_toke
     """Gradient of moe_balance_loss, times scale.  Returns dlogits [T, E]."""
     lib = load_library()
     T, E = logits.shape
-    _same(logits, "logits", torch.float32, T, E)
-    _same(counts, "counts", torch.int32, E)
-    _same(n_tokens, "n_tokens", torch.int32, 1)
+    f32, i32 = torch.float32, torch.int32
+    at_logits, at_counts = _arg(logits, "logits", f32, T, E), _arg(counts, "counts", i32, E)
     if dlogits is None:
         dlogits = (torch.empty_like if stream is None else _of(stream, torch.empty_like))(logits)
-    _same(dlogits, "dlogits", torch.float32, T, E)
-    st = lib.moe_balance_loss_backward(_dev(logits, "logits"), _mask(mask, T), _dev(counts, "counts"),
-                                       _dev(n_tokens, "n_tokens"), T, E, k, scale,
-                                       _dev(dlogits, "dlogits"), _stream(stream))
+    st = lib.moe_balance_loss_backward(at_logits, _mask(mask, T), at_counts, _arg(n_tokens, "n_tokens", i32, 1),
+                                       T, E, k, scale, _arg(dlogits, "dlogits", f32, T, E), _stream(stream))
     _check("moe_balance_loss_backward", st)
     return dlogits
 
@@ -1175,10 +1178,10 @@ def moe_grad_norm(table: GradTable, *, norm: Optional[torch.Tensor] = None,
         if not len(table):
             raise ValueError("a table without gradients needs norm")
         norm = _empty((1,), torch.float32, table.grads[0].device, stream)
-    _same(norm, "norm", torch.float32, 1)
     if ws is None:
         ws = workspace(moe_grad_norm_ws_bytes(table), norm.device, stream)
-    st = lib.moe_grad_norm(table.pointers, table.sizes, table.dtypes, len(table), _dev(norm, "norm"),
+    st = lib.moe_grad_norm(table.pointers, table.sizes, table.dtypes, len(table),
+                           _arg(norm, "norm", torch.float32, 1),
                            _dev(ws, "ws"), ws.numel(), _stream(stream))
     _check("moe_grad_norm", st)
     return norm
@@ -1187,8 +1190,7 @@ def moe_grad_norm(table: GradTable, *, norm: Optional[torch.Tensor] = None,
 def moe_clip_grads(table: GradTable, norm: torch.Tensor, max_norm: float, *, stream=None):
     """Scale a table's gradients by max_norm / norm where that is below 1.  Returns its outputs."""
     lib = load_library()
-    _same(norm, "norm", torch.float32, 1)
-    st = lib.moe_clip_grads(table.pointers, table.sizes, table.dtypes, len(table), _dev(norm, "norm"),
-                            max_norm, table.outputs, _stream(stream))
+    st = lib.moe_clip_grads(table.pointers, table.sizes, table.dtypes, len(table),
+                            _arg(norm, "norm", torch.float32, 1), max_norm, table.outputs, _stream(stream))
     _check("moe_clip_grads", st)
     return table.out
