@@ -387,10 +387,10 @@ int rmsnorm_backward(const Elem* dy, const Elem* h, const Elem* weight, const fl
         }
         if (st == MOE_OK && dw != nullptr) {
             const int columns = (int)ceil_div(d, THREADS);
-            st = launch_groups(ranges.n * columns, THREADS, [&](int64_t, unsigned groups) {
-                hipLaunchKernelGGL(rmsnorm_backward_columns_kernel<Elem>, dim3(groups), dim3(THREADS), 0, s, dy,
-                                   h, rstd, T, d, ranges.per, columns, parts);
-            });
+            // (512 ranges of 2^14 blocks of columns at most: one grid)
+            hipLaunchKernelGGL(rmsnorm_backward_columns_kernel<Elem>, dim3((unsigned)(ranges.n * columns)),
+                               dim3(THREADS), 0, s, dy, h, rstd, T, d, ranges.per, columns, parts);
+            st = launch_status();
         }
     }
     if (st != MOE_OK || dw == nullptr) return st;
