@@ -737,8 +737,9 @@ int moe_grouped_ffn_int8(const int8_t* xq, const float* x_scale, int64_t T, cons
  * rstd     device [T] float output, nullable (moe_rmsnorm_backward reads it)
  * q, scales  device [T][MOE_INT8_COLS(d)] and [T] outputs, nullable together
  * Apart from these, outputs must not overlap inputs or each other.
- * A row that is not finite makes its own outputs NaN or infinite, and no other row's.  A row of
- * zeros gives zeros (with eps > 0).  Sums are fp32 in a fixed order (deterministic).
+ * Squares are summed in 64 bits, in a fixed order (deterministic).  A row that holds a NaN gives
+ * NaN; one that holds an infinity has rstd 0 (NaN at its infinities, zeros beside them, q's row
+ * NaN); no other row is touched.  A row of zeros gives zeros (with eps > 0).
  * Requires T >= 0, 1 <= d < 2^22 (else MOE_ERR_SHAPE), eps >= 0 and finite, q 16-byte aligned.
  */
 int moe_rmsnorm(const void* x, const void* residual, int dtype, const void* weight, float eps, int64_t T,

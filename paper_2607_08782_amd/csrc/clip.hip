@@ -33,12 +33,6 @@ __device__ __forceinline__ int tensor_of(const Tensors& t, uint32_t chunk) {
     return __builtin_amdgcn_readfirstlane(n - 1);
 }
 
-__device__ __forceinline__ double lanes_sum64(double v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
-    return v;
-}
-
 // A chunk's pieces of a thread, AHEAD of them in flight: f(piece, its place).
 constexpr int AHEAD = 4;
 
@@ -92,7 +86,7 @@ __global__ __launch_bounds__(THREADS) void grad_squares_kernel(Tensors t, double
         const float* p = (const float*)t.in[i] + at;
         sum = whole ? squares<float, 4>(p, n) : squares<float, 1>(p, n);
     }
-    sum = lanes_sum64(sum);
+    sum = lanes_sum(sum);
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = sum;
     __syncthreads();
     if (threadIdx.x == 0) parts[blockIdx.x] = (s[0] + s[1]) + (s[2] + s[3]);
@@ -105,7 +99,7 @@ __global__ __launch_bounds__(JOIN) void grad_norm_kernel(const double* __restric
     __shared__ double s[JOIN / 64];
     double sum = 0.0;
     for (int64_t q = threadIdx.x; q < n; q += JOIN) sum += parts[q];
-    sum = lanes_sum64(sum);
+    sum = lanes_sum(sum);
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = sum;
     __syncthreads();
     if (threadIdx.x != 0) return;

@@ -67,6 +67,49 @@ struct StripStep {
 
 constexpr int QUANT_BYTES = 32 * 1024;                    // codes of a strip's rows in LDS, at most
 
+// h's rows row0 .. row0 + n - 1 as codes and scales in LDS, by all threads of a strip: a thread's first
+// pieces of a row come while the row's largest magnitude is looked up.
+__device__ __forceinline__ void quantize_rows(const I8Args& p, int8_t* codes, float* row_scale, int row0, int n,
+                                              int pitch, int tid, int threads) {
+    constexpr int HELD = 4;
+    const int lane = tid & 63, chunks = p.P / 8;
+    __syncthreads();                                     // the last row block's codes are read
+    for (int r = 0; r < n; ++r) {
+        const bf16_t* const h = p.h + (int64_t)(row0 + r) * p.P;
+        const uint32_t* const most = p.most + (int64_t)(row0 + r) * p.blocks;
+        Piece<bf16_t, 8> held[HELD];
+        auto load = [&](int c0) {
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) held[i].load(h + (int64_t)min(c0 + i * threads, chunks - 1) * 8);
+        };
+        load(tid);
+        uint32_t top = 0;
+        for (int b0 = lane; b0 < p.blocks; b0 += 64 * HELD) {
+            uint32_t m[HELD];
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) m[i] = most[min(b0 + 64 * i, p.blocks - 1)];
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) top = max(top, m[i]);
+        }
+        const Int8Scale scale(lanes_max(top));
+        if (tid == 0) row_scale[r] = scale.s;
+#pragma clang loop unroll(disable)
+        for (int c0 = tid; c0 < chunks; c0 += HELD * threads) {
+            if (c0 != tid) load(c0);
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) {
+                const int c = c0 + i * threads;
+                float v[8];
+                held[i].values(v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = c * 8 + e < p.K ? v[e] : 0.f;
+                if (c < chunks) scale.template store<true>(v, codes + r * pitch + c * 8);
+            }
+        }
+    }
+    __syncthreads();
+}
+
 // QUANT (down): p.h's rows, as many as `codes` holds at a time, are quantized as the strip begins, by
 // all of its threads, and their scales go to `row_scale`.  SPLIT (down): the strip's slice of K, its
 // sums to p.part.
@@ -76,6 +119,7 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
                                            int slice = 0) {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int ROWS = 16 * TILES, LD = ROWS + 4, BM = 16 * MS;
+    constexpr int PER_ROW = (SWIGLU ? ROWS / 2 : ROWS) / 4;          // threads of a row's columns
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int i16 = lane & 15, quarter = lane >> 4;
@@ -99,19 +143,19 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
     const int block = QUANT ? min(BM, QUANT_BYTES / (p.P + 16)) : BM;
     for (int m0 = 0; m0 < rows; m0 += block) {
         // rows past the group repeat its last one; their sums are not stored
-        const int8_t* at[MS];
         const int here = min(rows - m0, block), pitch = p.P + 16;    // (the latter: of rows in LDS)
+        int a_row[MS];
 #pragma unroll
         for (int m = 0; m < MS; ++m) {
             const int r = row0 + min(m0 + 16 * m + i16, rows - 1);
-            if (QUANT) at[m] = codes + min(i16, here - 1) * pitch + quarter * 16;
-            else at[m] = p.a + (int64_t)(p.a_rows ? p.a_rows[r] : r) * p.P + quarter * 16;
+            a_row[m] = !QUANT && p.a_rows ? p.a_rows[r] : r;
         }
         i32x4 acc[MS][TILES];
 #pragma unroll
         for (int m = 0; m < MS; ++m)
 #pragma unroll
             for (int j = 0; j < TILES; ++j) acc[m][j] = i32x4{0, 0, 0, 0};
+        const int8_t* at[MS];
         // past the end of K: no traffic of the weights, and the last step's rows again
         auto load_b = [&](StripStep<MS, TILES>& s, int t) {
             const int bytes = t < KT ? valid * p.P - t * STEP : 0;
@@ -145,35 +189,11 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
         StripStep<MS, TILES> s[D];
 #pragma unroll
         for (int i = 0; i < D; ++i) load_b(s[i], begin + wave + i * W);
-        if constexpr (QUANT) {
-            __syncthreads();                             // the last row block's codes are read
-            const bf16_t* const h = p.h + (int64_t)(row0 + m0) * p.P;
-            for (int r = wave; r < here; r += W) {
-                const uint32_t* const most = p.most + (int64_t)(row0 + m0 + r) * p.blocks;
-                uint32_t top = 0;
-                for (int b = lane; b < p.blocks; b += 64) top = max(top, most[b]);
-                top = lanes_max(top);
-                if (lane == 0) ((uint32_t*)row_scale)[r] = top;
-            }
-            __syncthreads();
-            const int chunks = p.P / 8;
-            for (int r = 0; r < here; ++r) {
-                const Int8Scale scale(((const uint32_t*)row_scale)[r]);
-                for (int c = tid; c < chunks; c += 64 * W) {
-                    Piece<bf16_t, 8> piece;
-                    float v[8];
-                    piece.load(h + (int64_t)r * p.P + c * 8);
-                    piece.values(v);
-                    if (c * 8 + 8 > p.K)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (c * 8 + e >= p.K) v[e] = 0.f;
-                    scale.template store<true>(v, codes + r * pitch + c * 8);
-                }
-            }
-            __syncthreads();
-            if (tid < here) row_scale[tid] = Int8Scale(((const uint32_t*)row_scale)[tid]).s;
-        }
+        for (int m = 0; m < MS; ++m)
+            at[m] = QUANT ? codes + min(i16, here - 1) * pitch + quarter * 16
+                          : p.a + (int64_t)a_row[m] * p.P + quarter * 16;
+        if constexpr (QUANT) quantize_rows(p, codes, row_scale, row0 + m0, here, pitch, tid, 64 * W);
 #pragma unroll
         for (int i = 0; i < D; ++i) load_a(s[i], begin + wave + i * W);
         for (int t = begin + wave; t < KT; t += D * W)
@@ -193,7 +213,6 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
                 *(i32x4*)&red[(wave * BM + 16 * m + i16) * LD + 16 * j + 4 * quarter] = acc[m][j];
         __syncthreads();
         // four output columns a thread
-        constexpr int PER_ROW = (SWIGLU ? ROWS / 2 : ROWS) / 4;
         for (int i = tid; i < BM * PER_ROW; i += 64 * W) {
             const int r = i / PER_ROW, c = (i % PER_ROW) * 4;
             const bool live = r < here && n0 + c < p.N;

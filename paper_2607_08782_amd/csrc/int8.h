@@ -125,7 +125,8 @@ struct Int8Scale {
 };
 
 // A value over the wave's lanes: the sum, the same order in each, and the largest.
-__device__ __forceinline__ float lanes_sum(float v) {
+template <typename F>
+__device__ __forceinline__ F lanes_sum(F v) {
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
     return v;

@@ -22,7 +22,7 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(const Elem* x, const E
                                                           const Elem* weight, float eps, int64_t T, int d,
                                                           Elem* h, Elem* y, float* rstd, int8_t* q,
                                                           float* scales) {
-    __shared__ float sums[THREADS / 64];
+    __shared__ double sums[THREADS / 64];
     __shared__ uint32_t most[THREADS / 64];
     constexpr int NT = 64 * W, PER = THREADS / NT;
     constexpr bool NARROW = sizeof(Elem) == 2;
@@ -34,8 +34,8 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(const Elem* x, const E
     for (int64_t t = (int64_t)blockIdx.x * PER + threadIdx.x / NT; t < T; t += (int64_t)gridDim.x * PER) {
         const int64_t row = t * d;
         Piece<Elem, V> held[CH];
-        float sum = 0.f;
-        // chunk c of the stored sum, made (first pass) or read again
+        // (64 bits: no row's sum of squares passes their range)
+        double sum = 0.0;
         auto add = [&](Piece<Elem, V>& a, const Piece<Elem, V>& b) {
             float u[V], v[V];
             a.values(u);
@@ -48,7 +48,7 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(const Elem* x, const E
             float v[V];
             a.values(v);
 #pragma unroll
-            for (int j = 0; j < V; ++j) sum = fmaf(v[j], v[j], sum);
+            for (int j = 0; j < V; ++j) sum = fma((double)v[j], (double)v[j], sum);
         };
         Piece<Elem, V> extra[CH];
 #pragma unroll
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(const Elem* x, const E
             __syncthreads();
             sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
         }
-        const float r = 1.0f / sqrtf(sum / (float)d + eps);
+        const float r = (float)(1.0 / sqrt(sum / d + (double)eps));
         if (rstd != nullptr && tid == 0) rstd[t] = r;
         // y of a chunk, rounded as it is stored
         const Elem* stored = residual != nullptr ? h : x;

@@ -897,14 +897,20 @@ def moe_route_topk_backward(dgate: torch.Tensor, topk_gate: torch.Tensor, topk_i
     return dlogits, dx, dw, dbias
 
 
+_current_gpu = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _arg(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, *shape: int):
-    """Device pointer of a contiguous GPU tensor of this type and shape (None -> NULL)."""
+    """Device pointer of a contiguous tensor of this type and shape on the current GPU, where the
+    call's stream is (None -> NULL)."""
     if t is None:
         return None
     if t.dtype is not dtype or t.shape != shape:
         raise ValueError("%s must be %s %s, got %s %s" % (name, dtype, shape, t.dtype, tuple(t.shape)))
     if not t.is_cuda:
         raise ValueError("%s must be a GPU tensor" % name)
+    if t.get_device() != _current_gpu():
+        raise ValueError("%s must be on the current GPU" % name)
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
     return t.data_ptr()
@@ -921,11 +927,13 @@ def moe_quantize_int8(x: torch.Tensor, *, q: Optional[torch.Tensor] = None,
     float32 [rows])."""
     lib = load_library()
     rows, cols = x.shape
+    at_x = _arg(x, "x", x.dtype, rows, cols)
+    new = x.new_empty if stream is None else _of(stream, x.new_empty)
     if q is None:
-        q = _empty((rows, int8_cols(cols)), torch.int8, x.device, stream)
+        q = new((rows, int8_cols(cols)), dtype=torch.int8)
     if scales is None:
-        scales = _empty((rows,), torch.float32, x.device, stream)
-    st = lib.moe_quantize_int8(_dev(x, "x"), _dtype_code(x), rows, cols,
+        scales = new(rows, dtype=torch.float32)
+    st = lib.moe_quantize_int8(at_x, _dtype_code(x), rows, cols,
                                _arg(q, "q", torch.int8, rows, int8_cols(cols)),
                                _arg(scales, "scales", torch.float32, rows), _stream(stream))
     _check("moe_quantize_int8", st)
@@ -944,8 +952,10 @@ def moe_dequantize_int8(q: torch.Tensor, scales: torch.Tensor, cols: int, *,
     if out is None:
         new = q.new_empty if stream is None else _of(stream, q.new_empty)
         out = new((rows, cols), dtype=dtype)
-    st = lib.moe_dequantize_int8(at_q, at_scales, rows, cols, _dtype_code(out),
-                                 _arg(out, "out", dtype, rows, cols), _stream(stream))
+        at_out = out.data_ptr()
+    else:
+        at_out = _arg(out, "out", dtype, rows, cols)
+    st = lib.moe_dequantize_int8(at_q, at_scales, rows, cols, _dtype_code(out), at_out, _stream(stream))
     _check("moe_dequantize_int8", st)
     return out
 
@@ -1005,6 +1015,8 @@ def moe_grouped_ffn_int8(xq: torch.Tensor, x_scale: torch.Tensor, group_offsets:
         raise ValueError("group_offsets must hold n_groups + 1 entries for the routed groups")
     rows = n_shared * T + cap_rows
     _holds(row_token, "row_token", rows)
+    if weights.w13[0][0].device != xq.device:
+        raise ValueError("the experts must be on the current GPU")
     if y_perm is None:
         y_perm = _empty((max(rows, 1), d), torch.bfloat16, xq.device, stream)
     _holds(y_perm, "y_perm", rows, d)
@@ -1028,8 +1040,13 @@ def moe_rmsnorm(x: torch.Tensor, weight: torch.Tensor, *, residual: Optional[tor
     itself without a residual; y; rstd [T]; q, scales: y in 8 bits), None for what is not wanted."""
     lib = load_library()
     T, d = x.shape
-    dt, f32 = x.dtype, torch.float32
-    at_weight, at_residual = _arg(weight, "weight", dt, d), _arg(residual, "residual", dt, T, d)
+    dt, f32, P = x.dtype, torch.float32, int8_cols(d)
+    at_x, at_weight = _arg(x, "x", dt, T, d), _arg(weight, "weight", dt, d)
+    at_residual, at_h = _arg(residual, "residual", dt, T, d), _arg(h, "h", dt, T, d)
+    at_y, at_rstd = _arg(y, "y", dt, T, d), _arg(rstd, "rstd", f32, T)
+    at_q, at_scales = _arg(q, "q", torch.int8, T, P), _arg(scales, "scales", f32, T)
+    if (q is None) != (scales is None):
+        raise ValueError("q and scales go together")
     like, new = torch.empty_like, x.new_empty
     if stream is not None:
         like, new = _of(stream, like), _of(stream, new)
@@ -1038,18 +1055,19 @@ def moe_rmsnorm(x: torch.Tensor, weight: torch.Tensor, *, residual: Optional[tor
             raise ValueError("h is x itself without a residual")
     elif h is None:
         h = like(x)
+        at_h = h.data_ptr()
     if want_y and y is None:
         y = like(x)
+        at_y = y.data_ptr()
     if want_rstd and rstd is None:
         rstd = new(T, dtype=f32)
-    if (q is None) != (scales is None):
-        raise ValueError("q and scales go together")
+        at_rstd = rstd.data_ptr()
     if want_q and q is None:
-        q, scales = new((T, int8_cols(d)), dtype=torch.int8), new(T, dtype=f32)
-    st = lib.moe_rmsnorm(_dev(x, "x"), at_residual, _dtype_code(x), at_weight, eps, T, d, _arg(h, "h", dt, T, d),
-                         _arg(y, "y", dt, T, d), _arg(rstd, "rstd", f32, T),
-                         _arg(q, "q", torch.int8, T, int8_cols(d)), _arg(scales, "scales", f32, T),
-                         _stream(stream))
+        q, scales = new((T, P), dtype=torch.int8), new(T, dtype=f32)
+        at_q, at_scales = q.data_ptr(), scales.data_ptr()
+    # (no rows have no address: nothing is written)
+    st = lib.moe_rmsnorm(at_x, at_residual, _dtype_code(x), at_weight, eps, T, d, at_h, at_y, at_rstd, at_q or None,
+                         at_scales or None, _stream(stream))
     _check("moe_rmsnorm", st)
     return (x if residual is None else h), y, rstd, q, scales
 
@@ -1067,19 +1085,21 @@ def moe_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor
     lib = load_library()
     T, d = dy.shape
     dt, dtype = dy.dtype, _dtype_code(dy)
-    at_h, at_weight = _arg(h, "h", dt, T, d), _arg(weight, "weight", dt, d)
+    at_dy, at_h, at_weight = _arg(dy, "dy", dt, T, d), _arg(h, "h", dt, T, d), _arg(weight, "weight", dt, d)
     at_rstd, at_add = _arg(rstd, "rstd", torch.float32, T), _arg(dh_add, "dh_add", dt, T, d)
+    at_dh, at_dw = _arg(dh, "dh", dt, T, d), _arg(dw, "dw", torch.float32, d)
     like, new = torch.empty_like, dy.new_empty
     if stream is not None:
         like, new = _of(stream, like), _of(stream, new)
     if want_dh and dh is None:
         dh = like(dy)
+        at_dh = dh.data_ptr()
     if want_dw and dw is None:
         dw = new(d, dtype=torch.float32)
+        at_dw = dw.data_ptr()
     if dw is not None and ws is None:
         ws = new(moe_rmsnorm_backward_ws_bytes(dtype, T, d), dtype=torch.uint8)
-    st = lib.moe_rmsnorm_backward(_dev(dy, "dy"), at_h, dtype, at_weight, at_rstd, at_add, T, d,
-                                  _arg(dh, "dh", dt, T, d), _arg(dw, "dw", torch.float32, d),
+    st = lib.moe_rmsnorm_backward(at_dy, at_h, dtype, at_weight, at_rstd, at_add, T, d, at_dh, at_dw,
                                   _dev(ws, "ws"), 0 if ws is None else ws.numel(), _stream(stream))
     _check("moe_rmsnorm_backward", st)
     return dh, dw
@@ -1087,9 +1107,9 @@ def moe_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor
 
 def _mask(mask: Optional[torch.Tensor], T: int):
     """Device pointer of a token mask (bool or uint8 [T]; None -> NULL)."""
-    if mask is not None and (mask.dtype not in (torch.bool, torch.uint8) or tuple(mask.shape) != (T,)):
+    if mask is not None and mask.dtype is not torch.bool and mask.dtype is not torch.uint8:
         raise ValueError("mask must be bool or uint8 [%d]" % T)
-    return _dev(mask, "mask")
+    return None if mask is None else _arg(mask, "mask", mask.dtype, T)
 
 
 def moe_balance_loss_ws_bytes(T: int, E: int) -> int:
@@ -1107,20 +1127,25 @@ def moe_balance_loss(logits: torch.Tensor, topk_idx: torch.Tensor, *, mask: Opti
     k = topk_idx.shape[1]
     f32, i32 = torch.float32, torch.int32
     at_logits, at_idx, at_mask = _arg(logits, "logits", f32, T, E), _arg(topk_idx, "topk_idx", i32, T, k), _mask(mask, T)
+    at_loss, at_n = _arg(loss, "loss", f32, 1), _arg(n_tokens, "n_tokens", i32, 1)
+    at_counts, at_sums = _arg(counts, "counts", i32, E), _arg(prob_sum, "prob_sum", f32, E)
     new = logits.new_empty if stream is None else _of(stream, logits.new_empty)
     if loss is None:
         loss = new(1)
+        at_loss = loss.data_ptr()
     if counts is None:
         counts = new(E, dtype=i32)
+        at_counts = counts.data_ptr()
     if prob_sum is None:
         prob_sum = new(E)
+        at_sums = prob_sum.data_ptr()
     if n_tokens is None:
         n_tokens = new(1, dtype=i32)
+        at_n = n_tokens.data_ptr()
     if ws is None:
         ws = new(moe_balance_loss_ws_bytes(T, E), dtype=torch.uint8)
-    st = lib.moe_balance_loss(at_logits, at_idx, at_mask, T, E, k, _arg(counts, "counts", i32, E),
-                              _arg(prob_sum, "prob_sum", f32, E), _arg(n_tokens, "n_tokens", i32, 1),
-                              _arg(loss, "loss", f32, 1), _dev(ws, "ws"), ws.numel(), _stream(stream))
+    st = lib.moe_balance_loss(at_logits, at_idx, at_mask, T, E, k, at_counts, at_sums, at_n, at_loss,
+                              _dev(ws, "ws"), ws.numel(), _stream(stream))
     _check("moe_balance_loss", st)
     return loss, counts, prob_sum, n_tokens
 
@@ -1133,10 +1158,12 @@ def moe_balance_loss_backward(logits: torch.Tensor, counts: torch.Tensor, n_toke
     T, E = logits.shape
     f32, i32 = torch.float32, torch.int32
     at_logits, at_counts = _arg(logits, "logits", f32, T, E), _arg(counts, "counts", i32, E)
+    at_n, at_out = _arg(n_tokens, "n_tokens", i32, 1), _arg(dlogits, "dlogits", f32, T, E)
     if dlogits is None:
         dlogits = (torch.empty_like if stream is None else _of(stream, torch.empty_like))(logits)
-    st = lib.moe_balance_loss_backward(at_logits, _mask(mask, T), at_counts, _arg(n_tokens, "n_tokens", i32, 1),
-                                       T, E, k, scale, _arg(dlogits, "dlogits", f32, T, E), _stream(stream))
+        at_out = dlogits.data_ptr()
+    st = lib.moe_balance_loss_backward(at_logits, _mask(mask, T), at_counts, at_n, T, E, k, scale, at_out,
+                                       _stream(stream))
     _check("moe_balance_loss_backward", st)
     return dlogits
 
@@ -1153,12 +1180,10 @@ class GradTable:
         n = len(self.grads)
         for g, o in zip(self.grads, self.out):
             _dtype_code(g)
-            if o.dtype != g.dtype or o.shape != g.shape or o.device != g.device:
-                raise ValueError("outputs must be of the gradients' types and shapes, on their device")
-            if g.device != self.grads[0].device:
-                raise ValueError("gradients must be on one device")
-        self.pointers = (ctypes.c_void_p * n)(*[_dev(g, "grads") for g in self.grads])
-        self.outputs = (ctypes.c_void_p * n)(*[_dev(o, "out") for o in self.out])
+            if o.dtype != g.dtype or o.shape != g.shape:
+                raise ValueError("outputs must be of the gradients' types and shapes")
+        self.pointers = (ctypes.c_void_p * n)(*[_arg(g, "grads", g.dtype, *g.shape) for g in self.grads])
+        self.outputs = (ctypes.c_void_p * n)(*[_arg(o, "out", o.dtype, *o.shape) for o in self.out])
         self.sizes = (ctypes.c_int64 * n)(*[g.numel() for g in self.grads])
         self.dtypes = (ctypes.c_int * n)(*[_dtype_code(g) for g in self.grads])
 

@@ -1,9 +1,9 @@
 """The norm in front of a layer and its gradient (marked `gpu`) against their definition in
 float64, and against differences.
 
-Tolerances.  A sum over a row of d values runs over at most C = ceil(d / 64) of them in one
-thread and a tree of 10 steps: relative error (C + 10) 2^-24 for squares, which have one sign, and
-that of the sum of magnitudes else.  rstd keeps half of it and 4 roundings; y that, two more
+Tolerances.  A sum in fp32 over a row of d values runs over at most C = ceil(d / 64) of them in one
+thread and a tree of 10 steps: an error of (C + 10) 2^-24 of the sum of magnitudes.  rstd, whose
+squares are summed in 64 bits, keeps at most half of that and 4 roundings; y that, two more
 and its own rounding (half a step: eps / 2 of its type).  dw's chains are a range's rows (at most
 ceil(T / 512), four at least) and 160 parts.
 """
@@ -120,6 +120,16 @@ def test_norm_of_rows_at_the_edges(dtype):
         assert torch.equal(a[5:], b[5:]) and torch.equal(a[0], b[0])
     # eps 0 of a row of zeros: 0 * infinity
     assert torch.isnan(moe.moe_rmsnorm(x[1:2], w, eps=0.0)[1]).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("scale", [1e18, 1e25, 1e36])
+@pytest.mark.parametrize("d", [384, 77])
+def test_norm_of_rows_whose_squares_pass_32_bits(dtype, scale, d):
+    x, w = (_rows(4, d, torch.float32, 8, 0.0) * scale).to(dtype), _weight(d, dtype, 5)
+    h, y, rstd, q, s = moe.moe_rmsnorm(x, w, want_rstd=True, want_q=True)
+    assert float(y.abs().max()) > 1.0
+    _check(x, None, w, 1e-6, x, y, rstd, q, s)
 
 
 def test_norm_of_rows_that_are_not_16_byte_aligned():
