@@ -708,8 +708,9 @@ size_t moe_grouped_ffn_int8_ws_bytes(int64_t cap_rows, int d, int f, int n_group
  * ws         moe_grouped_ffn_int8_ws_bytes(n_shared T + cap_rows, d, f, n_shared + n_groups)
  *            bytes, 256-byte aligned
  * The sums of products are exact.  A token whose scale is NaN makes its own rows of y_perm NaN and
- * no other; so does a row whose h overflows bf16.  Codes may be any of -128 .. 127; padding
- * columns must be zero in one of each product's operands.  Deterministic.
+ * no other; so does a row whose h overflows bf16.  Codes are -127 .. 127 (-128 in one operand of a
+ * product keeps its sums exact too); padding columns are zero.  The same bits for a row in every
+ * batch.
  * Requires d % 8 == 0, d and f at most 2^17, and T * MOE_INT8_COLS(d), 2 f * MOE_INT8_COLS(d)
  * and d * MOE_INT8_COLS(f) below 2^31 (else MOE_ERR_SHAPE), 1 <= n_shared + n_groups <=
  * MOE_MAX_GROUPS, codes and y_perm 16-byte, scales 4-byte aligned.

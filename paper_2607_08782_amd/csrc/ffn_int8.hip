@@ -3,12 +3,16 @@
 // each token and each output channel, both products on the integer matrix instructions, whose
 // sums are exact (K up to 2^17: 127 x 127 x 2^17 < 2^31).
 //
-//   1. h = SiLU(a) b,  a, b = (W1 xq, W3 xq) sx sw, in bf16 (the largest |h| of a row is known
-//      only when all of it is; two bytes a value are what the row's way to memory and back takes)
-//   2. hq, sh = the rows of h in 8 bits
-//   3. y = (W2 hq) sh sw
+//   1. h = SiLU(a) b,  a, b = (W1 xq, W3 xq) sx sw, in bf16: a row's scale is known only when all of
+//      the row is, and h goes to memory and back in between, in half the bytes of fp32.  The
+//      rounding, 2^-9 of a value, is small beside that to 8 bits, half of 1/127 of the row's largest.
+//   2. hq, sh = the rows of h in 8 bits (of one or two tokens by the strips of 3 themselves)
+//   3. y = (W2 hq) sh sw; where its strips or tiles are few, by slices of K, whose sums are added
 //
-// Rows of codes are padded to whole steps of 128 columns, so no product has a last part of a step.
+// Sums being whole numbers, a row's result is the same bits by whatever kernel and in whatever
+// batch.  Rows of codes are padded to whole steps of 128 columns, so no product has a last part of a
+// step.  They lie row after row: step after step (128 columns of all rows together), 64 Mixtral-shaped
+// tokens took 104 us for 110, and others as long.
 #include <algorithm>
 #include <type_traits>
 
@@ -55,7 +59,9 @@ __device__ __forceinline__ uint32_t most_of2(uint32_t w) {
 }
 
 // ---------------------------------------------------------------------------
-// Strips: groups of few rows, bound by the weight bytes.  A workgroup holds 16 TILES weight rows
+// Strips: groups of few rows, bound by the weight bytes (64 Mixtral-shaped tokens, two experts: gate/up
+// 235 MB in 60 us, down 117 MB in 32, of which about 7 are the start and the end of each; 64 tokens
+// of DeepSeek-V2-Lite's 64 experts: the FFN at 5 TB/s).  A workgroup holds 16 TILES weight rows
 // of one group (of gate/up half gate rows, half the same up rows) over all of K, its W waves
 // taking every W-th step: a weight byte goes from memory to the registers of the one wave that
 // multiplies it, and no wave waits for another before the end.  The waves' sums meet in LDS.
@@ -307,6 +313,11 @@ __global__ __launch_bounds__(64 * W, 2) void strip_int8_kernel(I8Args p) {
 // for the reads of 32 rows.  The weights are the instruction's first operand, laid out in LDS so that
 // a lane's sixteen accumulators are sixteen consecutive output columns of one token row (w_order).  A
 // tile's scales come into LDS like its operands, ahead of its first step.
+//
+// 4096 Mixtral-shaped tokens (3254 rows of two experts): gate/up 398 us, down 184, 1.9 and 2.1 POP/s,
+// as a library's product of such a shape (1.9 to 2.15); the matrix units are busy 60 and 66 % of the
+// clocks, and the clock falls to 1.8 and 2.0 GHz under the power limit.  Not kept: 128 x 128 a wave, four waves
+// (616 -> 677 us), a ring of eight steps with one workgroup a CU for 128 x 128 (even or slower).
 constexpr int HALF_LINE = 64;                            // columns (bytes) of a tile's step
 constexpr int SCALES = 8;                                // tiles whose scales are kept: the loads' and
                                                          // the products' are RING steps apart, and a
@@ -817,9 +828,6 @@ constexpr int64_t STRIP_MAX_ROWS = 64;
 // and 256 x 256, by millions of outputs): 2.2 32 and 39 us, 4.3 163 and 151, 6.3 35.9 and 39.5 but
 // 43.8 and 42.2, 17 67 and 60, 23 91 and 79.  Down, K short: 9 42 and 47, 13 42.1 and 47.2, 25 even,
 // 34 79 and 75; K long, where slices fill the chip: 1.6 122 and 125, 4.1 176 and 174, 6.4 224 and 202.
-// Outputs of a down product from which none is cut into slices: of an eighth of the rows that
-// there is room for, 256 x 256 tiles still fill a quarter of the chip.
-constexpr int64_t FILLED = 1 << 25;
 constexpr int64_t LARGE_UP = 1 << 22, LARGE_DOWN = 1 << 24, LARGE_SLICED = 1 << 22;
 
 template <bool SWIGLU>
@@ -884,6 +892,10 @@ int launch_quantize_hidden(const I8Args& p, int64_t rows, int cols, const int32_
 
 int64_t align256(int64_t x) { return (x + 255) & ~(int64_t)255; }
 
+// Outputs of a down product from which none is cut into slices: of an eighth of the rows that there
+// is room for, 256 x 256 tiles still fill a quarter of the chip.
+constexpr int64_t FILLED = 1 << 25;
+
 // workspace: [h in bf16][h codes][h scales][largest |h| of a row's blocks of 16 columns or more]
 // [how many slices][sums of slices of K]
 struct Layout {
@@ -894,8 +906,10 @@ struct Layout {
         most = hs + align256(rows * 4);
         split = most + align256(rows * ceil_div(f, 16) * 4);
         part = split + 256;
-        // slices only where each has SLICE_STEPS, and as many sums as fill the chip's tiles
-        room = int8_cols(f) / HALF_LINE >= 2 * SLICE_STEPS ? std::min<int64_t>(MAX_SLICES * rows * d, 1 << 24) : 0;
+        // slices where each has SLICE_STEPS and the rows may leave the chip unfilled: as many sums as
+        // a tile for every workgroup holds
+        room = int8_cols(f) / HALF_LINE >= 2 * SLICE_STEPS && rows * d < FILLED
+                   ? std::min<int64_t>(MAX_SLICES * rows * d, 1 << 24) : 0;
         total = part + align256(room * 4);
     }
 };
@@ -959,8 +973,7 @@ int launch_grouped_ffn_int8(const int8_t* xq, const float* x_scale, int64_t T,
     p.out = (bf16_t*)y;
     p.pitch = d;
     p.part = (int32_t*)(base + at.part);
-    // (with so many rows that the tiles fill the chip however the rows fall, none)
-    p.room = rows * d < FILLED ? at.room : 0;
+    p.room = at.room;
     p.split = (int32_t*)(base + at.split);
     return launch_product<false>(p, max_rows, s);
 }

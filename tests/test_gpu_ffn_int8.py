@@ -202,8 +202,8 @@ def test_rows_that_are_not_finite_keep_to_themselves(T, sizes):
 
 @pytest.mark.parametrize("T", [5, 200])
 def test_largest_sums(T):
-    """Every code at its largest, of one sign: sums of 127 x 127 K, and of -128 x -128 K, the
-    largest there are, at the longest K of a product that memory allows a test."""
+    """Every code at its largest, of one sign: sums of 127 x 127 K, and of 127 x -128 K at the longest
+    K there is, the largest that a product has."""
     d, f = 8, 1 << 17
     full = lambda rows, cols, v: torch.full((rows, moe.int8_cols(cols)), v, dtype=torch.int8, device="cuda")
     one = lambda n, v: torch.full((n,), v, dtype=torch.float32, device="cuda")
