@@ -7,6 +7,10 @@
 //
 // (c is constant: the choice has no gradient.)  Sums have one owner and a fixed order; the counts
 // are whole numbers, added by atomics in LDS.
+//
+// L lanes share a token, so that its scores come in 16-byte loads, side by side, and a softmax needs
+// few exchanges.  16384 tokens of 128 experts, 8.4 MB: sums 5.4 us, joining 7.2, gradient 8.0; launches
+// in a chain bound it (the bytes are 5 us in all), not the memory or the exponentials.
 #include <algorithm>
 
 #include "int8.h"

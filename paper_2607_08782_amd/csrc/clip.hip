@@ -4,6 +4,12 @@
 // Every tensor is cut into chunks of CHUNK elements, a workgroup each, numbered over all tensors.
 // Squares are summed in 64 bits (no gradient's square overflows or vanishes), a chunk's by its
 // threads and their tree, the chunks' in order: the same norm every time.
+//
+// Bound by the memory rate: 277 MB of fp32 (the matrices of 8 experts of 2048 x 1408) are read for the
+// norm in 73 us and read and written to be clipped in 83, where part of them is still in the caches and
+// part of what is written goes to memory during the next norm: 5.1 TB/s over both (a copy: 5.4).
+// Joining the chunks' sums takes 5.  Chunks of twice the length, last chunks first, and stores past the
+// caches were no faster.  81 small tensors: 6 + 2 + 6 us, a launch each.
 #include "int8.h"
 
 namespace moe {

@@ -60,8 +60,8 @@ __device__ __forceinline__ uint32_t most_of2(uint32_t w) {
 
 // ---------------------------------------------------------------------------
 // Strips: groups of few rows, bound by the weight bytes (64 Mixtral-shaped tokens, two experts: gate/up
-// 235 MB in 60 us, down 117 MB in 32, of which about 7 are the start and the end of each; 64 tokens
-// of DeepSeek-V2-Lite's 64 experts: the FFN at 5 TB/s).  A workgroup holds 16 TILES weight rows
+// 235 MB in 62 us, down 117 MB in 33, of which about 7 are the start and the end of each, and the last
+// of 1.75 rounds of the former's strips are half a chip).  A workgroup holds 16 TILES weight rows
 // of one group (of gate/up half gate rows, half the same up rows) over all of K, its W waves
 // taking every W-th step: a weight byte goes from memory to the registers of the one wave that
 // multiplies it, and no wave waits for another before the end.  The waves' sums meet in LDS.
@@ -714,7 +714,9 @@ __global__ __launch_bounds__(64 * 2 * WM, 2) void tile_int8_kernel(I8Args p) {
 #endif
 }
 
-// y of the slices' sums: four columns a thread, a workgroup's threads in one row.
+// y of the slices' sums: four columns a thread, a workgroup's threads in one row.  64 rows of 4096: 5 us,
+// as long as its launch; joined by a strip's last workgroup, whose release writes its XCD's L2 back, the
+// FFN takes 114 us in place of 105.
 __global__ __launch_bounds__(256) void join_slices_kernel(I8Args p, int64_t first) {
     const int slices = *p.split;
     if (slices == 1) return;                             // the tiles wrote y
@@ -841,38 +843,42 @@ int launch_product(I8Args& p, int64_t max_rows, hipStream_t s) {
 // ---------------------------------------------------------------------------
 // The hidden rows in 8 bits: a row's largest magnitude is that of its blocks', which the first
 // product left, so a row needs no pass of its own for it and any number of waves share one: a wave
-// takes 64 SEG chunks of eight values.
+// takes 64 SEG chunks of eight values.  Bound by the memory rate (3254 rows of 14336: 140 MB in 32 us,
+// 4.3 TB/s; 36 with a workgroup for every four units of the rows that there is room for, most of which
+// find none), of few rows by its launch (5 us).
 template <int SEG>
 __global__ __launch_bounds__(256) void quantize_hidden_kernel(const bf16_t* __restrict__ h, int64_t rows,
                                                               int cols, const uint32_t* __restrict__ most,
                                                               int blocks, const int32_t* __restrict__ end,
-                                                              int end_base, int units, int64_t first,
+                                                              int end_base, int units,
                                                               int8_t* __restrict__ q,
                                                               float* __restrict__ scales) {
     const int lane = threadIdx.x & 63;
-    const int64_t unit = (first + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int64_t row = unit / units;
-    const int part = (int)(unit - row * units);
-    if (row >= min(rows, (int64_t)end_base + end[0])) return;
     const int P = (int)int8_cols(cols), chunks = P / 8;
-    Piece<bf16_t, 8> held[SEG];
-    auto chunk = [&](int i) { return (part * SEG + i) * 64 + lane; };
+    const int64_t total = min(rows, (int64_t)end_base + end[0]) * units;
+    int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    for (; unit < total; unit += (int64_t)gridDim.x * 4) {
+        const int64_t row = unit / units;
+        const int part = (int)(unit - row * units);
+        Piece<bf16_t, 8> held[SEG];
+        auto chunk = [&](int i) { return (part * SEG + i) * 64 + lane; };
 #pragma unroll
-    for (int i = 0; i < SEG; ++i) held[i].load(h + row * P + (int64_t)min(chunk(i), chunks - 1) * 8);
-    uint32_t top = 0;
-    for (int b = lane; b < blocks; b += 64) top = max(top, most[row * blocks + b]);
-    const Int8Scale scale(lanes_max(top));
-    if (part == 0 && lane == 0) scales[row] = scale.s;
+        for (int i = 0; i < SEG; ++i) held[i].load(h + row * P + (int64_t)min(chunk(i), chunks - 1) * 8);
+        uint32_t top = 0;
+        for (int b = lane; b < blocks; b += 64) top = max(top, most[row * blocks + b]);
+        const Int8Scale scale(lanes_max(top));
+        if (part == 0 && lane == 0) scales[row] = scale.s;
 #pragma unroll
-    for (int i = 0; i < SEG; ++i) {
-        const int c = chunk(i);
-        float v[8];
-        held[i].values(v);
-        if (c * 8 + 8 > cols)
+        for (int i = 0; i < SEG; ++i) {
+            const int c = chunk(i);
+            float v[8];
+            held[i].values(v);
+            if (c * 8 + 8 > cols)
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (c * 8 + j >= cols) v[j] = 0.f;
-        if (c < chunks) scale.template store<true>(v, q + row * P + (int64_t)c * 8);
+                for (int j = 0; j < 8; ++j)
+                    if (c * 8 + j >= cols) v[j] = 0.f;
+            if (c < chunks) scale.template store<true>(v, q + row * P + (int64_t)c * 8);
+        }
     }
 }
 
@@ -880,14 +886,14 @@ int launch_quantize_hidden(const I8Args& p, int64_t rows, int cols, const int32_
                            float* scales, hipStream_t s) {
     const int64_t lanes = int8_cols(cols) / 8;
     const int seg = rows >= 1024 ? 4 : 1, units = (int)ceil_div(lanes, 64 * seg);
-    return launch_groups(ceil_div(rows * units, 4), 256, [&](int64_t first, unsigned n) {
-        if (seg == 4)
-            hipLaunchKernelGGL(quantize_hidden_kernel<4>, dim3(n), dim3(256), 0, s, p.out, rows, cols, p.most,
-                               p.blocks, end, end_base, units, first, q, scales);
-        else
-            hipLaunchKernelGGL(quantize_hidden_kernel<1>, dim3(n), dim3(256), 0, s, p.out, rows, cols, p.most,
-                               p.blocks, end, end_base, units, first, q, scales);
-    });
+    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(rows * units, 4), 8 * num_cus()));
+    if (seg == 4)
+        hipLaunchKernelGGL(quantize_hidden_kernel<4>, grid, dim3(256), 0, s, p.out, rows, cols, p.most,
+                           p.blocks, end, end_base, units, q, scales);
+    else
+        hipLaunchKernelGGL(quantize_hidden_kernel<1>, grid, dim3(256), 0, s, p.out, rows, cols, p.most,
+                           p.blocks, end, end_base, units, q, scales);
+    return launch_status();
 }
 
 int64_t align256(int64_t x) { return (x + 255) & ~(int64_t)255; }

