@@ -50,6 +50,7 @@ struct I8Args {
     int64_t rows;                        // rows of all groups at most
     int slices;                          // strips: slices of K
     int strips;                          // strips a group
+    int width;                           // and the output columns of one
     int slots;                           // groups that can hold rows at once
 };
 
@@ -60,7 +61,7 @@ __device__ __forceinline__ uint32_t most_of2(uint32_t w) {
 
 // ---------------------------------------------------------------------------
 // Strips: groups of few rows, bound by the weight bytes (64 Mixtral-shaped tokens, two experts: gate/up
-// 235 MB in 62 us, down 117 MB in 33, of which about 7 are the start and the end of each, and the last
+// 235 MB in 59 us, down 117 MB in 33, of which about 7 are the start and the end of each, and the last
 // of 1.75 rounds of the former's strips are half a chip).  A workgroup holds 16 TILES weight rows
 // of one group (of gate/up half gate rows, half the same up rows) over all of K, its W waves
 // taking every W-th step: a weight byte goes from memory to the registers of the one wave that
@@ -134,7 +135,10 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
     const int begin = SPLIT ? slice * per : 0, KT = SPLIT ? min(begin + per, p.P / STEP) : p.P / STEP;
     // weight rows of the strip: past the matrix's columns (of the gate half, past its N) they
     // read as zero
-    const int valid = max(min(SWIGLU ? ROWS / 2 : ROWS, p.N - n0), 0);
+    const int valid = max(min(p.width, p.N - n0), 0);
+    // the step that a strip of a long K starts with
+    const int turn = D > 1 ? (int)((unsigned)(n0 / p.width) * 3u % (unsigned)(KT - begin)) : 0;
+    auto column = [&](int t) { return (t + turn < KT ? t + turn : t + turn - (KT - begin)) * STEP; };
     int boff[TILES];
 #pragma unroll
     for (int j = 0; j < TILES; ++j) {
@@ -164,8 +168,8 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
         const int8_t* at[MS];
         // past the end of K: no traffic of the weights, and the last step's rows again
         auto load_b = [&](StripStep<MS, TILES>& s, int t) {
-            const int bytes = t < KT ? valid * p.P - t * STEP : 0;
-            const auto lo = rsrc(w_lo + (int64_t)t * STEP, bytes), hi = rsrc(w_hi + (int64_t)t * STEP, bytes);
+            const int at_k = column(t), bytes = t < KT ? valid * p.P - at_k : 0;
+            const auto lo = rsrc(w_lo + at_k, bytes), hi = rsrc(w_hi + at_k, bytes);
 #pragma unroll
             for (int j = 0; j < TILES; ++j)
 #pragma unroll
@@ -175,7 +179,7 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
                                                                      boff[j], 64 * u, 0));
         };
         auto load_a = [&](StripStep<MS, TILES>& s, int t) {
-            const int ta = min(t, KT - 1) * STEP;
+            const int ta = column(min(t, KT - 1));
 #pragma unroll
             for (int m = 0; m < MS; ++m)
 #pragma unroll
@@ -221,7 +225,7 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
         // four output columns a thread
         for (int i = tid; i < BM * PER_ROW; i += 64 * W) {
             const int r = i / PER_ROW, c = (i % PER_ROW) * 4;
-            const bool live = r < here && n0 + c < p.N;
+            const bool live = r < here && c < valid;
             const int row = row0 + min(m0 + r, rows - 1);
             if constexpr (SPLIT) {
                 i32x4 v = *(const i32x4*)&red[r * LD + c];
@@ -246,7 +250,7 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
                 sum(ROWS / 2 + c, p.N, b);
                 silu(y);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = n0 + c + e < p.N ? y[e] * b[e] : 0.f;
+                for (int e = 0; e < 4; ++e) y[e] = c + e < valid ? y[e] * b[e] : 0.f;
             }
             const uint2 w = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
             // (h's rows have room past N)
@@ -256,7 +260,7 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
                 uint32_t most = max(most_of2(w.x), most_of2(w.y));
 #pragma unroll
                 for (int o = 1; o < PER_ROW; o <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
-                if (c == 0 && live) p.most[(int64_t)row * p.blocks + n0 / (4 * PER_ROW)] = most;
+                if (c == 0 && live) p.most[(int64_t)row * p.blocks + n0 / p.width] = most;
             }
         }
     }
@@ -273,7 +277,7 @@ __global__ __launch_bounds__(64 * W, 2) void strip_int8_kernel(I8Args p) {
     __shared__ float row_scale[16];
     const int of_group = SPLIT ? p.strips * p.slices : p.strips, slot = blockIdx.x / of_group;
     const int strip = (int)blockIdx.x - slot * of_group, slice = SPLIT ? strip / p.strips : 0;
-    const int n0 = (strip - slice * p.strips) * 16 * TILES / (SWIGLU ? 2 : 1);
+    const int n0 = (strip - slice * p.strips) * p.width;
     if (SPLIT && blockIdx.x == 0 && threadIdx.x == 0) *p.split = p.slices;
     Group of;
     if (p.slots < p.n_groups) {
@@ -777,9 +781,20 @@ bool strips_quantize(int64_t max_rows, int f) {
     return max_rows <= 2 && max_rows * (int8_cols(f) + 16) <= QUANT_BYTES;
 }
 
+// Rows at most for which gate/up strips become as narrow as the rounds of two workgroups a CU allow, so
+// that the last round is as full as the others (Mixtral-shaped, 896 strips of 32 columns and 1024 of 28:
+// 16 tokens 73.7 and 71.6 us, 32 tokens 90.1 and 88.2; of more rows, which every strip reads, 64 tokens
+// 101.2 and 107.3).
+constexpr int64_t NARROW_MAX_ROWS = 32;
+
 template <bool SWIGLU, int W, int TILES, int D>
 int launch_strips_of(I8Args& p, int64_t max_rows, hipStream_t s) {
-    p.strips = (int)ceil_div(SWIGLU ? 2 * (int64_t)p.N : p.N, 16 * TILES);
+    p.width = 16 * TILES / (SWIGLU ? 2 : 1);
+    if (SWIGLU && max_rows <= NARROW_MAX_ROWS) {
+        const int64_t at_once = 2 * num_cus(), rounds = ceil_div(p.slots * ceil_div(p.N, p.width), at_once);
+        while (p.width > 16 && p.slots * ceil_div(p.N, p.width - 4) <= rounds * at_once) p.width -= 4;
+    }
+    p.strips = (int)ceil_div(p.N, p.width);
     if (SWIGLU) p.blocks = p.strips;                     // a strip is a block
     const dim3 grid((unsigned)(p.slots * p.strips)), block(64 * W);
     const bool few = max_rows <= 16;
@@ -806,17 +821,19 @@ int launch_strips_of(I8Args& p, int64_t max_rows, hipStream_t s) {
 
 // A short K gives a strip's waves few steps, and what a strip waits for at its start and end is
 // hidden by other workgroups: narrow strips, one step of loads in flight and registers for more
-// waves (FFN of 64 tokens, wide and two steps, narrow and one: DeepSeek-V2-Lite 97.3 and 91.2 us,
-// Qwen3-30B-A3B 22.7 and 20.3).  A long K: wide strips of gate and up rows, so that token rows are read
-// half as often (Mixtral-shaped 107 and 113), and two steps in the down product, whose strips are
-// few (16 tokens 73.2, with one 76.2).
+// waves (FFN of 64 tokens, wide and two steps, narrow and one: DeepSeek-V2-Lite 97.7 and 91.1 us,
+// Qwen3-30B-A3B 22.5 and 20.6).  A long K: wide strips of gate and up rows, so that token rows are read
+// half as often (64 Mixtral-shaped tokens 101.2 us, narrow 111.7), and two steps in flight (4 tokens 57.8,
+// one in gate/up 58.6, one in down 59.1; but 32 tokens 88.2, one in down 85.8).  Its strips start at other
+// steps of K than their neighbours, and go round: all at the same one, rows of a power of two of bytes,
+// they would ask few of the memory's channels at a time (1 token 32.1 and 33.7, 16 tokens 71.6 and 75.0,
+// 64 tokens 101.2 and 106.7; a short K is shorter without, 64 DeepSeek-V2-Lite tokens 91.1 and 92.1).
 constexpr int SHORT_K = 16 * STEP;
 
 template <bool SWIGLU>
 int launch_strips(I8Args& p, int64_t max_rows, hipStream_t s) {
     if (p.P <= SHORT_K) return launch_strips_of<SWIGLU, 4, 2, 1>(p, max_rows, s);
-    if constexpr (SWIGLU) return launch_strips_of<true, 4, 4, 1>(p, max_rows, s);
-    else return launch_strips_of<false, 4, 2, 2>(p, max_rows, s);
+    return launch_strips_of<SWIGLU, 4, SWIGLU ? 4 : 2, 2>(p, max_rows, s);
 }
 
 // Strips while no group can hold more rows than this, tiles past it (FFN, strips and tiles:

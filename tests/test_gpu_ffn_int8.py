@@ -113,6 +113,8 @@ def _run(sizes, d, f, T, *, gather=True, n_shared=0, seed=0, cap=None, x=None, s
     ([20, 1], 264, 4100, 20), ([70, 0, 300, 1], 512, 4224, 310), ([650, 30], 264, 8200, 700),
     # a token alone, two tokens: hidden rows quantized by the strips, also past what LDS holds
     ([1, 0, 1, 1], 520, 1000, 1), ([2, 1], 64, 15000, 2), ([2, 2], 128, 20000, 2),
+    # wide strips of a long K that go round from another step each, of other widths by the rounds
+    ([20, 7], 2104, 4590, 27), ([1], 4096, 1000, 1), ([2, 0, 1], 2304, 648, 2), ([30, 61], 2304, 4660, 64),
 ])
 def test_groups(sizes, d, f, T):
     say("[ffn int8]", sizes, d, f, T)
@@ -132,7 +134,7 @@ def test_shared_leading_groups(sizes, d, f, T, n_shared):
     _run(sizes, d, f, T, n_shared=n_shared, seed=5)
 
 
-@pytest.mark.parametrize("d,f", [(512, 1408), (1000, 328), (256, 4500)])
+@pytest.mark.parametrize("d,f", [(512, 1408), (1000, 328), (256, 4500), (2304, 4660)])
 def test_a_row_has_the_same_bits_in_every_batch(d, f):
     """Whatever kernels a batch takes: alone (strips that quantize), in a few rows (strips), in many
     (tiles of both sizes, slices of K)."""
