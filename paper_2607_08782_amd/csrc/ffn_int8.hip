@@ -120,7 +120,7 @@ __device__ __forceinline__ void quantize_rows(const I8Args& p, int8_t* codes, fl
 // QUANT (down): p.h's rows, as many as `codes` holds at a time, are quantized as the strip begins, by
 // all of its threads, and their scales go to `row_scale`.  SPLIT (down): the strip's slice of K, its
 // sums to p.part.
-template <bool SWIGLU, int W, int TILES, int MS, int D, bool QUANT = false, bool SPLIT = false>
+template <bool SWIGLU, int W, int TILES, int MS, int D, bool LONG, bool QUANT = false, bool SPLIT = false>
 __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int n0, int row0, int rows,
                                            int8_t* codes = nullptr, float* row_scale = nullptr,
                                            int slice = 0) {
@@ -137,7 +137,7 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
     // read as zero
     const int valid = max(min(p.width, p.N - n0), 0);
     // the step that a strip of a long K starts with
-    const int turn = D > 1 ? (int)((unsigned)(n0 / p.width) * 3u % (unsigned)(KT - begin)) : 0;
+    const int turn = LONG ? (int)((unsigned)(n0 / p.width) * 3u % (unsigned)(KT - begin)) : 0;
     auto column = [&](int t) { return (t + turn < KT ? t + turn : t + turn - (KT - begin)) * STEP; };
     int boff[TILES];
 #pragma unroll
@@ -268,7 +268,7 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
 }
 
 // MAX_MS = 1: no group holds more than 16 rows.  Otherwise each group takes the row blocks it needs.
-template <bool SWIGLU, int W, int TILES, int MAX_MS, int D, bool QUANT, bool SPLIT>
+template <bool SWIGLU, int W, int TILES, int MAX_MS, int D, bool LONG, bool QUANT, bool SPLIT>
 __global__ __launch_bounds__(64 * W, 2) void strip_int8_kernel(I8Args p) {
     constexpr int SUMS = W * 16 * MAX_MS * (16 * TILES + 4);
     static_assert(SUMS * 4 <= 80 * 1024, "two workgroups share a CU's LDS");
@@ -289,11 +289,11 @@ __global__ __launch_bounds__(64 * W, 2) void strip_int8_kernel(I8Args p) {
     }
     if (of.rows <= 0) return;
     if constexpr (QUANT) {
-        strip_rows<SWIGLU, W, TILES, 1, D, true>(p, red, of.g, n0, of.row0, of.rows, codes, row_scale);
+        strip_rows<SWIGLU, W, TILES, 1, D, LONG, true>(p, red, of.g, n0, of.row0, of.rows, codes, row_scale);
     } else {
         auto rows = [&](auto blocks) {
-            strip_rows<SWIGLU, W, TILES, decltype(blocks)::value, D, false, SPLIT>(p, red, of.g, n0, of.row0,
-                                                                                  of.rows, nullptr, nullptr, slice);
+            strip_rows<SWIGLU, W, TILES, decltype(blocks)::value, D, LONG, false, SPLIT>(
+                p, red, of.g, n0, of.row0, of.rows, nullptr, nullptr, slice);
         };
         if (MAX_MS == 1 || of.rows <= 16) rows(std::integral_constant<int, 1>{});
         else if (of.rows <= 32) rows(std::integral_constant<int, 2>{});
@@ -781,16 +781,16 @@ bool strips_quantize(int64_t max_rows, int f) {
     return max_rows <= 2 && max_rows * (int8_cols(f) + 16) <= QUANT_BYTES;
 }
 
-// Rows at most for which gate/up strips become as narrow as the rounds of two workgroups a CU allow, so
-// that the last round is as full as the others (Mixtral-shaped, 896 strips of 32 columns and 1024 of 28:
+// Few rows in a group at most: another shape of a long K's down strips (launch_strips), and gate/up strips
+// become as narrow as the rounds of two workgroups a CU allow, so that the last round is as full as the others (Mixtral-shaped, 896 strips of 32 columns and 1024 of 28:
 // 16 tokens 73.7 and 71.6 us, 32 tokens 90.1 and 88.2; of more rows, which every strip reads, 64 tokens
 // 101.2 and 107.3).
-constexpr int64_t NARROW_MAX_ROWS = 32;
+constexpr int64_t FEW_ROWS = 32;
 
-template <bool SWIGLU, int W, int TILES, int D>
+template <bool SWIGLU, int W, int TILES, int D, bool LONG>
 int launch_strips_of(I8Args& p, int64_t max_rows, hipStream_t s) {
     p.width = 16 * TILES / (SWIGLU ? 2 : 1);
-    if (SWIGLU && max_rows <= NARROW_MAX_ROWS) {
+    if (SWIGLU && max_rows <= FEW_ROWS) {
         const int64_t at_once = 2 * num_cus(), rounds = ceil_div(p.slots * ceil_div(p.N, p.width), at_once);
         while (p.width > 16 && p.slots * ceil_div(p.N, p.width - 4) <= rounds * at_once) p.width -= 4;
     }
@@ -800,22 +800,22 @@ int launch_strips_of(I8Args& p, int64_t max_rows, hipStream_t s) {
     const bool few = max_rows <= 16;
     if constexpr (!SWIGLU) {
         if (strips_quantize(max_rows, p.K)) {
-            hipLaunchKernelGGL((strip_int8_kernel<false, W, TILES, 1, D, true, false>), grid, block, 0, s, p);
+            hipLaunchKernelGGL((strip_int8_kernel<false, W, TILES, 1, D, LONG, true, false>), grid, block, 0, s, p);
             return launch_status();
         }
         // two slices of K where the strips alone give a CU one workgroup at most (Mixtral-shaped down
-        // product, 256 strips of K = 14336: 64 tokens 108 and 105 us, 32 tokens 93 and 91)
+        // product, 256 strips of K = 14336: 64 tokens 108 and 105 us)
         if ((int64_t)grid.x <= num_cus() && p.P >= 2 * SLICE_STEPS * HALF_LINE && 2 * p.rows * p.N <= p.room) {
             p.slices = 2;
             const dim3 more(grid.x * p.slices);
-            if (few) hipLaunchKernelGGL((strip_int8_kernel<false, W, TILES, 1, D, false, true>), more, block, 0, s, p);
-            else hipLaunchKernelGGL((strip_int8_kernel<false, W, TILES, 4, D, false, true>), more, block, 0, s, p);
+            if (few) hipLaunchKernelGGL((strip_int8_kernel<false, W, TILES, 1, D, LONG, false, true>), more, block, 0, s, p);
+            else hipLaunchKernelGGL((strip_int8_kernel<false, W, TILES, 4, D, LONG, false, true>), more, block, 0, s, p);
             const int st = launch_status();
             return st != MOE_OK ? st : launch_join_slices(p, s);
         }
     }
-    if (few) hipLaunchKernelGGL((strip_int8_kernel<SWIGLU, W, TILES, 1, D, false, false>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((strip_int8_kernel<SWIGLU, W, TILES, 4, D, false, false>), grid, block, 0, s, p);
+    if (few) hipLaunchKernelGGL((strip_int8_kernel<SWIGLU, W, TILES, 1, D, LONG, false, false>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((strip_int8_kernel<SWIGLU, W, TILES, 4, D, LONG, false, false>), grid, block, 0, s, p);
     return launch_status();
 }
 
@@ -824,16 +824,20 @@ int launch_strips_of(I8Args& p, int64_t max_rows, hipStream_t s) {
 // waves (FFN of 64 tokens, wide and two steps, narrow and one: DeepSeek-V2-Lite 97.7 and 91.1 us,
 // Qwen3-30B-A3B 22.5 and 20.6).  A long K: wide strips of gate and up rows, so that token rows are read
 // half as often (64 Mixtral-shaped tokens 101.2 us, narrow 111.7), and two steps in flight (4 tokens 57.8,
-// one in gate/up 58.6, one in down 59.1; but 32 tokens 88.2, one in down 85.8).  Its strips start at other
-// steps of K than their neighbours, and go round: all at the same one, rows of a power of two of bytes,
-// they would ask few of the memory's channels at a time (1 token 32.1 and 33.7, 16 tokens 71.6 and 75.0,
-// 64 tokens 101.2 and 106.7; a short K is shorter without, 64 DeepSeek-V2-Lite tokens 91.1 and 92.1).
+// one in gate/up 58.6).  Down strips of a long K are few: of 16 columns by eight waves while every strip
+// reads few rows (by four waves of 32 columns and by these: 1 token 32.1 and 28.3 us, 4 tokens 57.8 and
+// 53.4, 16 tokens 71.6 and 69.0, 32 tokens 88.1 and 87.0, 64 tokens 101.9 and 108.4).  Strips of a long K start
+// at other steps of it than their neighbours, and go round: all at the same one, rows of a power of two of
+// bytes, they would ask few of the memory's channels at a time (1 token 32.1 and 33.7, 16 tokens 71.6 and
+// 75.0, 64 tokens 101.2 and 106.7; a short K is shorter without, 64 DeepSeek-V2-Lite tokens 91.1 and 92.1).
 constexpr int SHORT_K = 16 * STEP;
 
 template <bool SWIGLU>
 int launch_strips(I8Args& p, int64_t max_rows, hipStream_t s) {
-    if (p.P <= SHORT_K) return launch_strips_of<SWIGLU, 4, 2, 1>(p, max_rows, s);
-    return launch_strips_of<SWIGLU, 4, SWIGLU ? 4 : 2, 2>(p, max_rows, s);
+    if (p.P <= SHORT_K) return launch_strips_of<SWIGLU, 4, 2, 1, false>(p, max_rows, s);
+    if constexpr (SWIGLU) return launch_strips_of<true, 4, 4, 2, true>(p, max_rows, s);
+    else if (max_rows <= FEW_ROWS) return launch_strips_of<false, 8, 1, 2, true>(p, max_rows, s);
+    else return launch_strips_of<false, 4, 2, 2, true>(p, max_rows, s);
 }
 
 // Strips while no group can hold more rows than this, tiles past it (FFN, strips and tiles:
