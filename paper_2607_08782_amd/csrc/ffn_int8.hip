@@ -267,7 +267,8 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
 #endif
 }
 
-// MAX_MS = 1: no group holds more than 16 rows.  Otherwise each group takes the row blocks it needs.
+// MAX_MS = 1: no group holds more than 16 rows.  Otherwise each group takes the row blocks it needs (of four,
+// two or one alone, 64 Mixtral-shaped tokens take 101.4 us for 100.4, 64 of DeepSeek-V2-Lite 91.6 for 90.1).
 template <bool SWIGLU, int W, int TILES, int MAX_MS, int D, bool LONG, bool QUANT, bool SPLIT>
 __global__ __launch_bounds__(64 * W, 2) void strip_int8_kernel(I8Args p) {
     constexpr int SUMS = W * 16 * MAX_MS * (16 * TILES + 4);
@@ -297,6 +298,7 @@ __global__ __launch_bounds__(64 * W, 2) void strip_int8_kernel(I8Args p) {
         };
         if (MAX_MS == 1 || of.rows <= 16) rows(std::integral_constant<int, 1>{});
         else if (of.rows <= 32) rows(std::integral_constant<int, 2>{});
+        else if (of.rows <= 48) rows(std::integral_constant<int, 3>{});
         else rows(std::integral_constant<int, MAX_MS>{});
     }
 }
@@ -782,9 +784,9 @@ bool strips_quantize(int64_t max_rows, int f) {
 }
 
 // Few rows in a group at most: another shape of a long K's down strips (launch_strips), and gate/up strips
-// become as narrow as the rounds of two workgroups a CU allow, so that the last round is as full as the others (Mixtral-shaped, 896 strips of 32 columns and 1024 of 28:
-// 16 tokens 73.7 and 71.6 us, 32 tokens 90.1 and 88.2; of more rows, which every strip reads, 64 tokens
-// 101.2 and 107.3).
+// become as narrow as the rounds of two workgroups a CU allow, so that the last round is as full as the
+// others (Mixtral-shaped, 896 strips of 32 columns and 1024 of 28: 16 tokens 73.7 and 71.6 us, 32 tokens
+// 90.1 and 88.2; of more rows, which every strip reads, 64 tokens 101.2 and 107.3).
 constexpr int64_t FEW_ROWS = 32;
 
 template <bool SWIGLU, int W, int TILES, int D, bool LONG>
