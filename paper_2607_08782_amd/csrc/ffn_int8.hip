@@ -60,9 +60,8 @@ __device__ __forceinline__ uint32_t most_of2(uint32_t w) {
 }
 
 // ---------------------------------------------------------------------------
-// Strips: groups of few rows, bound by the weight bytes (64 Mixtral-shaped tokens, two experts: gate/up
-// 235 MB in 59 us, down 117 MB in 33, of which about 7 are the start and the end of each, and the last
-// of 1.75 rounds of the former's strips are half a chip).  A workgroup holds 16 TILES weight rows
+// Strips: groups of few rows, bound by the weight bytes (16 Mixtral-shaped tokens, two experts: gate/up
+// 235 MB in 47 us, down 117 MB in 26, of which 5 or more are the start and the end of each).  A workgroup holds 16 TILES weight rows
 // of one group (of gate/up half gate rows, half the same up rows) over all of K, its W waves
 // taking every W-th step: a weight byte goes from memory to the registers of the one wave that
 // multiplies it, and no wave waits for another before the end.  The waves' sums meet in LDS.
@@ -301,6 +300,200 @@ __global__ __launch_bounds__(64 * W, 2) void strip_int8_kernel(I8Args p) {
         else if (of.rows <= 48) rows(std::integral_constant<int, 3>{});
         else rows(std::integral_constant<int, MAX_MS>{});
     }
+}
+
+// ---------------------------------------------------------------------------
+// Wide strips: groups of some rows over a long K.  A workgroup's four waves each hold 16 columns (of
+// gate/up 16 gate and the same 16 up rows) over all of K, or a slice of it, and share the token rows:
+// these come by direct loads into a ring of RING steps in LDS, once for four waves' weights, while
+// as many steps of weights are on their way to each wave's registers.  (Strips whose waves share K read
+// every row from the L2 for 32 columns: of 64 Mixtral-shaped tokens' gate/up 58 us, without their rows'
+// loads 49, these 49; down 32, 25 and 27.)  One barrier a step; no sums to join.  A step's rows of 128
+// bytes hold chunk c of row r at c ^ (r & 7).
+//
+// 64 Mixtral-shaped tokens: gate/up 235 MB in 50 us, down 117 MB in 28, 4.7 and 4.2 TB/s, of which about 7
+// each are the start and the end.
+constexpr int WIDE_COLS = 64, WIDE_LDS = 64 * 1024;
+
+template <bool SWIGLU, int MS>
+struct WideStrip {
+    static constexpr int TILES = SWIGLU ? 2 : 1, LB = 2 * TILES;               // weight loads of a wave's step
+    static constexpr int ROWS = MS <= 4 ? 64 : 128, STAGE = ROWS * STEP, LA = ROWS / 32;      // and rows'
+    static constexpr int RING = WIDE_LDS / STAGE, AHEAD = RING;
+    // behind a step's rows at the time they are waited for: its step's weights, RING - 2 steps
+    static constexpr int BEHIND = LB + (RING - 2) * (LA + LB);
+    static_assert(BEHIND < 64, "what a wait can count");
+};
+
+template <bool SWIGLU, int MS, bool SPLIT>
+__device__ __forceinline__ void wide_rows(const I8Args& p, char* ring, int g, int n_first, int row0, int rows,
+                                          int slice) {
+#ifdef __HIP_DEVICE_COMPILE__
+    typedef WideStrip<SWIGLU, MS> S;
+    constexpr int TILES = S::TILES;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int i16 = lane & 15, quarter = lane >> 4, n0 = n_first + 16 * wave;
+    const int per = SPLIT ? (p.P / STEP + p.slices - 1) / p.slices : 0;
+    const int begin = SPLIT ? slice * per : 0, KT = (SPLIT ? min(begin + per, p.P / STEP) : p.P / STEP) - begin;
+    const int turn = (int)((unsigned)(n_first / WIDE_COLS) * 3u % (unsigned)KT);
+    // column of step t; t < KT
+    auto column = [&](int t) { return (begin + (t + turn < KT ? t + turn : t + turn - KT)) * STEP; };
+    const int valid = max(min(16, p.N - n0), 0);
+    const int boff = i16 * p.P + quarter * 16;
+    const int8_t* const w_lo = p.w[g] + (int64_t)n0 * p.P;
+    const int8_t* const w_hi = w_lo + (SWIGLU ? (int64_t)p.N * p.P : 0);
+    auto rsrc = [](const void* base, int bytes) {
+        return __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, bytes, RSRC_WORD3);
+    };
+    for (int m0 = 0; m0 < rows; m0 += S::ROWS) {
+        const __amdgpu_buffer_rsrc_t ra = rsrc(p.a + (p.a_rows ? 0 : (int64_t)(row0 + m0) * p.P), -1);
+        // rows past the group repeat its last one; their sums are not stored
+        int aoff[S::LA];
+#pragma unroll
+        for (int i = 0; i < S::LA; ++i) {
+            const int r = min(32 * i + 8 * wave + (lane >> 3), rows - 1 - m0);
+            aoff[i] = (p.a_rows ? p.a_rows[row0 + m0 + r] : r) * p.P + ((lane & 7) ^ (lane >> 3)) * 16;
+        }
+        i32x4 acc[MS][TILES], b[S::AHEAD][TILES][2];
+#pragma unroll
+        for (int m = 0; m < MS; ++m)
+#pragma unroll
+            for (int j = 0; j < TILES; ++j) acc[m][j] = i32x4{0, 0, 0, 0};
+        // past the end of K, and of a wave whose columns all lie past N: no traffic of the weights; the
+        // last step's rows again
+        auto load_b = [&](i32x4 (&to)[TILES][2], int t) {
+            const int at_k = column(min(t, KT - 1)), bytes = t < KT ? max(valid * p.P - at_k, 0) : 0;
+            const auto lo = rsrc(w_lo + at_k, bytes), hi = rsrc(w_hi + at_k, bytes);
+#pragma unroll
+            for (int j = 0; j < TILES; ++j)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    to[j][u] = __builtin_bit_cast(
+                        i32x4, __builtin_amdgcn_raw_buffer_load_b128(j > 0 ? hi : lo, boff, 64 * u, 0));
+        };
+        auto load_a = [&](char* st, int t) {
+            const int at_k = column(min(t, KT - 1));
+#pragma unroll
+            for (int i = 0; i < S::LA; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void*)(st + (32 * i + 8 * wave) * STEP), 16, aoff[i],
+                                                         at_k, 0, 0);
+        };
+        // In the order of the steps below, which the waits count on: the barriers between them keep the
+        // compiler from another.
+#pragma unroll
+        for (int t = 0; t < S::AHEAD; ++t) {
+            const int rows_of = t - (S::AHEAD - (S::RING - 1));
+            if (rows_of >= 0) load_a(ring + rows_of * S::STAGE, rows_of);
+            __builtin_amdgcn_sched_barrier(0);
+            load_b(b[t], t);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        unsigned here = 0, fill = (S::RING - 1) * S::STAGE;
+#pragma clang loop unroll(disable)
+        for (int t0 = 0; t0 < KT; t0 += S::AHEAD) {
+            // (past the end of K: zero weights.  A way out between the steps would have the compiler wait for
+            // every load)
+#pragma unroll
+            for (int i = 0; i < S::AHEAD; ++i) {
+                const int t = t0 + i;
+                wait_vm<S::BEHIND>();
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                // every wave holds the last step's rows in registers: its slot is free
+                load_a(ring + fill, t + S::RING - 1);
+                __builtin_amdgcn_sched_barrier(0);
+                const char* const st = ring + here;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    i32x4 a[MS];
+#pragma unroll
+                    for (int m = 0; m < MS; ++m)
+                        a[m] = *(const i32x4*)(st + (16 * m + i16) * STEP + (((4 * u + quarter) ^ (i16 & 7)) * 16));
+#pragma unroll
+                    for (int j = 0; j < TILES; ++j)
+#pragma unroll
+                        for (int m = 0; m < MS; ++m)
+                            acc[m][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[i][j][u], a[m], acc[m][j], 0, 0, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                load_b(b[i], t + S::AHEAD);
+                __builtin_amdgcn_sched_barrier(0);
+                fill = here;
+                here = here == (S::RING - 1) * S::STAGE ? 0 : here + S::STAGE;
+            }
+        }
+        wait_vm<0>();                                    // the ring is written no more
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        // four columns of a row a lane
+        const int c = n0 + 4 * quarter;
+        uint32_t* const s_most = (uint32_t*)ring;        // [waves][ROWS]
+#pragma unroll
+        for (int m = 0; m < MS; ++m) {
+            const int r = m0 + 16 * m + i16, row = row0 + min(r, rows - 1);
+            const bool live = r < rows && c < p.N;
+            if constexpr (SPLIT) {
+                if (live) *(i32x4*)(p.part + (slice * (int64_t)first_row(p, p.n_groups) + row) * p.N + c) = acc[m][0];
+                continue;
+            }
+            const float sx = p.as[p.a_rows ? p.a_rows[row] : row];
+            float y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = (float)acc[m][0][e] * sx * p.ws[g][min(c + e, p.N - 1)];
+            if constexpr (SWIGLU) {
+                silu(y);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    y[e] = c + e < p.N ? y[e] * ((float)acc[m][1][e] * sx * p.ws[g][p.N + min(c + e, p.N - 1)]) : 0.f;
+            }
+            const uint2 w = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+            // (h's rows have room past N)
+            if (live) *(uint2*)(p.out + row * p.pitch + c) = w;
+            if (SWIGLU) {
+                uint32_t most = max(most_of2(w.x), most_of2(w.y));
+                most = max(most, (uint32_t)__shfl_xor((int)most, 16, 64));
+                most = max(most, (uint32_t)__shfl_xor((int)most, 32, 64));
+                if (quarter == 0) s_most[wave * S::ROWS + 16 * m + i16] = most;
+            }
+        }
+        if constexpr (SWIGLU) {                          // a strip is a block
+            __syncthreads();
+            if (tid < 16 * MS && m0 + tid < rows) {
+                uint32_t most = 0;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) most = max(most, s_most[q * S::ROWS + tid]);
+                p.most[(int64_t)(row0 + m0 + tid) * p.blocks + n_first / WIDE_COLS] = most;
+            }
+            __syncthreads();                             // the ring may be written again
+        }
+    }
+#endif
+}
+
+template <bool SWIGLU, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void wide_strip_int8_kernel(I8Args p) {
+    __shared__ __attribute__((aligned(1024))) char ring[WIDE_LDS];
+    const int of_group = SPLIT ? p.strips * p.slices : p.strips, slot = blockIdx.x / of_group;
+    const int strip = (int)blockIdx.x - slot * of_group, slice = SPLIT ? strip / p.strips : 0;
+    const int n0 = (strip - slice * p.strips) * WIDE_COLS;
+    if (SPLIT && blockIdx.x == 0 && threadIdx.x == 0) *p.split = p.slices;
+    Group of;
+    if (p.slots < p.n_groups) {
+        of = nth_group(p, slot);
+    } else {
+        of.g = slot;
+        of.row0 = __builtin_amdgcn_readfirstlane(first_row(p, slot));
+        of.rows = __builtin_amdgcn_readfirstlane(first_row(p, slot + 1)) - of.row0;
+    }
+    if (of.rows <= 0) return;
+    auto rows = [&](auto blocks) {
+        wide_rows<SWIGLU, decltype(blocks)::value, SPLIT>(p, ring, of.g, n0, of.row0, of.rows, slice);
+    };
+    if (of.rows <= 16) rows(std::integral_constant<int, 1>{});
+    else if (of.rows <= 32) rows(std::integral_constant<int, 2>{});
+    else if (of.rows <= 48) rows(std::integral_constant<int, 3>{});
+    else if (of.rows <= 64) rows(std::integral_constant<int, 4>{});
+    else if (of.rows <= 96) rows(std::integral_constant<int, 6>{});
+    else rows(std::integral_constant<int, 8>{});
 }
 
 // ---------------------------------------------------------------------------
@@ -821,6 +1014,26 @@ int launch_strips_of(I8Args& p, int64_t max_rows, hipStream_t s) {
     return launch_status();
 }
 
+template <bool SWIGLU>
+int launch_wide_strips(I8Args& p, hipStream_t s) {
+    p.strips = (int)ceil_div(p.N, WIDE_COLS);
+    if (SWIGLU) p.blocks = p.strips;
+    const int64_t groups = (int64_t)p.slots * p.strips;
+    if constexpr (!SWIGLU) {
+        // slices of K while the strips give a CU one workgroup at most
+        while (p.slices < MAX_SLICES && groups * p.slices <= num_cus() &&
+               p.P / HALF_LINE >= 2 * p.slices * SLICE_STEPS && 2 * p.slices * p.rows * p.N <= p.room)
+            p.slices *= 2;
+        if (p.slices > 1) {
+            hipLaunchKernelGGL((wide_strip_int8_kernel<false, true>), dim3((unsigned)(groups * p.slices)), dim3(256), 0, s, p);
+            const int st = launch_status();
+            return st != MOE_OK ? st : launch_join_slices(p, s);
+        }
+    }
+    hipLaunchKernelGGL((wide_strip_int8_kernel<SWIGLU, false>), dim3((unsigned)groups), dim3(256), 0, s, p);
+    return launch_status();
+}
+
 // A short K gives a strip's waves few steps, and what a strip waits for at its start and end is
 // hidden by other workgroups: narrow strips, one step of loads in flight and registers for more
 // waves (FFN of 64 tokens, wide and two steps, narrow and one: DeepSeek-V2-Lite 97.7 and 91.1 us,
@@ -842,6 +1055,13 @@ int launch_strips(I8Args& p, int64_t max_rows, hipStream_t s) {
     else return launch_strips_of<false, 4, 2, 2, true>(p, max_rows, s);
 }
 
+// Wide strips over a long K where a group can hold more than FEW_ROWS rows, up to what one pass over its
+// weights takes, and has room for more than 16 on average (FFN, strips or past 64 tokens tiles, and these:
+// Mixtral-shaped, 24 tokens 81.6 and 83.6 us, 32 tokens 86.0 and 84.2, 48 tokens 95.3 and 85.3, 64 tokens 100.5
+// and 86.8, 96 tokens 106.3 and 91.8, 128 tokens 109.5 and 97.0, 256 tokens 126 and 150; 64 tokens of 8 of 16
+// experts of 5120 x 2560, eight rows each, 78.6 and 83.2, 128 tokens 113.8 and 98.1).
+constexpr int64_t WIDE_MAX_ROWS = 128;
+
 // Strips while no group can hold more rows than this, tiles past it (FFN, strips and tiles:
 // Mixtral-shaped, 32 tokens 91 and 97 us, 64 tokens 105 and 102, 96 tokens 127 and 105; 64
 // DeepSeek-V2-Lite experts, 64 tokens 91 and 97, 128 tokens 125 and 125; Qwen3-30B-A3B, 64 tokens 20
@@ -857,6 +1077,8 @@ constexpr int64_t LARGE_UP = 1 << 22, LARGE_DOWN = 1 << 24, LARGE_SLICED = 1 << 
 
 template <bool SWIGLU>
 int launch_product(I8Args& p, int64_t max_rows, hipStream_t s) {
+    if (p.P > SHORT_K && max_rows > FEW_ROWS && max_rows <= WIDE_MAX_ROWS && p.rows > 16 * (int64_t)p.n_groups)
+        return launch_wide_strips<SWIGLU>(p, s);
     if (max_rows <= STRIP_MAX_ROWS) return launch_strips<SWIGLU>(p, max_rows, s);
     if (SWIGLU) p.blocks = (int)ceil_div(p.N, 32);
     const int64_t large = SWIGLU ? LARGE_UP : p.room > 0 ? LARGE_SLICED : LARGE_DOWN;

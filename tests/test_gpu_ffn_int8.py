@@ -115,6 +115,10 @@ def _run(sizes, d, f, T, *, gather=True, n_shared=0, seed=0, cap=None, x=None, s
     ([1, 0, 1, 1], 520, 1000, 1), ([2, 1], 64, 15000, 2), ([2, 2], 128, 20000, 2),
     # wide strips of a long K that go round from another step each, of other widths by the rounds
     ([20, 7], 2104, 4590, 27), ([1], 4096, 1000, 1), ([2, 0, 1], 2304, 648, 2), ([30, 61], 2304, 4660, 64),
+    # waves side by side that share a long K's rows: one to all of their row blocks, columns past the end
+    # of which most or all waves lie, slices of K
+    ([33, 1, 0, 49], 2304, 2312, 50), ([64, 17, 32], 4096, 72, 64), ([40, 100, 7], 2056, 3000, 100),
+    ([97, 128], 2304, 2600, 128), ([40], 8, 9000, 40), ([36, 3], 24, 3000, 36), ([90], 2104, 1, 90),
 ])
 def test_groups(sizes, d, f, T):
     say("[ffn int8]", sizes, d, f, T)
@@ -148,14 +152,14 @@ def test_a_row_has_the_same_bits_in_every_batch(d, f):
         off = torch.tensor([0, n], dtype=torch.int32, device="cuda")
         return moe.moe_grouped_ffn_int8(xq[:n], sx[:n], off, table)
     want = run(5000)
-    for n in (1, 2, 3, 16, 17, 33, 64, 65, 300, 2000):
+    for n in (1, 2, 3, 16, 17, 33, 64, 65, 90, 128, 300, 2000):
         assert torch.equal(run(n), want[:n]), n
 
 
-@pytest.mark.parametrize("T,n", [(1, 40), (2, 21)])
-def test_a_group_that_names_a_token_more_than_once(T, n):
+@pytest.mark.parametrize("T,n,d,f", [(1, 40, 256, 12000), (2, 21, 256, 12000), (40, 300, 2304, 3000),
+                                     (100, 290, 2304, 3000)])
+def test_a_group_that_names_a_token_more_than_once(T, n, d, f):
     """More rows in a group than tokens: every one is computed."""
-    d, f = 256, 12000
     xq, sx = moe.moe_quantize_int8(torch.randn(T, d, generator=torch.Generator().manual_seed(4)).cuda())
     w13, w2 = _experts(2, d, f, 3)
     table = moe.Int8WeightTable(w13, w2, d, f)
