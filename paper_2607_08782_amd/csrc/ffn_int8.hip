@@ -1059,7 +1059,8 @@ int launch_strips(I8Args& p, int64_t max_rows, hipStream_t s) {
 // weights takes, and has room for more than 16 on average (FFN, strips or past 64 tokens tiles, and these:
 // Mixtral-shaped, 24 tokens 81.6 and 83.6 us, 32 tokens 86.0 and 84.2, 48 tokens 95.3 and 85.3, 64 tokens 100.5
 // and 86.8, 96 tokens 106.3 and 91.8, 128 tokens 109.5 and 97.0, 256 tokens 126 and 150; 64 tokens of 8 of 16
-// experts of 5120 x 2560, eight rows each, 78.6 and 83.2, 128 tokens 113.8 and 98.1).
+// experts of 5120 x 2560, eight rows each, 78.6 and 83.2, 128 tokens 113.8 and 98.1; a short K, 64 tokens of 8
+// experts of DeepSeek-V2-Lite, 24.7 and 29.0).
 constexpr int64_t WIDE_MAX_ROWS = 128;
 
 // Strips while no group can hold more rows than this, tiles past it (FFN, strips and tiles:
