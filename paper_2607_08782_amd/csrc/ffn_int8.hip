@@ -266,7 +266,7 @@ __device__ __forceinline__ void strip_rows(const I8Args& p, int* red, int g, int
 #endif
 }
 
-// MAX_MS = 1: no group holds more than 16 rows.  Otherwise each group takes the row blocks it needs (of four,
+// MAX_MS = 1, 2: no group holds more than 16, 32 rows.  Otherwise each group takes the row blocks it needs (of four,
 // two or one alone, 64 Mixtral-shaped tokens take 101.4 us for 100.4, 64 of DeepSeek-V2-Lite 91.6 for 90.1).
 template <bool SWIGLU, int W, int TILES, int MAX_MS, int D, bool LONG, bool QUANT, bool SPLIT>
 __global__ __launch_bounds__(64 * W, 2) void strip_int8_kernel(I8Args p) {
@@ -295,10 +295,15 @@ __global__ __launch_bounds__(64 * W, 2) void strip_int8_kernel(I8Args p) {
             strip_rows<SWIGLU, W, TILES, decltype(blocks)::value, D, LONG, false, SPLIT>(
                 p, red, of.g, n0, of.row0, of.rows, nullptr, nullptr, slice);
         };
-        if (MAX_MS == 1 || of.rows <= 16) rows(std::integral_constant<int, 1>{});
-        else if (of.rows <= 32) rows(std::integral_constant<int, 2>{});
-        else if (of.rows <= 48) rows(std::integral_constant<int, 3>{});
-        else rows(std::integral_constant<int, MAX_MS>{});
+        if (MAX_MS == 1 || of.rows <= 16) {
+            rows(std::integral_constant<int, 1>{});
+        } else if constexpr (MAX_MS > 1) {
+            if (MAX_MS == 2 || of.rows <= 32) rows(std::integral_constant<int, 2>{});
+            else if constexpr (MAX_MS > 2) {
+                if (of.rows <= 48) rows(std::integral_constant<int, 3>{});
+                else rows(std::integral_constant<int, 4>{});
+            }
+        }
     }
 }
 
@@ -982,10 +987,10 @@ bool strips_quantize(int64_t max_rows, int f) {
 // 90.1 and 88.2; of more rows, which every strip reads, 64 tokens 101.2 and 107.3).
 constexpr int64_t FEW_ROWS = 32;
 
-template <bool SWIGLU, int W, int TILES, int D, bool LONG>
+template <bool SWIGLU, int W, int TILES, int D, bool LONG, int MAX_MS = 4>
 int launch_strips_of(I8Args& p, int64_t max_rows, hipStream_t s) {
     p.width = 16 * TILES / (SWIGLU ? 2 : 1);
-    if (SWIGLU && max_rows <= FEW_ROWS) {
+    if (SWIGLU && LONG && max_rows <= FEW_ROWS) {
         const int64_t at_once = 2 * num_cus(), rounds = ceil_div(p.slots * ceil_div(p.N, p.width), at_once);
         while (p.width > 16 && p.slots * ceil_div(p.N, p.width - 4) <= rounds * at_once) p.width -= 4;
     }
@@ -993,25 +998,34 @@ int launch_strips_of(I8Args& p, int64_t max_rows, hipStream_t s) {
     if (SWIGLU) p.blocks = p.strips;                     // a strip is a block
     const dim3 grid((unsigned)(p.slots * p.strips)), block(64 * W);
     const bool few = max_rows <= 16;
-    if constexpr (!SWIGLU) {
+    constexpr bool MANY = LONG && !SWIGLU && MAX_MS == 4;    // more than FEW_ROWS
+    if constexpr (!SWIGLU && !MANY)
         if (strips_quantize(max_rows, p.K)) {
             hipLaunchKernelGGL((strip_int8_kernel<false, W, TILES, 1, D, LONG, true, false>), grid, block, 0, s, p);
             return launch_status();
         }
-        // two slices of K where the strips alone give a CU one workgroup at most (Mixtral-shaped down
-        // product, 256 strips of K = 14336: 64 tokens 108 and 105 us)
-        if ((int64_t)grid.x <= num_cus() && p.P >= 2 * SLICE_STEPS * HALF_LINE && 2 * p.rows * p.N <= p.room) {
-            p.slices = 2;
-            const dim3 more(grid.x * p.slices);
-            if (few) hipLaunchKernelGGL((strip_int8_kernel<false, W, TILES, 1, D, LONG, false, true>), more, block, 0, s, p);
-            else hipLaunchKernelGGL((strip_int8_kernel<false, W, TILES, 4, D, LONG, false, true>), more, block, 0, s, p);
-            const int st = launch_status();
+    // two slices of K where the strips alone give a CU one workgroup at most (Mixtral-shaped down
+    // product, 256 strips of K = 14336: 64 tokens 108 and 105 us)
+    constexpr bool SLICED = !SWIGLU && LONG;
+    if (SLICED && (int64_t)grid.x <= num_cus() && p.P >= 2 * SLICE_STEPS * HALF_LINE && 2 * p.rows * p.N <= p.room)
+        p.slices = 2;
+    auto launch = [&](auto split) {
+        constexpr bool SPLIT = decltype(split)::value;
+        const dim3 all(grid.x * (SPLIT ? p.slices : 1));
+        if constexpr (!MANY)
+            if (few) {
+                hipLaunchKernelGGL((strip_int8_kernel<SWIGLU, W, TILES, 1, D, LONG, false, SPLIT>), all, block, 0, s, p);
+                return launch_status();
+            }
+        hipLaunchKernelGGL((strip_int8_kernel<SWIGLU, W, TILES, MAX_MS, D, LONG, false, SPLIT>), all, block, 0, s, p);
+        return launch_status();
+    };
+    if constexpr (SLICED)
+        if (p.slices > 1) {
+            const int st = launch(std::true_type{});
             return st != MOE_OK ? st : launch_join_slices(p, s);
         }
-    }
-    if (few) hipLaunchKernelGGL((strip_int8_kernel<SWIGLU, W, TILES, 1, D, LONG, false, false>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((strip_int8_kernel<SWIGLU, W, TILES, 4, D, LONG, false, false>), grid, block, 0, s, p);
-    return launch_status();
+    return launch(std::false_type{});
 }
 
 template <bool SWIGLU>
@@ -1051,7 +1065,7 @@ template <bool SWIGLU>
 int launch_strips(I8Args& p, int64_t max_rows, hipStream_t s) {
     if (p.P <= SHORT_K) return launch_strips_of<SWIGLU, 4, 2, 1, false>(p, max_rows, s);
     if constexpr (SWIGLU) return launch_strips_of<true, 4, 4, 2, true>(p, max_rows, s);
-    else if (max_rows <= FEW_ROWS) return launch_strips_of<false, 8, 1, 2, true>(p, max_rows, s);
+    else if (max_rows <= FEW_ROWS) return launch_strips_of<false, 8, 1, 2, true, 2>(p, max_rows, s);
     else return launch_strips_of<false, 4, 2, 2, true>(p, max_rows, s);
 }
 

@@ -119,6 +119,8 @@ def _run(sizes, d, f, T, *, gather=True, n_shared=0, seed=0, cap=None, x=None, s
     # of which most or all waves lie, slices of K
     ([33, 1, 0, 49], 2304, 2312, 50), ([64, 17, 32], 4096, 72, 64), ([40, 100, 7], 2056, 3000, 100),
     ([97, 128], 2304, 2600, 128), ([40], 8, 9000, 40), ([36, 3], 24, 3000, 36), ([90], 2104, 1, 90),
+    # a long K and as many tokens, but few rows a group on average
+    ([3, 0, 9, 16, 1, 2, 5, 33], 2304, 2400, 50), ([0, 64, 1, 0, 18, 0, 0, 2], 2104, 4200, 64),
 ])
 def test_groups(sizes, d, f, T):
     say("[ffn int8]", sizes, d, f, T)
