@@ -5,7 +5,8 @@
 //
 //   1. h = SiLU(a) b,  a, b = (W1 xq, W3 xq) sx sw, in bf16: a row's scale is known only when all of
 //      the row is, and h goes to memory and back in between, in half the bytes of fp32.  The
-//      rounding, 2^-9 of a value, is small beside that to 8 bits, half of 1/127 of the row's largest.
+//      rounding, 2^-8 of a value at most, is no more than that to 8 bits, half of 1/127 of the row's
+//      largest.
 //   2. hq, sh = the rows of h in 8 bits (of one or two tokens by the strips of 3 themselves)
 //   3. y = (W2 hq) sh sw; where its strips or tiles are few, by slices of K, whose sums are added
 //
@@ -1050,9 +1051,9 @@ int launch_wide_strips(I8Args& p, hipStream_t s) {
 
 // A short K gives a strip's waves few steps, and what a strip waits for at its start and end is
 // hidden by other workgroups: narrow strips, one step of loads in flight and registers for more
-// waves (FFN of 64 tokens, wide and two steps, narrow and one: DeepSeek-V2-Lite 97.7 and 91.1 us,
-// Qwen3-30B-A3B 22.5 and 20.6).  A long K: wide strips of gate and up rows, so that token rows are read
-// half as often (64 Mixtral-shaped tokens 101.2 us, narrow 111.7), and two steps in flight (4 tokens 57.8,
+// waves (FFN of 64 tokens, of twice the columns and two steps, of 16 and one: DeepSeek-V2-Lite 97.7 and 91.1 us,
+// Qwen3-30B-A3B 22.5 and 20.6).  A long K: 32 columns of gate and up rows, so that token rows are
+// read half as often (64 Mixtral-shaped tokens 101.2 us, of 16 columns 111.7), and two steps in flight (4 tokens 57.8,
 // one in gate/up 58.6).  Down strips of a long K are few: of 16 columns by eight waves while every strip
 // reads few rows (by four waves of 32 columns and by these: 1 token 32.1 and 28.3 us, 4 tokens 57.8 and
 // 53.4, 16 tokens 71.6 and 69.0, 32 tokens 88.1 and 87.0, 64 tokens 101.9 and 108.4).  Strips of a long K start
@@ -1077,7 +1078,7 @@ int launch_strips(I8Args& p, int64_t max_rows, hipStream_t s) {
 // experts of DeepSeek-V2-Lite, 24.7 and 29.0).
 constexpr int64_t WIDE_MAX_ROWS = 128;
 
-// Strips while no group can hold more rows than this, tiles past it (FFN, strips and tiles:
+// Strips while no group can hold more rows than this, tiles past it (FFN, strips and tiles, without wide ones:
 // Mixtral-shaped, 32 tokens 91 and 97 us, 64 tokens 105 and 102, 96 tokens 127 and 105; 64
 // DeepSeek-V2-Lite experts, 64 tokens 91 and 97, 128 tokens 125 and 125; Qwen3-30B-A3B, 64 tokens 20
 // and 25, 128 tokens 32 and 27).
