@@ -1186,6 +1186,8 @@ class GradTable:
         self.outputs = (ctypes.c_void_p * n)(*[_arg(o, "out", o.dtype, *o.shape) for o in self.out])
         self.sizes = (ctypes.c_int64 * n)(*[g.numel() for g in self.grads])
         self.dtypes = (ctypes.c_int * n)(*[_dtype_code(g) for g in self.grads])
+        places = [o for o, size in zip(self.outputs, self.sizes) if size]
+        self._distinct = len(set(places)) == len(places)
 
     def __len__(self):
         return len(self.grads)
@@ -1213,8 +1215,11 @@ def moe_grad_norm(table: GradTable, *, norm: Optional[torch.Tensor] = None,
 
 
 def moe_clip_grads(table: GradTable, norm: torch.Tensor, max_norm: float, *, stream=None):
-    """Scale a table's gradients by max_norm / norm where that is below 1.  Returns its outputs."""
+    """Scale a table's gradients by max_norm / norm where that is below 1.  Returns its outputs, no two
+    of which may be the same."""
     lib = load_library()
+    if not table._distinct:
+        raise ValueError("an output is in the table twice")
     st = lib.moe_clip_grads(table.pointers, table.sizes, table.dtypes, len(table),
                             _arg(norm, "norm", torch.float32, 1), max_norm, table.outputs, _stream(stream))
     _check("moe_clip_grads", st)

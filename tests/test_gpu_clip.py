@@ -189,3 +189,18 @@ def test_refusals():
         moe.moe_clip_grads(table, norm.double(), 1.0)
     with pytest.raises(moe.MoeError, match="workspace"):
         moe.moe_grad_norm(table, ws=torch.zeros(8, dtype=torch.uint8, device="cuda"))
+
+
+def test_a_gradient_that_is_listed_twice():
+    """It counts twice in the norm; clipped in place it would be scaled twice, or once, by chance."""
+    g = _grads([((9000,), F), ((0,), F), ((0,), F)], 3)
+    table = moe.GradTable(g + g[:1])
+    norm = moe.moe_grad_norm(table)
+    assert abs(float(norm) - 2 ** 0.5 * float(moe.moe_grad_norm(moe.GradTable(g)))) <= 2 ** -22 * float(norm)
+    with pytest.raises(ValueError, match="twice"):
+        moe.moe_clip_grads(table, norm, 1.0)
+    out = [torch.empty_like(t) for t in g + g[:1]]
+    moe.moe_clip_grads(moe.GradTable(g + g[:1], out=out), norm, 1.0)
+    assert torch.equal(out[0], out[-1]) and torch.equal(out[0], g[0] * (1.0 / norm))
+    moe.moe_clip_grads(moe.GradTable(g), norm, 1.0)
+    assert torch.equal(g[0], out[0])
