@@ -287,6 +287,8 @@ class LayerShare:
         self._grads_current = False                      # they are the last routing's
         self._balance = None                             # the balance loss's outputs and workspace
         self._normed_of = None                           # the rows that the last norm was of
+        # what router and experts read is of the present inputs (X itself always is)
+        self._rows_made = norm is None and not int8
 
     @property
     def rows(self) -> torch.Tensor:
@@ -299,16 +301,24 @@ class LayerShare:
         self.residual = residual
 
     def prepare_rows(self):
-        """Enqueue what a step's rows need before the routing, as `run` does: the residual's addition
-        and the norm, the rows in 8 bits for 8-bit experts (nothing without either)."""
+        """Enqueue what a step's rows need before the routing: the residual's addition and the norm,
+        the rows in 8 bits for 8-bit experts (nothing without either).  `run` and `route` begin
+        with it; the other phases refuse rows of inputs that `set_inputs` has replaced."""
         q = dict(q=self.xq, scales=self.x_scale) if self.int8 else {}
         if self.norm is not None:
+            self._rows = None                            # the last routing's are written over
             h = moe.moe_rmsnorm(self.X, self.norm, residual=self.residual, eps=self.norm_eps,
                                 h=None if self.residual is None else self.hidden, y=self.normed,
                                 rstd=self.rstd, **q)[0]
             self.hidden = self._normed_of = h
         elif self.int8:
             moe.moe_quantize_int8(self.X, **q)
+        self._rows_made = True
+
+    def _needs_rows(self, name: str):
+        if not self._rows_made:
+            raise ValueError("%s reads rows that a step makes of its inputs, and none were made of these: "
+                             "run, route or prepare_rows first" % name)
 
     def _table(self, w13: Sequence[torch.Tensor], w2: Sequence[torch.Tensor]):
         if self.mxfp4:
@@ -352,10 +362,13 @@ class LayerShare:
                 raise ValueError("the share was made without a residual")
             self._set_residual(residual)
         self.X = X
+        self._rows_made = self.norm is None and not self.int8
         if bias is not None:
             self.bias = bias
 
     def route(self, logits_in: Optional[torch.Tensor] = None):
+        """Enqueue a step's rows (`prepare_rows`) and their routing."""
+        self.prepare_rows()
         if logits_in is not None:
             moe.moe_route_topk(None, None, None, self.k, renorm=self.renorm, logits=logits_in,
                                logits_in=True, topk_idx=self.topk_idx, topk_gate=self.topk_gate)
@@ -375,6 +388,7 @@ class LayerShare:
         call, or there are none)."""
         if self.shared_weights is None:
             return
+        self._needs_rows("the shared experts' call")
         moe.moe_grouped_ffn(self.rows, self.shared_offsets, self.shared_weights, cap_rows=self.T,
                             y_perm=self.y_shared, ws=self.ws_shared, stream=stream,
                             products=self.shared_products)
@@ -404,14 +418,18 @@ class LayerShare:
     def package(self):
         """Enqueue the packaging step as `run` makes it (moe_permute; the row copy
         x_perm only when the FFN does not gather the rows itself)."""
+        self._needs_rows("package")
         moe.moe_permute(self.rows, self.topk_idx, self.topk_gate, self.counts, self.placement,
                         self.dev, E=self.E, cap_rows=self.cap_rows, out=self.perm, ws=self.ws_perm,
                         copy_rows=not self.gather_in_ffn)
         self._packaged = True
 
-    def _route_package(self, logits_in: Optional[torch.Tensor] = None):
-        """Enqueue routing, counts and packaging as one call: `route`, the histogram and
-        `package`, the same outputs in fewer launches over short batches."""
+    def _route_package(self, logits_in: Optional[torch.Tensor] = None, prepare: bool = True):
+        """Enqueue a step's rows (prepare=False: they are there), then routing, counts and packaging
+        as one call: `route`, the histogram and `package`, the same outputs in fewer launches
+        over short batches."""
+        if prepare:
+            self.prepare_rows()
         moe.moe_route_package(self.rows, self.Wr, self.bias, self.placement, self.dev,
                               logits=self.logits if logits_in is None else logits_in,
                               topk_idx=self.topk_idx, topk_gate=self.topk_gate,
@@ -427,6 +445,7 @@ class LayerShare:
         moe_grouped_ffn_rows, moe_grouped_ffn_mxfp4, moe_grouped_ffn_int8) into y_perm, or, when the share fuses the combine (fused
         None: as `run` does), moe_grouped_ffn_combine into y (which then reads y_shared:
         the shared experts' call must have completed on this stream)."""
+        self._needs_rows("routed_ffn")
         if self.shared_in_ffn:
             moe.moe_grouped_ffn_rows_shared(self.rows, self._row_token_all, self.perm["group_offsets"],
                                             self._ffn_weights, self.n_shared_blocks,
@@ -477,14 +496,14 @@ class LayerShare:
             # the fused call reads y_shared: the shared branch overlaps the routing
             if self._side is not None:
                 fork_shared()
-            self._route_package(logits_in)
+            self._route_package(logits_in, prepare=False)
             if self._side is not None:
                 main.wait_event(self._join)
             elif self.shared_weights is not None:
                 self._shared_ffn()
             self.routed_ffn()
             return self.y
-        self._route_package(logits_in)
+        self._route_package(logits_in, prepare=False)
         # the shared branch forks after the routing launches, which would otherwise
         # wait for CUs held by its GEMMs, and overlaps the routed experts' FFN, whose
         # launches leave CUs idle
@@ -551,6 +570,8 @@ class LayerShare:
         if balance and self._scores is None:
             raise ValueError("the balance loss is of the gate scores: it needs want_logits=True")
         self._needs_row_maps("backward")
+        if self._rows is None:
+            raise ValueError("backward goes through the rows of the last routing, and they were made anew since")
         if self._grads is None:
             f32 = dict(dtype=torch.float32, device=self.device)
             dcode = moe.MOE_BF16 if self.X.dtype == torch.bfloat16 else moe.MOE_F32
@@ -585,8 +606,8 @@ class LayerShare:
 
     def backward_norm(self, drows: torch.Tensor, dh_add: Optional[torch.Tensor] = None,
                       dh: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None):
-        """Enqueue the gradient of the norm: from drows [T, d], the gradient of the last run's rows,
-        to (dh [T, d], of X and of the residual alike, on top of dh_add, what reaches the sum
+        """Enqueue the gradient of the norm: from drows [T, d], the gradient of the rows made last (by
+        a run, or by `prepare_rows` where that came after it), to (dh [T, d], of X and of the residual alike, on top of dh_add, what reaches the sum
         through the residual stream; dw [d] fp32, of the norm's weight).  The sum that the norm was
         of has to be as that run left it: `hidden`, or X where there is no residual."""
         if self.norm is None:
