@@ -607,9 +607,10 @@ class LayerShare:
     def backward_norm(self, drows: torch.Tensor, dh_add: Optional[torch.Tensor] = None,
                       dh: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None):
         """Enqueue the gradient of the norm: from drows [T, d], the gradient of the rows made last (by
-        a run, or by `prepare_rows` where that came after it), to (dh [T, d], of X and of the residual alike, on top of dh_add, what reaches the sum
-        through the residual stream; dw [d] fp32, of the norm's weight).  The sum that the norm was
-        of has to be as that run left it: `hidden`, or X where there is no residual."""
+        a run, or by `prepare_rows` where that came after it), to (dh [T, d], of X and of the
+        residual alike, on top of dh_add, what reaches the sum through the residual stream; dw [d]
+        fp32, of the norm's weight).  The sum that the norm was of has to be as it was left:
+        `hidden`, or X where there is no residual."""
         if self.norm is None:
             raise ValueError("the share has no norm")
         if self._normed_of is None:
