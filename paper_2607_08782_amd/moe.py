@@ -1168,6 +1168,21 @@ def moe_balance_loss_backward(logits: torch.Tensor, counts: torch.Tensor, n_toke
     return dlogits
 
 
+def _outputs_apart(reads: Sequence[int], writes: Sequence[int], nbytes: Sequence[int]) -> bool:
+    """Whether entries that read nbytes[i] at reads[i] and write as many at writes[i], all at once, keep
+    apart: a write meets no other entry's write or read, and its own read only as the same place."""
+    spans = [(w, w + n, True) for w, n in zip(writes, nbytes) if n]
+    spans += [(r, r + n, False) for r, w, n in zip(reads, writes, nbytes) if n and r != w]
+    end = end_written = 0                            # of the spans before, of the written ones
+    for at, to, written in sorted(spans):
+        if at < (end if written else end_written):
+            return False
+        end = max(end, to)
+        if written:
+            end_written = max(end_written, to)
+    return True
+
+
 class GradTable:
     """Host arrays of a step's gradients (float32 or bfloat16, any shapes), as moe_grad_norm and
     moe_clip_grads take them; out (None: in place): where the clipped ones go."""
@@ -1186,8 +1201,8 @@ class GradTable:
         self.outputs = (ctypes.c_void_p * n)(*[_arg(o, "out", o.dtype, *o.shape) for o in self.out])
         self.sizes = (ctypes.c_int64 * n)(*[g.numel() for g in self.grads])
         self.dtypes = (ctypes.c_int * n)(*[_dtype_code(g) for g in self.grads])
-        places = [o for o, size in zip(self.outputs, self.sizes) if size]
-        self._distinct = len(set(places)) == len(places)
+        self._apart = _outputs_apart([g.data_ptr() for g in self.grads], [o.data_ptr() for o in self.out],
+                                     [g.numel() * g.element_size() for g in self.grads])
 
     def __len__(self):
         return len(self.grads)
@@ -1215,11 +1230,11 @@ def moe_grad_norm(table: GradTable, *, norm: Optional[torch.Tensor] = None,
 
 
 def moe_clip_grads(table: GradTable, norm: torch.Tensor, max_norm: float, *, stream=None):
-    """Scale a table's gradients by max_norm / norm where that is below 1.  Returns its outputs, no two
-    of which may be the same."""
+    """Scale a table's gradients by max_norm / norm where that is below 1.  Returns its outputs, of which
+    none may overlap another, or any gradient but its own in place."""
     lib = load_library()
-    if not table._distinct:
-        raise ValueError("an output is in the table twice")
+    if not table._apart:
+        raise ValueError("an output is in the table twice, or outputs and gradients overlap")
     st = lib.moe_clip_grads(table.pointers, table.sizes, table.dtypes, len(table),
                             _arg(norm, "norm", torch.float32, 1), max_norm, table.outputs, _stream(stream))
     _check("moe_clip_grads", st)
