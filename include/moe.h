@@ -784,7 +784,7 @@ size_t moe_balance_loss_ws_bytes(int64_t T, int E);
  * logits    device [T][E] float, as moe_route_topk leaves them
  * topk_idx  device [T][k] int32, values in [0, E)
  * mask      device [T] bytes, nullable (every token counts).  Where it is 0 (the padding of a
- *           batch) logits and topk_idx are not read.
+ *           batch) what logits and topk_idx hold, NaN and any index included, changes no output.
  * counts    device [E] int32, prob_sum  device [E] float, n_tokens  device [1] int32,
  * loss      device [1] float: outputs (all zero when no token counts).  counts, prob_sum and
  *           n_tokens may be summed over GPUs for the loss, and its gradient, of all their tokens.
