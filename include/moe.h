@@ -761,8 +761,9 @@ size_t moe_rmsnorm_backward_ws_bytes(int dtype, int64_t T, int d);
  * dh       device [T][d] of `dtype` output, nullable (fp32, then stored; may be dh_add)
  * dw       device [d] float output, nullable (zeros when T = 0)
  * ws       moe_rmsnorm_backward_ws_bytes(dtype, T, d) bytes, 256-byte aligned (may be NULL without dw)
- * Apart from dh over dh_add, outputs must not overlap inputs or each other.  Sums are fp32 in a
- * fixed order (deterministic).  Requires T >= 0, 1 <= d < 2^22 (else MOE_ERR_SHAPE).
+ * Apart from dh over dh_add, outputs must not overlap inputs or each other.  Sums are fp32, dw's over
+ * more than a range of ceil(T / 512) rows (4 at least) in 64 bits, in a fixed order (deterministic).
+ * Requires T >= 0, 1 <= d < 2^22 (else MOE_ERR_SHAPE).
  */
 int moe_rmsnorm_backward(const void* dy, const void* h, int dtype, const void* weight, const float* rstd,
                          const void* dh_add, int64_t T, int d, void* dh, float* dw, void* ws,

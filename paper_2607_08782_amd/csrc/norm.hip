@@ -316,31 +316,38 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_backward_columns_kernel(
     parts[range * d + c] = sum;
 }
 
-// dw[c] = the sum of the ranges' parts, by slices of them that are joined in order; eight of a
-// slice's parts in flight (2048 columns of 512 parts: 9.4 us one after the other by 16 slices).
+// dw[c] = the sum of the ranges' parts in 64 bits, by slices of them that are joined in a fixed order;
+// eight of a slice's parts in flight (2048 columns of 512 parts, one after the other by 16 slices: 9.4 us;
+// so 4; 16 columns a workgroup even).  In 32 bits dw was off by 1.5e-7 for 8192 rows, so by 8e-8.
 constexpr int JOIN = 1024, COLS = 32, SLICES = JOIN / COLS;
 
 __global__ __launch_bounds__(JOIN) void sum_ranges_kernel(const float* __restrict__ parts, int64_t n, int d,
                                                           float* __restrict__ dw) {
-    __shared__ float s[SLICES][COLS];
+    __shared__ double s[JOIN / 64][COLS];
+    constexpr int AHEAD = 8;
     const int slice = threadIdx.x / COLS, col = threadIdx.x % COLS;
     const int64_t c = (int64_t)blockIdx.x * COLS + col;
-    float v = 0.f;
-    constexpr int AHEAD = 8;
+    double v = 0.0;
     if (c < d)
         for (int64_t q0 = slice; q0 < n; q0 += SLICES * AHEAD) {
             float a[AHEAD];
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) a[i] = q0 + i * SLICES < n ? parts[(q0 + i * SLICES) * d + c] : 0.f;
+            // (without this the compiler converts, and waits, under each load's condition)
+            asm volatile("" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]), "+v"(a[4]), "+v"(a[5]), "+v"(a[6]), "+v"(a[7]));
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) v += a[i];
+            for (int i = 0; i < AHEAD; ++i) v += (double)a[i];
         }
-    s[slice][col] = v;
+    // slices side by side in a wave, then the waves'
+#pragma unroll
+    for (int o = COLS; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+    if ((threadIdx.x & 63) < COLS) s[threadIdx.x >> 6][col] = v;
     __syncthreads();
     if (slice > 0 || c >= d) return;
+    double sum[2] = {0.0, 0.0};
 #pragma unroll
-    for (int q = 1; q < SLICES; ++q) v += s[q][col];
-    dw[c] = v;
+    for (int q = 0; q < JOIN / 64; ++q) sum[q % 2] += s[q][col];
+    dw[c] = (float)(sum[0] + sum[1]);
 }
 
 // Ranges of the rows, and of each how many: as many as fill the chip, several rows each.
