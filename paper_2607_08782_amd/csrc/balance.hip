@@ -9,8 +9,10 @@
 // are whole numbers, added by atomics in LDS.
 //
 // L lanes share a token, so that its scores come in 16-byte loads, side by side, and a softmax needs
-// few exchanges.  16384 tokens of 128 experts, 8.4 MB: sums 5.4 us, joining 7.2, gradient 8.0; launches
-// in a chain bound it (the bytes are 5 us in all), not the memory or the exponentials.
+// few exchanges.  16384 tokens of 128 experts, 8.4 MB: sums 5.3 us, joining 7.7, gradient 8.0, where the
+// bytes of all three are 5.  Joining: eight workgroups, each with 512 parts of 16 experts through one CU, a
+// barrier, a wave's sums and a ticket, one after the other.  The gradient, 2.1 TB/s: the tokens' number and
+// the counts are read, and divisions in 64 bits done by every lane, before a wave's first product.
 #include <algorithm>
 
 #include "int8.h"

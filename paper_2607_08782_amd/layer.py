@@ -20,7 +20,7 @@ launches leave CUs idle) without holding CUs the routing launches wait for;
 the fork and join are stream events, so a graph capture of `run` holds both
 branches.  The expert placement can be swapped between batches
 (`set_placement`) by re-pointing the weight table; nothing is reallocated (but
-with 4-bit experts, whose table is made anew).
+with 4-bit or 8-bit experts, whose table is made anew).
 
 With ``mxfp4=True`` the routed experts are held and multiplied in 4 bits
 (moe_grouped_ffn_mxfp4; 17/64 of a decode step's weight bytes); shared experts
@@ -28,7 +28,8 @@ keep bf16 and their own call.  With ``int8=True`` they are held and multiplied i
 8-bit integers (moe_grouped_ffn_int8), over token rows that a step quantizes once.
 With ``norm`` the share begins at the residual stream: a step's rows are the
 root-mean-square norm of X (+ residual), in one launch with the addition and, for
-8-bit experts, their codes (moe_rmsnorm).
+8-bit experts, their codes (moe_rmsnorm).  `run` and `route` make such rows as they
+begin; the other phases refuse those of inputs that `set_inputs` has replaced.
 
 `backward` and `backward_rows` are the gradient of the layer around its experts:
 from the loss gradient of y to the expert outputs' and the router's, and from the

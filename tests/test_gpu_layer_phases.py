@@ -192,3 +192,28 @@ def test_8_bit_experts_that_migrate(front):
     share.set_inputs(**batch)
     run_step(share, None)
     _same(share, lambda **kw: make(new, *held(new), **kw), batch)
+
+
+@pytest.mark.parametrize("front", list(FRONTS))
+def test_phases_replay_from_a_graph(front):
+    """The rows are made within the graph: each replay's are those of what X and the residual hold."""
+    share, make = _share(front, 40)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        share.prepare_rows()
+        _phases(share)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        _phases(share)
+    for n in range(4):
+        batch = _next(share, front, 10 + n)
+        share.X.copy_(batch["X"])
+        if "residual" in batch:
+            share.residual.copy_(batch["residual"])
+        g.replay()
+        _same(share, make, batch)
+        share.run()                                  # eager work between the replays
+        _same(share, make, batch)
